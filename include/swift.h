@@ -352,6 +352,127 @@ swift_status swift_gemm_static(const void* w_dev, int32_t w_dtype, int32_t N, in
                                int32_t n_rows, float* y_dev, void* cuda_stream);
 const char* swift_gemm_static_error(void);
 
+/*
+ * Batches of sequences over one paged K,V cache.  The context calls above decode one sequence; the calls below are the
+ * per-layer steps of a program that runs many at once (several continuations of a prompt, candidates that share a long
+ * prefix, packed prompts) with its own projections in between.  They need no context: every buffer is the caller's, work
+ * is enqueued on cuda_stream (a cudaStream_t; NULL = default stream) of the current device and the calls return without
+ * synchronising.  They allocate nothing, keep nothing from one call for the next, and may be captured into a CUDA graph;
+ * row_start, kv_len, the page tables and the positions are read on the device when the work runs, so a replayed graph
+ * follows their new values.  Calls on different streams do not share state (a workspace belongs to one call at a time).
+ * On error nothing is enqueued; swift_batch_error() gives the text of the calling thread's last failure.
+ */
+enum { SWIFT_F16 = 2 };            /* third storage type, for these calls only */
+enum { SWIFT_MAX_SEQS = 4096 };    /* sequences of one batch */
+
+/* The cache: one pool for all layers, in the layout of the library's own: [page][block][0 = K, 1 = V][kv head][slot][dim]. */
+typedef struct {
+    void* pool;                 /* device, 16-byte aligned */
+    int32_t dtype;              /* SWIFT_F32, SWIFT_BF16 or SWIFT_F16 */
+    int32_t n_pages, n_blocks, n_kv_heads;
+    int32_t page_size;          /* positions per page; power of two, 8..128 */
+    int32_t head_dim;           /* even, at most 256 */
+} swift_paged_kv;
+
+/*
+ * Rows of several sequences, packed.  Sequence i holds rows row_start[i] .. row_start[i+1] - 1 (ascending; a sequence may
+ * be empty); rows from row_start[n_seqs] to n_rows are padding, which no call reads or writes.  kv_len[i] counts the
+ * cached positions of sequence i, its rows of this batch included: with n rows, row r is at own position
+ * kv_len[i] - n + r.  Own position p lives in slot p % page_size of page page_table[i * table_stride + p / page_size].
+ * With prefix_len > 0, all sequences continue the same prefix of prefix_len positions in prefix_pages[0 ..
+ * ceil(prefix_len / page_size) - 1], and own position p is position prefix_len + p of the sequence.  Pages are looked up
+ * in [0, n_pages): the positions of a page id outside it hold nothing and are neither read nor written.  kv_len is
+ * clipped to 0 .. table_stride * page_size.  Slots at and behind kv_len may hold anything, NaN included.
+ */
+typedef struct {
+    int32_t n_seqs, n_rows;
+    const int32_t* row_start;     /* device [n_seqs + 1] */
+    const int32_t* kv_len;        /* device [n_seqs] */
+    const int32_t* page_table;    /* device [n_seqs][table_stride] */
+    int32_t table_stride;
+    const int32_t* prefix_pages;  /* device, may be NULL with prefix_len 0 */
+    int32_t prefix_len;
+} swift_row_batch;
+
+/* A packed tensor [n_rows][heads][head_dim] with contiguous dims; strides in elements (a slice of a fused projection fits). */
+typedef struct { const void* ptr; int64_t row_stride, head_stride; } swift_rows;
+
+/*
+ * table_dev[p][i] = magnitude * (cos, sin)(p * f_i), i < rotary_dim / 2, p < n_positions; fp32 from 64-bit angles.
+ * f_i = theta^(-2i / rotary_dim), scaled for contexts longer than trained on: with original_positions = 0 every f_i is
+ * divided by factor (position interpolation); otherwise by parts (the rule of YaRN, arXiv 2309.00071, Section 3.2, which
+ * LLaMA 3 uses too): a pair that turns t = original_positions * f_i / (2 pi) times keeps the share
+ * g = clamp((t - low_turns) / (high_turns - low_turns), 0, 1) of f_i and divides the rest: f_i * (g + (1 - g) / factor).
+ */
+typedef struct {
+    int32_t n_positions, rotary_dim;
+    double theta, factor;
+    int32_t original_positions;
+    double low_turns, high_turns, magnitude;
+} swift_rope_desc;
+swift_status swift_rope_table(const swift_rope_desc* desc, float* table_dev, void* cuda_stream);
+
+/*
+ * One pass between a layer's fused projection and its attention: for every row of the batch
+ *   q, k: RMS norm per head over head_dim (x * rsqrt(mean x^2 + eps) * gain), where a gain is given; then the first
+ *         rotary_dim dims are rotated by the table's row of the row's position: pair i is (i, i + rotary_dim / 2), or
+ *         (2i, 2i + 1) with interleaved != 0.  fp32 throughout, rounded once.  v is copied.
+ *   q goes to q_out [n_rows][n_heads][head_dim] (the cache's type; may be q itself where type and strides agree),
+ *   k and v to the row's slot of the cache.
+ * The position is prefix_len + own position, or positions[row] if given (a token tree's depths).  A row whose own position
+ * is outside 0 .. table_stride * page_size - 1, whose page is outside the pool, or (with a table) whose position is outside
+ * 0 .. rope_positions - 1 is left out: nothing of it is written.  Two rows must not share a slot.
+ */
+typedef struct {
+    int32_t block, n_heads;
+    int32_t x_dtype;              /* of q, k, v: SWIFT_F32 or the cache's type */
+    swift_rows q, k, v;
+    const float* q_gain;          /* device [head_dim] or NULL (no norm) */
+    const float* k_gain;
+    float eps;
+    const float* rope;            /* device [rope_positions][rotary_dim / 2][2], 8-byte aligned, or NULL (no rotation) */
+    int32_t rope_positions, rotary_dim, interleaved;
+    const int32_t* positions;     /* device [n_rows] or NULL */
+    void* q_out;
+} swift_append_args;
+swift_status swift_kv_append(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_append_args* args,
+                             void* cuda_stream);
+
+/*
+ * Attention of the batch's rows over what they see: the whole prefix and own positions 0 .. the row's own.  Query head h
+ * reads kv head h / (n_heads / n_kv_heads).  out[row][h][:] = softmax(scale * q k^T) v, the softmax and the sums in fp32;
+ * a row that sees nothing gives 0.  q and out are of the cache's type, out [n_rows][n_heads][head_dim] contiguous;
+ * where the tensor cores compute (below), both and q's strides are multiples of 16 bytes.  scale > 0.
+ * Cached values of visible positions must be finite for the rows that do not see them yet to stay so: a row's result may
+ * be spoilt by a NaN or infinity in V of a later row of its own sequence, never by another sequence's.
+ *
+ * swift_prompt_attention takes each sequence by itself: prompts, chunks of prompts, any number of rows.
+ * swift_prefix_attention is for few rows per sequence (decoding steps, verification, scoring windows): the scores against
+ * the prefix are computed once for the rows of all sequences together and joined with each sequence's own part.  max_rows
+ * bounds the rows of one sequence; rows beyond it are left out.  Both compute the same function.
+ * 16-bit caches with head_dim a multiple of 8 up to 128 run on the tensor cores; fp32 caches and other head sizes are
+ * computed row by row in fp32 by either call.
+ * workspace: device memory of at least swift_prefix_workspace_bytes (0 on invalid arguments), 256-byte aligned,
+ * uninitialised; it belongs to the call until its work is done.
+ */
+typedef struct {
+    int32_t block, n_heads;
+    swift_rows q;
+    float scale;
+    void* out;
+} swift_attention_args;
+swift_status swift_prompt_attention(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args,
+                                    void* cuda_stream);
+size_t swift_prefix_workspace_bytes(const swift_paged_kv* kv, const swift_row_batch* batch, int32_t n_heads, int32_t max_rows);
+swift_status swift_prefix_attention(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args,
+                                    int32_t max_rows, swift_devbuf workspace, void* cuda_stream);
+const char* swift_batch_error(void);
+
+/* Waits for the stream's work and reports what only the device knows: SWIFT_ETIMEOUT when a bounded device-side wait of
+ * one of the attention calls above ran out on this device since the last report (the outputs of that call are then not
+ * complete), SWIFT_ECUDA when the work failed, else SWIFT_OK.  Not inside a stream capture. */
+swift_status swift_batch_sync(void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -55,7 +55,9 @@ SYMBOLS = ("swift_weights_bytes", "swift_kv_bytes", "swift_workspace_bytes", "sw
            "swift_last_error", "swift_pack_tensor", "swift_set_sampling", "swift_set_top_p", "swift_set_greedy_draft", "swift_forward_rows", "swift_prefill",
            "swift_set_pending", "swift_draft", "swift_verify", "swift_accept", "swift_score_skipsets", "swift_generate",
            "swift_committed_length", "swift_launch_count", "swift_round_times", "swift_round_bytes_stored", "swift_final_skip_mask", "swift_forward_bytes", "swift_read_kv", "swift_time_gemm", "swift_set_gemm_impl", "swift_gemm", "swift_gemm_static",
-           "swift_gemm_static_error", "swift_probe_wait_limit", "swift_many_row_schedule", "swift_set_tree", "swift_verify_tree", "swift_tree_rows", "swift_opt_create", "swift_opt_free", "swift_opt_suggest", "swift_opt_observe")
+           "swift_gemm_static_error", "swift_probe_wait_limit", "swift_many_row_schedule", "swift_set_tree", "swift_verify_tree", "swift_tree_rows", "swift_opt_create", "swift_opt_free", "swift_opt_suggest", "swift_opt_observe",
+           "swift_rope_table", "swift_kv_append", "swift_prompt_attention", "swift_prefix_workspace_bytes", "swift_prefix_attention",
+           "swift_batch_error", "swift_batch_sync")
 
 _lib = None
 
@@ -117,6 +119,15 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.swift_gemm.argtypes = [vp, i32, i32, vp, i32, vp]
     lib.swift_time_gemm.argtypes = [vp, i32, i32, i32, vp, vp]
     lib.swift_read_kv.argtypes = [vp, i32, i32, i32, i32, vp]
+    lib.swift_rope_table.argtypes = [vp, vp, vp]
+    lib.swift_kv_append.argtypes = [vp, vp, vp, vp]
+    lib.swift_prompt_attention.argtypes = [vp, vp, vp, vp]
+    lib.swift_prefix_workspace_bytes.argtypes = [vp, vp, i32, i32]
+    lib.swift_prefix_workspace_bytes.restype = C.c_size_t
+    lib.swift_prefix_attention.argtypes = [vp, vp, vp, i32, _DevBuf, vp]
+    lib.swift_batch_error.argtypes = []
+    lib.swift_batch_error.restype = C.c_char_p
+    lib.swift_batch_sync.argtypes = [vp]
     for name in SYMBOLS:
         fn = getattr(lib, name)          # AttributeError if a declared symbol is missing
         if fn.restype is C.c_int:

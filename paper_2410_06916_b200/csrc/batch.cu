@@ -1,0 +1,291 @@
+// Batches of sequences over one paged K,V cache: argument checks, launch shapes and entry points of swift_rope_table,
+// swift_kv_append, swift_prompt_attention and swift_prefix_attention.  No context and no state between calls.
+#include "../../include/swift.h"
+
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+// This translation unit gets its own copies of the shared device code (separate namespace).
+#define swk swk_batch
+#include "kernels_batch.cuh"
+
+using namespace swk;
+
+namespace {
+
+thread_local char g_batch_error[512] = "";
+
+swift_status fail_batch(swift_status s, const char* fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_batch_error, sizeof g_batch_error, fmt, ap);
+    va_end(ap);
+    return s;
+}
+
+constexpr int MAX_POSITIONS = 1 << 30;      // prefix_len and table_stride * page_size
+constexpr int MAX_HEADS = 4096;
+
+inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+inline bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
+inline int type_size(int dtype) { return dtype == SWIFT_F32 ? 4 : 2; }
+inline bool type_known(int dtype) { return dtype == SWIFT_F32 || dtype == SWIFT_BF16 || dtype == SWIFT_F16; }
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t stream, bool after_previous, Args&&... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = after_previous ? 1 : 0;   // only between the kernels of one call
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+swift_status check_batch(const swift_paged_kv* kv, const swift_row_batch* b, BatchView* out)
+{
+    if (!kv || !b) return fail_batch(SWIFT_EINVAL, "null cache or batch");
+    if (!kv->pool || !aligned(kv->pool, 16)) return fail_batch(SWIFT_EINVAL, "the pool must be 16-byte aligned device memory");
+    if (!type_known(kv->dtype)) return fail_batch(SWIFT_EINVAL, "cache type %d unknown", kv->dtype);
+    if (kv->n_pages < 1 || kv->n_blocks < 1 || kv->n_kv_heads < 1 || kv->n_kv_heads > MAX_HEADS)
+        return fail_batch(SWIFT_EINVAL, "cache of %d pages, %d blocks, %d heads", kv->n_pages, kv->n_blocks, kv->n_kv_heads);
+    if (kv->page_size < 8 || kv->page_size > 128 || (kv->page_size & (kv->page_size - 1)))
+        return fail_batch(SWIFT_EINVAL, "page_size %d is not a power of two in 8..128", kv->page_size);
+    if (kv->head_dim < 2 || kv->head_dim > 256 || kv->head_dim % 2) return fail_batch(SWIFT_EINVAL, "head_dim %d is not even in 2..256", kv->head_dim);
+    if ((long long)kv->n_blocks * 2 * kv->n_kv_heads > (1 << 24)) return fail_batch(SWIFT_EINVAL, "too many heads in a page");
+    if (b->n_seqs < 0 || b->n_rows < 0) return fail_batch(SWIFT_EINVAL, "n_seqs %d, n_rows %d", b->n_seqs, b->n_rows);
+    if (b->n_seqs > SWIFT_MAX_SEQS) return fail_batch(SWIFT_ECAPACITY, "n_seqs %d above %d", b->n_seqs, (int)SWIFT_MAX_SEQS);
+    if (b->n_seqs > 0 && (!b->row_start || !b->kv_len || !b->page_table)) return fail_batch(SWIFT_EINVAL, "null row_start, kv_len or page_table");
+    if (b->table_stride < 1 || (long long)b->table_stride * kv->page_size > MAX_POSITIONS)
+        return fail_batch(SWIFT_EINVAL, "table_stride %d outside 1..%d", b->table_stride, MAX_POSITIONS / kv->page_size);
+    if (b->prefix_len < 0 || b->prefix_len > MAX_POSITIONS) return fail_batch(SWIFT_EINVAL, "prefix_len %d", b->prefix_len);
+    if (b->prefix_len > 0 && !b->prefix_pages) return fail_batch(SWIFT_EINVAL, "null prefix_pages with prefix_len %d", b->prefix_len);
+    out->n_seqs = b->n_seqs;
+    out->n_rows = b->n_rows;
+    out->table_stride = b->table_stride;
+    out->prefix_len = b->prefix_len;
+    out->page_size = kv->page_size;
+    out->page_shift = __builtin_ctz(kv->page_size);
+    out->n_pages = kv->n_pages;
+    out->max_len = b->table_stride * kv->page_size;
+    out->row_start = b->row_start;
+    out->kv_len = b->kv_len;
+    out->page_table = b->page_table;
+    out->prefix_pages = b->prefix_pages;
+    return SWIFT_OK;
+}
+
+// what the tensor-core kernels take; the rest runs row by row
+inline bool tensor_core_shape(const swift_paged_kv* kv) { return kv->dtype != SWIFT_F32 && kv->head_dim % 8 == 0 && kv->head_dim <= 128; }
+inline long long kv_elems(const swift_paged_kv* kv) { return (long long)kv->n_kv_heads * kv->page_size * kv->head_dim; }
+inline const char* block_base(const swift_paged_kv* kv, int block)
+{
+    return reinterpret_cast<const char*>(kv->pool) + (size_t)block * 2 * kv_elems(kv) * type_size(kv->dtype);
+}
+
+swift_status check_attention(const swift_paged_kv* kv, const swift_row_batch* b, const swift_attention_args* a, BatchView* bv, AttnView* av)
+{
+    swift_status st = check_batch(kv, b, bv);
+    if (st != SWIFT_OK) return st;
+    if (!a) return fail_batch(SWIFT_EINVAL, "null arguments");
+    if (a->block < 0 || a->block >= kv->n_blocks) return fail_batch(SWIFT_EINVAL, "block %d outside 0..%d", a->block, kv->n_blocks - 1);
+    if (a->n_heads < 1 || a->n_heads > MAX_HEADS || a->n_heads % kv->n_kv_heads)
+        return fail_batch(SWIFT_EINVAL, "n_heads %d is not a multiple of the cache's %d (at most %d)", a->n_heads, kv->n_kv_heads, MAX_HEADS);
+    if (!(a->scale > 0.f) || std::isinf(a->scale)) return fail_batch(SWIFT_EINVAL, "scale must be positive and finite");
+    if (b->n_rows > 0) {
+        const int es = type_size(kv->dtype);
+        if (!a->q.ptr || !a->out) return fail_batch(SWIFT_EINVAL, "null q or out");
+        const int unit = tensor_core_shape(kv) ? 16 : es;
+        if (!aligned(a->q.ptr, unit) || !aligned(a->out, unit) || a->q.row_stride * es % unit || a->q.head_stride * es % unit)
+            return fail_batch(SWIFT_EINVAL, "q, its strides and out must be multiples of %d bytes", unit);
+        if (a->q.row_stride < 0 || a->q.head_stride < 0) return fail_batch(SWIFT_EINVAL, "negative strides");
+    }
+    av->q = a->q.ptr;
+    av->q_row_stride = a->q.row_stride;
+    av->q_head_stride = a->q.head_stride;
+    av->pool = block_base(kv, a->block);
+    av->page_elems = 2 * kv_elems(kv) * kv->n_blocks;
+    av->kv_elems = kv_elems(kv);
+    av->out = a->out;
+    av->n_heads = a->n_heads;
+    av->n_kv_heads = kv->n_kv_heads;
+    av->head_dim = kv->head_dim;
+    av->max_rows = b->n_rows;
+    av->scale = a->scale;
+    return SWIFT_OK;
+}
+
+cudaError_t launch_rows(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, cudaStream_t s)
+{
+    const dim3 grid(bv.n_rows, ceil_div(av.n_heads, 4));
+    switch (kv->dtype) {
+    case SWIFT_F32: return launch(attn_rows_kernel<float>, grid, 128, 0, s, false, bv, av);
+    case SWIFT_BF16: return launch(attn_rows_kernel<__nv_bfloat16>, grid, 128, 0, s, false, bv, av);
+    default: return launch(attn_rows_kernel<__half>, grid, 128, 0, s, false, bv, av);
+    }
+}
+
+template <typename TX, typename TC>
+cudaError_t launch_append(const BatchView& b, const AppendView& a, bool vec, cudaStream_t s)
+{
+    const int units = a.n_heads + 2 * a.n_kv_heads;
+    if (!vec) return launch(append_any_kernel<TX, TC>, dim3(b.n_rows, ceil_div(units, AP_THREADS / 32)), AP_THREADS, 0, s, false, b, a);
+    const int pieces = a.head_dim / 16;
+    const int lph = pieces <= 1 ? 1 : pieces <= 2 ? 2 : pieces <= 4 ? 4 : pieces <= 8 ? 8 : 16;
+    const dim3 grid(b.n_rows, ceil_div(units, AP_THREADS / lph * AP_UNROLL));
+    switch (lph) {
+    case 1: return launch(append_vec_kernel<TX, TC, 1>, grid, AP_THREADS, 0, s, false, b, a);
+    case 2: return launch(append_vec_kernel<TX, TC, 2>, grid, AP_THREADS, 0, s, false, b, a);
+    case 4: return launch(append_vec_kernel<TX, TC, 4>, grid, AP_THREADS, 0, s, false, b, a);
+    case 8: return launch(append_vec_kernel<TX, TC, 8>, grid, AP_THREADS, 0, s, false, b, a);
+    default: return launch(append_vec_kernel<TX, TC, 16>, grid, AP_THREADS, 0, s, false, b, a);
+    }
+}
+
+} // namespace
+
+extern "C" {
+
+const char* swift_batch_error(void) { return g_batch_error; }
+
+swift_status swift_rope_table(const swift_rope_desc* d, float* table_dev, void* cuda_stream)
+{
+    if (!d || !table_dev) return fail_batch(SWIFT_EINVAL, "null description or table");
+    if (!aligned(table_dev, 8)) return fail_batch(SWIFT_EINVAL, "the table must be 8-byte aligned");
+    if (d->n_positions < 0 || d->n_positions > MAX_POSITIONS) return fail_batch(SWIFT_EINVAL, "n_positions %d", d->n_positions);
+    if (d->rotary_dim < 2 || d->rotary_dim > 256 || d->rotary_dim % 2) return fail_batch(SWIFT_EINVAL, "rotary_dim %d is not even in 2..256", d->rotary_dim);
+    if (!(d->theta > 0.0) || std::isinf(d->theta) || !(d->factor > 0.0) || std::isinf(d->factor) || !std::isfinite(d->magnitude))
+        return fail_batch(SWIFT_EINVAL, "theta and factor must be positive and finite, magnitude finite");
+    if (d->original_positions < 0) return fail_batch(SWIFT_EINVAL, "original_positions %d", d->original_positions);
+    if (d->original_positions > 0 && !(std::isfinite(d->low_turns) && std::isfinite(d->high_turns) && d->low_turns < d->high_turns))
+        return fail_batch(SWIFT_EINVAL, "low_turns must be below high_turns");
+    if (d->n_positions == 0) return SWIFT_OK;
+    RopeTableArgs a;
+    a.table = reinterpret_cast<float2*>(table_dev);
+    a.n_positions = d->n_positions;
+    a.half = d->rotary_dim / 2;
+    a.log_theta_step = 2.0 * std::log(d->theta) / d->rotary_dim;
+    a.inv_factor = 1.0 / d->factor;
+    a.turns_per_freq = d->original_positions / (2.0 * 3.14159265358979323846);
+    a.low = d->low_turns;
+    a.inv_range = d->original_positions > 0 ? 1.0 / (d->high_turns - d->low_turns) : 0.0;
+    a.magnitude = d->magnitude;
+    const long long threads = (long long)ceil_div(d->n_positions, RT_RUN) * a.half;
+    const cudaError_t e = launch(rope_run_kernel, dim3((unsigned)((threads + 127) / 128)), 128, 0, (cudaStream_t)cuda_stream, false, a);
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+
+swift_status swift_kv_append(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_append_args* x, void* cuda_stream)
+{
+    BatchView bv;
+    swift_status st = check_batch(kv, batch, &bv);
+    if (st != SWIFT_OK) return st;
+    if (!x) return fail_batch(SWIFT_EINVAL, "null arguments");
+    if (x->block < 0 || x->block >= kv->n_blocks) return fail_batch(SWIFT_EINVAL, "block %d outside 0..%d", x->block, kv->n_blocks - 1);
+    if (x->n_heads < 0 || x->n_heads > MAX_HEADS) return fail_batch(SWIFT_EINVAL, "n_heads %d", x->n_heads);
+    if (x->x_dtype != SWIFT_F32 && x->x_dtype != kv->dtype) return fail_batch(SWIFT_EUNSUPPORTED, "q, k, v must be fp32 or of the cache's type");
+    if (x->rope && (x->rotary_dim < 2 || x->rotary_dim > kv->head_dim || x->rotary_dim % 2 || x->rope_positions < 0 || !aligned(x->rope, 8)))
+        return fail_batch(SWIFT_EINVAL, "rotary_dim %d is not even in 2..head_dim, or the table is not 8-byte aligned", x->rotary_dim);
+    if ((x->q_gain || x->k_gain) && !(x->eps >= 0.f && std::isfinite(x->eps))) return fail_batch(SWIFT_EINVAL, "eps must be finite and not negative");
+    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
+    if (!x->k.ptr || !x->v.ptr || (x->n_heads > 0 && (!x->q.ptr || !x->q_out))) return fail_batch(SWIFT_EINVAL, "null q, k, v or q_out");
+    AppendView a;
+    const int es = type_size(x->x_dtype), rd = x->rope ? x->rotary_dim : 0;
+    const swift_rows* in[3] = {&x->q, &x->k, &x->v};
+    bool vec = kv->head_dim % 16 == 0 && rd % 16 == 0 && (!x->rope || aligned(x->rope, 16)) && aligned(x->q_out, 16);
+    // with pairs (i, i + R/2) the second piece starts at R/2: 16-byte loads need R/2 in whole pieces of 8, which R % 16 gives
+    for (int w = 0; w < 3; ++w) {
+        const bool used = w > 0 || x->n_heads > 0;
+        a.x[w] = in[w]->ptr;
+        a.row_stride[w] = in[w]->row_stride;
+        a.head_stride[w] = in[w]->head_stride;
+        if (used && !aligned(in[w]->ptr, es)) return fail_batch(SWIFT_EINVAL, "q, k, v must be aligned to their element size");
+        if (used && (in[w]->row_stride < 0 || in[w]->head_stride < 0)) return fail_batch(SWIFT_EINVAL, "negative strides");
+        vec = vec && (!used || (aligned(in[w]->ptr, 16) && in[w]->row_stride * es % 16 == 0 && in[w]->head_stride * es % 16 == 0));
+    }
+    if (x->n_heads > 0 && !aligned(x->q_out, type_size(kv->dtype))) return fail_batch(SWIFT_EINVAL, "q_out must be aligned to its element size");
+    a.n_heads = x->n_heads;
+    a.n_kv_heads = kv->n_kv_heads;
+    a.head_dim = kv->head_dim;
+    a.rotary_dim = rd;
+    a.interleaved = x->interleaved != 0;
+    a.rope_positions = x->rope_positions;
+    a.gain[0] = x->q_gain;
+    a.gain[1] = x->k_gain;
+    if ((x->q_gain && !aligned(x->q_gain, 4)) || (x->k_gain && !aligned(x->k_gain, 4))) return fail_batch(SWIFT_EINVAL, "gains must be 4-byte aligned");
+    vec = vec && aligned(x->q_gain, 16) && aligned(x->k_gain, 16);
+    a.eps = x->eps;
+    a.rope = reinterpret_cast<const float2*>(x->rope);
+    a.positions = x->positions;
+    a.q_out = x->q_out;
+    a.pool = const_cast<char*>(block_base(kv, x->block));
+    a.page_elems = 2 * kv_elems(kv) * kv->n_blocks;
+    a.kv_elems = kv_elems(kv);
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    cudaError_t e;
+    if (kv->dtype == SWIFT_F32) e = launch_append<float, float>(bv, a, vec, s);
+    else if (kv->dtype == SWIFT_BF16) e = x->x_dtype == SWIFT_F32 ? launch_append<float, __nv_bfloat16>(bv, a, vec, s) : launch_append<__nv_bfloat16, __nv_bfloat16>(bv, a, vec, s);
+    else e = x->x_dtype == SWIFT_F32 ? launch_append<float, __half>(bv, a, vec, s) : launch_append<__half, __half>(bv, a, vec, s);
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+
+swift_status swift_prompt_attention(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args, void* cuda_stream)
+{
+    BatchView bv;
+    AttnView av;
+    swift_status st = check_attention(kv, batch, args, &bv, &av);
+    if (st != SWIFT_OK) return st;
+    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
+    const cudaError_t e = launch_rows(kv, bv, av, (cudaStream_t)cuda_stream);
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+
+size_t swift_prefix_workspace_bytes(const swift_paged_kv* kv, const swift_row_batch* batch, int32_t n_heads, int32_t max_rows)
+{
+    BatchView bv;
+    if (check_batch(kv, batch, &bv) != SWIFT_OK) return 0;
+    if (n_heads < 1 || n_heads > MAX_HEADS || n_heads % kv->n_kv_heads || max_rows < 1) {
+        fail_batch(SWIFT_EINVAL, "n_heads %d, max_rows %d", n_heads, max_rows);
+        return 0;
+    }
+    return 256;
+}
+
+swift_status swift_prefix_attention(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args, int32_t max_rows,
+                                    swift_devbuf workspace, void* cuda_stream)
+{
+    BatchView bv;
+    AttnView av;
+    swift_status st = check_attention(kv, batch, args, &bv, &av);
+    if (st != SWIFT_OK) return st;
+    if (max_rows < 1) return fail_batch(SWIFT_EINVAL, "max_rows %d", max_rows);
+    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
+    const size_t need = swift_prefix_workspace_bytes(kv, batch, args->n_heads, max_rows);
+    if (!workspace.dptr || !aligned(workspace.dptr, 256)) return fail_batch(SWIFT_EINVAL, "the workspace must be 256-byte aligned device memory");
+    if (workspace.bytes < need) return fail_batch(SWIFT_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace.bytes, need);
+    av.max_rows = max_rows;
+    const cudaError_t e = launch_rows(kv, bv, av, (cudaStream_t)cuda_stream);
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+
+swift_status swift_batch_sync(void* cuda_stream)
+{
+    const cudaError_t e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "the stream's work failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+
+} // extern "C"

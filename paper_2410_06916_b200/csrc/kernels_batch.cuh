@@ -1,0 +1,398 @@
+// Batches of sequences over one paged cache: the shared row and page arithmetic, the rotary table, the pass between a
+// layer's projection and its attention (norm + rotation + append), and attention row by row for the types and head sizes
+// the tensor-core kernels next door do not take.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace swk {
+
+constexpr unsigned FULL_WARP = 0xFFFFFFFFu;
+
+// ------------------------------------------------------------------------------ the batch as kernels see it
+struct BatchView {
+    int n_seqs, n_rows, table_stride, prefix_len;
+    int page_size, page_shift, n_pages, max_len;          // max_len = table_stride * page_size
+    const int* row_start;
+    const int* kv_len;
+    const int* page_table;
+    const int* prefix_pages;
+};
+struct SeqSpan { int r0, n, len; };                       // first row, rows, cached positions (own)
+
+__device__ __forceinline__ SeqSpan make_span(const BatchView& b, int start, int end, int len)
+{
+    SeqSpan s;
+    s.r0 = min(max(start, 0), b.n_rows);
+    s.n = min(max(end, s.r0), b.n_rows) - s.r0;
+    s.len = min(max(len, 0), b.max_len);
+    return s;
+}
+__device__ __forceinline__ SeqSpan seq_span(const BatchView& b, int i)
+{
+    return make_span(b, b.row_start[i], b.row_start[i + 1], b.kv_len[i]);
+}
+
+// The sequence that holds row `row`, found by a whole warp: 32 row starts per step are compared at once, so a batch of up
+// to 32 sequences costs one trip to memory (the spans' three numbers come with it) and one of 1024 two.  Returns -1 for
+// padding rows.  All lanes get the result.
+__device__ __forceinline__ int find_seq(const BatchView& b, int row, SeqSpan& span)
+{
+    const int lane = threadIdx.x & 31;
+    int base = 0, n = b.n_seqs;                           // the last i in [base, base + n) with row_start[i] <= row
+    while (n > 32) {
+        const int step = (n + 31) >> 5;
+        const int i = base + lane * step;
+        const bool le = lane * step < n && b.row_start[i] <= row;
+        const unsigned m = __ballot_sync(FULL_WARP, le);
+        if (m == 0) return -1;
+        const int at = 31 - __clz(m);
+        n = min(step, n - at * step);
+        base += at * step;
+    }
+    int start = 0, end = 0, len = 0;
+    if (lane < n) {
+        start = b.row_start[base + lane];
+        end = b.row_start[base + lane + 1];
+        len = b.kv_len[base + lane];
+    }
+    const unsigned m = __ballot_sync(FULL_WARP, lane < n && start <= row);
+    if (m == 0) return -1;
+    const int at = 31 - __clz(m);
+    span = make_span(b, __shfl_sync(FULL_WARP, start, at), __shfl_sync(FULL_WARP, end, at), __shfl_sync(FULL_WARP, len, at));
+    if (row < span.r0 || row >= span.r0 + span.n) return -1;
+    return base + at;
+}
+
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ void store_val(__half* p, float v) { *p = __float2half_rn(v); }
+
+// eight values as fp32, from 16-byte loads
+__device__ __forceinline__ void load8(const float* p, float (&x)[8])
+{
+    const float4 a = reinterpret_cast<const float4*>(p)[0], c = reinterpret_cast<const float4*>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = c.x; x[5] = c.y; x[6] = c.z; x[7] = c.w;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) { load_vec(p, x); }
+__device__ __forceinline__ void load8(const __half* p, float (&x)[8])
+{
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16)      // a in the low half
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __half)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8])
+{
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1], T()), pack2(x[2], x[3], T()), pack2(x[4], x[5], T()), pack2(x[6], x[7], T()));
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8])
+{
+    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+// ------------------------------------------------------------------------------ rotary table
+constexpr int RT_RUN = 16;          // positions one thread writes
+
+struct RopeTableArgs {
+    float2* table;
+    int n_positions, half;
+    double log_theta_step;          // ln(theta) * 2 / rotary_dim
+    double inv_factor, turns_per_freq, low, inv_range, magnitude;   // turns_per_freq = original_positions / (2 pi); 0: no parts
+};
+
+// table[p][i] = magnitude * (cos, sin)(p f_i).  A thread takes one pair i and RT_RUN positions: two 64-bit sincos, then a
+// 64-bit rotation per position (its error grows by about 2^-53 a step, far below the fp32 result's half step).  Bound by
+// the table's writes, which neighbouring threads make to neighbouring pairs.  block = 128, grid = ceil(half * runs / 128).
+__global__ void __launch_bounds__(128) rope_run_kernel(RopeTableArgs a)
+{
+    const int runs = (a.n_positions + RT_RUN - 1) / RT_RUN;
+    const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    if (idx >= (long long)runs * a.half) return;
+    const int run = (int)(idx / a.half), i = (int)(idx - (long long)run * a.half);
+    double f = exp(-a.log_theta_step * (double)i);
+    double keep = 0.0;
+    if (a.turns_per_freq > 0.0) keep = fmin(1.0, fmax(0.0, (a.turns_per_freq * f - a.low) * a.inv_range));
+    f = keep * f + (1.0 - keep) * f * a.inv_factor;
+    const int p0 = run * RT_RUN, p1 = min(p0 + RT_RUN, a.n_positions);
+    double s, c, ds, dc;
+    sincos((double)p0 * f, &s, &c);
+    sincos(f, &ds, &dc);
+    s *= a.magnitude;
+    c *= a.magnitude;
+    float2* out = a.table + (size_t)p0 * a.half + i;
+    for (int p = p0; p < p1; ++p, out += a.half) {
+        *out = make_float2((float)c, (float)s);
+        const double c1 = c * dc - s * ds;
+        s = s * dc + c * ds;
+        c = c1;
+    }
+}
+
+// ------------------------------------------------------------------------------ norm + rotation + append
+struct AppendView {
+    const void* x[3];                                     // q, k, v
+    long long row_stride[3], head_stride[3];
+    int n_heads, n_kv_heads, head_dim, rotary_dim, interleaved, rope_positions;
+    const float* gain[2];
+    float eps;
+    const float2* rope;
+    const int* positions;
+    void* q_out;
+    void* pool;                                           // of this block: + block's offset within a page
+    long long page_elems, kv_elems;                       // elements per page (all blocks), per K or V of a block
+};
+
+// What a row needs to know besides its data: where it goes and which table row turns it.  `slot` < 0: the row is left out.
+struct RowPlace { long long kv_off; int slot, rope_row; };
+
+__device__ __forceinline__ bool place_row(const BatchView& b, const AppendView& a, int row, RowPlace& p)
+{
+    SeqSpan sp;
+    const int given = a.positions ? a.positions[row] : 0;
+    const int seq = find_seq(b, row, sp);
+    if (seq < 0) return false;
+    const int own = sp.len - sp.n + (row - sp.r0);
+    if (own < 0) return false;                            // own < len <= max_len
+    const int page = b.page_table[(size_t)seq * b.table_stride + (own >> b.page_shift)];
+    p.rope_row = a.positions ? given : b.prefix_len + own;
+    if ((unsigned)page >= (unsigned)b.n_pages) return false;
+    if (a.rope && (unsigned)p.rope_row >= (unsigned)a.rope_positions) return false;
+    p.slot = own & (b.page_size - 1);
+    p.kv_off = (long long)page * a.page_elems;
+    return true;
+}
+
+// Vector form.  A group of LPH lanes (a power of two >= head_dim / 16) takes one head; a lane holds two pieces of 8 dims
+// that a rotation pairs up: with pairs (i, i + R/2), piece c and the piece R/2 further on; with neighbouring pairs, or
+// behind the rotated part, two pieces side by side.  So no value crosses lanes except the norm's sum.  A warp stays
+// within one row: the row is located once per warp, and its 8 (cos, sin) pairs stay in registers for all its heads.
+// Loads of a lane's UNROLL heads are issued together.  Bound by HBM for many rows, by three dependent trips to memory
+// (row start, page table or cos/sin, data) for few.  grid = (rows, head chunks), block = 128.
+constexpr int AP_THREADS = 128, AP_UNROLL = 4;
+
+template <typename TX, typename TC, int LPH>
+__global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, AppendView a)
+{
+    constexpr int GROUPS = AP_THREADS / LPH;
+    const int row = blockIdx.x, c = threadIdx.x & (LPH - 1), grp = threadIdx.x / LPH;
+    const int D = a.head_dim, half = a.rotary_dim >> 1, pieces = D >> 4;
+    const int units = a.n_heads + 2 * a.n_kv_heads, u0 = blockIdx.y * (GROUPS * AP_UNROLL) + grp;
+    const bool lane_live = c < pieces;
+    int oa, ob;                                           // the two pieces' first dims
+    bool turned;
+    if (a.interleaved) {
+        oa = 16 * c;
+        ob = oa + 8;
+        turned = oa < a.rotary_dim;                       // rotary_dim is a multiple of 16 here
+    } else {
+        const int rc = half >> 3;
+        turned = c < rc;
+        oa = turned ? 8 * c : a.rotary_dim + 16 * (c - rc);
+        ob = turned ? oa + half : oa + 8;
+    }
+    float xa[AP_UNROLL][8], xb[AP_UNROLL][8];
+#pragma unroll
+    for (int j = 0; j < AP_UNROLL; ++j) {
+        const int u = u0 + j * GROUPS;
+        if (lane_live && u < units) {
+            const int w = u < a.n_heads ? 0 : u < a.n_heads + a.n_kv_heads ? 1 : 2;
+            const int h = w == 0 ? u : w == 1 ? u - a.n_heads : u - a.n_heads - a.n_kv_heads;
+            const TX* src = reinterpret_cast<const TX*>(a.x[w]) + row * a.row_stride[w] + h * a.head_stride[w];
+            load8(src + oa, xa[j]);
+            load8(src + ob, xb[j]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) xa[j][e] = xb[j][e] = 0.f;
+        }
+    }
+    RowPlace place;
+    if (!place_row(b, a, row, place)) return;             // the same for the whole block
+    float2 cs[8];
+    turned = turned && a.rope != nullptr && lane_live;
+    if (turned) {
+        const float4* t = reinterpret_cast<const float4*>(a.rope + (size_t)place.rope_row * half + (a.interleaved ? oa >> 1 : oa));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float4 v = t[e];
+            cs[2 * e] = make_float2(v.x, v.y);
+            cs[2 * e + 1] = make_float2(v.z, v.w);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < AP_UNROLL; ++j) {
+        const int u = u0 + j * GROUPS;
+        const int w = u < a.n_heads ? 0 : u < a.n_heads + a.n_kv_heads ? 1 : 2;
+        const int h = w == 0 ? u : w == 1 ? u - a.n_heads : u - a.n_heads - a.n_kv_heads;
+        if (a.gain[0] != nullptr || a.gain[1] != nullptr) {
+            float ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss += xa[j][e] * xa[j][e] + xb[j][e] * xb[j][e];
+#pragma unroll
+            for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(FULL_WARP, ss, o);
+            const float* gain = w < 2 ? a.gain[w] : nullptr;
+            if (gain != nullptr && lane_live) {
+                const float r = rsqrtf(ss / (float)D + a.eps);
+                float ga[8], gb[8];
+                load8(gain + oa, ga);
+                load8(gain + ob, gb);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    xa[j][e] *= r * ga[e];
+                    xb[j][e] *= r * gb[e];
+                }
+            }
+        }
+        if (!lane_live || u >= units) continue;
+        if (turned && w < 2) {
+            if (a.interleaved) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x0 = xa[j][2 * e], y0 = xa[j][2 * e + 1], x1 = xb[j][2 * e], y1 = xb[j][2 * e + 1];
+                    xa[j][2 * e] = x0 * cs[e].x - y0 * cs[e].y;
+                    xa[j][2 * e + 1] = y0 * cs[e].x + x0 * cs[e].y;
+                    xb[j][2 * e] = x1 * cs[4 + e].x - y1 * cs[4 + e].y;
+                    xb[j][2 * e + 1] = y1 * cs[4 + e].x + x1 * cs[4 + e].y;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = xa[j][e], y = xb[j][e];
+                    xa[j][e] = x * cs[e].x - y * cs[e].y;
+                    xb[j][e] = y * cs[e].x + x * cs[e].y;
+                }
+            }
+        }
+        TC* dst = w == 0 ? reinterpret_cast<TC*>(a.q_out) + ((size_t)row * a.n_heads + h) * D
+                         : reinterpret_cast<TC*>(a.pool) + place.kv_off + (w == 2 ? a.kv_elems : 0) + ((size_t)h * b.page_size + place.slot) * D;
+        store8(dst + oa, xa[j]);
+        store8(dst + ob, xb[j]);
+    }
+}
+
+// Scalar form: any even head_dim and rotary_dim, any alignment.  One warp per head of a row, lanes over pairs.
+// grid = (rows, ceil(heads / 4)), block = 128.
+template <typename TX, typename TC>
+__global__ void __launch_bounds__(AP_THREADS) append_any_kernel(BatchView b, AppendView a)
+{
+    const int row = blockIdx.x, lane = threadIdx.x & 31, u = blockIdx.y * (AP_THREADS / 32) + (threadIdx.x >> 5);
+    if (u >= a.n_heads + 2 * a.n_kv_heads) return;
+    RowPlace place;
+    if (!place_row(b, a, row, place)) return;
+    const int w = u < a.n_heads ? 0 : u < a.n_heads + a.n_kv_heads ? 1 : 2;
+    const int h = w == 0 ? u : w == 1 ? u - a.n_heads : u - a.n_heads - a.n_kv_heads, D = a.head_dim;
+    const TX* src = reinterpret_cast<const TX*>(a.x[w]) + row * a.row_stride[w] + h * a.head_stride[w];
+    TC* dst = w == 0 ? reinterpret_cast<TC*>(a.q_out) + ((size_t)row * a.n_heads + h) * D
+                     : reinterpret_cast<TC*>(a.pool) + place.kv_off + (w == 2 ? a.kv_elems : 0) + ((size_t)h * b.page_size + place.slot) * D;
+    const float* gain = w < 2 ? a.gain[w] : nullptr;
+    float r = 1.f;
+    if (gain) {
+        float ss = 0.f;
+        for (int i = lane; i < D; i += 32) { const float v = to_float(src[i]); ss += v * v; }
+        r = rsqrtf(warp_sum(ss) / (float)D + a.eps);
+    }
+    const int R = (w < 2 && a.rope) ? a.rotary_dim : 0, half = a.rotary_dim >> 1;
+    for (int i = lane; i < (R >> 1); i += 32) {
+        const int ia = a.interleaved ? 2 * i : i, ib = a.interleaved ? 2 * i + 1 : i + half;
+        float x = to_float(src[ia]), y = to_float(src[ib]);
+        if (gain) { x *= r * gain[ia]; y *= r * gain[ib]; }
+        const float2 cs = a.rope[(size_t)place.rope_row * half + i];
+        store_val(dst + ia, x * cs.x - y * cs.y);
+        store_val(dst + ib, y * cs.x + x * cs.y);
+    }
+    for (int i = R + lane; i < D; i += 32) {
+        float x = to_float(src[i]);
+        if (gain) x *= r * gain[i];
+        store_val(dst + i, x);
+    }
+}
+
+// ------------------------------------------------------------------------------ attention, row by row
+struct AttnView {
+    const void* q;
+    long long q_row_stride, q_head_stride;
+    const void* pool;                                     // of this block
+    long long page_elems, kv_elems;
+    void* out;
+    int n_heads, n_kv_heads, head_dim, max_rows;
+    float scale;
+};
+
+// One warp per (row, query head), any type and head size: 32 positions at a time, a lane computes one position's score
+// (q from shared memory, K from the cache in order), the running maximum and sum are joined across lanes, and the
+// weighted sum of V runs with lanes over dims.  fp32 throughout.  grid = (rows, ceil(n_heads / 4)), block = 128.
+template <typename T>
+__global__ void __launch_bounds__(128) attn_rows_kernel(BatchView b, AttnView a)
+{
+    __shared__ float q_sh[4][256];
+    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y * 4 + warp;
+    if (h >= a.n_heads) return;
+    SeqSpan sp;
+    const int seq = find_seq(b, row, sp);
+    if (seq < 0 || row - sp.r0 >= a.max_rows) return;
+    const int D = a.head_dim, kvh = h / (a.n_heads / a.n_kv_heads);
+    const T* q = reinterpret_cast<const T*>(a.q) + row * a.q_row_stride + h * a.q_head_stride;
+    for (int d = lane; d < D; d += 32) q_sh[warp][d] = to_float(q[d]) * a.scale;
+    __syncwarp();
+    const int own = max(0, sp.len - sp.n + (row - sp.r0) + 1), total = b.prefix_len + own;    // visible positions
+    const T* head = reinterpret_cast<const T*>(a.pool) + (size_t)kvh * b.page_size * D;
+    float m = -INFINITY, l = 0.f, o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.f;
+    for (int p0 = 0; p0 < total; p0 += 32) {
+        const int p = p0 + lane;
+        long long at = -1;                                // element offset of the position's K, -1: nothing there
+        if (p < total) {
+            const int own_p = p - b.prefix_len, pp = own_p < 0 ? p : own_p;
+            const int page = own_p < 0 ? b.prefix_pages[pp >> b.page_shift] : b.page_table[(size_t)seq * b.table_stride + (pp >> b.page_shift)];
+            if ((unsigned)page < (unsigned)b.n_pages) at = (long long)page * a.page_elems + (long long)(pp & (b.page_size - 1)) * D;
+        }
+        float s = -INFINITY;
+        if (at >= 0) {
+            const T* k = head + at;
+            s = 0.f;
+            for (int d = 0; d < D; ++d) s = fmaf(q_sh[warp][d], to_float(k[d]), s);
+        }
+        const float m_new = fmaxf(m, warp_max(s));
+        if (m_new == -INFINITY) continue;                 // nothing visible so far
+        const float shrink = expf(m - m_new), e_s = expf(s - m_new);
+        l = l * shrink + warp_sum(e_s);
+        m = m_new;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= shrink;
+        const int n = min(32, total - p0);
+        for (int j = 0; j < n; ++j) {
+            const float pj = __shfl_sync(FULL_WARP, e_s, j);
+            const long long aj = __shfl_sync(FULL_WARP, at, j);
+            if (aj < 0) continue;
+            const T* v = head + aj + a.kv_elems;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (lane + 32 * e < D) o[e] = fmaf(pj, to_float(v[lane + 32 * e]), o[e]);
+        }
+    }
+    T* out = reinterpret_cast<T*>(a.out) + ((size_t)row * a.n_heads + h) * D;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (lane + 32 * e < D) store_val(out + lane + 32 * e, o[e] * inv);
+}
+
+} // namespace swk

@@ -1,0 +1,275 @@
+"""Batches of sequences over one paged K,V cache: the torch side of swift_rope_table, swift_kv_append,
+swift_prompt_attention and swift_prefix_attention (include/swift.h says what each computes).  As in binding.py, torch only
+provides memory and streams; every call enqueues hand-written kernels and returns without waiting.
+
+A program that runs several sequences keeps one PagedKV for all layers, makes a RowBatch per step (or keeps one whose
+device tensors it rewrites), and calls per layer:
+
+    q = batch.append(block, q, k, v, rope=table)      # norm + rotation of q and k, K and V into the pages
+    o = batch.prompt_attention(block, q)              # whole prompts, or chunks of them
+    o = batch.prefix_attention(block, q)              # a few rows per sequence behind a shared prefix
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+from typing import Optional
+
+import torch
+
+from .binding import SwiftError, _DevBuf, lib
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+class _Kv(C.Structure):
+    _fields_ = [("pool", C.c_void_p)] + [(n, C.c_int32) for n in ("dtype", "n_pages", "n_blocks", "n_kv_heads", "page_size", "head_dim")]
+
+
+class _Batch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("row_start", C.c_void_p), ("kv_len", C.c_void_p),
+                ("page_table", C.c_void_p), ("table_stride", C.c_int32), ("prefix_pages", C.c_void_p), ("prefix_len", C.c_int32)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _RopeDesc(C.Structure):
+    _fields_ = [("n_positions", C.c_int32), ("rotary_dim", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
+                ("original_positions", C.c_int32), ("low_turns", C.c_double), ("high_turns", C.c_double), ("magnitude", C.c_double)]
+
+
+class _Append(C.Structure):
+    _fields_ = [("block", C.c_int32), ("n_heads", C.c_int32), ("x_dtype", C.c_int32), ("q", _Rows), ("k", _Rows), ("v", _Rows),
+                ("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("eps", C.c_float), ("rope", C.c_void_p),
+                ("rope_positions", C.c_int32), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("positions", C.c_void_p),
+                ("q_out", C.c_void_p)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("block", C.c_int32), ("n_heads", C.c_int32), ("q", _Rows), ("scale", C.c_float), ("out", C.c_void_p)]
+
+
+def _check(status: int) -> None:
+    if status != 0:
+        raise SwiftError(status, lib().swift_batch_error().decode())
+
+
+class _Target:
+    """The device and stream one call runs on.  `stream` None: the current stream of the tensors' device."""
+
+    __slots__ = ("device", "stream", "guards")
+
+    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+        self.device, self.stream, self.guards = device, stream, []
+
+    def __enter__(self) -> C.c_void_p:
+        if self.stream is not None:
+            g = torch.cuda.stream(self.stream)      # outputs and workspaces made inside belong to that stream
+            g.__enter__()
+            self.guards.append(g)
+        elif torch.cuda.current_device() != self.device.index:
+            g = torch.cuda.device(self.device)
+            g.__enter__()
+            self.guards.append(g)
+        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def __exit__(self, *exc) -> None:
+        while self.guards:
+            self.guards.pop().__exit__(*exc)
+
+
+def _cuda_tensor(name: str, t: torch.Tensor, device: Optional[torch.device] = None) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {device}")
+    return t
+
+
+def _int32(name: str, t: torch.Tensor, device: torch.device) -> torch.Tensor:
+    _cuda_tensor(name, t, device)
+    if t.dtype != torch.int32 or not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous int32")
+    return t
+
+
+def rope_table(n_positions: int, rotary_dim: int, theta: float = 10000.0, factor: float = 1.0, original_positions: int = 0,
+               low_turns: float = 1.0, high_turns: float = 4.0, magnitude: float = 1.0, device="cuda",
+               out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """fp32 [n_positions, rotary_dim / 2, 2]: (cos, sin) of every position and pair.  factor > 1 stretches the positions: all
+    alike (original_positions 0), or by parts with low_turns / high_turns as the ramp (LLaMA 3: 1 and 4; YaRN: 1 and 32,
+    with magnitude = 0.1 ln(factor) + 1)."""
+    device = torch.device(device) if out is None else _cuda_tensor("out", out).device
+    if device.type != "cuda":
+        raise ValueError("rope_table needs a CUDA device")
+    if device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    if out is not None and (out.dtype != torch.float32 or not out.is_contiguous() or tuple(out.shape) != (n_positions, rotary_dim // 2, 2)):
+        raise ValueError("out must be contiguous float32 [n_positions, rotary_dim / 2, 2]")
+    desc = _RopeDesc(n_positions, rotary_dim, theta, factor, original_positions, low_turns, high_turns, magnitude)
+    if n_positions < 0 or rotary_dim < 2:
+        raise ValueError("n_positions >= 0 and rotary_dim >= 2")
+    with _Target(device, stream) as s:
+        if out is None:
+            out = torch.empty(n_positions, rotary_dim // 2, 2, dtype=torch.float32, device=device)
+        if n_positions > 0:
+            _check(lib().swift_rope_table(C.byref(desc), C.c_void_p(out.data_ptr()), s))
+    return out
+
+
+class PagedKV:
+    """One K,V pool for all layers: a contiguous CUDA tensor [n_pages, n_blocks, 2, n_kv_heads, page_size, head_dim] the
+    caller made (fp32, bf16 or fp16); [.., 0, ..] is K, [.., 1, ..] is V."""
+
+    def __init__(self, pool: torch.Tensor):
+        _cuda_tensor("pool", pool)
+        if pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_contiguous() or pool.dtype not in _TYPES:
+            raise ValueError("pool must be contiguous [n_pages, n_blocks, 2, n_kv_heads, page_size, head_dim] in fp32, bf16 or fp16")
+        self.pool, self.device, self.dtype = pool, pool.device, pool.dtype
+        self.n_pages, self.n_blocks, _, self.n_kv_heads, self.page_size, self.head_dim = pool.shape
+        self._c = _Kv(pool.data_ptr(), _TYPES[pool.dtype], self.n_pages, self.n_blocks, self.n_kv_heads, self.page_size, self.head_dim)
+
+
+class RowBatch:
+    """Rows of several sequences over a PagedKV.
+
+    row_start  int32 [n_seqs + 1]: sequence i holds rows row_start[i] .. row_start[i + 1] - 1 of the packed tensors
+    kv_len     int32 [n_seqs]: cached positions of each sequence, its rows of this batch included
+    page_table int32 [n_seqs, stride]: pages of each sequence's own positions
+    n_rows     rows of the packed tensors (rows from row_start[-1] on are padding)
+    max_rows   upper bound of the rows of one sequence (default n_rows); prefix_attention leaves out rows beyond it
+    prefix_pages, prefix_len: a prefix that all sequences continue (its pages, its length in positions)
+
+    The tensors are read on the device when a call's work runs; they may be rewritten between calls, and between replays
+    of a captured graph.
+    """
+
+    def __init__(self, kv: PagedKV, row_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, n_rows: int,
+                 max_rows: Optional[int] = None, prefix_pages: Optional[torch.Tensor] = None, prefix_len: int = 0):
+        dev = kv.device
+        _int32("row_start", row_start, dev)
+        _int32("kv_len", kv_len, dev)
+        _int32("page_table", page_table, dev)
+        if row_start.dim() != 1 or kv_len.dim() != 1 or page_table.dim() != 2:
+            raise ValueError("row_start [n_seqs + 1], kv_len [n_seqs], page_table [n_seqs, stride]")
+        n_seqs = kv_len.shape[0]
+        if row_start.shape[0] != n_seqs + 1 or page_table.shape[0] != n_seqs or page_table.shape[1] < 1:
+            raise ValueError("row_start [n_seqs + 1], kv_len [n_seqs], page_table [n_seqs, stride]")
+        if n_rows < 0 or prefix_len < 0 or (max_rows is not None and max_rows < 1):
+            raise ValueError("n_rows and prefix_len must not be negative, max_rows at least 1")
+        if prefix_len > 0:
+            if prefix_pages is None or _int32("prefix_pages", prefix_pages, dev).numel() * kv.page_size < prefix_len:
+                raise ValueError("prefix_pages must hold prefix_len positions")
+        self.kv, self.n_seqs, self.n_rows = kv, n_seqs, n_rows
+        self.max_rows = max(1, n_rows if max_rows is None else min(max_rows, n_rows))
+        self._keep = (row_start, kv_len, page_table, prefix_pages)
+        self._c = _Batch(n_seqs, n_rows, row_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), page_table.shape[1],
+                         prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len)
+        self._kv_p, self._c_p = C.byref(kv._c), C.byref(self._c)
+        self._ws_bytes = {}
+
+    # ------------------------------------------------------------------ checks shared by the calls
+    def _rows(self, name: str, t: torch.Tensor, heads: Optional[int], dtypes) -> _Rows:
+        _cuda_tensor(name, t, self.kv.device)
+        if t.dim() != 3 or t.shape[0] != self.n_rows or t.shape[2] != self.kv.head_dim or (heads is not None and t.shape[1] != heads):
+            raise ValueError(f"{name} must be [{self.n_rows}, {heads if heads is not None else 'heads'}, {self.kv.head_dim}], got {tuple(t.shape)}")
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name} must be one of {dtypes}, got {t.dtype}")
+        if t.stride(2) != 1:
+            raise ValueError(f"the dims of {name} must be contiguous")
+        return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+    def _out(self, out: Optional[torch.Tensor], q: torch.Tensor) -> torch.Tensor:
+        shape = (self.n_rows, q.shape[1], self.kv.head_dim)
+        if out is None:
+            return torch.empty(shape, dtype=self.kv.dtype, device=self.kv.device)
+        _cuda_tensor("out", out, self.kv.device)
+        if tuple(out.shape) != shape or out.dtype != self.kv.dtype or not out.is_contiguous():
+            raise ValueError(f"out must be contiguous {shape} of {self.kv.dtype}")
+        return out
+
+    # ------------------------------------------------------------------ the calls
+    def append(self, block: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rope: Optional[torch.Tensor] = None,
+               interleaved: bool = False, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
+               eps: float = 1e-5, positions: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Norm (where a gain fp32 [head_dim] is given) and rotation (where a rope_table is given) of q and k, K and V into the
+        cache's block; returns the finished q [n_rows, heads, head_dim] in the cache's type.  q, k, v: [n_rows, heads, head_dim]
+        views (slices of a fused projection), fp32 or the cache's type.  Rows left out (padding, pages or positions out of
+        range) keep what `out` held.  positions: int32 [n_rows], instead of prefix_len + own position."""
+        kv = self.kv
+        types = (kv.dtype, torch.float32)
+        a = _Append()
+        a.q, a.k, a.v = self._rows("q", q, None, types), self._rows("k", k, kv.n_kv_heads, types), self._rows("v", v, kv.n_kv_heads, types)
+        if q.dtype != k.dtype or q.dtype != v.dtype:
+            raise TypeError("q, k and v must have one type")
+        a.block, a.n_heads, a.x_dtype, a.eps, a.interleaved = block, q.shape[1], _TYPES[q.dtype], eps, 1 if interleaved else 0
+        for name, g in (("q_gain", q_gain), ("k_gain", k_gain)):
+            if g is not None:
+                _cuda_tensor(name, g, kv.device)
+                if g.dtype != torch.float32 or tuple(g.shape) != (kv.head_dim,) or not g.is_contiguous():
+                    raise ValueError(f"{name} must be contiguous float32 [{kv.head_dim}]")
+                setattr(a, name, g.data_ptr())
+        if rope is not None:
+            _cuda_tensor("rope", rope, kv.device)
+            if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or 2 * rope.shape[1] > kv.head_dim:
+                raise ValueError("rope must be a rope_table of at most head_dim dims")
+            a.rope, a.rope_positions, a.rotary_dim = rope.data_ptr(), rope.shape[0], 2 * rope.shape[1]
+        if positions is not None:
+            if tuple(_int32("positions", positions, kv.device).shape) != (self.n_rows,):
+                raise ValueError(f"positions must be [{self.n_rows}]")
+            a.positions = positions.data_ptr()
+        with _Target(kv.device, stream) as s:
+            out = self._out(out, q)
+            a.q_out = out.data_ptr()
+            _check(lib().swift_kv_append(self._kv_p, self._c_p, C.byref(a), s))
+        return out
+
+    def _attention(self, block: int, q: torch.Tensor, scale: Optional[float]) -> _Attention:
+        rows = self._rows("q", q, None, (self.kv.dtype,))
+        return _Attention(block, q.shape[1], rows, 1.0 / math.sqrt(self.kv.head_dim) if scale is None else scale, None)
+
+    def prompt_attention(self, block: int, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Causal attention of every row over the prefix and its sequence's own positions up to its own; [n_rows, heads,
+        head_dim] in the cache's type.  scale defaults to head_dim ** -0.5.  Padding rows keep what `out` held."""
+        a = self._attention(block, q, scale)
+        with _Target(self.kv.device, stream) as s:
+            out = self._out(out, q)
+            a.out = out.data_ptr()
+            _check(lib().swift_prompt_attention(self._kv_p, self._c_p, C.byref(a), s))
+        return out
+
+    def prefix_attention(self, block: int, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """The same function for few rows per sequence: what all rows share of the prefix is computed once for all of them.
+        Rows of a sequence beyond max_rows are left out."""
+        a = self._attention(block, q, scale)
+        heads = q.shape[1]
+        need = self._ws_bytes.get(heads)
+        if need is None:
+            need = lib().swift_prefix_workspace_bytes(self._kv_p, self._c_p, heads, self.max_rows)
+            if need == 0:
+                raise SwiftError(1, lib().swift_batch_error().decode())
+            self._ws_bytes[heads] = need
+        with _Target(self.kv.device, stream) as s:
+            out = self._out(out, q)
+            a.out = out.data_ptr()
+            ws = torch.empty(need, dtype=torch.uint8, device=self.kv.device)     # of this call alone; the allocator aligns to 512
+            _check(lib().swift_prefix_attention(self._kv_p, self._c_p, C.byref(a), self.max_rows, _DevBuf(ws.data_ptr(), need), s))
+        return out
+
+
+def batch_sync(device="cuda", stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Waits for the stream and raises SwiftError if a bounded device-side wait of an attention call ran out (ETIMEOUT)."""
+    device = stream.device if stream is not None else torch.device(device)
+    if device.type != "cuda":
+        raise ValueError("batch_sync needs a CUDA device")
+    if device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    with _Target(device, stream) as s:
+        _check(lib().swift_batch_sync(s))
