@@ -2,15 +2,17 @@
 // swift_kv_append, swift_prompt_attention and swift_prefix_attention.  No context and no state between calls.
 #include "../../include/swift.h"
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
 
 // This translation unit gets its own copies of the shared device code (separate namespace).
 #define swk swk_batch
-#include "kernels_batch.cuh"
+#include "kernels_batch_tc.cuh"
 
 using namespace swk;
 
@@ -110,7 +112,7 @@ swift_status check_attention(const swift_paged_kv* kv, const swift_row_batch* b,
         if (a->q.row_stride < 0 || a->q.head_stride < 0) return fail_batch(SWIFT_EINVAL, "negative strides");
     }
     av->q = a->q.ptr;
-    av->q_row_stride = a->q.row_stride;
+    av->q_row_stride = a->q.row_stride;                   // a stride over a single row or head means nothing
     av->q_head_stride = a->q.head_stride;
     av->pool = block_base(kv, a->block);
     av->page_elems = 2 * kv_elems(kv) * kv->n_blocks;
@@ -122,6 +124,102 @@ swift_status check_attention(const swift_paged_kv* kv, const swift_row_batch* b,
     av->max_rows = b->n_rows;
     av->scale = a->scale;
     return SWIFT_OK;
+}
+
+// ------------------------------------------------------------------------------ tensor-core attention
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder()
+{
+    static const EncodeTiled fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) f = nullptr;
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return fn;
+}
+
+// 16-bit tensor of `rank` dims, contiguous in the first; boxes start with 64 of them (128 bytes, one swizzle row).
+swift_status make_map(CUtensorMap* out, int dtype, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box)
+{
+    const EncodeTiled encode = encoder();
+    if (!encode) return fail_batch(SWIFT_ECUDA, "cuTensorMapEncodeTiled not available from the driver");
+    const cuuint32_t one[4] = {1, 1, 1, 1};
+    const CUresult r = encode(out, dtype == SWIFT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void*>(base),
+                              dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail_batch(SWIFT_EINVAL, "cuTensorMapEncodeTiled refused the tensor (code %d): strides of q beyond 2^40 bytes, or a cache of odd size", (int)r);
+    return SWIFT_OK;
+}
+
+// [page][block, K/V, kv head][slot][dim]; a box is one page's slots of one plane
+swift_status make_kv_map(const swift_paged_kv* kv, CUtensorMap* out)
+{
+    const cuuint64_t D2 = 2ull * kv->head_dim, planes = 2ull * kv->n_blocks * kv->n_kv_heads;
+    const cuuint64_t dims[4] = {(cuuint64_t)kv->head_dim, (cuuint64_t)kv->page_size, planes, (cuuint64_t)kv->n_pages};
+    const cuuint64_t strides[3] = {D2, D2 * kv->page_size, D2 * kv->page_size * planes};
+    const cuuint32_t box[4] = {64, (cuuint32_t)kv->page_size, 1, 1};
+    return make_map(out, kv->dtype, kv->pool, 4, dims, strides, box);
+}
+
+// [row][head][dim]; a box is one tile: the heads of a group for rows_per_tile rows
+swift_status make_q_map(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, int rows_per_tile, CUtensorMap* out)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)kv->head_dim, (cuuint64_t)av.n_heads, (cuuint64_t)bv.n_rows};
+    const cuuint64_t strides[2] = {2ull * av.q_head_stride, 2ull * av.q_row_stride};
+    const cuuint32_t box[3] = {64, (cuuint32_t)(av.n_heads / av.n_kv_heads), (cuuint32_t)rows_per_tile};
+    return make_map(out, kv->dtype, av.q, 3, dims, strides, box);
+}
+
+int multiprocessors()
+{
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+    return n;
+}
+
+// A kernel's shared-memory size is set once per device.
+template <typename K> cudaError_t allow_smem(K kernel, int bytes, std::atomic<unsigned long long>& done)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < 64 && (done.load() >> dev & 1))) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev);
+    return e;
+}
+
+template <typename T, int HALVES>
+cudaError_t launch_tc(const CUtensorMap& kv_map, const CUtensorMap& q_map, const BatchView& bv, const BtArgs& g, int grid, cudaStream_t s)
+{
+    static std::atomic<unsigned long long> done{0};
+    const cudaError_t e = allow_smem(attn_batch_tc_kernel<T, HALVES>, BtShape<HALVES>::SMEM_BYTES, done);
+    if (e != cudaSuccess) return e;
+    return launch(attn_batch_tc_kernel<T, HALVES>, dim3(grid), BT_THREADS, BtShape<HALVES>::SMEM_BYTES, s, false, kv_map, q_map, bv, g);
+}
+
+// The many-row kernel in one of its three modes; items: an upper bound of its pieces of work.
+swift_status run_tc(const swift_paged_kv* kv, const BatchView& bv, BtArgs g, long long items, cudaStream_t s)
+{
+    CUtensorMap kv_map, q_map;
+    swift_status st = make_kv_map(kv, &kv_map);
+    if (st == SWIFT_OK) st = make_q_map(kv, bv, g.a, g.rows_per_tile, &q_map);
+    if (st != SWIFT_OK) return st;
+    const int sms = multiprocessors(), grid = (int)(items < sms ? items : sms);
+    const bool wide = kv->head_dim > 64, bf16 = kv->dtype == SWIFT_BF16;
+    const cudaError_t e = bf16 ? (wide ? launch_tc<__nv_bfloat16, 2>(kv_map, q_map, bv, g, grid, s) : launch_tc<__nv_bfloat16, 1>(kv_map, q_map, bv, g, grid, s))
+                               : (wide ? launch_tc<__half, 2>(kv_map, q_map, bv, g, grid, s) : launch_tc<__half, 1>(kv_map, q_map, bv, g, grid, s));
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+
+// Pieces of work of the modes that take each sequence by itself: pairs of tiles per sequence, at most.
+long long pair_bound(const BatchView& bv, int n_kv_heads, int rows_per_tile)
+{
+    const long long some = bv.n_seqs < bv.n_rows ? bv.n_seqs : bv.n_rows;
+    return (bv.n_rows / (2 * rows_per_tile) + some) * n_kv_heads;
 }
 
 cudaError_t launch_rows(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, cudaStream_t s)
@@ -247,9 +345,18 @@ swift_status swift_prompt_attention(const swift_paged_kv* kv, const swift_row_ba
     swift_status st = check_attention(kv, batch, args, &bv, &av);
     if (st != SWIFT_OK) return st;
     if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
-    const cudaError_t e = launch_rows(kv, bv, av, (cudaStream_t)cuda_stream);
-    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
-    return SWIFT_OK;
+    const int group = av.n_heads / av.n_kv_heads;
+    if (!tensor_core_shape(kv) || group > BT_ROWS) {
+        const cudaError_t e = launch_rows(kv, bv, av, (cudaStream_t)cuda_stream);
+        if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+        return SWIFT_OK;
+    }
+    BtArgs g = {};
+    g.a = av;
+    g.mode = BT_PROMPT;
+    g.block = args->block;
+    g.rows_per_tile = BT_ROWS / group;
+    return run_tc(kv, bv, g, pair_bound(bv, av.n_kv_heads, g.rows_per_tile), (cudaStream_t)cuda_stream);
 }
 
 size_t swift_prefix_workspace_bytes(const swift_paged_kv* kv, const swift_row_batch* batch, int32_t n_heads, int32_t max_rows)
@@ -283,8 +390,17 @@ swift_status swift_prefix_attention(const swift_paged_kv* kv, const swift_row_ba
 
 swift_status swift_batch_sync(void* cuda_stream)
 {
-    const cudaError_t e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
+    int error = 0;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&error, batch_wait_error, sizeof error, 0, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "the stream's work failed: %s", cudaGetErrorString(e));
+    if (error) {
+        const int none = 0;
+        e = cudaMemcpyToSymbolAsync(batch_wait_error, &none, sizeof none, 0, cudaMemcpyHostToDevice, s);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+        return fail_batch(SWIFT_ETIMEOUT, "a device-side wait of an attention call ran out of time");
+    }
     return SWIFT_OK;
 }
 

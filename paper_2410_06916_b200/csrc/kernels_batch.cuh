@@ -370,9 +370,9 @@ __global__ void __launch_bounds__(128) attn_rows_kernel(BatchView b, AttnView a)
             s = 0.f;
             for (int d = 0; d < D; ++d) s = fmaf(q_sh[warp][d], to_float(k[d]), s);
         }
+        if (!__any_sync(FULL_WARP, at >= 0)) continue;    // nothing here
         const float m_new = fmaxf(m, warp_max(s));
-        if (m_new == -INFINITY) continue;                 // nothing visible so far
-        const float shrink = expf(m - m_new), e_s = expf(s - m_new);
+        const float shrink = expf(m - m_new), e_s = at >= 0 ? expf(s - m_new) : 0.f;
         l = l * shrink + warp_sum(e_s);
         m = m_new;
 #pragma unroll
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(128) attn_rows_kernel(BatchView b, AttnView a)
         }
     }
     T* out = reinterpret_cast<T*>(a.out) + ((size_t)row * a.n_heads + h) * D;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;           // 0: the row sees nothing
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (lane + 32 * e < D) store_val(out + lane + 32 * e, o[e] * inv);

@@ -1,0 +1,573 @@
+// Attention of many query rows over the paged cache on the 5th-generation tensor cores (sm_100a): whole prompts, and the
+// rows of all sequences against a prefix that they share.
+//
+//     O = softmax(scale Q K^T) V,   one pass over the keys with a running maximum m and sum l per query row.
+//
+// Tiles.  A CTA takes two tiles of 128 query rows of one kv head; a tile packs the G query heads of that kv head's group,
+// TQ = 128 / G tokens of G heads, so that a key is read once for the whole group, short sequences still fill a tile and
+// the causal edge cuts through few tokens.  Keys come in tiles of 128.  S = Q K^T (128 x 128, fp32) and O (128 x D, fp32)
+// live in TMEM; the softmax warps overwrite S with the 16-bit probabilities P, which the second product reads as its
+// A operand straight from TMEM.  With both tiles 2 (128 + D) of the 512 columns are in use.
+//
+// Overlap.  While the softmax of tile A runs, the tensor pipe works on tile B, and the other way round: per key tile the
+// pipe has 2 x 4 x 128^3 multiply-adds (2048 cycles at D = 128) and each of the SM's four schedulers 2 warps x 128
+// exponentials (2048 cycles of its special function unit), so neither may wait for the other.  P is handed over in two
+// halves, so that its product starts while the second half is still being computed.
+//
+// Rescaling.  O is rescaled only when a row's maximum has grown by more than 2^8 since the last time (the probabilities
+// are then at most 2^8, which both 16-bit types hold); a softmax warp does it itself, between the arrival of S and its own
+// hand-over of P: S(j) is committed behind the product with P(j-1), so nothing else touches O then.
+//
+// P is rounded to the cache's type: a relative error of half a step per probability, of the size of the result's own
+// rounding.  The second product has no mixed-type form, and two of them (P as hi + lo) would cost half as much again.
+// With fp16 the probabilities carry a factor 2^7, which keeps those a millionth of the largest away from subnormals.
+//
+// Pages.  A key tile is fetched page by page with 4-D TMA boxes {64 dims, page slots, 1 plane, 1 page}, 128-byte swizzle;
+// pages outside the pool and pages behind the end are asked for beyond the last page, which fills zeros.  V's slots behind
+// the end within the last page are zeroed in shared memory, since 0 x NaN would reach O; K needs no such care, its scores
+// are masked.  Every wait is bounded.
+#pragma once
+#include <type_traits>
+
+#include "kernels_batch.cuh"
+#include "kernels_gemm_tc.cuh"
+
+namespace swk {
+
+// Three warpgroups: two of softmax warps, one with the TMA warp, the MMA warp and two idle ones.  Launched with 168 registers
+// per thread (64512 of the SM's 65536); the third group gives up 80 of them and the softmax groups, which hold a row of
+// 128 scores per thread, take 40 more: 2 x 128 x 208 + 128 x 88 = 64512.
+constexpr int BT_THREADS = 384;
+constexpr int BT_SOFTMAX_REGS = 208, BT_OTHER_REGS = 88;
+constexpr int BT_KEYS = 128;        // keys per tile
+constexpr int BT_ROWS = 128;        // packed query rows per tile
+constexpr int BT_PAGE_RING = 16;    // page-validity words kept (more than the key tiles ever in flight)
+constexpr float BT_GROW = 8.f;      // growth of the maximum (in powers of two) that triggers a rescaling
+
+enum { BT_PROMPT = 0, BT_PREFIX = 1, BT_OWN = 2 };
+
+template <int HALVES> struct BtShape {                                // D up to 64 * HALVES
+    static constexpr int DP = 64 * HALVES;
+    static constexpr int SLOT_BYTES = BT_KEYS * 128 * HALVES;         // one K or V tile
+    static constexpr int Q_BYTES = BT_ROWS * 128 * HALVES;            // one query tile
+    static constexpr int SLOTS = HALVES == 2 ? 5 : 10;
+    static constexpr int BAR_BYTES = 512;
+    static constexpr int SMEM_BYTES = 1024 + 2 * Q_BYTES + SLOTS * SLOT_BYTES + BAR_BYTES;
+};
+
+struct BtArgs {
+    AttnView a;
+    int mode, block, rows_per_tile;                                   // rows_per_tile: tokens of a tile (TQ)
+    int splits;                                                       // BT_PREFIX: cuts of the prefix
+    float* part_o;                                                    // [slot][row][head][DP] fp32, unnormalised
+    float2* part_ml;                                                  // [slot][row][head]: maximum in powers of two, sum
+    int part_slot;                                                    // BT_OWN: its slot
+};
+
+struct BtItem {
+    int seq, r0, n, len, t0, kvh;                                     // t0: first token of the pair within the sequence
+    int first_tile, np, slot;                                         // np: prefix tiles counted from first_tile on (then own tiles)
+    int tiles[2];                                                     // key tiles of tile A and of tile B
+};
+
+// The idx-th piece of work, found by a whole warp; false when there are fewer.
+__device__ __forceinline__ bool bt_locate(const BatchView& b, const BtArgs& g, int idx, BtItem& it)
+{
+    const int lane = threadIdx.x & 31, Hk = g.a.n_kv_heads, TQ = g.rows_per_tile, pair_rows = 2 * TQ;
+    const int prefix_tiles = (b.prefix_len + BT_KEYS - 1) / BT_KEYS;
+    it.first_tile = 0;
+    it.slot = g.part_slot;
+    if (g.mode == BT_PREFIX) {
+        const int n = min(max(b.row_start[b.n_seqs], 0), b.n_rows), pairs = (n + pair_rows - 1) / pair_rows;
+        if (idx >= pairs * Hk * g.splits) return false;
+        const int s = idx % g.splits, rest = idx / g.splits;
+        it.seq = -1;
+        it.r0 = 0;
+        it.n = n;
+        it.len = 0;
+        it.kvh = rest % Hk;
+        it.t0 = rest / Hk * pair_rows;
+        it.slot = s;
+        it.first_tile = (int)((long long)prefix_tiles * s / g.splits);
+        it.np = (int)((long long)prefix_tiles * (s + 1) / g.splits) - it.first_tile;
+        it.tiles[0] = it.np;
+        it.tiles[1] = it.t0 + TQ < n ? it.np : 0;
+        return true;
+    }
+    for (int base = 0; base < b.n_seqs; base += 32) {
+        SeqSpan sp = {0, 0, 0};
+        if (base + lane < b.n_seqs) sp = seq_span(b, base + lane);
+        const int mine = (sp.n + pair_rows - 1) / pair_rows * Hk;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(FULL_WARP, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const unsigned m = __ballot_sync(FULL_WARP, idx < upto);
+        if (m == 0) {
+            idx -= __shfl_sync(FULL_WARP, upto, 31);
+            continue;
+        }
+        const int at = __ffs(m) - 1;
+        it.seq = base + at;
+        it.r0 = __shfl_sync(FULL_WARP, sp.r0, at);
+        it.n = __shfl_sync(FULL_WARP, sp.n, at);
+        it.len = __shfl_sync(FULL_WARP, sp.len, at);
+        idx -= __shfl_sync(FULL_WARP, upto - mine, at);
+        const int pairs = (it.n + pair_rows - 1) / pair_rows;
+        it.kvh = idx % Hk;
+        it.t0 = (pairs - 1 - idx / Hk) * pair_rows;                   // the longest pieces of a sequence first
+        it.np = g.mode == BT_OWN ? 0 : prefix_tiles;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int t_end = min(it.n, it.t0 + (x + 1) * TQ);        // tokens of this tile end here
+            const bool some = it.t0 + x * TQ < it.n;
+            const int seen = min(max(it.len - it.n + t_end, 0), it.len);
+            it.tiles[x] = some ? it.np + (seen + BT_KEYS - 1) / BT_KEYS : 0;
+        }
+        return true;
+    }
+    return false;
+}
+
+// ------------------------------------------------------------------------------ PTX wrappers
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Descriptor of a V tile as the B operand [keys][dims], dims contiguous ("MN-major"): 64-dim groups one box apart, groups
+// of 8 keys 1024 bytes apart, 128-byte swizzle.
+__device__ __forceinline__ uint64_t tc_smem_desc_mn(uint32_t addr)
+{
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)((BT_KEYS * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+                 "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+                   "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]),
+                   "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]),
+                   "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const float (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+                 "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+                 ::"f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]),
+                   "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]), "f"(r[16]), "f"(r[17]), "f"(r[18]), "f"(r[19]), "f"(r[20]),
+                   "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]), "f"(r[25]), "f"(r[26]), "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]),
+                   "f"(r[31]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&u)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+                 ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]),
+                   "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ int batch_wait_error;                                      // set when a bounded wait ran out; swift_batch_sync reports it
+
+// A wait of one role: bounded, and over at once when another role has given up.
+__device__ __forceinline__ bool bt_wait(uint32_t bar, uint32_t parity, volatile int* abort_sh)
+{
+    const long long t0 = clock64();
+    for (uint32_t it = 0;; ++it) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if ((it & 63u) == 63u) {
+            if (*abort_sh) return false;
+            if (clock64() - t0 > TC_WAIT_CYCLES) {
+                *abort_sh = 1;
+                atomicExch(&batch_wait_error, TC_ERR_TIMEOUT);
+                return false;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------ the kernel
+// grid = persistent CTAs (at most one per SM), each taking pieces blockIdx.x, + gridDim.x, ...; block = 384.
+template <typename T, int HALVES>
+__global__ void __launch_bounds__(BT_THREADS, 1)
+attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_q, BatchView b, BtArgs g)
+{
+    typedef BtShape<HALVES> S;
+    constexpr int DP = S::DP;
+    constexpr bool HALF = std::is_same<T, __half>::value;
+    constexpr uint32_t TYPE = HALF ? 0u : 1u;                         // operand format of both products
+    constexpr uint32_t IDESC_QK = (1u << 4) | (TYPE << 7) | (TYPE << 10) | ((uint32_t)(BT_KEYS >> 3) << 17) | ((uint32_t)(BT_ROWS >> 4) << 24);
+    constexpr uint32_t IDESC_PV = (1u << 4) | (TYPE << 7) | (TYPE << 10) | (1u << 16) | ((uint32_t)(DP >> 3) << 17) | ((uint32_t)(BT_ROWS >> 4) << 24);
+    constexpr float BIAS = HALF ? 7.f : 0.f;
+
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t q_sh = base, ring = base + 2 * S::Q_BYTES, bars = ring + S::SLOTS * S::SLOT_BYTES;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (S::SLOTS + s); };
+    const uint32_t b2 = bars + 16u * S::SLOTS;
+    auto q_full = [&](int x) { return b2 + 8u * x; };
+    auto q_empty = [&](int x) { return b2 + 16u + 8u * x; };
+    auto s_full = [&](int x) { return b2 + 32u + 8u * x; };
+    auto p_ready = [&](int x, int h) { return b2 + 48u + 8u * (2 * x + h); };
+    auto o_full = [&](int x) { return b2 + 80u + 8u * x; };
+    const uint32_t landed = b2 + 96u;
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ int abort_flag;
+    __shared__ unsigned page_bits[BT_PAGE_RING];                      // bit p: page p of that key tile lies in the pool
+    volatile int* abort_sh = &abort_flag;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G = g.a.n_heads / g.a.n_kv_heads, TQ = g.rows_per_tile;
+    if (warp == 9) {
+        if (lane == 0) {
+            for (int s = 0; s < S::SLOTS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+            for (int x = 0; x < 2; ++x) {
+                mbar_init(q_full(x), 1); mbar_init(q_empty(x), 1); mbar_init(s_full(x), 1); mbar_init(o_full(x), 1);
+                mbar_init(p_ready(x, 0), 4); mbar_init(p_ready(x, 1), 4);
+            }
+            mbar_init(landed, 1);
+            abort_flag = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_sh)), "r"(512));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (tid == 256) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_kv) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_sh;
+    auto s_col = [&](int x) { return tmem + 128u * x; };              // S, then P, of tile x
+    auto o_col = [&](int x) { return tmem + 256u + 128u * x; };
+
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(BT_OTHER_REGS));
+    if (warp == 8) {
+        // ---------------------------------------------------------------- TMA: queries, then K and V tiles in turn
+        const int per_tile = BT_KEYS >> b.page_shift;                 // pages per key tile, 1..16
+        const int pg = lane / HALVES, half = lane % HALVES;           // this lane's box of a tile
+        const bool boxed = pg < per_tile;
+        const uint32_t box_at = half * (BT_KEYS * 128) + (pg << b.page_shift) * 128;
+        uint32_t slot = 0, turn = 0, q_turn[2] = {0, 0}, landed_turn = 0;   // turn: parity of the ring's current pass
+        int tile_no = 0;
+        bool ok = true;
+        BtItem it;
+        for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
+            const int n_tiles = max(it.tiles[0], it.tiles[1]);
+            const int plane_k = (g.block * 2) * g.a.n_kv_heads + it.kvh, plane_v = plane_k + g.a.n_kv_heads;
+            if (lane == 0) {
+                for (int x = 0; ok && x < 2; ++x) {
+                    if (it.tiles[x] == 0) continue;
+                    ok = bt_wait(q_empty(x), q_turn[x] ^ 1u, abort_sh);
+                    if (!ok) break;
+                    mbar_expect_tx(q_full(x), (uint32_t)(TQ * G * 128 * HALVES));
+                    for (int hf = 0; hf < HALVES; ++hf)
+                        tma_load_3d(q_sh + x * S::Q_BYTES + hf * (BT_ROWS * 128), &map_q, 64 * hf, it.kvh * G, it.r0 + it.t0 + x * TQ, q_full(x));
+                }
+            }
+            for (int x = 0; x < 2; ++x)
+                if (it.tiles[x]) q_turn[x] ^= 1u;
+            ok = __shfl_sync(FULL_WARP, ok ? 1 : 0, 0) != 0;
+            for (int j = 0; ok && j < n_tiles; ++j, ++tile_no) {
+                const bool shared_part = j < it.np;
+                const int key0 = (shared_part ? it.first_tile + j : j - it.np) * BT_KEYS;
+                const int left = (shared_part ? b.prefix_len : it.len) - key0;            // keys of this tile that exist
+                int page = b.n_pages;                                 // beyond the last page: zeros
+                if (boxed && (pg << b.page_shift) < left) {
+                    const int at = (key0 >> b.page_shift) + pg;
+                    page = shared_part ? b.prefix_pages[at] : b.page_table[(size_t)it.seq * b.table_stride + at];
+                }
+                const bool good = (unsigned)page < (unsigned)b.n_pages;
+                if (!good) page = b.n_pages;
+                const unsigned bits = __ballot_sync(FULL_WARP, boxed && good && half == 0);
+                unsigned pages = 0;
+#pragma unroll
+                for (int p = 0; p < 32 / HALVES; ++p) pages |= ((bits >> (p * HALVES)) & 1u) << p;
+                const int tail = left & (b.page_size - 1);            // slots of the last page that hold something
+                const bool cut = left < BT_KEYS && tail != 0 && ((pages >> (left >> b.page_shift)) & 1u);
+#pragma unroll 1
+                for (int kv = 0; kv < 2; ++kv) {
+                    const bool mend = kv == 1 && cut;                 // V tile with unwritten slots: zeroed before the product may read them
+                    if (lane == 0) {
+                        ok = bt_wait(empty(slot), turn ^ 1u, abort_sh);
+                        if (ok) {
+                            if (kv == 0) page_bits[tile_no & (BT_PAGE_RING - 1)] = pages;
+                            mbar_expect_tx(mend ? landed : full(slot), (uint32_t)S::SLOT_BYTES);
+                        }
+                    }
+                    ok = __shfl_sync(FULL_WARP, ok ? 1 : 0, 0) != 0;
+                    if (!ok) break;
+                    const uint32_t dst = ring + slot * S::SLOT_BYTES;
+                    if (boxed) tma_load_4d(dst + box_at, &map_kv, 64 * half, 0, kv ? plane_v : plane_k, page, mend ? landed : full(slot));
+                    if (mend) {
+                        bool here = true;
+                        if (lane == 0) here = bt_wait(landed, landed_turn, abort_sh);
+                        landed_turn ^= 1u;
+                        ok = __shfl_sync(FULL_WARP, here ? 1 : 0, 0) != 0;
+                        if (!ok) break;
+                        const int row1 = ((left >> b.page_shift) + 1) << b.page_shift;
+                        for (int i = lane; i < (row1 - left) * 8 * HALVES; i += 32) {
+                            const int row = left + i / (8 * HALVES), piece = i % (8 * HALVES);
+                            const uint32_t a = dst + (piece >> 3) * (BT_KEYS * 128) + row * 128 + (piece & 7) * 16;    // whole rows: the swizzle stays inside
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a), "r"(0) : "memory");
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(full(slot));
+                    }
+                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                }
+            }
+        }
+        // After a wait that ran out: the copies still on their way must land before the block's shared memory is given back.
+        if (!ok && lane == 0) {
+            const long long t0 = clock64();
+            while (clock64() - t0 < 2000000LL) { }                    // about a millisecond
+        }
+    } else if (warp == 9) {
+        // ---------------------------------------------------------------- tensor pipe
+        uint32_t slot = 0, turn = 0, q_turn[2] = {0, 0}, p_turn[2] = {0, 0};
+        bool ok = true;
+        BtItem it;
+        for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
+            if (lane == 0) {
+                const int n_tiles = max(it.tiles[0], it.tiles[1]);
+                auto scores = [&](int x, uint32_t k_sh) {             // S(x) = Q(x) K^T
+                    const uint64_t qd = tc_smem_desc(q_sh + x * S::Q_BYTES), kd = tc_smem_desc(k_sh);
+#pragma unroll
+                    for (int k = 0; k < 4 * HALVES; ++k) {            // 16 dims a step: 32 bytes, 64 dims a box
+                        const uint64_t step = (uint64_t)(((k >> 2) * (BT_KEYS * 128) + (k & 3) * 32) >> 4);
+                        tc_mma(s_col(x), qd + step, kd + step, IDESC_QK, k > 0);
+                    }
+                    tc_commit(s_full(x));
+                };
+                auto weigh = [&](int x, uint32_t v_sh, bool first) {  // O(x) (+)= P(x) V
+                    const uint64_t vd = tc_smem_desc_mn(v_sh);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (!bt_wait(p_ready(x, h), p_turn[x], abort_sh)) return false;
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 4 * h; k < 4 * h + 4; ++k)       // 16 keys a step: 8 columns of P, 2048 bytes of V
+                            tc_mma_ts(o_col(x), s_col(x) + 8 * k, vd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, !first || k > 0);
+                    }
+                    p_turn[x] ^= 1u;
+                    return true;
+                };
+                for (int x = 0; ok && x < 2; ++x)
+                    if (it.tiles[x]) { ok = bt_wait(q_full(x), q_turn[x], abort_sh); q_turn[x] ^= 1u; }
+                if (ok && n_tiles > 0) {
+                    ok = bt_wait(full(slot), turn, abort_sh);
+                    tc_fence_after();
+                    if (ok) {
+                        for (int x = 0; x < 2; ++x)
+                            if (it.tiles[x]) {
+                                scores(x, ring + slot * S::SLOT_BYTES);
+                                if (it.tiles[x] == 1) tc_commit(q_empty(x));
+                            }
+                        tc_commit(empty(slot));
+                        if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                    }
+                }
+                for (int j = 0; ok && j < n_tiles; ++j) {
+                    const uint32_t v_slot = slot, v_turn = turn;
+                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                    ok = bt_wait(full(v_slot), v_turn, abort_sh);
+                    const bool more = j + 1 < n_tiles;
+                    for (int x = 0; ok && x < 2; ++x) {
+                        if (j < it.tiles[x]) {
+                            ok = weigh(x, ring + v_slot * S::SLOT_BYTES, j == 0);
+                            if (!ok) break;
+                            if (j + 1 == it.tiles[x]) tc_commit(o_full(x));
+                        }
+                        if (x == 1) tc_commit(empty(v_slot));
+                        if (j + 1 < it.tiles[x]) {
+                            ok = bt_wait(full(slot), turn, abort_sh);
+                            if (!ok) break;
+                            tc_fence_after();
+                            scores(x, ring + slot * S::SLOT_BYTES);
+                            if (j + 2 == it.tiles[x]) tc_commit(q_empty(x));
+                        }
+                    }
+                    if (ok && more) {
+                        tc_commit(empty(slot));
+                        if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                    }
+                }
+            }
+            ok = __shfl_sync(FULL_WARP, ok ? 1 : 0, 0) != 0;
+        }
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(BT_SOFTMAX_REGS));
+        // ---------------------------------------------------------------- softmax: a thread owns one packed query row
+        const int x = warp >> 2, rho = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_at = s_col(x) + lanes, o_at = o_col(x) + lanes;
+        const int tok = rho / G, head_in = rho - tok * G;
+        const float c = g.a.scale * 1.4426950408889634f;              // scores in powers of two
+        uint32_t s_turn = 0, o_turn = 0;
+        int tile_no = 0;
+        bool ok = true;
+        BtItem it;
+        for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
+            const int n_tiles = max(it.tiles[0], it.tiles[1]), mine = it.tiles[x];
+            const int t = it.t0 + x * TQ + tok;                       // token within the sequence
+            const bool live = tok < TQ && t < it.n;
+            const int own = it.len - it.n + t;                        // own position: keys 0 .. own are seen
+            float m = -INFINITY, l = 0.f;
+            for (int j = 0; j < mine; ++j) {
+                ok = bt_wait(s_full(x), s_turn, abort_sh);
+                if (!ok) break;
+                s_turn ^= 1u;
+                tc_fence_after();
+                float s[4][32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, s[i]);
+                const int key0 = (j < it.np ? it.first_tile + j : j - it.np) * BT_KEYS;
+                const int seen = j < it.np ? b.prefix_len - key0 : own + 1 - key0;        // this row sees keys below this
+                const unsigned pages = page_bits[(tile_no + j) & (BT_PAGE_RING - 1)];
+                const unsigned all = 0xFFFFu >> (16 - (BT_KEYS >> b.page_shift));
+                tmem_wait_ld();
+                if (__any_sync(FULL_WARP, seen < BT_KEYS) || pages != all) {
+#pragma unroll
+                    for (int i = 0; i < BT_KEYS; ++i)
+                        if (i >= seen || !((pages >> (i >> b.page_shift)) & 1u)) s[i >> 5][i & 31] = -INFINITY;
+                }
+                float mx[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    mx[q] = fmaxf(s[q][0], s[q][1]);
+#pragma unroll
+                    for (int i = 2; i < 32; i += 2) mx[q] = fmaxf(fmaxf(mx[q], s[q][i]), s[q][i + 1]);
+                }
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                // a warp rescales when a row of its own has outgrown what its sums are scaled by
+                const bool grow = top > m && (m == -INFINITY || (top - m) * c > BT_GROW);
+                if (__any_sync(FULL_WARP, grow)) {
+                    const float m_new = fmaxf(m, top);
+                    const float shrink = m == m_new ? 1.f : ex2((m - m_new) * c);
+                    l *= shrink;
+                    m = m_new;
+                    if (j > 0) {
+#pragma unroll 1
+                        for (int i = 0; i < DP; i += 32) {
+                            float o[32];
+                            tmem_ld32(o_at + i, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] *= shrink;
+                            tmem_st32(o_at + i, o);
+                        }
+                    }
+                }
+                const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int q = 2 * h; q < 2 * h + 2; ++q) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            const float p0 = ex2(fmaf(s[q][i], c, off)), p1 = ex2(fmaf(s[q][i + 1], c, off));
+                            sum[i & 2] += p0;
+                            sum[(i & 2) + 1] += p1;
+                            p[i >> 1] = pack2(p0, p1, T());
+                        }
+                        tmem_st16(s_at + 16 * q, p);
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_ready(x, h));
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            }
+            tile_no += n_tiles;
+            if (!ok) break;
+            if (mine > 0) {
+                ok = bt_wait(o_full(x), o_turn, abort_sh);
+                if (!ok) break;
+                o_turn ^= 1u;
+                tc_fence_after();
+            }
+            const int row = it.r0 + t, head = it.kvh * G + head_in;
+            const float inv = l == 0.f ? 0.f : 1.f / l;              // 0: the row sees nothing
+            if (g.mode != BT_PROMPT) {
+                const size_t at = ((size_t)it.slot * b.n_rows + row) * g.a.n_heads + head;
+                if (live) g.part_ml[at] = make_float2(m * c - BIAS, l);
+#pragma unroll 1
+                for (int i = 0; i < DP; i += 32) {
+                    float o[32];
+                    if (mine > 0) {
+                        tmem_ld32(o_at + i, o);
+                        tmem_wait_ld();
+                    }
+                    if (live && l != 0.f) {
+                        float4* dst = reinterpret_cast<float4*>(g.part_o + at * DP + i);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    }
+                }
+            } else {
+                T* dst = reinterpret_cast<T*>(g.a.out) + ((size_t)row * g.a.n_heads + head) * g.a.head_dim;
+#pragma unroll 1
+                for (int i = 0; i < DP; i += 32) {
+                    float o[32];
+                    if (mine > 0) {
+                        tmem_ld32(o_at + i, o);
+                        tmem_wait_ld();
+                    }
+                    if (live) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float v[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = l == 0.f ? 0.f : o[8 * e + k] * inv;
+                            if (i + 8 * e < g.a.head_dim) store8(dst + i + 8 * e, v);
+                        }
+                    }
+                }
+            }
+            tc_fence_before();                                        // O is read: the next piece's product may overwrite it
+        }
+    }
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+    }
+}
+
+} // namespace swk
