@@ -12,7 +12,7 @@
 
 // This translation unit gets its own copies of the shared device code (separate namespace).
 #define swk swk_batch
-#include "kernels_batch_tc.cuh"
+#include "kernels_batch_dec.cuh"
 
 using namespace swk;
 
@@ -154,13 +154,13 @@ swift_status make_map(CUtensorMap* out, int dtype, const void* base, int rank, c
     return SWIFT_OK;
 }
 
-// [page][block, K/V, kv head][slot][dim]; a box is one page's slots of one plane
-swift_status make_kv_map(const swift_paged_kv* kv, CUtensorMap* out)
+// [page][block, K/V, kv head][slot][dim]; a box is one plane's slots of a page, at most a tile of them
+swift_status make_kv_map(const swift_paged_kv* kv, int most_slots, CUtensorMap* out)
 {
     const cuuint64_t D2 = 2ull * kv->head_dim, planes = 2ull * kv->n_blocks * kv->n_kv_heads;
     const cuuint64_t dims[4] = {(cuuint64_t)kv->head_dim, (cuuint64_t)kv->page_size, planes, (cuuint64_t)kv->n_pages};
     const cuuint64_t strides[3] = {D2, D2 * kv->page_size, D2 * kv->page_size * planes};
-    const cuuint32_t box[4] = {64, (cuuint32_t)kv->page_size, 1, 1};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(kv->page_size < most_slots ? kv->page_size : most_slots), 1, 1};
     return make_map(out, kv->dtype, kv->pool, 4, dims, strides, box);
 }
 
@@ -192,25 +192,25 @@ template <typename K> cudaError_t allow_smem(K kernel, int bytes, std::atomic<un
 }
 
 template <typename T, int HALVES>
-cudaError_t launch_tc(const CUtensorMap& kv_map, const CUtensorMap& q_map, const BatchView& bv, const BtArgs& g, int grid, cudaStream_t s)
+cudaError_t launch_tc(const CUtensorMap& kv_map, const CUtensorMap& q_map, const BatchView& bv, const BtArgs& g, int grid, cudaStream_t s, bool after_previous)
 {
     static std::atomic<unsigned long long> done{0};
     const cudaError_t e = allow_smem(attn_batch_tc_kernel<T, HALVES>, BtShape<HALVES>::SMEM_BYTES, done);
     if (e != cudaSuccess) return e;
-    return launch(attn_batch_tc_kernel<T, HALVES>, dim3(grid), BT_THREADS, BtShape<HALVES>::SMEM_BYTES, s, false, kv_map, q_map, bv, g);
+    return launch(attn_batch_tc_kernel<T, HALVES>, dim3(grid), BT_THREADS, BtShape<HALVES>::SMEM_BYTES, s, after_previous, kv_map, q_map, bv, g);
 }
 
 // The many-row kernel in one of its three modes; items: an upper bound of its pieces of work.
-swift_status run_tc(const swift_paged_kv* kv, const BatchView& bv, BtArgs g, long long items, cudaStream_t s)
+swift_status run_tc(const swift_paged_kv* kv, const BatchView& bv, const BtArgs& g, long long items, cudaStream_t s, bool after_previous)
 {
     CUtensorMap kv_map, q_map;
-    swift_status st = make_kv_map(kv, &kv_map);
+    swift_status st = make_kv_map(kv, BT_KEYS, &kv_map);
     if (st == SWIFT_OK) st = make_q_map(kv, bv, g.a, g.rows_per_tile, &q_map);
     if (st != SWIFT_OK) return st;
     const int sms = multiprocessors(), grid = (int)(items < sms ? items : sms);
     const bool wide = kv->head_dim > 64, bf16 = kv->dtype == SWIFT_BF16;
-    const cudaError_t e = bf16 ? (wide ? launch_tc<__nv_bfloat16, 2>(kv_map, q_map, bv, g, grid, s) : launch_tc<__nv_bfloat16, 1>(kv_map, q_map, bv, g, grid, s))
-                               : (wide ? launch_tc<__half, 2>(kv_map, q_map, bv, g, grid, s) : launch_tc<__half, 1>(kv_map, q_map, bv, g, grid, s));
+    const cudaError_t e = bf16 ? (wide ? launch_tc<__nv_bfloat16, 2>(kv_map, q_map, bv, g, grid, s, after_previous) : launch_tc<__nv_bfloat16, 1>(kv_map, q_map, bv, g, grid, s, after_previous))
+                               : (wide ? launch_tc<__half, 2>(kv_map, q_map, bv, g, grid, s, after_previous) : launch_tc<__half, 1>(kv_map, q_map, bv, g, grid, s, after_previous));
     if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
     return SWIFT_OK;
 }
@@ -220,6 +220,158 @@ long long pair_bound(const BatchView& bv, int n_kv_heads, int rows_per_tile)
 {
     const long long some = bv.n_seqs < bv.n_rows ? bv.n_seqs : bv.n_rows;
     return (bv.n_rows / (2 * rows_per_tile) + some) * n_kv_heads;
+}
+
+swift_status run_prompt(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, int block, cudaStream_t s)
+{
+    BtArgs g = {};
+    g.a = av;
+    g.mode = BT_PROMPT;
+    g.block = block;
+    g.rows_per_tile = BT_ROWS / (av.n_heads / av.n_kv_heads);
+    return run_tc(kv, bv, g, pair_bound(bv, av.n_kv_heads, g.rows_per_tile), s, false);
+}
+
+// ------------------------------------------------------------------------------ few rows per sequence
+// How swift_prefix_attention runs a batch, from sizes the host knows.
+struct PrefixPlan {
+    bool rows;                  // row by row: no tensor-core form
+    bool prompt;                // each sequence by itself, no prefix to share and too many rows for the few-row kernel
+    bool few, prefix_few;       // the few-row kernel takes the sequences' own parts; and the prefix
+    int group, dp, mt, grid;
+    long long items;
+    int splits;                 // cuts of the prefix by the many-row kernel (0: it has no prefix work)
+    int slots;                  // parts per row that the many-row kernel leaves: splits, and the own part if it takes it
+    size_t many_o, many_ml, few_o, few_ml, first, last, bytes;   // offsets in the workspace
+};
+
+swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_heads, int max_rows, PrefixPlan* p)
+{
+    *p = PrefixPlan();
+    const int Hk = kv->n_kv_heads, sms = multiprocessors();
+    if (max_rows > bv.n_rows) max_rows = bv.n_rows;
+    p->group = n_heads / Hk;
+    p->dp = kv->head_dim > 64 ? 128 : 64;
+    size_t at = 0;
+    auto take = [&](size_t n) { const size_t o = at; at += (n + 255) / 256 * 256; return o; };
+    p->rows = !tensor_core_shape(kv) || p->group > BT_ROWS;
+    if (!p->rows) {
+        const long long own = (long long)max_rows * p->group, all = (long long)bv.n_rows * p->group;
+        p->few = own <= BD_MAX_ROWS;
+        p->prefix_few = p->few && bv.prefix_len > 0 && all <= BD_MAX_ROWS;
+        p->prompt = !p->few && bv.prefix_len == 0;
+        if (bv.prefix_len > 0 && !p->prefix_few && !p->prompt) {
+            // Cuts of the prefix: as many waves of (tile pairs x kv heads x cuts) as give the shortest time, a wave costing its
+            // share of the prefix and about one key tile of set-up and write-back.
+            const int tiles = ceil_div(bv.prefix_len, BT_KEYS), TQ = BT_ROWS / p->group;
+            const long long pairs = (long long)ceil_div(bv.n_rows, 2 * TQ) * Hk;
+            double best = 0;
+            for (int s = 1; s <= 64 && s <= tiles; ++s) {
+                const double cost = (double)ceil_div(pairs * s, sms) * (ceil_div(tiles, s) + 1.0);
+                if (p->splits == 0 || cost < best) { best = cost; p->splits = s; }
+            }
+        }
+        p->slots = p->splits + (!p->few && !p->prompt ? 1 : 0);
+        const size_t many = (size_t)p->slots * bv.n_rows * n_heads;
+        p->many_o = take(many * p->dp * 4);
+        p->many_ml = take(many * 8);
+        if (p->few) {
+            const long long rows = p->prefix_few ? (all > own ? all : own) : own;
+            p->mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+            p->items = (long long)(bv.n_seqs + (p->prefix_few ? 1 : 0)) * Hk;
+            p->grid = sms;
+            const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, BD_KEYS) + ceil_div(bv.prefix_len, BD_KEYS)) * Hk;
+            if (units > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a page table of %d x %d for %d kv heads is beyond 2^31 units of work", bv.n_seqs, bv.table_stride, Hk);
+            const size_t rows_all = (size_t)(p->items + p->grid) * 16 * p->mt;
+            p->few_o = take(rows_all * p->dp * 4);
+            p->few_ml = take(rows_all * 8);
+            p->first = take((size_t)p->items * 4);
+            p->last = take((size_t)p->items * 4);
+        }
+    }
+    p->bytes = at > 256 ? at : 256;
+    return SWIFT_OK;
+}
+
+template <typename T, int HALVES, int MT>
+cudaError_t launch_dec(const CUtensorMap& kv_map, const CUtensorMap& q_map, const BatchView& bv, const BdArgs& g, int grid, cudaStream_t s, bool after_previous)
+{
+    static std::atomic<unsigned long long> done{0};
+    const cudaError_t e = allow_smem(attn_batch_dec_kernel<T, HALVES, MT>, BdShape<HALVES>::smem_bytes(MT), done);
+    if (e != cudaSuccess) return e;
+    return launch(attn_batch_dec_kernel<T, HALVES, MT>, dim3(grid), BD_THREADS, BdShape<HALVES>::smem_bytes(MT), s, after_previous, kv_map, q_map, bv, g);
+}
+
+template <typename T>
+cudaError_t launch_dec_any(const PrefixPlan& p, const CUtensorMap& kv_map, const CUtensorMap& q_map, const BatchView& bv, const BdArgs& g, cudaStream_t s, bool after)
+{
+    if (p.dp == 128) {
+        if (p.mt == 1) return launch_dec<T, 2, 1>(kv_map, q_map, bv, g, p.grid, s, after);
+        if (p.mt == 2) return launch_dec<T, 2, 2>(kv_map, q_map, bv, g, p.grid, s, after);
+        return launch_dec<T, 2, 4>(kv_map, q_map, bv, g, p.grid, s, after);
+    }
+    if (p.mt == 1) return launch_dec<T, 1, 1>(kv_map, q_map, bv, g, p.grid, s, after);
+    if (p.mt == 2) return launch_dec<T, 1, 2>(kv_map, q_map, bv, g, p.grid, s, after);
+    return launch_dec<T, 1, 4>(kv_map, q_map, bv, g, p.grid, s, after);
+}
+
+swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, int block, const PrefixPlan& p, unsigned char* ws, cudaStream_t s)
+{
+    bool before = false;                                  // a kernel of this call has been launched
+    BtArgs t = {};
+    t.a = av;
+    t.block = block;
+    t.rows_per_tile = BT_ROWS / p.group;
+    t.part_o = reinterpret_cast<float*>(ws + p.many_o);
+    t.part_ml = reinterpret_cast<float2*>(ws + p.many_ml);
+    if (p.splits > 0) {
+        t.mode = BT_PREFIX;
+        t.splits = p.splits;
+        const swift_status st = run_tc(kv, bv, t, (long long)ceil_div(bv.n_rows, 2 * t.rows_per_tile) * av.n_kv_heads * p.splits, s, before);
+        if (st != SWIFT_OK) return st;
+        before = true;
+    }
+    BjArgs j = {};
+    j.a = av;
+    j.dp = p.dp;
+    j.item_rows = 16 * p.mt;
+    j.prefix_here = p.prefix_few;
+    j.own_here = p.few;
+    j.splits = p.slots;
+    j.many_o = t.part_o;
+    j.many_ml = t.part_ml;
+    j.few_o = reinterpret_cast<float*>(ws + p.few_o);
+    j.few_ml = reinterpret_cast<float2*>(ws + p.few_ml);
+    j.item_first = reinterpret_cast<int*>(ws + p.first);
+    j.item_last = reinterpret_cast<int*>(ws + p.last);
+    cudaError_t e = cudaSuccess;
+    if (p.few) {
+        BdArgs g = {};
+        g.a = av;
+        g.block = block;
+        g.prefix_here = p.prefix_few;
+        g.rows_per_box = 16 * p.mt / p.group;
+        g.part_o = reinterpret_cast<float*>(ws + p.few_o);
+        g.part_ml = reinterpret_cast<float2*>(ws + p.few_ml);
+        g.item_first = reinterpret_cast<int*>(ws + p.first);
+        g.item_last = reinterpret_cast<int*>(ws + p.last);
+        CUtensorMap kv_map, q_map;
+        swift_status st = make_kv_map(kv, BD_KEYS, &kv_map);
+        if (st == SWIFT_OK) st = make_q_map(kv, bv, av, g.rows_per_box, &q_map);
+        if (st != SWIFT_OK) return st;
+        e = kv->dtype == SWIFT_BF16 ? launch_dec_any<__nv_bfloat16>(p, kv_map, q_map, bv, g, s, before) : launch_dec_any<__half>(p, kv_map, q_map, bv, g, s, before);
+    } else {
+        t.mode = BT_OWN;
+        t.part_slot = p.splits;
+        const swift_status st = run_tc(kv, bv, t, pair_bound(bv, av.n_kv_heads, t.rows_per_tile), s, before);
+        if (st != SWIFT_OK) return st;
+    }
+    if (e == cudaSuccess) {
+        const dim3 grid(bv.n_rows, ceil_div(av.n_heads, 4));
+        e = kv->dtype == SWIFT_BF16 ? launch(attn_join_kernel<__nv_bfloat16>, grid, 128, 0, s, true, bv, j) : launch(attn_join_kernel<__half>, grid, 128, 0, s, true, bv, j);
+    }
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
 }
 
 cudaError_t launch_rows(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, cudaStream_t s)
@@ -345,18 +497,13 @@ swift_status swift_prompt_attention(const swift_paged_kv* kv, const swift_row_ba
     swift_status st = check_attention(kv, batch, args, &bv, &av);
     if (st != SWIFT_OK) return st;
     if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
-    const int group = av.n_heads / av.n_kv_heads;
-    if (!tensor_core_shape(kv) || group > BT_ROWS) {
-        const cudaError_t e = launch_rows(kv, bv, av, (cudaStream_t)cuda_stream);
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (!tensor_core_shape(kv) || av.n_heads / av.n_kv_heads > BT_ROWS) {
+        const cudaError_t e = launch_rows(kv, bv, av, s);
         if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
         return SWIFT_OK;
     }
-    BtArgs g = {};
-    g.a = av;
-    g.mode = BT_PROMPT;
-    g.block = args->block;
-    g.rows_per_tile = BT_ROWS / group;
-    return run_tc(kv, bv, g, pair_bound(bv, av.n_kv_heads, g.rows_per_tile), (cudaStream_t)cuda_stream);
+    return run_prompt(kv, bv, av, args->block, s);
 }
 
 size_t swift_prefix_workspace_bytes(const swift_paged_kv* kv, const swift_row_batch* batch, int32_t n_heads, int32_t max_rows)
@@ -367,7 +514,8 @@ size_t swift_prefix_workspace_bytes(const swift_paged_kv* kv, const swift_row_ba
         fail_batch(SWIFT_EINVAL, "n_heads %d, max_rows %d", n_heads, max_rows);
         return 0;
     }
-    return 256;
+    PrefixPlan p;
+    return plan_prefix(kv, bv, n_heads, max_rows, &p) == SWIFT_OK ? p.bytes : 0;
 }
 
 swift_status swift_prefix_attention(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args, int32_t max_rows,
@@ -379,13 +527,20 @@ swift_status swift_prefix_attention(const swift_paged_kv* kv, const swift_row_ba
     if (st != SWIFT_OK) return st;
     if (max_rows < 1) return fail_batch(SWIFT_EINVAL, "max_rows %d", max_rows);
     if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
-    const size_t need = swift_prefix_workspace_bytes(kv, batch, args->n_heads, max_rows);
+    PrefixPlan p;
+    st = plan_prefix(kv, bv, av.n_heads, max_rows, &p);
+    if (st != SWIFT_OK) return st;
     if (!workspace.dptr || !aligned(workspace.dptr, 256)) return fail_batch(SWIFT_EINVAL, "the workspace must be 256-byte aligned device memory");
-    if (workspace.bytes < need) return fail_batch(SWIFT_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace.bytes, need);
+    if (workspace.bytes < p.bytes) return fail_batch(SWIFT_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace.bytes, p.bytes);
     av.max_rows = max_rows;
-    const cudaError_t e = launch_rows(kv, bv, av, (cudaStream_t)cuda_stream);
-    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
-    return SWIFT_OK;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (p.rows) {
+        const cudaError_t e = launch_rows(kv, bv, av, s);
+        if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+        return SWIFT_OK;
+    }
+    if (p.prompt) return run_prompt(kv, bv, av, args->block, s);
+    return run_prefix(kv, bv, av, args->block, p, reinterpret_cast<unsigned char*>(workspace.dptr), s);
 }
 
 swift_status swift_batch_sync(void* cuda_stream)

@@ -225,6 +225,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
     constexpr uint32_t IDESC_PV = (1u << 4) | (TYPE << 7) | (TYPE << 10) | (1u << 16) | ((uint32_t)(DP >> 3) << 17) | ((uint32_t)(BT_ROWS >> 4) << 24);
     constexpr float BIAS = HALF ? 7.f : 0.f;
 
+    pdl_trigger();
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_sh = base, ring = base + 2 * S::Q_BYTES, bars = ring + S::SLOTS * S::SLOT_BYTES;
@@ -443,7 +444,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
         for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
             const int n_tiles = max(it.tiles[0], it.tiles[1]), mine = it.tiles[x];
             const int t = it.t0 + x * TQ + tok;                       // token within the sequence
-            const bool live = tok < TQ && t < it.n;
+            const bool live = tok < TQ && t < it.n && (g.mode == BT_PREFIX || t < g.a.max_rows);
             const int own = it.len - it.n + t;                        // own position: keys 0 .. own are seen
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < mine; ++j) {
@@ -564,6 +565,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
         }
     }
     __syncthreads();
+    pdl_wait();                                           // (a launch before this one in the same call ends first)
     if (warp == 9) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
