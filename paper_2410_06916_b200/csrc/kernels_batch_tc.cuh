@@ -34,11 +34,7 @@
 
 namespace swk {
 
-// Three warpgroups: two of softmax warps, one with the TMA warp, the MMA warp and two idle ones.  Launched with 168 registers
-// per thread (64512 of the SM's 65536); the third group gives up 80 of them and the softmax groups, which hold a row of
-// 128 scores per thread, take 40 more: 2 x 128 x 208 + 128 x 88 = 64512.
-constexpr int BT_THREADS = 384;
-constexpr int BT_SOFTMAX_REGS = 208, BT_OTHER_REGS = 88;
+constexpr int BT_THREADS = 320;     // 2 x 4 softmax warps, the TMA warp, the MMA warp
 constexpr int BT_KEYS = 128;        // keys per tile
 constexpr int BT_ROWS = 128;        // packed query rows per tile
 constexpr int BT_PAGE_RING = 16;    // page-validity words kept (more than the key tiles ever in flight)
@@ -165,23 +161,38 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&r)[32])
                    "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
                  : "r"(addr));
 }
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const float (&r)[32])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-                 "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-                 ::"f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]),
-                   "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]), "f"(r[16]), "f"(r[17]), "f"(r[18]), "f"(r[19]), "f"(r[20]),
-                   "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]), "f"(r[25]), "f"(r[26]), "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]),
-                   "f"(r[31]), "r"(addr) : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&u)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
                  ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]),
                    "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, float (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]) : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const float (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "r"(addr) : "memory");
+}
+// The registers a load fills are operands of the wait, so that nothing reads them before it.
+template <int N> __device__ __forceinline__ void tmem_wait_ld(float (&r)[N])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+        asm volatile("" : "+f"(r[i]), "+f"(r[i + 1]), "+f"(r[i + 2]), "+f"(r[i + 3]), "+f"(r[i + 4]), "+f"(r[i + 5]), "+f"(r[i + 6]), "+f"(r[i + 7]));
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// two fp32 operations in one instruction
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void split2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -192,14 +203,18 @@ __device__ __forceinline__ float ex2(float x)
 __device__ int batch_wait_error;                                      // set when a bounded wait ran out; swift_batch_sync reports it
 
 // A wait of one role: bounded, and over at once when another role has given up.
-__device__ __forceinline__ bool bt_wait(uint32_t bar, uint32_t parity, volatile int* abort_sh)
+__device__ __forceinline__ bool bt_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __noinline__ bool bt_wait_long(uint32_t bar, uint32_t parity, volatile int* abort_sh)
 {
     const long long t0 = clock64();
     for (uint32_t it = 0;; ++it) {
-        uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return true;
+        if (bt_try(bar, parity)) return true;
         if ((it & 63u) == 63u) {
             if (*abort_sh) return false;
             if (clock64() - t0 > TC_WAIT_CYCLES) {
@@ -210,9 +225,129 @@ __device__ __forceinline__ bool bt_wait(uint32_t bar, uint32_t parity, volatile 
         }
     }
 }
+__device__ __forceinline__ bool bt_wait(uint32_t bar, uint32_t parity, volatile int* abort_sh)
+{
+    for (int it = 0; it < 4; ++it)
+        if (bt_try(bar, parity)) return true;
+    return bt_wait_long(bar, parity, abort_sh);
+}
+
+// Bit i: key 32 q + i of a tile is shown to a row that sees the tile's keys below `seen`, and lies on a page of the pool.
+__device__ __forceinline__ unsigned bt_shown(unsigned pages, int page_shift, int seen, int q)
+{
+    unsigned w = 0;
+    if (page_shift >= 5) {
+        w = (pages >> ((32 * q) >> page_shift)) & 1u ? 0xFFFFFFFFu : 0u;
+    } else {
+        const int slots = 1 << page_shift;                            // 8 or 16
+        const unsigned one = (1u << slots) - 1u;
+        unsigned bits = pages >> ((32 * q) >> page_shift);
+        for (int at = 0; at < 32; at += slots, bits >>= 1)
+            if (bits & 1u) w |= one << at;
+    }
+    const int n = seen - 32 * q;
+    return n >= 32 ? w : n <= 0 ? 0u : w & ((1u << n) - 1u);
+}
+
+// The softmax warps' part of one key tile: S in, P out, the row's maximum m and sum l brought up to date; O rescaled where the
+// maximum has outgrown it.  s_at, o_at: this warp's lanes of S and O; p_bar: the two hand-over barriers of the tile.
+template <typename T, int DP, bool MASKED>
+__device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, int seen, unsigned pages, int page_shift, bool first, float& m, float& l)
+{
+    constexpr float BIAS = std::is_same<T, __half>::value ? 7.f : 0.f;
+    const int lane = threadIdx.x & 31;
+    // Scores are read twice, a quarter (32 keys) at a time: once for the maximum, once for the exponentials, the
+    // upper half of the keys going straight from one to the other.  P overwrites the upper half of S.
+    auto hide = [&](int q, float (&s)[32]) {
+        if (!MASKED) return;
+        const unsigned shown = bt_shown(pages, page_shift, seen, q);
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (!((shown >> i) & 1u)) s[i] = -INFINITY;
+    };
+    auto highest = [&](const float (&s)[32]) {
+        float x0 = s[0], x1 = s[1];
+#pragma unroll
+        for (int i = 2; i < 30; i += 4) { x0 = max3(x0, s[i], s[i + 1]); x1 = max3(x1, s[i + 2], s[i + 3]); }
+        return fmaxf(max3(x0, s[30], s[31]), x1);
+    };
+    float s0[32], s1[32], s2[32], s3[32];
+    tmem_ld32(s_at, s0);
+    tmem_wait_ld(s0);
+    tmem_ld32(s_at + 32, s1);
+    hide(0, s0);
+    float top = highest(s0);
+    tmem_wait_ld(s1);
+    tmem_ld32(s_at + 64, s2);
+    hide(1, s1);
+    top = fmaxf(top, highest(s1));
+    tmem_wait_ld(s2);
+    tmem_ld32(s_at + 96, s3);
+    hide(2, s2);
+    top = fmaxf(top, highest(s2));
+    tmem_wait_ld(s3);
+    hide(3, s3);
+    top = fmaxf(top, highest(s3));
+    // a warp rescales when a row of its own has outgrown what its sums are scaled by
+    const bool grow = top > m && (m == -INFINITY || (top - m) * c > BT_GROW);
+    if (__any_sync(FULL_WARP, grow)) {
+        const float m_new = fmaxf(m, top);
+        const float shrink = m == m_new ? 1.f : ex2((m - m_new) * c);
+        l *= shrink;
+        m = m_new;
+        if (!first) {
+#pragma unroll 1
+            for (int i = 0; i < DP; i += 8) {             // rare; few registers beside the scores
+                float o[8];
+                tmem_ld8(o_at + i, o);
+                tmem_wait_ld(o);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] *= shrink;
+                tmem_st8(o_at + i, o);
+            }
+        }
+    }
+    const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
+    const f32x2 c2 = pair2(c, c), off2 = pair2(off, off);
+    f32x2 sum[2] = {0ull, 0ull};
+    auto weights = [&](int q, const float (&s)[32]) {
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            float p0, p1;
+            split2(fma2(pair2(s[i], s[i + 1]), c2, off2), p0, p1);
+            p0 = ex2(p0);
+            p1 = ex2(p1);
+            sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pair2(p0, p1));
+            p[i >> 1] = pack2(p0, p1, T());
+        }
+        tmem_st16(s_at + 64 + 16 * q, p);
+    };
+    auto hand_over = [&](int h) {
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_bar + 8u * h);
+    };
+    tmem_ld32(s_at, s0);
+    weights(2, s2);
+    weights(3, s3);
+    hand_over(1);
+    tmem_wait_ld(s0);
+    tmem_ld32(s_at + 32, s1);
+    hide(0, s0);
+    weights(0, s0);
+    tmem_wait_ld(s1);
+    hide(1, s1);
+    weights(1, s1);
+    hand_over(0);
+    float l0, l1;
+    split2(add2(sum[0], sum[1]), l0, l1);
+    l += l0 + l1;
+}
 
 // ------------------------------------------------------------------------------ the kernel
-// grid = persistent CTAs (at most one per SM), each taking pieces blockIdx.x, + gridDim.x, ...; block = 384.
+// grid = persistent CTAs (at most one per SM), each taking pieces blockIdx.x, + gridDim.x, ...; block = 320.
 template <typename T, int HALVES>
 __global__ void __launch_bounds__(BT_THREADS, 1)
 attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_q, BatchView b, BtArgs g)
@@ -271,8 +406,6 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
     auto s_col = [&](int x) { return tmem + 128u * x; };              // S, then P, of tile x
     auto o_col = [&](int x) { return tmem + 256u + 128u * x; };
 
-    if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(BT_OTHER_REGS));
     if (warp == 8) {
         // ---------------------------------------------------------------- TMA: queries, then K and V tiles in turn
         const int per_tile = BT_KEYS >> b.page_shift;                 // pages per key tile, 1..16
@@ -375,12 +508,12 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 auto weigh = [&](int x, uint32_t v_sh, bool first) {  // O(x) (+)= P(x) V
                     const uint64_t vd = tc_smem_desc_mn(v_sh);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    for (int h = 1; h >= 0; --h) {                    // the upper half of the keys is ready first
                         if (!bt_wait(p_ready(x, h), p_turn[x], abort_sh)) return false;
                         tc_fence_after();
 #pragma unroll
                         for (int k = 4 * h; k < 4 * h + 4; ++k)       // 16 keys a step: 8 columns of P, 2048 bytes of V
-                            tc_mma_ts(o_col(x), s_col(x) + 8 * k, vd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, !first || k > 0);
+                            tc_mma_ts(o_col(x), s_col(x) + 64 + 8 * k, vd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, !first || k != 4);
                     }
                     p_turn[x] ^= 1u;
                     return true;
@@ -428,15 +561,14 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             }
             ok = __shfl_sync(FULL_WARP, ok ? 1 : 0, 0) != 0;
         }
-    }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(BT_SOFTMAX_REGS));
         // ---------------------------------------------------------------- softmax: a thread owns one packed query row
         const int x = warp >> 2, rho = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = s_col(x) + lanes, o_at = o_col(x) + lanes;
         const int tok = rho / G, head_in = rho - tok * G;
         const float c = g.a.scale * 1.4426950408889634f;              // scores in powers of two
+        const unsigned all_pages = 0xFFFFu >> (16 - (BT_KEYS >> b.page_shift));
         uint32_t s_turn = 0, o_turn = 0;
         int tile_no = 0;
         bool ok = true;
@@ -452,68 +584,12 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 if (!ok) break;
                 s_turn ^= 1u;
                 tc_fence_after();
-                float s[4][32];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_ld32(s_at + 32 * i, s[i]);
                 const int key0 = (j < it.np ? it.first_tile + j : j - it.np) * BT_KEYS;
                 const int seen = j < it.np ? b.prefix_len - key0 : own + 1 - key0;        // this row sees keys below this
                 const unsigned pages = page_bits[(tile_no + j) & (BT_PAGE_RING - 1)];
-                const unsigned all = 0xFFFFu >> (16 - (BT_KEYS >> b.page_shift));
-                tmem_wait_ld();
-                if (__any_sync(FULL_WARP, seen < BT_KEYS) || pages != all) {
-#pragma unroll
-                    for (int i = 0; i < BT_KEYS; ++i)
-                        if (i >= seen || !((pages >> (i >> b.page_shift)) & 1u)) s[i >> 5][i & 31] = -INFINITY;
-                }
-                float mx[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    mx[q] = fmaxf(s[q][0], s[q][1]);
-#pragma unroll
-                    for (int i = 2; i < 32; i += 2) mx[q] = fmaxf(fmaxf(mx[q], s[q][i]), s[q][i + 1]);
-                }
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                // a warp rescales when a row of its own has outgrown what its sums are scaled by
-                const bool grow = top > m && (m == -INFINITY || (top - m) * c > BT_GROW);
-                if (__any_sync(FULL_WARP, grow)) {
-                    const float m_new = fmaxf(m, top);
-                    const float shrink = m == m_new ? 1.f : ex2((m - m_new) * c);
-                    l *= shrink;
-                    m = m_new;
-                    if (j > 0) {
-#pragma unroll 1
-                        for (int i = 0; i < DP; i += 32) {
-                            float o[32];
-                            tmem_ld32(o_at + i, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] *= shrink;
-                            tmem_st32(o_at + i, o);
-                        }
-                    }
-                }
-                const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                    for (int q = 2 * h; q < 2 * h + 2; ++q) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const float p0 = ex2(fmaf(s[q][i], c, off)), p1 = ex2(fmaf(s[q][i + 1], c, off));
-                            sum[i & 2] += p0;
-                            sum[(i & 2) + 1] += p1;
-                            p[i >> 1] = pack2(p0, p1, T());
-                        }
-                        tmem_st16(s_at + 16 * q, p);
-                    }
-                    tmem_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(p_ready(x, h));
-                }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                const bool masked = __any_sync(FULL_WARP, seen < BT_KEYS) || pages != all_pages;
+                if (masked) bt_softmax<T, DP, true>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
+                else bt_softmax<T, DP, false>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
             }
             tile_no += n_tiles;
             if (!ok) break;
@@ -533,7 +609,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                     float o[32];
                     if (mine > 0) {
                         tmem_ld32(o_at + i, o);
-                        tmem_wait_ld();
+                        tmem_wait_ld(o);
                     }
                     if (live && l != 0.f) {
                         float4* dst = reinterpret_cast<float4*>(g.part_o + at * DP + i);
@@ -548,7 +624,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                     float o[32];
                     if (mine > 0) {
                         tmem_ld32(o_at + i, o);
-                        tmem_wait_ld();
+                        tmem_wait_ld(o);
                     }
                     if (live) {
 #pragma unroll
