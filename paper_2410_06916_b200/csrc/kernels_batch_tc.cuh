@@ -38,6 +38,7 @@ constexpr int BT_THREADS = 320;     // 2 x 4 softmax warps, the TMA warp, the MM
 constexpr int BT_KEYS = 128;        // keys per tile
 constexpr int BT_ROWS = 128;        // packed query rows per tile
 constexpr int BT_PAGE_RING = 16;    // page-validity words kept (more than the key tiles ever in flight)
+constexpr unsigned BT_POLY = 0x5252u;   // pairs of every 16 whose exponentials are polynomials: 6 of 16
 constexpr float BT_GROW = 8.f;      // growth of the maximum (in powers of two) that triggers a rescaling
 
 enum { BT_PROMPT = 0, BT_PREFIX = 1, BT_OWN = 2 };
@@ -137,6 +138,15 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+// The MMA warp runs its loop with all lanes, and one of them issues: the operands then stay in uniform registers, which the
+// instructions want (issued from under a per-lane branch, each one first moved its descriptors over and took about 165 cycles,
+// three times what the tensor pipe needs for it).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(p));
+    return p != 0;
 }
 // D[tmem] (+)= A[tmem] * B[smem]
 __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
@@ -249,98 +259,177 @@ __device__ __forceinline__ unsigned bt_shown(unsigned pages, int page_shift, int
     return n >= 32 ? w : n <= 0 ? 0u : w & ((1u << n) - 1u);
 }
 
-// The softmax warps' part of one key tile: S in, P out, the row's maximum m and sum l brought up to date; O rescaled where the
-// maximum has outgrown it.  s_at, o_at: this warp's lanes of S and O; p_bar: the two hand-over barriers of the tile.
-template <typename T, int DP, bool MASKED>
-__device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, int seen, unsigned pages, int page_shift, bool first, float& m, float& l)
+// 2^x for two values on the multiply-add pipe, x in about [-126, 127] (below: 2^-126): x = n + f with n the nearest integer,
+// 2^f as a polynomial, n added to its exponent.  The coefficients minimise the largest relative error on [-1/2, 1/2] (a linear
+// programme over 2001 Chebyshev points): 7.5e-5 for degree 3, which is a fiftieth of half a step of bf16; 2.6e-6 for degree 4, with
+// which fp16's half step is 180 times as large.
+template <typename T> __device__ __forceinline__ void ex2_poly(float x0, float x1, float& y0, float& y1)
+{
+    const float round = 12582912.f;                                   // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
+    const f32x2 x = pair2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+    const f32x2 t = add2(x, pair2(round, round));
+    const f32x2 f = fma2(add2(t, pair2(-round, -round)), pair2(-1.f, -1.f), x);
+    f32x2 p;
+    if (std::is_same<T, __half>::value) {
+        p = fma2(pair2(0.009567738510668278f, 0.009567738510668278f), f, pair2(0.05591749772429466f, 0.05591749772429466f));
+        p = fma2(p, f, pair2(0.24024811387062073f, 0.24024811387062073f));
+        p = fma2(p, f, pair2(0.6931219100952148f, 0.6931219100952148f));
+        p = fma2(p, f, pair2(0.9999992251396179f, 0.9999992251396179f));
+    } else {
+        p = fma2(pair2(0.0551714189350605f, 0.0551714189350605f), f, pair2(0.24261116981506348f, 0.24261116981506348f));
+        p = fma2(p, f, pair2(0.6932610273361206f, 0.6932610273361206f));
+        p = fma2(p, f, pair2(0.9999280571937561f, 0.9999280571937561f));
+    }
+    float p0, p1, t0, t1;
+    split2(p, p0, p1);
+    split2(t, t0, t1);
+    y0 = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
+    y1 = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
+}
+
+// 32 scores -> probabilities (16 bits each, two to a register), their sum added up.  POLY: which of the 16 pairs take the
+// polynomial instead of the special function unit.
+template <typename T, unsigned POLY>
+__device__ __forceinline__ void bt_weights(const float (&s)[32], f32x2 c2, f32x2 off2, f32x2 (&sum)[2], uint32_t (&p)[16])
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float p0, p1;
+        split2(fma2(pair2(s[2 * i], s[2 * i + 1]), c2, off2), p0, p1);
+        if ((POLY >> i) & 1u) {
+            ex2_poly<T>(p0, p1, p0, p1);
+        } else {
+            p0 = ex2(p0);
+            p1 = ex2(p1);
+        }
+        sum[i & 1] = add2(sum[i & 1], pair2(p0, p1));
+        p[i] = pack2(p0, p1, T());
+    }
+}
+__device__ __forceinline__ float bt_highest(const float (&s)[32])
+{
+    float x0 = s[0], x1 = s[1];
+#pragma unroll
+    for (int i = 2; i < 30; i += 4) {
+        x0 = max3(x0, s[i], s[i + 1]);
+        x1 = max3(x1, s[i + 2], s[i + 3]);
+    }
+    return fmaxf(max3(x0, s[30], s[31]), x1);
+}
+// P of half h of the keys is in TMEM: the MMA warp may use it.
+__device__ __forceinline__ void bt_hand_over(uint32_t p_bar, int h)
+{
+    tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(p_bar + 8u * h);
+}
+// Rows whose maximum has outgrown what their sums are scaled by: new maximum, sums and (behind the first tile) O rescaled.
+template <int DP> __device__ __forceinline__ void bt_rescale(uint32_t o_at, float c, float top, bool first, float& m, float& l)
+{
+    const float m_new = fmaxf(m, top), shrink = m == m_new ? 1.f : ex2((m - m_new) * c);
+    l *= shrink;
+    m = m_new;
+    if (first) return;
+#pragma unroll 1
+    for (int i = 0; i < DP; i += 8) {                                 // rare; few registers beside the scores
+        float o[8];
+        tmem_ld8(o_at + i, o);
+        tmem_wait_ld(o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= shrink;
+        tmem_st8(o_at + i, o);
+    }
+}
+__device__ __forceinline__ bool bt_outgrown(float top, float m, float c)
+{
+    return __any_sync(FULL_WARP, top > m && (m == -INFINITY || (top - m) * c > BT_GROW));
+}
+
+// The softmax warps' part of one key tile: S in, P out (over the upper half of S), the row's maximum m and sum l brought up to
+// date.  s_at, o_at: this warp's lanes of S and O; p_bar: the two hand-over barriers.  Scores come a quarter (32 keys) at a
+// time; the upper half of the keys goes first.
+// General form, for tiles with hidden keys: the maximum first, then the exponentials.
+template <typename T, int DP>
+__device__ __forceinline__ void bt_softmax_any(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, int seen, unsigned pages, int page_shift, bool first, float& m, float& l)
 {
     constexpr float BIAS = std::is_same<T, __half>::value ? 7.f : 0.f;
-    const int lane = threadIdx.x & 31;
-    // Scores are read twice, a quarter (32 keys) at a time: once for the maximum, once for the exponentials, the
-    // upper half of the keys going straight from one to the other.  P overwrites the upper half of S.
     auto hide = [&](int q, float (&s)[32]) {
-        if (!MASKED) return;
         const unsigned shown = bt_shown(pages, page_shift, seen, q);
 #pragma unroll
         for (int i = 0; i < 32; ++i)
             if (!((shown >> i) & 1u)) s[i] = -INFINITY;
     };
-    auto highest = [&](const float (&s)[32]) {
-        float x0 = s[0], x1 = s[1];
-#pragma unroll
-        for (int i = 2; i < 30; i += 4) { x0 = max3(x0, s[i], s[i + 1]); x1 = max3(x1, s[i + 2], s[i + 3]); }
-        return fmaxf(max3(x0, s[30], s[31]), x1);
-    };
+    float s[32], top = -INFINITY;
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) {
+        tmem_ld32(s_at + 32 * q, s);
+        tmem_wait_ld(s);
+        hide(q, s);
+        top = fmaxf(top, bt_highest(s));
+    }
+    if (bt_outgrown(top, m, c)) bt_rescale<DP>(o_at, c, top, first, m, l);
+    const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
+    const f32x2 c2 = pair2(c, c), off2 = pair2(off, off);
+    f32x2 sum[2] = {0ull, 0ull};
+#pragma unroll 1
+    for (int h = 1; h >= 0; --h) {                                    // both quarters are read before P overwrites one of them
+        float s2[32];
+        uint32_t p[16];
+        tmem_ld32(s_at + 64 * h, s);
+        tmem_ld32(s_at + 64 * h + 32, s2);
+        tmem_wait_ld(s);
+        tmem_wait_ld(s2);
+        hide(2 * h, s);
+        hide(2 * h + 1, s2);
+        bt_weights<T, 0u>(s, c2, off2, sum, p);
+        tmem_st16(s_at + 64 + 32 * h, p);
+        bt_weights<T, 0u>(s2, c2, off2, sum, p);
+        tmem_st16(s_at + 80 + 32 * h, p);
+        bt_hand_over(p_bar, h);
+    }
+    float l0, l1;
+    split2(add2(sum[0], sum[1]), l0, l1);
+    l += l0 + l1;
+}
+
+// Every key shown: the same without the hiding, with each quarter's load under the arithmetic of the one before.
+template <typename T, int DP>
+__device__ __forceinline__ void bt_softmax_full(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, bool first, float& m, float& l)
+{
+    constexpr float BIAS = std::is_same<T, __half>::value ? 7.f : 0.f;
     float s0[32], s1[32], s2[32], s3[32];
     tmem_ld32(s_at, s0);
     tmem_wait_ld(s0);
     tmem_ld32(s_at + 32, s1);
-    hide(0, s0);
-    float top = highest(s0);
+    float top = bt_highest(s0);
     tmem_wait_ld(s1);
     tmem_ld32(s_at + 64, s2);
-    hide(1, s1);
-    top = fmaxf(top, highest(s1));
+    top = fmaxf(top, bt_highest(s1));
     tmem_wait_ld(s2);
     tmem_ld32(s_at + 96, s3);
-    hide(2, s2);
-    top = fmaxf(top, highest(s2));
+    top = fmaxf(top, bt_highest(s2));
     tmem_wait_ld(s3);
-    hide(3, s3);
-    top = fmaxf(top, highest(s3));
-    // a warp rescales when a row of its own has outgrown what its sums are scaled by
-    const bool grow = top > m && (m == -INFINITY || (top - m) * c > BT_GROW);
-    if (__any_sync(FULL_WARP, grow)) {
-        const float m_new = fmaxf(m, top);
-        const float shrink = m == m_new ? 1.f : ex2((m - m_new) * c);
-        l *= shrink;
-        m = m_new;
-        if (!first) {
-#pragma unroll 1
-            for (int i = 0; i < DP; i += 8) {             // rare; few registers beside the scores
-                float o[8];
-                tmem_ld8(o_at + i, o);
-                tmem_wait_ld(o);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] *= shrink;
-                tmem_st8(o_at + i, o);
-            }
-        }
-    }
+    top = fmaxf(top, bt_highest(s3));
+    if (bt_outgrown(top, m, c)) bt_rescale<DP>(o_at, c, top, first, m, l);
     const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
     const f32x2 c2 = pair2(c, c), off2 = pair2(off, off);
     f32x2 sum[2] = {0ull, 0ull};
-    auto weights = [&](int q, const float (&s)[32]) {
-        uint32_t p[16];
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-            float p0, p1;
-            split2(fma2(pair2(s[i], s[i + 1]), c2, off2), p0, p1);
-            p0 = ex2(p0);
-            p1 = ex2(p1);
-            sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pair2(p0, p1));
-            p[i >> 1] = pack2(p0, p1, T());
-        }
-        tmem_st16(s_at + 64 + 16 * q, p);
-    };
-    auto hand_over = [&](int h) {
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_bar + 8u * h);
-    };
+    uint32_t p[16];
     tmem_ld32(s_at, s0);
-    weights(2, s2);
-    weights(3, s3);
-    hand_over(1);
+    bt_weights<T, BT_POLY>(s2, c2, off2, sum, p);
+    tmem_st16(s_at + 96, p);
+    bt_weights<T, BT_POLY>(s3, c2, off2, sum, p);
+    tmem_st16(s_at + 112, p);
+    bt_hand_over(p_bar, 1);
     tmem_wait_ld(s0);
     tmem_ld32(s_at + 32, s1);
-    hide(0, s0);
-    weights(0, s0);
+    bt_weights<T, BT_POLY>(s0, c2, off2, sum, p);
+    tmem_st16(s_at + 64, p);
     tmem_wait_ld(s1);
-    hide(1, s1);
-    weights(1, s1);
-    hand_over(0);
+    bt_weights<T, BT_POLY>(s1, c2, off2, sum, p);
+    tmem_st16(s_at + 80, p);
+    bt_hand_over(p_bar, 0);
     float l0, l1;
     split2(add2(sum[0], sum[1]), l0, l1);
     l += l0 + l1;
@@ -494,9 +583,10 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
         bool ok = true;
         BtItem it;
         for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
-            if (lane == 0) {
-                const int n_tiles = max(it.tiles[0], it.tiles[1]);
-                auto scores = [&](int x, uint32_t k_sh) {             // S(x) = Q(x) K^T
+            const int n_tiles = max(it.tiles[0], it.tiles[1]);
+            auto commit = [&](uint32_t bar) { if (elect_one()) tc_commit(bar); };
+            auto scores = [&](int x, uint32_t k_sh) {                 // S(x) = Q(x) K^T
+                if (elect_one()) {
                     const uint64_t qd = tc_smem_desc(q_sh + x * S::Q_BYTES), kd = tc_smem_desc(k_sh);
 #pragma unroll
                     for (int k = 0; k < 4 * HALVES; ++k) {            // 16 dims a step: 32 bytes, 64 dims a box
@@ -504,62 +594,66 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                         tc_mma(s_col(x), qd + step, kd + step, IDESC_QK, k > 0);
                     }
                     tc_commit(s_full(x));
-                };
-                auto weigh = [&](int x, uint32_t v_sh, bool first) {  // O(x) (+)= P(x) V
-                    const uint64_t vd = tc_smem_desc_mn(v_sh);
+                }
+            };
+            auto weigh = [&](int x, uint32_t v_sh, bool first) {      // O(x) (+)= P(x) V
+                const uint64_t vd = tc_smem_desc_mn(v_sh);
 #pragma unroll
-                    for (int h = 1; h >= 0; --h) {                    // the upper half of the keys is ready first
-                        if (!bt_wait(p_ready(x, h), p_turn[x], abort_sh)) return false;
-                        tc_fence_after();
+                for (int h = 1; h >= 0; --h) {                        // the upper half of the keys is ready first
+                    if (!bt_wait(p_ready(x, h), p_turn[x], abort_sh)) return false;
+                    tc_fence_after();
+                    if (elect_one()) {
 #pragma unroll
                         for (int k = 4 * h; k < 4 * h + 4; ++k)       // 16 keys a step: 8 columns of P, 2048 bytes of V
                             tc_mma_ts(o_col(x), s_col(x) + 64 + 8 * k, vd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, !first || k != 4);
                     }
-                    p_turn[x] ^= 1u;
-                    return true;
-                };
-                for (int x = 0; ok && x < 2; ++x)
-                    if (it.tiles[x]) { ok = bt_wait(q_full(x), q_turn[x], abort_sh); q_turn[x] ^= 1u; }
-                if (ok && n_tiles > 0) {
-                    ok = bt_wait(full(slot), turn, abort_sh);
-                    tc_fence_after();
-                    if (ok) {
-                        for (int x = 0; x < 2; ++x)
-                            if (it.tiles[x]) {
-                                scores(x, ring + slot * S::SLOT_BYTES);
-                                if (it.tiles[x] == 1) tc_commit(q_empty(x));
-                            }
-                        tc_commit(empty(slot));
-                        if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
-                    }
                 }
-                for (int j = 0; ok && j < n_tiles; ++j) {
-                    const uint32_t v_slot = slot, v_turn = turn;
-                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
-                    ok = bt_wait(full(v_slot), v_turn, abort_sh);
-                    const bool more = j + 1 < n_tiles;
-                    for (int x = 0; ok && x < 2; ++x) {
-                        if (j < it.tiles[x]) {
-                            ok = weigh(x, ring + v_slot * S::SLOT_BYTES, j == 0);
-                            if (!ok) break;
-                            if (j + 1 == it.tiles[x]) tc_commit(o_full(x));
-                        }
-                        if (x == 1) tc_commit(empty(v_slot));
-                        if (j + 1 < it.tiles[x]) {
-                            ok = bt_wait(full(slot), turn, abort_sh);
-                            if (!ok) break;
-                            tc_fence_after();
+                p_turn[x] ^= 1u;
+                return true;
+            };
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                if (ok && it.tiles[x]) { ok = bt_wait(q_full(x), q_turn[x], abort_sh); q_turn[x] ^= 1u; }
+            if (ok && n_tiles > 0) {
+                ok = bt_wait(full(slot), turn, abort_sh);
+                tc_fence_after();
+                if (ok) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (it.tiles[x]) {
                             scores(x, ring + slot * S::SLOT_BYTES);
-                            if (j + 2 == it.tiles[x]) tc_commit(q_empty(x));
+                            if (it.tiles[x] == 1) commit(q_empty(x));
                         }
-                    }
-                    if (ok && more) {
-                        tc_commit(empty(slot));
-                        if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
-                    }
+                    commit(empty(slot));
+                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
                 }
             }
-            ok = __shfl_sync(FULL_WARP, ok ? 1 : 0, 0) != 0;
+            for (int j = 0; ok && j < n_tiles; ++j) {
+                const uint32_t v_slot = slot, v_turn = turn;
+                if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                ok = bt_wait(full(v_slot), v_turn, abort_sh);
+                const bool more = j + 1 < n_tiles;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (ok && j < it.tiles[x]) {
+                        ok = weigh(x, ring + v_slot * S::SLOT_BYTES, j == 0);
+                        if (ok && j + 1 == it.tiles[x]) commit(o_full(x));
+                    }
+                    if (ok && x == 1) commit(empty(v_slot));
+                    if (ok && j + 1 < it.tiles[x]) {
+                        ok = bt_wait(full(slot), turn, abort_sh);
+                        if (ok) {
+                            tc_fence_after();
+                            scores(x, ring + slot * S::SLOT_BYTES);
+                            if (j + 2 == it.tiles[x]) commit(q_empty(x));
+                        }
+                    }
+                }
+                if (ok && more) {
+                    commit(empty(slot));
+                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                }
+            }
         }
     } else {
         // ---------------------------------------------------------------- softmax: a thread owns one packed query row
@@ -588,8 +682,8 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 const int seen = j < it.np ? b.prefix_len - key0 : own + 1 - key0;        // this row sees keys below this
                 const unsigned pages = page_bits[(tile_no + j) & (BT_PAGE_RING - 1)];
                 const bool masked = __any_sync(FULL_WARP, seen < BT_KEYS) || pages != all_pages;
-                if (masked) bt_softmax<T, DP, true>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
-                else bt_softmax<T, DP, false>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
+                if (masked) bt_softmax_any<T, DP>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
+                else bt_softmax_full<T, DP>(s_at, o_at, p_ready(x, 0), c, j == 0, m, l);
             }
             tile_no += n_tiles;
             if (!ok) break;
