@@ -21,6 +21,7 @@ namespace swk {
 
 constexpr int BD_THREADS = 288;                           // 8 consumer warps, the TMA warp
 constexpr int BD_KEYS = 64;                               // keys per unit
+constexpr int BD_AHEAD = 4;                               // units by which page ids are looked up ahead of their use
 constexpr int BD_MAX_ROWS = 64;                           // packed query rows (tokens x heads of a group) of an item
 
 template <int HALVES> struct BdShape {
@@ -44,15 +45,29 @@ struct BdArgs {
 
 __device__ __forceinline__ int bd_units(const SeqSpan& s) { return s.n > 0 ? (s.len + BD_KEYS - 1) / BD_KEYS : 0; }
 
-// A walk over a CTA's units.  All lanes of a warp hold the same values.
+// A walk over a CTA's units by a whole warp; all lanes hold the same values, except that lane i keeps the span of sequence
+// base + i, so that going on to the next sequence costs a trip to memory once in 32.
 struct BdWalk {
     int item, seq, kvh, unit, units;                      // seq -1: the prefix
     SeqSpan sp;
+    int base;
+    SeqSpan ahead;
 };
-__device__ __forceinline__ void bd_enter_seq(const BatchView& b, const BdArgs& g, BdWalk& w)
+__device__ __forceinline__ SeqSpan bd_span(const BatchView& b, BdWalk& w, int seq)
+{
+    if (seq < w.base || seq >= w.base + 32) {
+        const int i = seq + (threadIdx.x & 31);
+        w.base = seq;
+        w.ahead = {0, 0, 0};
+        if (i < b.n_seqs) w.ahead = seq_span(b, i);
+    }
+    const int at = seq - w.base;
+    return {__shfl_sync(FULL_WARP, w.ahead.r0, at), __shfl_sync(FULL_WARP, w.ahead.n, at), __shfl_sync(FULL_WARP, w.ahead.len, at)};
+}
+__device__ __forceinline__ void bd_enter(const BatchView& b, const BdArgs& g, BdWalk& w)
 {
     while (w.seq < b.n_seqs) {                            // skips sequences without units; the caller has units left
-        w.sp = seq_span(b, w.seq);
+        w.sp = bd_span(b, w, w.seq);
         w.units = bd_units(w.sp);
         if (w.units > 0) break;
         ++w.seq;
@@ -62,6 +77,7 @@ __device__ __forceinline__ void bd_enter_seq(const BatchView& b, const BdArgs& g
 __device__ __forceinline__ void bd_start(const BatchView& b, const BdArgs& g, int prefix_units, long long u, BdWalk& w)
 {
     const int Hk = g.a.n_kv_heads, lane = threadIdx.x & 31;
+    w.base = -64;
     if (u < (long long)prefix_units * Hk) {
         w.seq = -1;
         w.kvh = (int)(u / prefix_units);
@@ -74,8 +90,12 @@ __device__ __forceinline__ void bd_start(const BatchView& b, const BdArgs& g, in
         return;
     }
     u -= (long long)prefix_units * Hk;
+    w.seq = 0;
     for (int base = 0; base < b.n_seqs; base += 32) {
-        const int mine = base + lane < b.n_seqs ? bd_units(seq_span(b, base + lane)) * Hk : 0;
+        w.base = base;
+        w.ahead = {0, 0, 0};
+        if (base + lane < b.n_seqs) w.ahead = seq_span(b, base + lane);
+        const int mine = bd_units(w.ahead) * Hk;
         int upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -92,7 +112,7 @@ __device__ __forceinline__ void bd_start(const BatchView& b, const BdArgs& g, in
         w.seq = base + at;
         break;
     }
-    w.sp = seq_span(b, w.seq);
+    w.sp = bd_span(b, w, w.seq);
     w.units = bd_units(w.sp);
     w.kvh = (int)(u / w.units);
     w.unit = (int)(u - (long long)w.kvh * w.units);
@@ -106,7 +126,7 @@ __device__ __forceinline__ void bd_next(const BatchView& b, const BdArgs& g, BdW
     if (++w.kvh < g.a.n_kv_heads) return;
     w.kvh = 0;
     ++w.seq;
-    bd_enter_seq(b, g, w);
+    bd_enter(b, g, w);
 }
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr)
@@ -186,13 +206,30 @@ attn_batch_dec_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_c
 
     if (count > 0 && warp == 8) {
         // ---------------------------------------------------------------- TMA
-        BdWalk w;
+        BdWalk w, wa;                                                     // the unit being fetched; one whose page ids are being fetched
         bd_start(b, g, prefix_units, u0, w);
+        wa = w;
         const int per_unit = max(1, BD_KEYS >> b.page_shift);             // pages per unit, 1..8
         const int kv = lane >> 4, pg = (lane & 15) / HALVES, half = (lane & 15) % HALVES;
         const bool boxed = pg < per_unit;
         const int box_rows = min(b.page_size, BD_KEYS);
         const uint32_t box_at = kv * S::TILE_BYTES + half * (BD_KEYS * 128) + pg * box_rows * 128;
+        // Page ids come BD_AHEAD units before they are needed: a trip to memory takes as long as a unit streams.
+        auto page_of = [&]() {
+            int page = b.n_pages;                                         // beyond the last page: zeros
+            const int key0 = wa.unit * BD_KEYS;
+            if (boxed && pg * box_rows < wa.sp.len - key0) {
+                const int at = (key0 >> b.page_shift) + pg;
+                page = wa.seq < 0 ? b.prefix_pages[at] : b.page_table[(size_t)wa.seq * b.table_stride + at];
+            }
+            return page;
+        };
+        int ids[BD_AHEAD];
+#pragma unroll
+        for (int i = 0; i < BD_AHEAD; ++i) {
+            ids[i] = i < count ? page_of() : b.n_pages;
+            if (i + 1 < count) bd_next(b, g, wa);
+        }
         uint32_t turn = 0, q_turn = 0;
         int stage = 0, qb = 0;
         bool ok = true, fresh = true;                                     // fresh: first unit of a segment
@@ -206,11 +243,13 @@ attn_batch_dec_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_c
                     if (w.unit == 0) g.item_first[w.item] = blockIdx.x;
                 }
             }
-            const int key0 = w.unit * BD_KEYS, left = w.sp.len - key0;
-            int page = b.n_pages;                                         // beyond the last page: zeros
-            if (boxed && pg * box_rows < left) {
-                const int at = (key0 >> b.page_shift) + pg;
-                page = w.seq < 0 ? b.prefix_pages[at] : b.page_table[(size_t)w.seq * b.table_stride + at];
+            const int key0 = w.unit * BD_KEYS;
+            int page = ids[0];
+#pragma unroll
+            for (int i = 0; i + 1 < BD_AHEAD; ++i) ids[i] = ids[i + 1];
+            if (k + BD_AHEAD < count) {
+                ids[BD_AHEAD - 1] = page_of();
+                if (k + BD_AHEAD + 1 < count) bd_next(b, g, wa);
             }
             const bool good = (unsigned)page < (unsigned)b.n_pages;
             if (!good) page = b.n_pages;

@@ -38,7 +38,7 @@ constexpr int BT_THREADS = 320;     // 2 x 4 softmax warps, the TMA warp, the MM
 constexpr int BT_KEYS = 128;        // keys per tile
 constexpr int BT_ROWS = 128;        // packed query rows per tile
 constexpr int BT_PAGE_RING = 16;    // page-validity words kept (more than the key tiles ever in flight)
-constexpr unsigned BT_POLY = 0x5252u;   // pairs of every 16 whose exponentials are polynomials: 6 of 16
+constexpr unsigned BT_POLY = 0x0101u;   // pairs of every 16 whose exponentials are polynomials: 2 of 16
 constexpr float BT_GROW = 8.f;      // growth of the maximum (in powers of two) that triggers a rescaling
 
 enum { BT_PROMPT = 0, BT_PREFIX = 1, BT_OWN = 2 };
@@ -672,6 +672,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             const int t = it.t0 + x * TQ + tok;                       // token within the sequence
             const bool live = tok < TQ && t < it.n && (g.mode == BT_PREFIX || t < g.a.max_rows);
             const int own = it.len - it.n + t;                        // own position: keys 0 .. own are seen
+            const int all_see = it.len - it.n + it.t0 + x * TQ + 1;    // own keys that every row of the tile sees
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < mine; ++j) {
                 ok = bt_wait(s_full(x), s_turn, abort_sh);
@@ -681,7 +682,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 const int key0 = (j < it.np ? it.first_tile + j : j - it.np) * BT_KEYS;
                 const int seen = j < it.np ? b.prefix_len - key0 : own + 1 - key0;        // this row sees keys below this
                 const unsigned pages = page_bits[(tile_no + j) & (BT_PAGE_RING - 1)];
-                const bool masked = __any_sync(FULL_WARP, seen < BT_KEYS) || pages != all_pages;
+                const bool masked = key0 + BT_KEYS > (j < it.np ? b.prefix_len : all_see) || pages != all_pages;
                 if (masked) bt_softmax_any<T, DP>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
                 else bt_softmax_full<T, DP>(s_at, o_at, p_ready(x, 0), c, j == 0, m, l);
             }
