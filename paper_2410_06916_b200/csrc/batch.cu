@@ -280,9 +280,10 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
             p->mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
             p->items = (long long)(bv.n_seqs + (p->prefix_few ? 1 : 0)) * Hk;
             p->grid = sms;
-            const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, BD_KEYS) + ceil_div(bv.prefix_len, BD_KEYS)) * Hk;
+            const int keys = 16 * p->mt;
+            const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, keys) + ceil_div(bv.prefix_len, keys)) * Hk;
             if (units > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a page table of %d x %d for %d kv heads is beyond 2^31 units of work", bv.n_seqs, bv.table_stride, Hk);
-            const size_t rows_all = (size_t)(p->items + p->grid) * 16 * p->mt;
+            const size_t rows_all = (size_t)(p->items + (long long)p->grid * (8 / p->mt)) * 16 * p->mt;
             p->few_o = take(rows_all * p->dp * 4);
             p->few_ml = take(rows_all * 8);
             p->first = take((size_t)p->items * 4);
@@ -294,25 +295,34 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
 }
 
 template <typename T, int HALVES, int MT>
-cudaError_t launch_dec(const CUtensorMap& kv_map, const CUtensorMap& q_map, const BatchView& bv, const BdArgs& g, int grid, cudaStream_t s, bool after_previous)
+cudaError_t launch_dec(const CUtensorMap& kv_map, const BatchView& bv, const BdArgs& g, int grid, cudaStream_t s, bool after_previous)
 {
     static std::atomic<unsigned long long> done{0};
-    const cudaError_t e = allow_smem(attn_batch_dec_kernel<T, HALVES, MT>, BdShape<HALVES>::smem_bytes(MT), done);
+    const cudaError_t e = allow_smem(attn_batch_dec_kernel<T, HALVES, MT>, BdShape<HALVES, MT>::SMEM_BYTES, done);
     if (e != cudaSuccess) return e;
-    return launch(attn_batch_dec_kernel<T, HALVES, MT>, dim3(grid), BD_THREADS, BdShape<HALVES>::smem_bytes(MT), s, after_previous, kv_map, q_map, bv, g);
+    return launch(attn_batch_dec_kernel<T, HALVES, MT>, dim3(grid), BD_THREADS, BdShape<HALVES, MT>::SMEM_BYTES, s, after_previous, kv_map, bv, g);
 }
 
 template <typename T>
-cudaError_t launch_dec_any(const PrefixPlan& p, const CUtensorMap& kv_map, const CUtensorMap& q_map, const BatchView& bv, const BdArgs& g, cudaStream_t s, bool after)
+cudaError_t launch_dec_any(const PrefixPlan& p, const CUtensorMap& kv_map, const BatchView& bv, const BdArgs& g, cudaStream_t s, bool after)
 {
     if (p.dp == 128) {
-        if (p.mt == 1) return launch_dec<T, 2, 1>(kv_map, q_map, bv, g, p.grid, s, after);
-        if (p.mt == 2) return launch_dec<T, 2, 2>(kv_map, q_map, bv, g, p.grid, s, after);
-        return launch_dec<T, 2, 4>(kv_map, q_map, bv, g, p.grid, s, after);
+        if (p.mt == 1) return launch_dec<T, 2, 1>(kv_map, bv, g, p.grid, s, after);
+        if (p.mt == 2) return launch_dec<T, 2, 2>(kv_map, bv, g, p.grid, s, after);
+        return launch_dec<T, 2, 4>(kv_map, bv, g, p.grid, s, after);
     }
-    if (p.mt == 1) return launch_dec<T, 1, 1>(kv_map, q_map, bv, g, p.grid, s, after);
-    if (p.mt == 2) return launch_dec<T, 1, 2>(kv_map, q_map, bv, g, p.grid, s, after);
-    return launch_dec<T, 1, 4>(kv_map, q_map, bv, g, p.grid, s, after);
+    if (p.mt == 1) return launch_dec<T, 1, 1>(kv_map, bv, g, p.grid, s, after);
+    if (p.mt == 2) return launch_dec<T, 1, 2>(kv_map, bv, g, p.grid, s, after);
+    return launch_dec<T, 1, 4>(kv_map, bv, g, p.grid, s, after);
+}
+
+template <typename T>
+cudaError_t launch_join(const BatchView& bv, const BjArgs& j, cudaStream_t s)
+{
+    // four warps per head where a warp each would not fill the machine
+    const bool spread = (long long)bv.n_rows * j.a.n_heads < 148 * 32;
+    return spread ? launch(attn_join_kernel<T, 4>, dim3(bv.n_rows, j.a.n_heads), 128, 0, s, true, bv, j)
+                  : launch(attn_join_kernel<T, 1>, dim3(bv.n_rows, ceil_div(j.a.n_heads, 4)), 128, 0, s, true, bv, j);
 }
 
 swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, int block, const PrefixPlan& p, unsigned char* ws, cudaStream_t s)
@@ -350,16 +360,14 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
         g.a = av;
         g.block = block;
         g.prefix_here = p.prefix_few;
-        g.rows_per_box = 16 * p.mt / p.group;
         g.part_o = reinterpret_cast<float*>(ws + p.few_o);
         g.part_ml = reinterpret_cast<float2*>(ws + p.few_ml);
         g.item_first = reinterpret_cast<int*>(ws + p.first);
         g.item_last = reinterpret_cast<int*>(ws + p.last);
-        CUtensorMap kv_map, q_map;
-        swift_status st = make_kv_map(kv, BD_KEYS, &kv_map);
-        if (st == SWIFT_OK) st = make_q_map(kv, bv, av, g.rows_per_box, &q_map);
+        CUtensorMap kv_map;
+        const swift_status st = make_kv_map(kv, 16 * p.mt, &kv_map);
         if (st != SWIFT_OK) return st;
-        e = kv->dtype == SWIFT_BF16 ? launch_dec_any<__nv_bfloat16>(p, kv_map, q_map, bv, g, s, before) : launch_dec_any<__half>(p, kv_map, q_map, bv, g, s, before);
+        e = kv->dtype == SWIFT_BF16 ? launch_dec_any<__nv_bfloat16>(p, kv_map, bv, g, s, before) : launch_dec_any<__half>(p, kv_map, bv, g, s, before);
     } else {
         t.mode = BT_OWN;
         t.part_slot = p.splits;
@@ -367,8 +375,7 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
         if (st != SWIFT_OK) return st;
     }
     if (e == cudaSuccess) {
-        const dim3 grid(bv.n_rows, ceil_div(av.n_heads, 4));
-        e = kv->dtype == SWIFT_BF16 ? launch(attn_join_kernel<__nv_bfloat16>, grid, 128, 0, s, true, bv, j) : launch(attn_join_kernel<__half>, grid, 128, 0, s, true, bv, j);
+        e = kv->dtype == SWIFT_BF16 ? launch_join<__nv_bfloat16>(bv, j, s) : launch_join<__half>(bv, j, s);
     }
     if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
     return SWIFT_OK;
