@@ -215,11 +215,12 @@ swift_status run_tc(const swift_paged_kv* kv, const BatchView& bv, const BtArgs&
     return SWIFT_OK;
 }
 
-// Pieces of work of the modes that take each sequence by itself: pairs of tiles per sequence, at most.
-long long pair_bound(const BatchView& bv, int n_kv_heads, int rows_per_tile)
+// Pieces of `rows` tokens of the modes that take each sequence by itself, at most.
+long long piece_bound(const BatchView& bv, int n_kv_heads, int rows)
 {
+    if (bv.n_seqs == 1) return (long long)ceil_div(bv.n_rows, rows) * n_kv_heads;
     const long long some = bv.n_seqs < bv.n_rows ? bv.n_seqs : bv.n_rows;
-    return (bv.n_rows / (2 * rows_per_tile) + some) * n_kv_heads;
+    return (bv.n_rows / rows + some) * n_kv_heads;
 }
 
 swift_status run_prompt(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, int block, cudaStream_t s)
@@ -229,7 +230,11 @@ swift_status run_prompt(const swift_paged_kv* kv, const BatchView& bv, const Att
     g.mode = BT_PROMPT;
     g.block = block;
     g.rows_per_tile = BT_ROWS / (av.n_heads / av.n_kv_heads);
-    return run_tc(kv, bv, g, pair_bound(bv, av.n_kv_heads, g.rows_per_tile), s, false);
+    g.wide_out = aligned(av.out, 32) && av.head_dim % 16 == 0;
+    // A pair of tiles takes little longer than one tile (each works while the other waits), so pieces are pairs unless even
+    // single tiles leave no SM more than one.
+    g.tiles = piece_bound(bv, av.n_kv_heads, g.rows_per_tile) <= multiprocessors() ? 1 : 2;
+    return run_tc(kv, bv, g, piece_bound(bv, av.n_kv_heads, g.tiles * g.rows_per_tile), s, false);
 }
 
 // ------------------------------------------------------------------------------ few rows per sequence
@@ -332,6 +337,7 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
     t.a = av;
     t.block = block;
     t.rows_per_tile = BT_ROWS / p.group;
+    t.tiles = 2;
     t.part_o = reinterpret_cast<float*>(ws + p.many_o);
     t.part_ml = reinterpret_cast<float2*>(ws + p.many_ml);
     if (p.splits > 0) {
@@ -371,7 +377,7 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
     } else {
         t.mode = BT_OWN;
         t.part_slot = p.splits;
-        const swift_status st = run_tc(kv, bv, t, pair_bound(bv, av.n_kv_heads, t.rows_per_tile), s, before);
+        const swift_status st = run_tc(kv, bv, t, piece_bound(bv, av.n_kv_heads, 2 * t.rows_per_tile), s, before);
         if (st != SWIFT_OK) return st;
     }
     if (e == cudaSuccess) {

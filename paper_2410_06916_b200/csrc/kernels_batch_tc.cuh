@@ -55,6 +55,8 @@ template <int HALVES> struct BtShape {                                // D up to
 struct BtArgs {
     AttnView a;
     int mode, block, rows_per_tile;                                   // rows_per_tile: tokens of a tile (TQ)
+    int tiles;                                                        // tiles of a piece: 2, or 1 where pairs would leave SMs idle
+    int wide_out;                                                     // out's rows are multiples of 32 bytes
     int splits;                                                       // BT_PREFIX: cuts of the prefix
     float* part_o;                                                    // [slot][row][head][DP] fp32, unnormalised
     float2* part_ml;                                                  // [slot][row][head]: maximum in powers of two, sum
@@ -70,7 +72,7 @@ struct BtItem {
 // The idx-th piece of work, found by a whole warp; false when there are fewer.
 __device__ __forceinline__ bool bt_locate(const BatchView& b, const BtArgs& g, int idx, BtItem& it)
 {
-    const int lane = threadIdx.x & 31, Hk = g.a.n_kv_heads, TQ = g.rows_per_tile, pair_rows = 2 * TQ;
+    const int lane = threadIdx.x & 31, Hk = g.a.n_kv_heads, TQ = g.rows_per_tile, pair_rows = g.tiles * TQ;
     const int prefix_tiles = (b.prefix_len + BT_KEYS - 1) / BT_KEYS;
     it.first_tile = 0;
     it.slot = g.part_slot;
@@ -88,7 +90,7 @@ __device__ __forceinline__ bool bt_locate(const BatchView& b, const BtArgs& g, i
         it.first_tile = (int)((long long)prefix_tiles * s / g.splits);
         it.np = (int)((long long)prefix_tiles * (s + 1) / g.splits) - it.first_tile;
         it.tiles[0] = it.np;
-        it.tiles[1] = it.t0 + TQ < n ? it.np : 0;
+        it.tiles[1] = g.tiles > 1 && it.t0 + TQ < n ? it.np : 0;
         return true;
     }
     for (int base = 0; base < b.n_seqs; base += 32) {
@@ -119,7 +121,7 @@ __device__ __forceinline__ bool bt_locate(const BatchView& b, const BtArgs& g, i
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int t_end = min(it.n, it.t0 + (x + 1) * TQ);        // tokens of this tile end here
-            const bool some = it.t0 + x * TQ < it.n;
+            const bool some = x < g.tiles && it.t0 + x * TQ < it.n;
             const int seen = min(max(it.len - it.n + t_end, 0), it.len);
             it.tiles[x] = some ? it.np + (seen + BT_KEYS - 1) / BT_KEYS : 0;
         }
@@ -203,6 +205,11 @@ __device__ __forceinline__ void split2(f32x2 v, float& a, float& b) { asm("mov.b
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+// 32 bytes at once: a full sector per lane, where lanes write rows of their own (p 32-byte aligned)
+__device__ __forceinline__ void store32(void* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
+}
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -349,67 +356,35 @@ __device__ __forceinline__ bool bt_outgrown(float top, float m, float c)
 // The softmax warps' part of one key tile: S in, P out (over the upper half of S), the row's maximum m and sum l brought up to
 // date.  s_at, o_at: this warp's lanes of S and O; p_bar: the two hand-over barriers.  Scores come a quarter (32 keys) at a
 // time; the upper half of the keys goes first.
-// General form, for tiles with hidden keys: the maximum first, then the exponentials.
-template <typename T, int DP>
-__device__ __forceinline__ void bt_softmax_any(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, int seen, unsigned pages, int page_shift, bool first, float& m, float& l)
+// MASKED: some keys are hidden from some rows.
+template <typename T, int DP, bool MASKED>
+__device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, int seen, unsigned pages, int page_shift, bool first, float& m, float& l)
 {
-    constexpr float BIAS = std::is_same<T, __half>::value ? 7.f : 0.f;
+    constexpr unsigned POLY = MASKED ? 0u : BT_POLY;                  // (the polynomial does not give 0 for a hidden key)
     auto hide = [&](int q, float (&s)[32]) {
+        if (!MASKED) return;
         const unsigned shown = bt_shown(pages, page_shift, seen, q);
 #pragma unroll
         for (int i = 0; i < 32; ++i)
             if (!((shown >> i) & 1u)) s[i] = -INFINITY;
     };
-    float s[32], top = -INFINITY;
-#pragma unroll 1
-    for (int q = 0; q < 4; ++q) {
-        tmem_ld32(s_at + 32 * q, s);
-        tmem_wait_ld(s);
-        hide(q, s);
-        top = fmaxf(top, bt_highest(s));
-    }
-    if (bt_outgrown(top, m, c)) bt_rescale<DP>(o_at, c, top, first, m, l);
-    const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
-    const f32x2 c2 = pair2(c, c), off2 = pair2(off, off);
-    f32x2 sum[2] = {0ull, 0ull};
-#pragma unroll 1
-    for (int h = 1; h >= 0; --h) {                                    // both quarters are read before P overwrites one of them
-        float s2[32];
-        uint32_t p[16];
-        tmem_ld32(s_at + 64 * h, s);
-        tmem_ld32(s_at + 64 * h + 32, s2);
-        tmem_wait_ld(s);
-        tmem_wait_ld(s2);
-        hide(2 * h, s);
-        hide(2 * h + 1, s2);
-        bt_weights<T, 0u>(s, c2, off2, sum, p);
-        tmem_st16(s_at + 64 + 32 * h, p);
-        bt_weights<T, 0u>(s2, c2, off2, sum, p);
-        tmem_st16(s_at + 80 + 32 * h, p);
-        bt_hand_over(p_bar, h);
-    }
-    float l0, l1;
-    split2(add2(sum[0], sum[1]), l0, l1);
-    l += l0 + l1;
-}
-
-// Every key shown: the same without the hiding, with each quarter's load under the arithmetic of the one before.
-template <typename T, int DP>
-__device__ __forceinline__ void bt_softmax_full(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, bool first, float& m, float& l)
-{
     constexpr float BIAS = std::is_same<T, __half>::value ? 7.f : 0.f;
     float s0[32], s1[32], s2[32], s3[32];
     tmem_ld32(s_at, s0);
     tmem_wait_ld(s0);
     tmem_ld32(s_at + 32, s1);
+    hide(0, s0);
     float top = bt_highest(s0);
     tmem_wait_ld(s1);
     tmem_ld32(s_at + 64, s2);
+    hide(1, s1);
     top = fmaxf(top, bt_highest(s1));
     tmem_wait_ld(s2);
     tmem_ld32(s_at + 96, s3);
+    hide(2, s2);
     top = fmaxf(top, bt_highest(s2));
     tmem_wait_ld(s3);
+    hide(3, s3);
     top = fmaxf(top, bt_highest(s3));
     if (bt_outgrown(top, m, c)) bt_rescale<DP>(o_at, c, top, first, m, l);
     const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
@@ -417,17 +392,19 @@ __device__ __forceinline__ void bt_softmax_full(uint32_t s_at, uint32_t o_at, ui
     f32x2 sum[2] = {0ull, 0ull};
     uint32_t p[16];
     tmem_ld32(s_at, s0);
-    bt_weights<T, BT_POLY>(s2, c2, off2, sum, p);
+    bt_weights<T, POLY>(s2, c2, off2, sum, p);
     tmem_st16(s_at + 96, p);
-    bt_weights<T, BT_POLY>(s3, c2, off2, sum, p);
+    bt_weights<T, POLY>(s3, c2, off2, sum, p);
     tmem_st16(s_at + 112, p);
     bt_hand_over(p_bar, 1);
     tmem_wait_ld(s0);
     tmem_ld32(s_at + 32, s1);
-    bt_weights<T, BT_POLY>(s0, c2, off2, sum, p);
+    hide(0, s0);
+    bt_weights<T, POLY>(s0, c2, off2, sum, p);
     tmem_st16(s_at + 64, p);
     tmem_wait_ld(s1);
-    bt_weights<T, BT_POLY>(s1, c2, off2, sum, p);
+    hide(1, s1);
+    bt_weights<T, POLY>(s1, c2, off2, sum, p);
     tmem_st16(s_at + 80, p);
     bt_hand_over(p_bar, 0);
     float l0, l1;
@@ -670,7 +647,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
         for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
             const int n_tiles = max(it.tiles[0], it.tiles[1]), mine = it.tiles[x];
             const int t = it.t0 + x * TQ + tok;                       // token within the sequence
-            const bool live = tok < TQ && t < it.n && (g.mode == BT_PREFIX || t < g.a.max_rows);
+            const bool live = x < g.tiles && tok < TQ && t < it.n && (g.mode == BT_PREFIX || t < g.a.max_rows);
             const int own = it.len - it.n + t;                        // own position: keys 0 .. own are seen
             const int all_see = it.len - it.n + it.t0 + x * TQ + 1;    // own keys that every row of the tile sees
             float m = -INFINITY, l = 0.f;
@@ -683,8 +660,8 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 const int seen = j < it.np ? b.prefix_len - key0 : own + 1 - key0;        // this row sees keys below this
                 const unsigned pages = page_bits[(tile_no + j) & (BT_PAGE_RING - 1)];
                 const bool masked = key0 + BT_KEYS > (j < it.np ? b.prefix_len : all_see) || pages != all_pages;
-                if (masked) bt_softmax_any<T, DP>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
-                else bt_softmax_full<T, DP>(s_at, o_at, p_ready(x, 0), c, j == 0, m, l);
+                if (masked) bt_softmax<T, DP, true>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
+                else bt_softmax<T, DP, false>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
             }
             tile_no += n_tiles;
             if (!ok) break;
@@ -707,9 +684,11 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                         tmem_wait_ld(o);
                     }
                     if (live && l != 0.f) {
-                        float4* dst = reinterpret_cast<float4*>(g.part_o + at * DP + i);
+                        float* dst = g.part_o + at * DP + i;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        for (int e = 0; e < 32; e += 8)
+                            store32(dst + e, __float_as_uint(o[e]), __float_as_uint(o[e + 1]), __float_as_uint(o[e + 2]), __float_as_uint(o[e + 3]),
+                                    __float_as_uint(o[e + 4]), __float_as_uint(o[e + 5]), __float_as_uint(o[e + 6]), __float_as_uint(o[e + 7]));
                     }
                 }
             } else {
@@ -722,12 +701,18 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                         tmem_wait_ld(o);
                     }
                     if (live) {
+                        uint32_t v[16];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float v[8];
+                        for (int e = 0; e < 16; ++e) v[e] = l == 0.f ? 0u : pack2(o[2 * e] * inv, o[2 * e + 1] * inv, T());
+                        if (g.wide_out) {
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] = l == 0.f ? 0.f : o[8 * e + k] * inv;
-                            if (i + 8 * e < g.a.head_dim) store8(dst + i + 8 * e, v);
+                            for (int e = 0; e < 16; e += 8)
+                                if (i + 2 * e < g.a.head_dim)
+                                    store32(dst + i + 2 * e, v[e], v[e + 1], v[e + 2], v[e + 3], v[e + 4], v[e + 5], v[e + 6], v[e + 7]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4)
+                                if (i + 2 * e < g.a.head_dim) *reinterpret_cast<uint4*>(dst + i + 2 * e) = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
                         }
                     }
                 }
