@@ -12,7 +12,6 @@ device tensors it rewrites), and calls per layer:
 from __future__ import annotations
 
 import ctypes as C
-import math
 from typing import Optional
 
 import torch
@@ -56,30 +55,38 @@ def _check(status: int) -> None:
         raise SwiftError(status, lib().swift_batch_error().decode())
 
 
-class _Target:
-    """The device and stream one call runs on.  `stream` None: the current stream of the tensors' device."""
+def _raw_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
 
-    __slots__ = ("device", "stream", "guards")
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)     # the same handle without a Stream object
+
+
+class _Target:
+    """Makes `device` current, and `stream` if one is given: outputs and workspaces made inside then belong to that stream."""
+
+    __slots__ = ("guards",)
 
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
         if stream is not None and stream.device != device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-        self.device, self.stream, self.guards = device, stream, []
+        self.guards = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
 
-    def __enter__(self) -> C.c_void_p:
-        if self.stream is not None:
-            g = torch.cuda.stream(self.stream)      # outputs and workspaces made inside belong to that stream
+    def __enter__(self) -> None:
+        for g in self.guards:
             g.__enter__()
-            self.guards.append(g)
-        elif torch.cuda.current_device() != self.device.index:
-            g = torch.cuda.device(self.device)
-            g.__enter__()
-            self.guards.append(g)
-        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
 
     def __exit__(self, *exc) -> None:
-        while self.guards:
-            self.guards.pop().__exit__(*exc)
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+
+
+def _on(device: torch.device, stream: Optional[torch.cuda.Stream], call, *args):
+    """call(raw stream, *args) with `device` current, on `stream` or else the device's current stream."""
+    if stream is None and torch.cuda.current_device() == device.index:
+        return call(_raw_stream(device.index), *args)
+    with _Target(device, stream):
+        return call(_raw_stream(device.index), *args)
 
 
 def _cuda_tensor(name: str, t: torch.Tensor, device: Optional[torch.device] = None) -> torch.Tensor:
@@ -113,11 +120,14 @@ def rope_table(n_positions: int, rotary_dim: int, theta: float = 10000.0, factor
     desc = _RopeDesc(n_positions, rotary_dim, theta, factor, original_positions, low_turns, high_turns, magnitude)
     if n_positions < 0 or rotary_dim < 2:
         raise ValueError("n_positions >= 0 and rotary_dim >= 2")
-    with _Target(device, stream) as s:
-        if out is None:
-            out = torch.empty(n_positions, rotary_dim // 2, 2, dtype=torch.float32, device=device)
-        if n_positions > 0:
-            _check(lib().swift_rope_table(C.byref(desc), C.c_void_p(out.data_ptr()), s))
+    return _on(device, stream, _rope_table, desc, device, out)
+
+
+def _rope_table(s: int, desc: _RopeDesc, device: torch.device, out: Optional[torch.Tensor]) -> torch.Tensor:
+    if out is None:
+        out = torch.empty(desc.n_positions, desc.rotary_dim // 2, 2, dtype=torch.float32, device=device)
+    if desc.n_positions > 0:
+        _check(lib().swift_rope_table(C.byref(desc), out.data_ptr(), s))
     return out
 
 
@@ -170,26 +180,33 @@ class RowBatch:
         self._c = _Batch(n_seqs, n_rows, row_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), page_table.shape[1],
                          prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len)
         self._kv_p, self._c_p = C.byref(kv._c), C.byref(self._c)
+        self._lib, self._types, self._scale = lib(), (kv.dtype,), kv.head_dim ** -0.5
         self._ws_bytes = {}
 
     # ------------------------------------------------------------------ checks shared by the calls
     def _rows(self, name: str, t: torch.Tensor, heads: Optional[int], dtypes) -> _Rows:
-        _cuda_tensor(name, t, self.kv.device)
-        if t.dim() != 3 or t.shape[0] != self.n_rows or t.shape[2] != self.kv.head_dim or (heads is not None and t.shape[1] != heads):
-            raise ValueError(f"{name} must be [{self.n_rows}, {heads if heads is not None else 'heads'}, {self.kv.head_dim}], got {tuple(t.shape)}")
+        kv = self.kv
+        if not isinstance(t, torch.Tensor) or t.device != kv.device:
+            _cuda_tensor(name, t, kv.device)
+        shape = t.shape
+        if len(shape) != 3 or shape[0] != self.n_rows or shape[2] != kv.head_dim or (heads is not None and shape[1] != heads):
+            raise ValueError(f"{name} must be [{self.n_rows}, {heads if heads is not None else 'heads'}, {kv.head_dim}], got {tuple(shape)}")
         if t.dtype not in dtypes:
             raise TypeError(f"{name} must be one of {dtypes}, got {t.dtype}")
-        if t.stride(2) != 1:
+        row, head, dim = t.stride()
+        if dim != 1:
             raise ValueError(f"the dims of {name} must be contiguous")
-        return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+        # a stride over a single row or head means nothing
+        return _Rows(t.data_ptr(), row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2])
 
-    def _out(self, out: Optional[torch.Tensor], q: torch.Tensor) -> torch.Tensor:
-        shape = (self.n_rows, q.shape[1], self.kv.head_dim)
+    def _out(self, out: Optional[torch.Tensor], heads: int) -> torch.Tensor:
+        kv = self.kv
         if out is None:
-            return torch.empty(shape, dtype=self.kv.dtype, device=self.kv.device)
-        _cuda_tensor("out", out, self.kv.device)
-        if tuple(out.shape) != shape or out.dtype != self.kv.dtype or not out.is_contiguous():
-            raise ValueError(f"out must be contiguous {shape} of {self.kv.dtype}")
+            return torch.empty(self.n_rows, heads, kv.head_dim, dtype=kv.dtype, device=kv.device)
+        if not isinstance(out, torch.Tensor) or out.device != kv.device:
+            _cuda_tensor("out", out, kv.device)
+        if out.shape != (self.n_rows, heads, kv.head_dim) or out.dtype != kv.dtype or not out.is_contiguous():
+            raise ValueError(f"out must be contiguous {(self.n_rows, heads, kv.head_dim)} of {kv.dtype}")
         return out
 
     # ------------------------------------------------------------------ the calls
@@ -223,44 +240,47 @@ class RowBatch:
             if tuple(_int32("positions", positions, kv.device).shape) != (self.n_rows,):
                 raise ValueError(f"positions must be [{self.n_rows}]")
             a.positions = positions.data_ptr()
-        with _Target(kv.device, stream) as s:
-            out = self._out(out, q)
-            a.q_out = out.data_ptr()
-            _check(lib().swift_kv_append(self._kv_p, self._c_p, C.byref(a), s))
+        return _on(kv.device, stream, self._append, a, out)
+
+    def _append(self, s: int, a: _Append, out: Optional[torch.Tensor]) -> torch.Tensor:
+        out = self._out(out, a.n_heads)
+        a.q_out = out.data_ptr()
+        _check(self._lib.swift_kv_append(self._kv_p, self._c_p, C.byref(a), s))
         return out
 
     def _attention(self, block: int, q: torch.Tensor, scale: Optional[float]) -> _Attention:
-        rows = self._rows("q", q, None, (self.kv.dtype,))
-        return _Attention(block, q.shape[1], rows, 1.0 / math.sqrt(self.kv.head_dim) if scale is None else scale, None)
+        rows = self._rows("q", q, None, self._types)
+        return _Attention(block, q.shape[1], rows, self._scale if scale is None else scale, None)
 
     def prompt_attention(self, block: int, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Causal attention of every row over the prefix and its sequence's own positions up to its own; [n_rows, heads,
         head_dim] in the cache's type.  scale defaults to head_dim ** -0.5.  Padding rows keep what `out` held."""
-        a = self._attention(block, q, scale)
-        with _Target(self.kv.device, stream) as s:
-            out = self._out(out, q)
-            a.out = out.data_ptr()
-            _check(lib().swift_prompt_attention(self._kv_p, self._c_p, C.byref(a), s))
+        return _on(self.kv.device, stream, self._prompt, self._attention(block, q, scale), out)
+
+    def _prompt(self, s: int, a: _Attention, out: Optional[torch.Tensor]) -> torch.Tensor:
+        out = self._out(out, a.n_heads)
+        a.out = out.data_ptr()
+        _check(self._lib.swift_prompt_attention(self._kv_p, self._c_p, C.byref(a), s))
         return out
 
     def prefix_attention(self, block: int, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The same function for few rows per sequence: what all rows share of the prefix is computed once for all of them.
         Rows of a sequence beyond max_rows are left out."""
-        a = self._attention(block, q, scale)
-        heads = q.shape[1]
-        need = self._ws_bytes.get(heads)
+        return _on(self.kv.device, stream, self._prefix, self._attention(block, q, scale), out)
+
+    def _prefix(self, s: int, a: _Attention, out: Optional[torch.Tensor]) -> torch.Tensor:
+        need = self._ws_bytes.get(a.n_heads)
         if need is None:
-            need = lib().swift_prefix_workspace_bytes(self._kv_p, self._c_p, heads, self.max_rows)
+            need = self._lib.swift_prefix_workspace_bytes(self._kv_p, self._c_p, a.n_heads, self.max_rows)
             if need == 0:
-                raise SwiftError(1, lib().swift_batch_error().decode())
-            self._ws_bytes[heads] = need
-        with _Target(self.kv.device, stream) as s:
-            out = self._out(out, q)
-            a.out = out.data_ptr()
-            ws = torch.empty(need, dtype=torch.uint8, device=self.kv.device)     # of this call alone; the allocator aligns to 512
-            _check(lib().swift_prefix_attention(self._kv_p, self._c_p, C.byref(a), self.max_rows, _DevBuf(ws.data_ptr(), need), s))
+                raise SwiftError(1, self._lib.swift_batch_error().decode())
+            self._ws_bytes[a.n_heads] = need
+        out = self._out(out, a.n_heads)
+        a.out = out.data_ptr()
+        ws = torch.empty(need, dtype=torch.uint8, device=self.kv.device)     # of this call alone; the allocator aligns to 512
+        _check(self._lib.swift_prefix_attention(self._kv_p, self._c_p, C.byref(a), self.max_rows, _DevBuf(ws.data_ptr(), need), s))
         return out
 
 
@@ -271,5 +291,4 @@ def batch_sync(device="cuda", stream: Optional[torch.cuda.Stream] = None) -> Non
         raise ValueError("batch_sync needs a CUDA device")
     if device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
-    with _Target(device, stream) as s:
-        _check(lib().swift_batch_sync(s))
+    _on(device, stream, lambda s: _check(lib().swift_batch_sync(s)))
