@@ -404,13 +404,15 @@ cudaError_t launch_append(const BatchView& b, const AppendView& a, bool vec, cud
     if (!vec) return launch(append_any_kernel<TX, TC>, dim3(b.n_rows, ceil_div(units, AP_THREADS / 32)), AP_THREADS, 0, s, false, b, a);
     const int pieces = a.head_dim / 16;
     const int lph = pieces <= 1 ? 1 : pieces <= 2 ? 2 : pieces <= 4 ? 4 : pieces <= 8 ? 8 : 16;
-    const dim3 grid(b.n_rows, ceil_div(units, AP_THREADS / lph * AP_UNROLL));
+    // heads of a row shared evenly among as few blocks as hold them
+    const int groups = AP_THREADS / lph, chunks = ceil_div(units, groups * AP_UNROLL), per_block = ceil_div(ceil_div(units, chunks), groups) * groups;
+    const dim3 grid(b.n_rows, ceil_div(units, per_block));
     switch (lph) {
-    case 1: return launch(append_vec_kernel<TX, TC, 1>, grid, AP_THREADS, 0, s, false, b, a);
-    case 2: return launch(append_vec_kernel<TX, TC, 2>, grid, AP_THREADS, 0, s, false, b, a);
-    case 4: return launch(append_vec_kernel<TX, TC, 4>, grid, AP_THREADS, 0, s, false, b, a);
-    case 8: return launch(append_vec_kernel<TX, TC, 8>, grid, AP_THREADS, 0, s, false, b, a);
-    default: return launch(append_vec_kernel<TX, TC, 16>, grid, AP_THREADS, 0, s, false, b, a);
+    case 1: return launch(append_vec_kernel<TX, TC, 1>, grid, AP_THREADS, 0, s, false, b, a, per_block);
+    case 2: return launch(append_vec_kernel<TX, TC, 2>, grid, AP_THREADS, 0, s, false, b, a, per_block);
+    case 4: return launch(append_vec_kernel<TX, TC, 4>, grid, AP_THREADS, 0, s, false, b, a, per_block);
+    case 8: return launch(append_vec_kernel<TX, TC, 8>, grid, AP_THREADS, 0, s, false, b, a, per_block);
+    default: return launch(append_vec_kernel<TX, TC, 16>, grid, AP_THREADS, 0, s, false, b, a, per_block);
     }
 }
 

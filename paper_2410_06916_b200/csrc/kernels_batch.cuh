@@ -68,23 +68,10 @@ __device__ __forceinline__ int find_seq(const BatchView& b, int row, SeqSpan& sp
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 __device__ __forceinline__ void store_val(__half* p, float v) { *p = __float2half_rn(v); }
 
-// eight values as fp32, from 16-byte loads
-__device__ __forceinline__ void load8(const float* p, float (&x)[8])
+__device__ __forceinline__ void load8(const float* p, float (&x)[8])      // from 16-byte loads
 {
     const float4 a = reinterpret_cast<const float4*>(p)[0], c = reinterpret_cast<const float4*>(p)[1];
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = c.x; x[5] = c.y; x[6] = c.z; x[7] = c.w;
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) { load_vec(p, x); }
-__device__ __forceinline__ void load8(const __half* p, float (&x)[8])
-{
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
-    }
 }
 __device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16)      // a in the low half
 {
@@ -106,6 +93,39 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8])
 {
     reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+// eight values as they lie in memory, to be widened when they are used
+template <typename T> struct Raw8 { uint4 v; };
+template <> struct Raw8<float> { float4 a, b; };
+template <typename T> __device__ __forceinline__ void fetch8(const T* p, Raw8<T>& r) { r.v = __ldcs(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ void fetch8(const float* p, Raw8<float>& r)
+{
+    r.a = __ldcs(reinterpret_cast<const float4*>(p));
+    r.b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+}
+__device__ __forceinline__ void widen8(const Raw8<float>& r, float (&x)[8])
+{
+    x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w; x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
+}
+__device__ __forceinline__ void widen8(const Raw8<__nv_bfloat16>& r, float (&x)[8])
+{
+    const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void widen8(const Raw8<__half>& r, float (&x)[8])
+{
+    const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
 }
 
 // ------------------------------------------------------------------------------ rotary table
@@ -182,19 +202,20 @@ __device__ __forceinline__ bool place_row(const BatchView& b, const AppendView& 
 
 // Vector form.  A group of LPH lanes (a power of two >= head_dim / 16) takes one head; a lane holds two pieces of 8 dims
 // that a rotation pairs up: with pairs (i, i + R/2), piece c and the piece R/2 further on; with neighbouring pairs, or
-// behind the rotated part, two pieces side by side.  So no value crosses lanes except the norm's sum.  A warp stays
+// behind the rotated part, two pieces side by side.  So no value crosses lanes except the norm's sum.  A block stays
 // within one row: the row is located once per warp, and its 8 (cos, sin) pairs stay in registers for all its heads.
-// Loads of a lane's UNROLL heads are issued together.  Bound by HBM for many rows, by three dependent trips to memory
-// (row start, page table or cos/sin, data) for few.  grid = (rows, head chunks), block = 128.
+// A lane's UNROLL heads are loaded together and before the row is located, in the 16 bytes that they have in memory.  Bound
+// by HBM for many rows, by three dependent trips to memory (row start, page table or cos/sin, stores) for few.
+// grid = (rows, head chunks), block = 128; a block takes `per_block` heads.
 constexpr int AP_THREADS = 128, AP_UNROLL = 4;
 
 template <typename TX, typename TC, int LPH>
-__global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, AppendView a)
+__global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, AppendView a, int per_block)
 {
     constexpr int GROUPS = AP_THREADS / LPH;
     const int row = blockIdx.x, c = threadIdx.x & (LPH - 1), grp = threadIdx.x / LPH;
     const int D = a.head_dim, half = a.rotary_dim >> 1, pieces = D >> 4;
-    const int units = a.n_heads + 2 * a.n_kv_heads, u0 = blockIdx.y * (GROUPS * AP_UNROLL) + grp;
+    const int u0 = blockIdx.y * per_block, units = min(u0 + per_block, a.n_heads + 2 * a.n_kv_heads);
     const bool lane_live = c < pieces;
     int oa, ob;                                           // the two pieces' first dims
     bool turned;
@@ -208,19 +229,23 @@ __global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, App
         oa = turned ? 8 * c : a.rotary_dim + 16 * (c - rc);
         ob = turned ? oa + half : oa + 8;
     }
-    float xa[AP_UNROLL][8], xb[AP_UNROLL][8];
+    auto which = [&](int u, int& h) {                     // 0 q, 1 k, 2 v; its head
+        const int w = u < a.n_heads ? 0 : u < a.n_heads + a.n_kv_heads ? 1 : 2;
+        h = w == 0 ? u : w == 1 ? u - a.n_heads : u - a.n_heads - a.n_kv_heads;
+        return w;
+    };
+    Raw8<TX> ra[AP_UNROLL], rb[AP_UNROLL];
 #pragma unroll
     for (int j = 0; j < AP_UNROLL; ++j) {
-        const int u = u0 + j * GROUPS;
+        const int u = u0 + grp + j * GROUPS;
+        ra[j] = {};
+        rb[j] = {};
         if (lane_live && u < units) {
-            const int w = u < a.n_heads ? 0 : u < a.n_heads + a.n_kv_heads ? 1 : 2;
-            const int h = w == 0 ? u : w == 1 ? u - a.n_heads : u - a.n_heads - a.n_kv_heads;
+            int h;
+            const int w = which(u, h);
             const TX* src = reinterpret_cast<const TX*>(a.x[w]) + row * a.row_stride[w] + h * a.head_stride[w];
-            load8(src + oa, xa[j]);
-            load8(src + ob, xb[j]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) xa[j][e] = xb[j][e] = 0.f;
+            fetch8(src + oa, ra[j]);
+            fetch8(src + ob, rb[j]);
         }
     }
     RowPlace place;
@@ -238,13 +263,17 @@ __global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, App
     }
 #pragma unroll
     for (int j = 0; j < AP_UNROLL; ++j) {
-        const int u = u0 + j * GROUPS;
-        const int w = u < a.n_heads ? 0 : u < a.n_heads + a.n_kv_heads ? 1 : 2;
-        const int h = w == 0 ? u : w == 1 ? u - a.n_heads : u - a.n_heads - a.n_kv_heads;
+        const int u = u0 + grp + j * GROUPS;
+        if (u0 + j * GROUPS >= units) break;              // the same for the whole block
+        int h;
+        const int w = which(u, h);
+        float xa[8], xb[8];
+        widen8(ra[j], xa);
+        widen8(rb[j], xb);
         if (a.gain[0] != nullptr || a.gain[1] != nullptr) {
             float ss = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss += xa[j][e] * xa[j][e] + xb[j][e] * xb[j][e];
+            for (int e = 0; e < 8; ++e) ss += xa[e] * xa[e] + xb[e] * xb[e];
 #pragma unroll
             for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(FULL_WARP, ss, o);
             const float* gain = w < 2 ? a.gain[w] : nullptr;
@@ -255,8 +284,8 @@ __global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, App
                 load8(gain + ob, gb);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    xa[j][e] *= r * ga[e];
-                    xb[j][e] *= r * gb[e];
+                    xa[e] *= r * ga[e];
+                    xb[e] *= r * gb[e];
                 }
             }
         }
@@ -265,25 +294,25 @@ __global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, App
             if (a.interleaved) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x0 = xa[j][2 * e], y0 = xa[j][2 * e + 1], x1 = xb[j][2 * e], y1 = xb[j][2 * e + 1];
-                    xa[j][2 * e] = x0 * cs[e].x - y0 * cs[e].y;
-                    xa[j][2 * e + 1] = y0 * cs[e].x + x0 * cs[e].y;
-                    xb[j][2 * e] = x1 * cs[4 + e].x - y1 * cs[4 + e].y;
-                    xb[j][2 * e + 1] = y1 * cs[4 + e].x + x1 * cs[4 + e].y;
+                    const float x0 = xa[2 * e], y0 = xa[2 * e + 1], x1 = xb[2 * e], y1 = xb[2 * e + 1];
+                    xa[2 * e] = x0 * cs[e].x - y0 * cs[e].y;
+                    xa[2 * e + 1] = y0 * cs[e].x + x0 * cs[e].y;
+                    xb[2 * e] = x1 * cs[4 + e].x - y1 * cs[4 + e].y;
+                    xb[2 * e + 1] = y1 * cs[4 + e].x + x1 * cs[4 + e].y;
                 }
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float x = xa[j][e], y = xb[j][e];
-                    xa[j][e] = x * cs[e].x - y * cs[e].y;
-                    xb[j][e] = y * cs[e].x + x * cs[e].y;
+                    const float x = xa[e], y = xb[e];
+                    xa[e] = x * cs[e].x - y * cs[e].y;
+                    xb[e] = y * cs[e].x + x * cs[e].y;
                 }
             }
         }
         TC* dst = w == 0 ? reinterpret_cast<TC*>(a.q_out) + ((size_t)row * a.n_heads + h) * D
                          : reinterpret_cast<TC*>(a.pool) + place.kv_off + (w == 2 ? a.kv_elems : 0) + ((size_t)h * b.page_size + place.slot) * D;
-        store8(dst + oa, xa[j]);
-        store8(dst + ob, xb[j]);
+        store8(dst + oa, xa);
+        store8(dst + ob, xb);
     }
 }
 
