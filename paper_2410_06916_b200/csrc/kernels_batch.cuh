@@ -202,20 +202,23 @@ __device__ __forceinline__ bool place_row(const BatchView& b, const AppendView& 
 
 // Vector form.  A group of LPH lanes (a power of two >= head_dim / 16) takes one head; a lane holds two pieces of 8 dims
 // that a rotation pairs up: with pairs (i, i + R/2), piece c and the piece R/2 further on; with neighbouring pairs, or
-// behind the rotated part, two pieces side by side.  So no value crosses lanes except the norm's sum.  A block stays
-// within one row: the row is located once per warp, and its 8 (cos, sin) pairs stay in registers for all its heads.
-// A lane's UNROLL heads are loaded together and before the row is located, in the 16 bytes that they have in memory.  Bound
-// by HBM for many rows, by three dependent trips to memory (row start, page table or cos/sin, stores) for few.
-// grid = (rows, head chunks), block = 128; a block takes `per_block` heads.
+// behind the rotated part, two pieces side by side.  So no value crosses lanes except the norm's sum.  A warp stays within
+// one row: it locates the row once (three dependent trips to memory), keeps the row's 8 (cos, sin) pairs and the gains in
+// registers, and goes through `per_warp` of its heads, AP_UNROLL loads ahead, kept in the 16 bytes they have in memory until
+// used.  Many rows: a whole row per warp, bound by HBM; few rows: as few heads per warp as one batch of loads holds, bound
+// by the trips.  grid = ceil(rows x chunks / 4), block = 128.
 constexpr int AP_THREADS = 128, AP_UNROLL = 4;
 
 template <typename TX, typename TC, int LPH>
-__global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, AppendView a, int per_block)
+__global__ void __launch_bounds__(AP_THREADS, 5) append_vec_kernel(BatchView b, AppendView a, int per_warp, int chunks)
 {
-    constexpr int GROUPS = AP_THREADS / LPH;
-    const int row = blockIdx.x, c = threadIdx.x & (LPH - 1), grp = threadIdx.x / LPH;
+    constexpr int GROUPS = 32 / LPH;
+    const int lane = threadIdx.x & 31, c = lane & (LPH - 1), grp = lane / LPH;
+    const long long job = (long long)blockIdx.x * (AP_THREADS / 32) + (threadIdx.x >> 5);
+    const int row = (int)(job / chunks);
+    if (row >= b.n_rows) return;
     const int D = a.head_dim, half = a.rotary_dim >> 1, pieces = D >> 4;
-    const int u0 = blockIdx.y * per_block, units = min(u0 + per_block, a.n_heads + 2 * a.n_kv_heads);
+    const int u0 = (int)(job - (long long)row * chunks) * per_warp, units = min(u0 + per_warp, a.n_heads + 2 * a.n_kv_heads);
     const bool lane_live = c < pieces;
     int oa, ob;                                           // the two pieces' first dims
     bool turned;
@@ -235,21 +238,24 @@ __global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, App
         return w;
     };
     Raw8<TX> ra[AP_UNROLL], rb[AP_UNROLL];
+    auto fetch = [&](int first) {                         // heads first + grp, + GROUPS, ...
 #pragma unroll
-    for (int j = 0; j < AP_UNROLL; ++j) {
-        const int u = u0 + grp + j * GROUPS;
-        ra[j] = {};
-        rb[j] = {};
-        if (lane_live && u < units) {
-            int h;
-            const int w = which(u, h);
-            const TX* src = reinterpret_cast<const TX*>(a.x[w]) + row * a.row_stride[w] + h * a.head_stride[w];
-            fetch8(src + oa, ra[j]);
-            fetch8(src + ob, rb[j]);
+        for (int j = 0; j < AP_UNROLL; ++j) {
+            const int u = first + grp + j * GROUPS;
+            ra[j] = {};
+            rb[j] = {};
+            if (lane_live && u < units) {
+                int h;
+                const int w = which(u, h);
+                const TX* src = reinterpret_cast<const TX*>(a.x[w]) + row * a.row_stride[w] + h * a.head_stride[w];
+                fetch8(src + oa, ra[j]);
+                fetch8(src + ob, rb[j]);
+            }
         }
-    }
+    };
+    fetch(u0);
     RowPlace place;
-    if (!place_row(b, a, row, place)) return;             // the same for the whole block
+    if (!place_row(b, a, row, place)) return;             // the same for the whole warp
     float2 cs[8];
     turned = turned && a.rope != nullptr && lane_live;
     if (turned) {
@@ -261,58 +267,62 @@ __global__ void __launch_bounds__(AP_THREADS) append_vec_kernel(BatchView b, App
             cs[2 * e + 1] = make_float2(v.z, v.w);
         }
     }
+    const bool normed = a.gain[0] != nullptr || a.gain[1] != nullptr;
+    for (int first = u0; first < units; first += AP_UNROLL * GROUPS) {
 #pragma unroll
-    for (int j = 0; j < AP_UNROLL; ++j) {
-        const int u = u0 + grp + j * GROUPS;
-        if (u0 + j * GROUPS >= units) break;              // the same for the whole block
-        int h;
-        const int w = which(u, h);
-        float xa[8], xb[8];
-        widen8(ra[j], xa);
-        widen8(rb[j], xb);
-        if (a.gain[0] != nullptr || a.gain[1] != nullptr) {
-            float ss = 0.f;
+        for (int j = 0; j < AP_UNROLL; ++j) {
+            if (first + j * GROUPS >= units) break;       // the same for the whole warp
+            const int u = first + grp + j * GROUPS;
+            int h;
+            const int w = which(u, h);
+            float xa[8], xb[8];
+            widen8(ra[j], xa);
+            widen8(rb[j], xb);
+            if (normed) {
+                float ss = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss += xa[e] * xa[e] + xb[e] * xb[e];
+                for (int e = 0; e < 8; ++e) ss += xa[e] * xa[e] + xb[e] * xb[e];
 #pragma unroll
-            for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(FULL_WARP, ss, o);
-            const float* gain = w < 2 ? a.gain[w] : nullptr;
-            if (gain != nullptr && lane_live) {
-                const float r = rsqrtf(ss / (float)D + a.eps);
-                float ga[8], gb[8];
-                load8(gain + oa, ga);
-                load8(gain + ob, gb);
+                for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(FULL_WARP, ss, o);
+                const float* gain = w < 2 ? a.gain[w] : nullptr;
+                if (gain != nullptr && lane_live) {
+                    const float r = rsqrtf(ss / (float)D + a.eps);
+                    float ga[8], gb[8];
+                    load8(gain + oa, ga);
+                    load8(gain + ob, gb);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    xa[e] *= r * ga[e];
-                    xb[e] *= r * gb[e];
+                    for (int e = 0; e < 8; ++e) {
+                        xa[e] *= r * ga[e];
+                        xb[e] *= r * gb[e];
+                    }
                 }
             }
-        }
-        if (!lane_live || u >= units) continue;
-        if (turned && w < 2) {
-            if (a.interleaved) {
+            if (!lane_live || u >= units) continue;
+            if (turned && w < 2) {
+                if (a.interleaved) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x0 = xa[2 * e], y0 = xa[2 * e + 1], x1 = xb[2 * e], y1 = xb[2 * e + 1];
-                    xa[2 * e] = x0 * cs[e].x - y0 * cs[e].y;
-                    xa[2 * e + 1] = y0 * cs[e].x + x0 * cs[e].y;
-                    xb[2 * e] = x1 * cs[4 + e].x - y1 * cs[4 + e].y;
-                    xb[2 * e + 1] = y1 * cs[4 + e].x + x1 * cs[4 + e].y;
-                }
-            } else {
+                    for (int e = 0; e < 4; ++e) {
+                        const float x0 = xa[2 * e], y0 = xa[2 * e + 1], x1 = xb[2 * e], y1 = xb[2 * e + 1];
+                        xa[2 * e] = x0 * cs[e].x - y0 * cs[e].y;
+                        xa[2 * e + 1] = y0 * cs[e].x + x0 * cs[e].y;
+                        xb[2 * e] = x1 * cs[4 + e].x - y1 * cs[4 + e].y;
+                        xb[2 * e + 1] = y1 * cs[4 + e].x + x1 * cs[4 + e].y;
+                    }
+                } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = xa[e], y = xb[e];
-                    xa[e] = x * cs[e].x - y * cs[e].y;
-                    xb[e] = y * cs[e].x + x * cs[e].y;
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = xa[e], y = xb[e];
+                        xa[e] = x * cs[e].x - y * cs[e].y;
+                        xb[e] = y * cs[e].x + x * cs[e].y;
+                    }
                 }
             }
+            TC* dst = w == 0 ? reinterpret_cast<TC*>(a.q_out) + ((size_t)row * a.n_heads + h) * D
+                             : reinterpret_cast<TC*>(a.pool) + place.kv_off + (w == 2 ? a.kv_elems : 0) + ((size_t)h * b.page_size + place.slot) * D;
+            store8(dst + oa, xa);
+            store8(dst + ob, xb);
         }
-        TC* dst = w == 0 ? reinterpret_cast<TC*>(a.q_out) + ((size_t)row * a.n_heads + h) * D
-                         : reinterpret_cast<TC*>(a.pool) + place.kv_off + (w == 2 ? a.kv_elems : 0) + ((size_t)h * b.page_size + place.slot) * D;
-        store8(dst + oa, xa);
-        store8(dst + ob, xb);
+        if (first + AP_UNROLL * GROUPS < units) fetch(first + AP_UNROLL * GROUPS);
     }
 }
 
