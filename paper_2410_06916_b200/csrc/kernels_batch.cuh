@@ -180,6 +180,13 @@ struct AppendView {
     long long page_elems, kv_elems;                       // elements per page (all blocks), per K or V of a block
 };
 
+// One pair turned.  The contraction is spelt out so that both forms of the kernel give the same bits.
+__device__ __forceinline__ void turn_pair(float x, float y, float2 cs, float& a, float& b)   // x, y by value: a, b may be they
+{
+    a = fmaf(x, cs.x, -__fmul_rn(y, cs.y));
+    b = fmaf(y, cs.x, __fmul_rn(x, cs.y));
+}
+
 // What a row needs to know besides its data: where it goes and which table row turns it.  `slot` < 0: the row is left out.
 struct RowPlace { long long kv_off; int slot, rope_row; };
 
@@ -302,19 +309,12 @@ __global__ void __launch_bounds__(AP_THREADS, 5) append_vec_kernel(BatchView b, 
                 if (a.interleaved) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float x0 = xa[2 * e], y0 = xa[2 * e + 1], x1 = xb[2 * e], y1 = xb[2 * e + 1];
-                        xa[2 * e] = x0 * cs[e].x - y0 * cs[e].y;
-                        xa[2 * e + 1] = y0 * cs[e].x + x0 * cs[e].y;
-                        xb[2 * e] = x1 * cs[4 + e].x - y1 * cs[4 + e].y;
-                        xb[2 * e + 1] = y1 * cs[4 + e].x + x1 * cs[4 + e].y;
+                        turn_pair(xa[2 * e], xa[2 * e + 1], cs[e], xa[2 * e], xa[2 * e + 1]);
+                        turn_pair(xb[2 * e], xb[2 * e + 1], cs[4 + e], xb[2 * e], xb[2 * e + 1]);
                     }
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = xa[e], y = xb[e];
-                        xa[e] = x * cs[e].x - y * cs[e].y;
-                        xb[e] = y * cs[e].x + x * cs[e].y;
-                    }
+                    for (int e = 0; e < 8; ++e) turn_pair(xa[e], xb[e], cs[e], xa[e], xb[e]);
                 }
             }
             TC* dst = w == 0 ? reinterpret_cast<TC*>(a.q_out) + ((size_t)row * a.n_heads + h) * D
@@ -353,8 +353,9 @@ __global__ void __launch_bounds__(AP_THREADS) append_any_kernel(BatchView b, App
         float x = to_float(src[ia]), y = to_float(src[ib]);
         if (gain) { x *= r * gain[ia]; y *= r * gain[ib]; }
         const float2 cs = a.rope[(size_t)place.rope_row * half + i];
-        store_val(dst + ia, x * cs.x - y * cs.y);
-        store_val(dst + ib, y * cs.x + x * cs.y);
+        turn_pair(x, y, cs, x, y);
+        store_val(dst + ia, x);
+        store_val(dst + ib, y);
     }
     for (int i = R + lane; i < D; i += 32) {
         float x = to_float(src[i]);
