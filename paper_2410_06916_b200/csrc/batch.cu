@@ -404,9 +404,10 @@ cudaError_t launch_append(const BatchView& b, const AppendView& a, bool vec, cud
     if (!vec) return launch(append_any_kernel<TX, TC>, dim3(b.n_rows, ceil_div(units, AP_THREADS / 32)), AP_THREADS, 0, s, false, b, a);
     const int pieces = a.head_dim / 16;
     const int lph = pieces <= 1 ? 1 : pieces <= 2 ? 2 : pieces <= 4 ? 4 : pieces <= 8 ? 8 : 16;
-    // A row's heads go to one warp where the rows alone fill the machine, else to as many warps as one batch of loads each takes
-    // (8192 rows of 80 heads: a row per warp against five warps per row: see the kernel's comment).
-    const int batch = 32 / lph * AP_UNROLL, chunks = b.n_rows >= 148 * 16 ? 1 : ceil_div(units, batch), per_warp = ceil_div(ceil_div(units, chunks), 32 / lph) * (32 / lph);
+    // A row's heads go to one warp where the rows alone make two waves of warps (20 per SM), else to as many warps as that takes, at
+    // most one per batch of loads (8192 rows of 80 heads: 70 us with one warp per row, 84 with two blocks per row).
+    const int batch = 32 / lph * AP_UNROLL<TX>, most = ceil_div(units, batch), wanted = ceil_div(148 * 40, b.n_rows);
+    const int chunks = wanted < most ? wanted : most, per_warp = ceil_div(ceil_div(units, chunks), 32 / lph) * (32 / lph);
     const dim3 grid((unsigned)(((long long)b.n_rows * chunks + AP_THREADS / 32 - 1) / (AP_THREADS / 32)));
     switch (lph) {
     case 1: return launch(append_vec_kernel<TX, TC, 1>, grid, AP_THREADS, 0, s, false, b, a, per_warp, chunks);

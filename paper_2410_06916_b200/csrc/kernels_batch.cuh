@@ -211,15 +211,16 @@ __device__ __forceinline__ bool place_row(const BatchView& b, const AppendView& 
 // that a rotation pairs up: with pairs (i, i + R/2), piece c and the piece R/2 further on; with neighbouring pairs, or
 // behind the rotated part, two pieces side by side.  So no value crosses lanes except the norm's sum.  A warp stays within
 // one row: it locates the row once (three dependent trips to memory), keeps the row's 8 (cos, sin) pairs and the gains in
-// registers, and goes through `per_warp` of its heads, AP_UNROLL loads ahead, kept in the 16 bytes they have in memory until
+// registers, and goes through `per_warp` of its heads, two or four loads ahead, kept in the 16 bytes they have in memory until
 // used.  Many rows: a whole row per warp, bound by HBM; few rows: as few heads per warp as one batch of loads holds, bound
 // by the trips.  grid = ceil(rows x chunks / 4), block = 128.
-constexpr int AP_THREADS = 128, AP_UNROLL = 4;
+constexpr int AP_THREADS = 128;
+template <typename TX> constexpr int AP_UNROLL = sizeof(TX) == 2 ? 4 : 2;      // 32 registers of loads in flight
 
 template <typename TX, typename TC, int LPH>
 __global__ void __launch_bounds__(AP_THREADS, 5) append_vec_kernel(BatchView b, AppendView a, int per_warp, int chunks)
 {
-    constexpr int GROUPS = 32 / LPH;
+    constexpr int GROUPS = 32 / LPH, UNROLL = AP_UNROLL<TX>;
     const int lane = threadIdx.x & 31, c = lane & (LPH - 1), grp = lane / LPH;
     const long long job = (long long)blockIdx.x * (AP_THREADS / 32) + (threadIdx.x >> 5);
     const int row = (int)(job / chunks);
@@ -244,10 +245,10 @@ __global__ void __launch_bounds__(AP_THREADS, 5) append_vec_kernel(BatchView b, 
         h = w == 0 ? u : w == 1 ? u - a.n_heads : u - a.n_heads - a.n_kv_heads;
         return w;
     };
-    Raw8<TX> ra[AP_UNROLL], rb[AP_UNROLL];
+    Raw8<TX> ra[UNROLL], rb[UNROLL];
     auto fetch = [&](int first) {                         // heads first + grp, + GROUPS, ...
 #pragma unroll
-        for (int j = 0; j < AP_UNROLL; ++j) {
+        for (int j = 0; j < UNROLL; ++j) {
             const int u = first + grp + j * GROUPS;
             ra[j] = {};
             rb[j] = {};
@@ -275,9 +276,9 @@ __global__ void __launch_bounds__(AP_THREADS, 5) append_vec_kernel(BatchView b, 
         }
     }
     const bool normed = a.gain[0] != nullptr || a.gain[1] != nullptr;
-    for (int first = u0; first < units; first += AP_UNROLL * GROUPS) {
+    for (int first = u0; first < units; first += UNROLL * GROUPS) {
 #pragma unroll
-        for (int j = 0; j < AP_UNROLL; ++j) {
+        for (int j = 0; j < UNROLL; ++j) {
             if (first + j * GROUPS >= units) break;       // the same for the whole warp
             const int u = first + grp + j * GROUPS;
             int h;
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(AP_THREADS, 5) append_vec_kernel(BatchView b, 
             store8(dst + oa, xa);
             store8(dst + ob, xb);
         }
-        if (first + AP_UNROLL * GROUPS < units) fetch(first + AP_UNROLL * GROUPS);
+        if (first + UNROLL * GROUPS < units) fetch(first + UNROLL * GROUPS);
     }
 }
 
