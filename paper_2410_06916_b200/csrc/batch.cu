@@ -322,12 +322,13 @@ cudaError_t launch_dec_any(const PrefixPlan& p, const CUtensorMap& kv_map, const
 }
 
 template <typename T>
-cudaError_t launch_join(const BatchView& bv, const BjArgs& j, cudaStream_t s)
+cudaError_t launch_join(const PrefixPlan& p, const BatchView& bv, const BjArgs& j, cudaStream_t s)
 {
-    // four warps per head where a warp each would not fill the machine
-    const bool spread = (long long)bv.n_rows * j.a.n_heads < 148 * 32;
-    return spread ? launch(attn_join_kernel<T, 4>, dim3(bv.n_rows, j.a.n_heads), 128, 0, s, true, bv, j)
-                  : launch(attn_join_kernel<T, 1>, dim3(bv.n_rows, ceil_div(j.a.n_heads, 4)), 128, 0, s, true, bv, j);
+    // An item has about (workers / items + 1) parts of the few-row kernel: with more than eight of them the four warps of a block
+    // share a head, else each takes one.
+    const bool cut = p.few && (long long)p.grid * (8 / p.mt) > 8 * p.items;
+    return cut ? launch(attn_join_parts_kernel<T>, dim3(bv.n_rows, j.a.n_heads), 128, 0, s, true, bv, j)
+               : launch(attn_join_rows_kernel<T>, dim3(bv.n_rows, ceil_div(j.a.n_heads, 4)), 128, 0, s, true, bv, j);
 }
 
 swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, int block, const PrefixPlan& p, unsigned char* ws, cudaStream_t s)
@@ -381,7 +382,7 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
         if (st != SWIFT_OK) return st;
     }
     if (e == cudaSuccess) {
-        e = kv->dtype == SWIFT_BF16 ? launch_join<__nv_bfloat16>(bv, j, s) : launch_join<__half>(bv, j, s);
+        e = kv->dtype == SWIFT_BF16 ? launch_join<__nv_bfloat16>(p, bv, j, s) : launch_join<__half>(p, bv, j, s);
     }
     if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
     return SWIFT_OK;

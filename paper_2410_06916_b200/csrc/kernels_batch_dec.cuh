@@ -422,40 +422,107 @@ struct BjArgs {
     const int* item_last;
 };
 
-// out[row][h] = sum_i 2^(M_i - M) O_i / sum_i 2^(M_i - M) l_i over the parts of a row, in a fixed order.  WARPS warps per
-// (row, head), each taking every WARPS-th part, lanes over dims; the parts' maxima are fetched 32 at a time.  Many warps
-// per head are for few rows, whose items are cut into many parts.  grid = (rows, ceil(heads / (4 / WARPS))), block = 128.
-template <typename T, int WARPS>
-__global__ void __launch_bounds__(128) attn_join_kernel(BatchView b, BjArgs g)
+// out[row][h] = sum_i 2^(M_i - M) O_i / sum_i 2^(M_i - M) l_i over the parts of a row, in a fixed order: the many-row
+// kernel's parts, then the prefix item's, then the own item's.
+struct BjHead {                                           // where the parts of one (row, head) are
+    int first[2], n[2], item[2], rho[2];
+};
+__device__ __forceinline__ BjHead bj_head(const BatchView& b, const BjArgs& g, int row, int seq, const SeqSpan& sp, int h)
+{
+    const int Hk = g.a.n_kv_heads, G = g.a.n_heads / Hk, kvh = h / G, hg = h - kvh * G;
+    BjHead p = {{0, 0}, {0, 0}, {kvh, (g.prefix_here ? Hk : 0) + seq * Hk + kvh}, {row * G + hg, (row - sp.r0) * G + hg}};
+    if (g.prefix_here) { p.first[0] = g.item_first[p.item[0]]; p.n[0] = g.item_last[p.item[0]] - p.first[0] + 1; }
+    if (g.own_here && sp.len > 0) { p.first[1] = g.item_first[p.item[1]]; p.n[1] = g.item_last[p.item[1]] - p.first[1] + 1; }
+    return p;
+}
+__device__ __forceinline__ size_t bj_place(const BatchView& b, const BjArgs& g, const BjHead& p, int row, int h, int i)   // part i's (maximum, sum); its sums times dp
+{
+    if (i < g.splits) return ((size_t)i * b.n_rows + row) * g.a.n_heads + h;
+    const int j = i - g.splits < p.n[0] ? 0 : 1;
+    return (size_t)(p.item[j] + p.first[j] + i - g.splits - (j ? p.n[0] : 0)) * g.item_rows + p.rho[j];
+}
+template <typename T> __device__ __forceinline__ void bj_store(const BjArgs& g, int row, int h, float4 acc, float l)
+{
+    const int lane = threadIdx.x & 31;
+    const float inv = l == 0.f ? 0.f : 1.f / l;           // 0: the row sees nothing
+    if (4 * lane < g.a.head_dim) {
+        T* out = reinterpret_cast<T*>(g.a.out) + ((size_t)row * g.a.n_heads + h) * g.a.head_dim + 4 * lane;
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
+    }
+}
+
+// Few parts: a warp per (row, head).  The sums of eight parts are fetched at once and along with their maxima, so that a head
+// costs four dependent trips to memory (its sequence, its items' first and last worker, its parts, the store).
+// grid = (rows, ceil(heads / 4)), block = 128.
+constexpr int BJ_PARTS = 8;
+
+template <typename T>
+__global__ void __launch_bounds__(128) attn_join_rows_kernel(BatchView b, BjArgs g)
 {
     pdl_wait();
-    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y * (4 / WARPS) + warp / WARPS, part0 = warp % WARPS;
-    if (h >= g.a.n_heads) return;                         // (WARPS 4: all or none of a block)
+    const int row = blockIdx.x, lane = threadIdx.x & 31, h = blockIdx.y * 4 + (threadIdx.x >> 5);
+    if (h >= g.a.n_heads) return;
+    SeqSpan sp;
+    const int seq = find_seq(b, row, sp);
+    if (seq < 0 || row - sp.r0 >= g.a.max_rows) return;
+    const bool mine = 4 * lane < g.dp;
+    const BjHead p = bj_head(b, g, row, seq, sp, h);
+    const int parts = g.splits + p.n[0] + p.n[1];
+    float M = -INFINITY, l = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = 0; p0 < parts; p0 += BJ_PARTS) {
+        float2 ml[BJ_PARTS];
+        float4 v[BJ_PARTS];
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < BJ_PARTS; ++i) {
+            ml[i] = make_float2(-INFINITY, 0.f);
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (p0 + i < parts) {
+                const size_t at = bj_place(b, g, p, row, h, p0 + i);
+                const bool many = p0 + i < g.splits;
+                ml[i] = (many ? g.many_ml : g.few_ml)[at];
+                if (mine) v[i] = *reinterpret_cast<const float4*>((many ? g.many_o : g.few_o) + at * g.dp + 4 * lane);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < BJ_PARTS; ++i)
+            if (ml[i].y != 0.f) top = fmaxf(top, ml[i].x);
+        const float shrink = M == top ? 1.f : exp2f(M - top);
+        l *= shrink;
+        acc.x *= shrink; acc.y *= shrink; acc.z *= shrink; acc.w *= shrink;
+        M = top;
+#pragma unroll
+        for (int i = 0; i < BJ_PARTS; ++i) {
+            if (ml[i].y == 0.f) continue;                 // an empty part: its sums were not written
+            const float f = exp2f(ml[i].x - M);
+            l += ml[i].y * f;
+            acc.x += f * v[i].x; acc.y += f * v[i].y; acc.z += f * v[i].z; acc.w += f * v[i].w;
+        }
+    }
+    bj_store<T>(g, row, h, acc, l);
+}
+
+// Few rows whose items are cut into many parts: four warps per (row, head), each taking every fourth part; the parts' maxima
+// are fetched 32 at a time.  grid = (rows, heads), block = 128.
+template <typename T>
+__global__ void __launch_bounds__(128) attn_join_parts_kernel(BatchView b, BjArgs g)
+{
+    constexpr int WARPS = 4;
+    pdl_wait();
+    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y;
     SeqSpan sp;
     const int seq = find_seq(b, row, sp);
     if (seq < 0 || row - sp.r0 >= g.a.max_rows) return;   // the same for the whole block
-    const int Hk = g.a.n_kv_heads, G = g.a.n_heads / Hk, kvh = h / G, hg = h - kvh * G;
-    // parts: the many-row kernel's, then the prefix item's, then the own item's
-    int first[2] = {0, 0}, n[2] = {0, 0}, item[2], rho[2];
-    item[0] = kvh;
-    rho[0] = row * G + hg;
-    item[1] = (g.prefix_here ? Hk : 0) + seq * Hk + kvh;
-    rho[1] = (row - sp.r0) * G + hg;
-    if (g.prefix_here) { first[0] = g.item_first[item[0]]; n[0] = g.item_last[item[0]] - first[0] + 1; }
-    if (g.own_here && sp.len > 0) { first[1] = g.item_first[item[1]]; n[1] = g.item_last[item[1]] - first[1] + 1; }
-    const int parts = g.splits + n[0] + n[1];
-    auto place = [&](int i) {                             // index of part i in (sums, maxima); the many-row kernel's come first
-        if (i < g.splits) return ((size_t)i * b.n_rows + row) * g.a.n_heads + h;
-        const int j = i - g.splits < n[0] ? 0 : 1;
-        return (size_t)(item[j] + first[j] + i - g.splits - (j ? n[0] : 0)) * g.item_rows + rho[j];
-    };
+    const BjHead p = bj_head(b, g, row, seq, sp, h);
+    const int parts = g.splits + p.n[0] + p.n[1];
     float M = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const bool mine = 4 * lane < g.dp;
-    for (int p0 = part0; p0 < parts; p0 += 32 * WARPS) {
+    for (int p0 = warp; p0 < parts; p0 += 32 * WARPS) {
         float2 ml = make_float2(-INFINITY, 0.f);
         const int i_lane = p0 + lane * WARPS;
-        if (i_lane < parts) ml = (i_lane < g.splits ? g.many_ml : g.few_ml)[place(i_lane)];
+        if (i_lane < parts) ml = (i_lane < g.splits ? g.many_ml : g.few_ml)[bj_place(b, g, p, row, h, i_lane)];
         if (ml.y == 0.f) ml.x = -INFINITY;                // an empty part: its sums were not written
         const float M_new = fmaxf(M, warp_max(ml.x));
         const float shrink = M == M_new ? 1.f : exp2f(M - M_new);
@@ -469,36 +536,30 @@ __global__ void __launch_bounds__(128) attn_join_kernel(BatchView b, BjArgs g)
             const float fi = __shfl_sync(FULL_WARP, f, i);
             const int part = p0 + i * WARPS;
             if (mine && fi != 0.f) {
-                const float4 v = *reinterpret_cast<const float4*>((part < g.splits ? g.many_o : g.few_o) + place(part) * g.dp + 4 * lane);
+                const float4 v = *reinterpret_cast<const float4*>((part < g.splits ? g.many_o : g.few_o) + bj_place(b, g, p, row, h, part) * g.dp + 4 * lane);
                 acc.x += fi * v.x; acc.y += fi * v.y; acc.z += fi * v.z; acc.w += fi * v.w;
             }
         }
     }
-    if (WARPS > 1) {
-        __shared__ float4 acc_sh[4][32];
-        __shared__ float2 ml_sh[4];
-        acc_sh[warp][lane] = acc;
-        if (lane == 0) ml_sh[warp] = make_float2(M, l);
-        __syncthreads();
-        if (warp > 0) return;
-        M = ml_sh[0].x;
+    __shared__ float4 acc_sh[4][32];
+    __shared__ float2 ml_sh[4];
+    acc_sh[warp][lane] = acc;
+    if (lane == 0) ml_sh[warp] = make_float2(M, l);
+    __syncthreads();
+    if (warp > 0) return;
+    M = ml_sh[0].x;
 #pragma unroll
-        for (int w = 1; w < WARPS; ++w) M = fmaxf(M, ml_sh[w].x);
-        l = 0.f;
-        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w = 1; w < WARPS; ++w) M = fmaxf(M, ml_sh[w].x);
+    l = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            const float f = ml_sh[w].y == 0.f ? 0.f : exp2f(ml_sh[w].x - M);
-            const float4 v = acc_sh[w][lane];
-            l += f * ml_sh[w].y;
-            acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
-        }
+    for (int w = 0; w < WARPS; ++w) {
+        const float f = ml_sh[w].y == 0.f ? 0.f : exp2f(ml_sh[w].x - M);
+        const float4 v = acc_sh[w][lane];
+        l += f * ml_sh[w].y;
+        acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;           // 0: the row sees nothing
-    if (4 * lane < g.a.head_dim) {
-        T* out = reinterpret_cast<T*>(g.a.out) + ((size_t)row * g.a.n_heads + h) * g.a.head_dim + 4 * lane;
-        *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
-    }
+    bj_store<T>(g, row, h, acc, l);
 }
 
 } // namespace swk
