@@ -191,26 +191,34 @@ template <typename K> cudaError_t allow_smem(K kernel, int bytes, std::atomic<un
     return e;
 }
 
-template <typename T, int HALVES>
+template <typename T, int HALVES, bool PART>
 cudaError_t launch_tc(const CUtensorMap& kv_map, const CUtensorMap& q_map, const BatchView& bv, const BtArgs& g, int grid, cudaStream_t s, bool after_previous)
 {
     static std::atomic<unsigned long long> done{0};
-    const cudaError_t e = allow_smem(attn_batch_tc_kernel<T, HALVES>, BtShape<HALVES>::SMEM_BYTES, done);
+    const cudaError_t e = allow_smem(attn_batch_tc_kernel<T, HALVES, PART>, BtShape<HALVES>::SMEM_BYTES, done);
     if (e != cudaSuccess) return e;
-    return launch(attn_batch_tc_kernel<T, HALVES>, dim3(grid), BT_THREADS, BtShape<HALVES>::SMEM_BYTES, s, after_previous, kv_map, q_map, bv, g);
+    return launch(attn_batch_tc_kernel<T, HALVES, PART>, dim3(grid), BT_THREADS, BtShape<HALVES>::SMEM_BYTES, s, after_previous, kv_map, q_map, bv, g);
 }
 
-// The many-row kernel in one of its three modes; items: an upper bound of its pieces of work.
-swift_status run_tc(const swift_paged_kv* kv, const BatchView& bv, const BtArgs& g, long long items, cudaStream_t s, bool after_previous)
+template <bool PART>
+cudaError_t launch_tc_any(bool bf16, bool wide, const CUtensorMap& kv_map, const CUtensorMap& q_map, const BatchView& bv, const BtArgs& g, int grid,
+                          cudaStream_t s, bool after)
+{
+    if (bf16) return wide ? launch_tc<__nv_bfloat16, 2, PART>(kv_map, q_map, bv, g, grid, s, after) : launch_tc<__nv_bfloat16, 1, PART>(kv_map, q_map, bv, g, grid, s, after);
+    return wide ? launch_tc<__half, 2, PART>(kv_map, q_map, bv, g, grid, s, after) : launch_tc<__half, 1, PART>(kv_map, q_map, bv, g, grid, s, after);
+}
+
+// The many-row kernel in one of its three modes on at most `most` SMs; items: an upper bound of its pieces of work.
+swift_status run_tc(const swift_paged_kv* kv, const BatchView& bv, const BtArgs& g, long long items, int most, cudaStream_t s, bool after_previous)
 {
     CUtensorMap kv_map, q_map;
     swift_status st = make_kv_map(kv, BT_KEYS, &kv_map);
     if (st == SWIFT_OK) st = make_q_map(kv, bv, g.a, g.rows_per_tile, &q_map);
     if (st != SWIFT_OK) return st;
-    const int sms = multiprocessors(), grid = (int)(items < sms ? items : sms);
+    const int grid = (int)(items < most ? items : most);
     const bool wide = kv->head_dim > 64, bf16 = kv->dtype == SWIFT_BF16;
-    const cudaError_t e = bf16 ? (wide ? launch_tc<__nv_bfloat16, 2>(kv_map, q_map, bv, g, grid, s, after_previous) : launch_tc<__nv_bfloat16, 1>(kv_map, q_map, bv, g, grid, s, after_previous))
-                               : (wide ? launch_tc<__half, 2>(kv_map, q_map, bv, g, grid, s, after_previous) : launch_tc<__half, 1>(kv_map, q_map, bv, g, grid, s, after_previous));
+    const cudaError_t e = g.mode == BT_PROMPT ? launch_tc_any<false>(bf16, wide, kv_map, q_map, bv, g, grid, s, after_previous)
+                                              : launch_tc_any<true>(bf16, wide, kv_map, q_map, bv, g, grid, s, after_previous);
     if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
     return SWIFT_OK;
 }
@@ -234,7 +242,7 @@ swift_status run_prompt(const swift_paged_kv* kv, const BatchView& bv, const Att
     // A pair of tiles takes little longer than one tile (each works while the other waits), so pieces are pairs unless even
     // single tiles leave no SM more than one.
     g.tiles = piece_bound(bv, av.n_kv_heads, g.rows_per_tile) <= multiprocessors() ? 1 : 2;
-    return run_tc(kv, bv, g, piece_bound(bv, av.n_kv_heads, g.tiles * g.rows_per_tile), s, false);
+    return run_tc(kv, bv, g, piece_bound(bv, av.n_kv_heads, g.tiles * g.rows_per_tile), multiprocessors(), s, false);
 }
 
 // ------------------------------------------------------------------------------ few rows per sequence
@@ -243,7 +251,7 @@ struct PrefixPlan {
     bool rows;                  // row by row: no tensor-core form
     bool prompt;                // each sequence by itself, no prefix to share and too many rows for the few-row kernel
     bool few, prefix_few;       // the few-row kernel takes the sequences' own parts; and the prefix
-    int group, dp, mt, grid;
+    int group, dp, mt, grid, pre_grid;   // grid: CTAs of the few-row kernel; pre_grid: of the prefix's
     long long items;
     int splits;                 // cuts of the prefix by the many-row kernel (0: it has no prefix work)
     int slots;                  // parts per row that the many-row kernel leaves: splits, and the own part if it takes it
@@ -266,14 +274,29 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
         p->prefix_few = p->few && bv.prefix_len > 0 && all <= BD_MAX_ROWS;
         p->prompt = !p->few && bv.prefix_len == 0;
         if (bv.prefix_len > 0 && !p->prefix_few && !p->prompt) {
-            // Cuts of the prefix: as many waves of (tile pairs x kv heads x cuts) as give the shortest time, a wave costing its
-            // share of the prefix and about one key tile of set-up and write-back.
+            // The prefix is tensor work, the sequences' own parts are HBM work: both kernels run at once, on SMs of their own, and
+            // the share of SMs and the cuts of the prefix are chosen for the earliest common end.  Costs in microseconds: a key
+            // tile of a pair of query tiles 1.75, a piece's set-up and write-back 4; own parts at 44 GB/s per SM up to 6 TB/s, 4 an item,
+            // their lengths (which only the device knows) taken as 0.6 of the page table's width, and never more than 3/4 of the
+            // SMs for them.  (64 continuations of 8192 positions, 64 heads on 8, about 750 own positions: 86 us one after the other.)
             const int tiles = ceil_div(bv.prefix_len, BT_KEYS), TQ = BT_ROWS / p->group;
             const long long pairs = (long long)ceil_div(bv.n_rows, 2 * TQ) * Hk;
+            const double own_bytes = 0.6 * bv.n_seqs * bv.max_len * Hk * kv->head_dim * 4.0;
+            const int own_mt = own <= 16 ? 1 : own <= 32 ? 2 : 4;
             double best = 0;
-            for (int s = 1; s <= 64 && s <= tiles; ++s) {
-                const double cost = (double)ceil_div(pairs * s, sms) * (ceil_div(tiles, s) + 1.0);
-                if (p->splits == 0 || cost < best) { best = cost; p->splits = s; }
+            for (int g = p->few ? sms / 4 : sms; g <= sms; g += sms / 37 > 0 ? sms / 37 : 1) {
+                const int rest = g == sms ? sms : sms - g;
+                const double stream_us = own_bytes / (rest * 44e3 < 6e6 ? rest * 44e3 : 6e6), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * (8 / own_mt));
+                const double own_us = p->few ? 3.0 + (stream_us > item_us ? stream_us : item_us) : 0.0;
+                for (int c = 1; c <= 64 && c <= tiles; ++c) {
+                    const double pre_us = ceil_div(pairs * c, g) * (ceil_div(tiles, c) * 1.75 + 4.0);
+                    const double cost = (g == sms ? pre_us + own_us : pre_us > own_us ? pre_us : own_us) + 0.5 * c;   // every cut is read again by the join
+                    if (p->splits == 0 || cost < best) {
+                        best = cost;
+                        p->splits = c;
+                        p->pre_grid = g;
+                    }
+                }
             }
         }
         p->slots = p->splits + (!p->few && !p->prompt ? 1 : 0);
@@ -284,7 +307,7 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
             const long long rows = p->prefix_few ? (all > own ? all : own) : own;
             p->mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
             p->items = (long long)(bv.n_seqs + (p->prefix_few ? 1 : 0)) * Hk;
-            p->grid = sms;
+            p->grid = p->splits > 0 && p->pre_grid < sms ? sms - p->pre_grid : sms;
             const int keys = 16 * p->mt;
             const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, keys) + ceil_div(bv.prefix_len, keys)) * Hk;
             if (units > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a page table of %d x %d for %d kv heads is beyond 2^31 units of work", bv.n_seqs, bv.table_stride, Hk);
@@ -344,7 +367,7 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
     if (p.splits > 0) {
         t.mode = BT_PREFIX;
         t.splits = p.splits;
-        const swift_status st = run_tc(kv, bv, t, (long long)ceil_div(bv.n_rows, 2 * t.rows_per_tile) * av.n_kv_heads * p.splits, s, before);
+        const swift_status st = run_tc(kv, bv, t, (long long)ceil_div(bv.n_rows, 2 * t.rows_per_tile) * av.n_kv_heads * p.splits, p.pre_grid, s, before);
         if (st != SWIFT_OK) return st;
         before = true;
     }
@@ -378,7 +401,7 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
     } else {
         t.mode = BT_OWN;
         t.part_slot = p.splits;
-        const swift_status st = run_tc(kv, bv, t, piece_bound(bv, av.n_kv_heads, 2 * t.rows_per_tile), s, before);
+        const swift_status st = run_tc(kv, bv, t, piece_bound(bv, av.n_kv_heads, 2 * t.rows_per_tile), multiprocessors(), s, before);
         if (st != SWIFT_OK) return st;
     }
     if (e == cudaSuccess) {

@@ -38,7 +38,7 @@ constexpr int BT_THREADS = 320;     // 2 x 4 softmax warps, the TMA warp, the MM
 constexpr int BT_KEYS = 128;        // keys per tile
 constexpr int BT_ROWS = 128;        // packed query rows per tile
 constexpr int BT_PAGE_RING = 16;    // page-validity words kept (more than the key tiles ever in flight)
-constexpr unsigned BT_POLY = 0x0101u;   // pairs of every 16 whose exponentials are polynomials: 2 of 16
+constexpr unsigned BT_POLY = 0x1111u;   // pairs of every 16 whose exponentials are polynomials: 4 of 16
 constexpr float BT_GROW = 8.f;      // growth of the maximum (in powers of two) that triggers a rescaling
 
 enum { BT_PROMPT = 0, BT_PREFIX = 1, BT_OWN = 2 };
@@ -412,9 +412,39 @@ __device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_
     l += l0 + l1;
 }
 
+// A row's result to the output (a function of its own: inlined, its registers crowd out the softmax's).  Every lane takes
+// part in the reading; `live` lanes store.
+template <typename T, int COLS> __device__ __noinline__ void bt_store_out(uint32_t o_at, T* dst, int dims, bool some, bool live, bool wide, float l)
+{
+    const float inv = l == 0.f ? 0.f : 1.f / l;                       // 0: the row sees nothing
+#pragma unroll 1
+    for (int i = 0; i < COLS; i += 32) {
+        float o[32];
+        if (some) {
+            tmem_ld32(o_at + i, o);
+            tmem_wait_ld(o);
+        }
+        if (live) {
+            uint32_t v[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = l == 0.f ? 0u : pack2(o[2 * e] * inv, o[2 * e + 1] * inv, T());
+            if (wide) {
+#pragma unroll
+                for (int e = 0; e < 16; e += 8)
+                    if (i + 2 * e < dims) store32(dst + i + 2 * e, v[e], v[e + 1], v[e + 2], v[e + 3], v[e + 4], v[e + 5], v[e + 6], v[e + 7]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    if (i + 2 * e < dims) *reinterpret_cast<uint4*>(dst + i + 2 * e) = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+            }
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------ the kernel
 // grid = persistent CTAs (at most one per SM), each taking pieces blockIdx.x, + gridDim.x, ...; block = 320.
-template <typename T, int HALVES>
+// PART: leaves parts in the workspace (BT_PREFIX, BT_OWN) rather than results (BT_PROMPT).
+template <typename T, int HALVES, bool PART>
 __global__ void __launch_bounds__(BT_THREADS, 1)
 attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_q, BatchView b, BtArgs g)
 {
@@ -565,10 +595,12 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             auto scores = [&](int x, uint32_t k_sh) {                 // S(x) = Q(x) K^T
                 if (elect_one()) {
                     const uint64_t qd = tc_smem_desc(q_sh + x * S::Q_BYTES), kd = tc_smem_desc(k_sh);
+                    uint32_t q_lo = (uint32_t)qd, k_lo = (uint32_t)kd;
+                    asm volatile("" : "+r"(q_lo), "+r"(k_lo));        // (kept from being precomputed for all steps, slots and tiles)
 #pragma unroll
                     for (int k = 0; k < 4 * HALVES; ++k) {            // 16 dims a step: 32 bytes, 64 dims a box
-                        const uint64_t step = (uint64_t)(((k >> 2) * (BT_KEYS * 128) + (k & 3) * 32) >> 4);
-                        tc_mma(s_col(x), qd + step, kd + step, IDESC_QK, k > 0);
+                        const uint32_t step = ((k >> 2) * (BT_KEYS * 128) + (k & 3) * 32) >> 4;
+                        tc_mma(s_col(x), (qd >> 32 << 32) | (q_lo + step), (kd >> 32 << 32) | (k_lo + step), IDESC_QK, k > 0);
                     }
                     tc_commit(s_full(x));
                 }
@@ -672,8 +704,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 tc_fence_after();
             }
             const int row = it.r0 + t, head = it.kvh * G + head_in;
-            const float inv = l == 0.f ? 0.f : 1.f / l;              // 0: the row sees nothing
-            if (g.mode != BT_PROMPT) {
+            if (PART) {
                 const size_t at = ((size_t)it.slot * b.n_rows + row) * g.a.n_heads + head;
                 if (live) g.part_ml[at] = make_float2(m * c - BIAS, l);
 #pragma unroll 1
@@ -693,29 +724,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 }
             } else {
                 T* dst = reinterpret_cast<T*>(g.a.out) + ((size_t)row * g.a.n_heads + head) * g.a.head_dim;
-#pragma unroll 1
-                for (int i = 0; i < DP; i += 32) {
-                    float o[32];
-                    if (mine > 0) {
-                        tmem_ld32(o_at + i, o);
-                        tmem_wait_ld(o);
-                    }
-                    if (live) {
-                        uint32_t v[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) v[e] = l == 0.f ? 0u : pack2(o[2 * e] * inv, o[2 * e + 1] * inv, T());
-                        if (g.wide_out) {
-#pragma unroll
-                            for (int e = 0; e < 16; e += 8)
-                                if (i + 2 * e < g.a.head_dim)
-                                    store32(dst + i + 2 * e, v[e], v[e + 1], v[e + 2], v[e + 3], v[e + 4], v[e + 5], v[e + 6], v[e + 7]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; e += 4)
-                                if (i + 2 * e < g.a.head_dim) *reinterpret_cast<uint4*>(dst + i + 2 * e) = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-                        }
-                    }
-                }
+                bt_store_out<T, DP>(o_at, dst, g.a.head_dim, mine > 0, live, g.wide_out != 0, l);
             }
             tc_fence_before();                                        // O is read: the next piece's product may overwrite it
         }
