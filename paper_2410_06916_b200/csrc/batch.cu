@@ -286,7 +286,7 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
             double best = 0;
             for (int g = p->few ? sms / 4 : sms; g <= sms; g += sms / 37 > 0 ? sms / 37 : 1) {
                 const int rest = g == sms ? sms : sms - g;
-                const double stream_us = own_bytes / (rest * 44e3 < 6e6 ? rest * 44e3 : 6e6), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * (8 / own_mt));
+                const double stream_us = own_bytes / (rest * 44e3 < 6e6 ? rest * 44e3 : 6e6), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * (BD_WARPS / own_mt));
                 const double own_us = p->few ? 3.0 + (stream_us > item_us ? stream_us : item_us) : 0.0;
                 for (int c = 1; c <= 64 && c <= tiles; ++c) {
                     const double pre_us = ceil_div(pairs * c, g) * (ceil_div(tiles, c) * 1.75 + 4.0);
@@ -311,7 +311,7 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
             const int keys = 16 * p->mt;
             const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, keys) + ceil_div(bv.prefix_len, keys)) * Hk;
             if (units > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a page table of %d x %d for %d kv heads is beyond 2^31 units of work", bv.n_seqs, bv.table_stride, Hk);
-            const size_t rows_all = (size_t)(p->items + (long long)p->grid * (8 / p->mt)) * 16 * p->mt;
+            const size_t rows_all = (size_t)(p->items + (long long)p->grid * (BD_WARPS / p->mt)) * 16 * p->mt;
             p->few_o = take(rows_all * p->dp * 4);
             p->few_ml = take(rows_all * 8);
             p->first = take((size_t)p->items * 4);
@@ -349,9 +349,9 @@ cudaError_t launch_join(const PrefixPlan& p, const BatchView& bv, const BjArgs& 
 {
     // An item has about (workers / items + 1) parts of the few-row kernel: with more than eight of them the four warps of a block
     // share a head, else each takes one.
-    const bool cut = p.few && (long long)p.grid * (8 / p.mt) > 8 * p.items;
-    return cut ? launch(attn_join_parts_kernel<T>, dim3(bv.n_rows, j.a.n_heads), 128, 0, s, true, bv, j)
-               : launch(attn_join_rows_kernel<T>, dim3(bv.n_rows, ceil_div(j.a.n_heads, 4)), 128, 0, s, true, bv, j);
+    const bool cut = p.few && (long long)p.grid * (BD_WARPS / p.mt) > 8 * p.items;
+    return cut ? launch(attn_join_kernel<T, 4>, dim3(bv.n_rows, j.a.n_heads), 128, 0, s, true, bv, j)
+               : launch(attn_join_kernel<T, 1>, dim3(bv.n_rows, ceil_div(j.a.n_heads, 4)), 128, 0, s, true, bv, j);
 }
 
 swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, int block, const PrefixPlan& p, unsigned char* ws, cudaStream_t s)

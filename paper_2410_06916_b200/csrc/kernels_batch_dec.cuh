@@ -21,17 +21,18 @@
 
 namespace swk {
 
-constexpr int BD_THREADS = 256;
+constexpr int BD_WARPS = 8, BD_THREADS = 32 * BD_WARPS;
 constexpr int BD_MAX_ROWS = 64;                           // packed query rows (tokens x heads of a group) of an item
-constexpr int BD_AHEAD = 2;                               // units by which page ids are looked up ahead of their use
 
 template <int HALVES, int MT> struct BdShape {
     static constexpr int DP = 64 * HALVES;
     static constexpr int KEYS = 16 * MT;                          // keys per unit
-    static constexpr int WORKERS = 8 / MT;                        // of a CTA
+    static constexpr int WORKERS = BD_WARPS / MT;                       // of a CTA
     static constexpr int TILE_BYTES = KEYS * 128 * HALVES;        // K or V of a unit
     static constexpr int STAGES = HALVES == 2 ? 3 : 6;
-    static constexpr int SMEM_BYTES = 1024 + WORKERS * STAGES * 2 * TILE_BYTES;
+    static constexpr int RING_BYTES = WORKERS * STAGES * 2 * TILE_BYTES;
+    static constexpr int Q_BYTES = 16 * 128 * HALVES;             // a warp's queries
+    static constexpr int SMEM_BYTES = 1024 + RING_BYTES + BD_WARPS * Q_BYTES;
 };
 
 struct BdArgs {
@@ -209,7 +210,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
         const bool boxed = pg < per_unit;
         const uint32_t box_at = kv * S::TILE_BYTES + half * (KEYS * 128) + pg * box_rows * 128;
         BdWalk wf = w, wa = w;
-        int asked = 0, looked = 0, f_stage = 0, ids[BD_AHEAD];
+        int asked = 0, looked = 0, f_stage = 0, next_page = 0;            // next_page: of unit `asked`, looked up one unit ahead
         uint32_t f_turn = 0;
         auto look_up = [&]() {                                            // -> this lane's page of unit `looked`
             int page = b.n_pages;                                         // beyond the last page: zeros
@@ -224,10 +225,8 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
             return page;
         };
         auto ask = [&]() {                                                // asks for unit `asked`; its stage is free
-            int page = ids[0];
-#pragma unroll
-            for (int i = 0; i + 1 < BD_AHEAD; ++i) ids[i] = ids[i + 1];
-            ids[BD_AHEAD - 1] = look_up();
+            int page = next_page;
+            next_page = look_up();
             const bool good = (unsigned)page < (unsigned)b.n_pages;
             if (!good) page = b.n_pages;
             const unsigned bits = __ballot_sync(FULL_WARP, boxed && good && half == 0 && kv == 0);
@@ -250,8 +249,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
             if (++asked < count) bd_next<KEYS>(b, g, wf);
         };
         if (mt == 0) {
-#pragma unroll
-            for (int i = 0; i < BD_AHEAD; ++i) ids[i] = look_up();
+            next_page = look_up();
             for (int i = 0; i < S::STAGES && asked < count; ++i) ask();
         }
 
@@ -262,21 +260,31 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
         float o[8 * HALVES][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
         const int rho[2] = {16 * mt + gq, 16 * mt + gq + 8};              // this thread's two packed rows, their tokens
         const int tok[2] = {rho[0] / G, rho[1] / G};
+        const uint32_t q_sh = base + S::RING_BYTES + warp * S::Q_BYTES;
+        auto fetch_q = [&](const BdWalk& item) {                          // this warp's 16 rows of an item's queries; dead rows zero
+#pragma unroll
+            for (int i = 0; i < 4 * HALVES; ++i) {
+                const int row = (i * 32 + lane) / (8 * HALVES), piece = (i * 32 + lane) % (8 * HALVES), r = 16 * mt + row, tk = r / G;
+                const bool live = r < item.sp.n * G && 8 * piece < g.a.head_dim;
+                const T* q = reinterpret_cast<const T*>(g.a.q) + (size_t)(item.sp.r0 + (live ? tk : 0)) * g.a.q_row_stride +
+                             (size_t)(item.kvh * G + (live ? r - tk * G : 0)) * g.a.q_head_stride + (live ? 8 * piece : 0);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(q_sh + swizzled(row, piece, 16)), "l"(q), "r"(live ? 16 : 0) : "memory");
+            }
+        };
+        fetch_q(w);
         for (int k = 0; k < count; ++k) {
             if (fresh) {
-                // queries straight into fragments: rows rho, dims 16 ks + 2 t, + 1, + 8, + 9
+                // queries into fragments; those of the next item set off for shared memory
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                __syncwarp();
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const bool live = rho[e] < w.sp.n * G;
-                    const T* q = reinterpret_cast<const T*>(g.a.q) + (size_t)(w.sp.r0 + (live ? tok[e] : 0)) * g.a.q_row_stride +
-                                 (size_t)(w.kvh * G + rho[e] - tok[e] * G) * g.a.q_head_stride;
-#pragma unroll
-                    for (int ks = 0; ks < 4 * HALVES; ++ks)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const int d = 16 * ks + 8 * x + 2 * t;
-                            qf[ks][e + 2 * x] = live && d < g.a.head_dim ? __ldg(reinterpret_cast<const unsigned*>(q + d)) : 0u;
-                        }
+                for (int ks = 0; ks < 4 * HALVES; ++ks) ldsm4(qf[ks], q_sh + swizzled(lane & 15, 2 * ks + (lane >> 4), 16));
+                __syncwarp();
+                if (count - k > w.units - w.unit) {
+                    BdWalk wn = w;
+                    wn.unit = wn.units - 1;
+                    bd_next<KEYS>(b, g, wn);
+                    fetch_q(wn);
                 }
 #pragma unroll
                 for (int nt = 0; nt < 8 * HALVES; ++nt) o[nt][0] = o[nt][1] = o[nt][2] = o[nt][3] = 0.f;
@@ -441,36 +449,27 @@ __device__ __forceinline__ size_t bj_place(const BatchView& b, const BjArgs& g, 
     const int j = i - g.splits < p.n[0] ? 0 : 1;
     return (size_t)(p.item[j] + p.first[j] + i - g.splits - (j ? p.n[0] : 0)) * g.item_rows + p.rho[j];
 }
-template <typename T> __device__ __forceinline__ void bj_store(const BjArgs& g, int row, int h, float4 acc, float l)
-{
-    const int lane = threadIdx.x & 31;
-    const float inv = l == 0.f ? 0.f : 1.f / l;           // 0: the row sees nothing
-    if (4 * lane < g.a.head_dim) {
-        T* out = reinterpret_cast<T*>(g.a.out) + ((size_t)row * g.a.n_heads + h) * g.a.head_dim + 4 * lane;
-        *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
-    }
-}
-
-// Few parts: a warp per (row, head).  The sums of eight parts are fetched at once and along with their maxima, so that a head
-// costs four dependent trips to memory (its sequence, its items' first and last worker, its parts, the store).
-// grid = (rows, ceil(heads / 4)), block = 128.
+// WARPS warps per (row, head), each taking every WARPS-th part.  The sums of eight parts are fetched at once and along with
+// their maxima, so that a head costs four dependent trips to memory (its sequence, its items' first and last worker, its
+// parts, the store) and one more for every 8 WARPS further parts.  Four warps are for few rows, whose items are cut into many
+// parts (one row, 64 heads, 148 parts each).  grid = (rows, ceil(heads / (4 / WARPS))), block = 128.
 constexpr int BJ_PARTS = 8;
 
-template <typename T>
-__global__ void __launch_bounds__(128) attn_join_rows_kernel(BatchView b, BjArgs g)
+template <typename T, int WARPS>
+__global__ void __launch_bounds__(128) attn_join_kernel(BatchView b, BjArgs g)
 {
     pdl_wait();
-    const int row = blockIdx.x, lane = threadIdx.x & 31, h = blockIdx.y * 4 + (threadIdx.x >> 5);
-    if (h >= g.a.n_heads) return;
+    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y * (4 / WARPS) + warp / WARPS;
+    if (h >= g.a.n_heads) return;                         // (WARPS 4: all or none of a block)
     SeqSpan sp;
     const int seq = find_seq(b, row, sp);
-    if (seq < 0 || row - sp.r0 >= g.a.max_rows) return;
+    if (seq < 0 || row - sp.r0 >= g.a.max_rows) return;   // the same for the whole block
     const bool mine = 4 * lane < g.dp;
     const BjHead p = bj_head(b, g, row, seq, sp, h);
     const int parts = g.splits + p.n[0] + p.n[1];
     float M = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p0 = 0; p0 < parts; p0 += BJ_PARTS) {
+    for (int p0 = warp % WARPS; p0 < parts; p0 += BJ_PARTS * WARPS) {
         float2 ml[BJ_PARTS];
         float4 v[BJ_PARTS];
         float top = M;
@@ -478,9 +477,10 @@ __global__ void __launch_bounds__(128) attn_join_rows_kernel(BatchView b, BjArgs
         for (int i = 0; i < BJ_PARTS; ++i) {
             ml[i] = make_float2(-INFINITY, 0.f);
             v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (p0 + i < parts) {
-                const size_t at = bj_place(b, g, p, row, h, p0 + i);
-                const bool many = p0 + i < g.splits;
+            const int part = p0 + i * WARPS;
+            if (part < parts) {
+                const size_t at = bj_place(b, g, p, row, h, part);
+                const bool many = part < g.splits;
                 ml[i] = (many ? g.many_ml : g.few_ml)[at];
                 if (mine) v[i] = *reinterpret_cast<const float4*>((many ? g.many_o : g.few_o) + at * g.dp + 4 * lane);
             }
@@ -500,66 +500,32 @@ __global__ void __launch_bounds__(128) attn_join_rows_kernel(BatchView b, BjArgs
             acc.x += f * v[i].x; acc.y += f * v[i].y; acc.z += f * v[i].z; acc.w += f * v[i].w;
         }
     }
-    bj_store<T>(g, row, h, acc, l);
-}
-
-// Few rows whose items are cut into many parts: four warps per (row, head), each taking every fourth part; the parts' maxima
-// are fetched 32 at a time.  grid = (rows, heads), block = 128.
-template <typename T>
-__global__ void __launch_bounds__(128) attn_join_parts_kernel(BatchView b, BjArgs g)
-{
-    constexpr int WARPS = 4;
-    pdl_wait();
-    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y;
-    SeqSpan sp;
-    const int seq = find_seq(b, row, sp);
-    if (seq < 0 || row - sp.r0 >= g.a.max_rows) return;   // the same for the whole block
-    const BjHead p = bj_head(b, g, row, seq, sp, h);
-    const int parts = g.splits + p.n[0] + p.n[1];
-    float M = -INFINITY, l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    const bool mine = 4 * lane < g.dp;
-    for (int p0 = warp; p0 < parts; p0 += 32 * WARPS) {
-        float2 ml = make_float2(-INFINITY, 0.f);
-        const int i_lane = p0 + lane * WARPS;
-        if (i_lane < parts) ml = (i_lane < g.splits ? g.many_ml : g.few_ml)[bj_place(b, g, p, row, h, i_lane)];
-        if (ml.y == 0.f) ml.x = -INFINITY;                // an empty part: its sums were not written
-        const float M_new = fmaxf(M, warp_max(ml.x));
-        const float shrink = M == M_new ? 1.f : exp2f(M - M_new);
-        const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - M_new);
-        l = l * shrink + warp_sum(ml.y * f);
-        acc.x *= shrink; acc.y *= shrink; acc.z *= shrink; acc.w *= shrink;
-        M = M_new;
-        const int m = min(32, (parts - p0 + WARPS - 1) / WARPS);
-#pragma unroll 4
-        for (int i = 0; i < m; ++i) {
-            const float fi = __shfl_sync(FULL_WARP, f, i);
-            const int part = p0 + i * WARPS;
-            if (mine && fi != 0.f) {
-                const float4 v = *reinterpret_cast<const float4*>((part < g.splits ? g.many_o : g.few_o) + bj_place(b, g, p, row, h, part) * g.dp + 4 * lane);
-                acc.x += fi * v.x; acc.y += fi * v.y; acc.z += fi * v.z; acc.w += fi * v.w;
-            }
+    if (WARPS > 1) {
+        __shared__ float4 acc_sh[4][32];
+        __shared__ float2 ml_sh[4];
+        acc_sh[warp][lane] = acc;
+        if (lane == 0) ml_sh[warp] = make_float2(M, l);
+        __syncthreads();
+        if (warp > 0) return;
+        M = ml_sh[0].x;
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) M = fmaxf(M, ml_sh[w].x);
+        l = 0.f;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            if (ml_sh[w].y == 0.f) continue;
+            const float f = exp2f(ml_sh[w].x - M);
+            const float4 v = acc_sh[w][lane];
+            l += f * ml_sh[w].y;
+            acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
         }
     }
-    __shared__ float4 acc_sh[4][32];
-    __shared__ float2 ml_sh[4];
-    acc_sh[warp][lane] = acc;
-    if (lane == 0) ml_sh[warp] = make_float2(M, l);
-    __syncthreads();
-    if (warp > 0) return;
-    M = ml_sh[0].x;
-#pragma unroll
-    for (int w = 1; w < WARPS; ++w) M = fmaxf(M, ml_sh[w].x);
-    l = 0.f;
-    acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-        const float f = ml_sh[w].y == 0.f ? 0.f : exp2f(ml_sh[w].x - M);
-        const float4 v = acc_sh[w][lane];
-        l += f * ml_sh[w].y;
-        acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+    const float inv = l == 0.f ? 0.f : 1.f / l;           // 0: the row sees nothing
+    if (4 * lane < g.a.head_dim) {
+        T* out = reinterpret_cast<T*>(g.a.out) + ((size_t)row * g.a.n_heads + h) * g.a.head_dim + 4 * lane;
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
     }
-    bj_store<T>(g, row, h, acc, l);
 }
 
 } // namespace swk
