@@ -146,7 +146,7 @@ swift_status make_map(CUtensorMap* out, int dtype, const void* base, int rank, c
 {
     const EncodeTiled encode = encoder();
     if (!encode) return fail_batch(SWIFT_ECUDA, "cuTensorMapEncodeTiled not available from the driver");
-    const cuuint32_t one[4] = {1, 1, 1, 1};
+    const cuuint32_t one[5] = {1, 1, 1, 1, 1};
     const CUresult r = encode(out, dtype == SWIFT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void*>(base),
                               dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -162,6 +162,17 @@ swift_status make_kv_map(const swift_paged_kv* kv, int most_slots, CUtensorMap* 
     const cuuint64_t strides[3] = {D2, D2 * kv->page_size, D2 * kv->page_size * planes};
     const cuuint32_t box[4] = {64, (cuuint32_t)(kv->page_size < most_slots ? kv->page_size : most_slots), 1, 1};
     return make_map(out, kv->dtype, kv->pool, 4, dims, strides, box);
+}
+
+// The same pool for head_dim 64 or 128, seen as [plane][K, V][64-dim half][slot][64 dims] with overlapping planes (plane + n_kv_heads
+// holds the V of plane's K): one box brings a page's K and V for a kv head.
+swift_status make_kv_whole_map(const swift_paged_kv* kv, int most_slots, CUtensorMap* out)
+{
+    const cuuint64_t D2 = 2ull * kv->head_dim, halves = kv->head_dim / 64, plane = D2 * kv->page_size;
+    const cuuint64_t dims[5] = {64, (cuuint64_t)kv->page_size, halves, 2, 2ull * kv->n_blocks * kv->n_kv_heads * kv->n_pages};
+    const cuuint64_t strides[4] = {D2, 128, plane * kv->n_kv_heads, plane};
+    const cuuint32_t box[5] = {64, (cuuint32_t)(kv->page_size < most_slots ? kv->page_size : most_slots), (cuuint32_t)halves, 2, 1};
+    return make_map(out, kv->dtype, kv->pool, 5, dims, strides, box);
 }
 
 // [row][head][dim]; a box is one tile: the heads of a group for rows_per_tile rows
@@ -395,7 +406,10 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
         g.item_first = reinterpret_cast<int*>(ws + p.first);
         g.item_last = reinterpret_cast<int*>(ws + p.last);
         CUtensorMap kv_map;
-        const swift_status st = make_kv_map(kv, 16 * p.mt, &kv_map);
+        const long long planes = 2ll * kv->n_blocks * kv->n_kv_heads * kv->n_pages;
+        g.whole_boxes = kv->head_dim % 64 == 0 && planes < 0x7FFFFFFFll;
+        g.planes = g.whole_boxes ? (int)planes : 0;
+        const swift_status st = g.whole_boxes ? make_kv_whole_map(kv, 16 * p.mt, &kv_map) : make_kv_map(kv, 16 * p.mt, &kv_map);
         if (st != SWIFT_OK) return st;
         e = kv->dtype == SWIFT_BF16 ? launch_dec_any<__nv_bfloat16>(p, kv_map, bv, g, s, before) : launch_dec_any<__half>(p, kv_map, bv, g, s, before);
     } else {

@@ -38,6 +38,7 @@ template <int HALVES, int MT> struct BdShape {
 struct BdArgs {
     AttnView a;
     int block, prefix_here;                               // prefix_here: the prefix is part of this launch's items
+    int whole_boxes, planes;                              // a box holds K and V with all dims (head_dim 64 or 128); planes of the pool then
     float* part_o;                                        // [item + worker][16 MT][DP]
     float2* part_ml;                                      // [item + worker][16 MT]
     int* item_first;                                      // [item]: first and last worker that holds units of it
@@ -205,53 +206,68 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
         BdWalk w;
         bd_start<KEYS>(b, g, prefix_units, u0, w);
 
-        // ---- the fetching side, by the worker's first warp: `wf` is the next unit to ask for, `wa` one whose page ids are looked up
-        const int kv = lane >> 4, pg = (lane & 15) / HALVES, half = (lane & 15) % HALVES;    // this lane's box of a unit
-        const bool boxed = pg < per_unit;
-        const uint32_t box_at = kv * S::TILE_BYTES + half * (KEYS * 128) + pg * box_rows * 128;
-        BdWalk wf = w, wa = w;
-        int asked = 0, looked = 0, f_stage = 0, next_page = 0;            // next_page: of unit `asked`, looked up one unit ahead
+        // ---- the fetching side, by the worker's first warp: `wf` is the next unit to ask for, its page ids are looked up already
+        // Shared memory: box after box [K, V][64-dim half][slot][64 dims]
+        const uint32_t box_half = box_rows * 128, box_v = HALVES * box_half, box_bytes = 2 * box_v;
+        BdWalk wf = w;
+        int asked = 0, f_stage = 0, next_page = 0;                        // next_page: lane p: page of box p of unit `asked`
         uint32_t f_turn = 0;
-        auto look_up = [&]() {                                            // -> this lane's page of unit `looked`
-            int page = b.n_pages;                                         // beyond the last page: zeros
-            if (looked < count) {
-                const int key0 = wa.unit * KEYS;
-                if (boxed && pg * box_rows < wa.sp.len - key0) {
-                    const int at = (key0 + pg * box_rows) >> b.page_shift;
-                    page = wa.seq < 0 ? b.prefix_pages[at] : b.page_table[(size_t)wa.seq * b.table_stride + at];
-                }
-                if (++looked < count) bd_next<KEYS>(b, g, wa);
+        auto look_up = [&]() {
+            next_page = -1;                                               // beyond the end: no page
+            const int key0 = wf.unit * KEYS;
+            if (lane < per_unit && lane * box_rows < wf.sp.len - key0) {
+                const int at = (key0 + lane * box_rows) >> b.page_shift;
+                next_page = wf.seq < 0 ? b.prefix_pages[at] : b.page_table[(size_t)wf.seq * b.table_stride + at];
             }
-            return page;
         };
         auto ask = [&]() {                                                // asks for unit `asked`; its stage is free
-            int page = next_page;
-            next_page = look_up();
-            const bool good = (unsigned)page < (unsigned)b.n_pages;
-            if (!good) page = b.n_pages;
-            const unsigned bits = __ballot_sync(FULL_WARP, boxed && good && half == 0 && kv == 0);
-            unsigned pages = 0;
-#pragma unroll
-            for (int p = 0; p < 16 / HALVES; ++p) pages |= ((bits >> (p * HALVES)) & 1u) << p;
-            if (lane == 0) {
+            const bool good = (unsigned)next_page < (unsigned)b.n_pages;
+            const int page = good ? next_page : b.n_pages;                // beyond the last page: zeros
+            const unsigned pages = __ballot_sync(FULL_WARP, good) & all_boxes;
+            if (elect_one()) {
                 page_bits[wk * S::STAGES + f_stage] = pages;
                 mbar_expect_tx(full(f_stage), 2u * S::TILE_BYTES);
             }
             __syncwarp();
-            if (boxed)
-                tma_load_4d(stages + f_stage * 2 * S::TILE_BYTES + box_at, &map_kv, 64 * half, (wf.unit * KEYS + pg * box_rows) & (b.page_size - 1),
-                            (g.block * 2 + kv) * Hk + wf.kvh, page, full(f_stage));
-            if (lane == 0) {
-                if (wf.unit == 0) g.item_first[wf.item] = me;
+            // one lane asks for all boxes in turn (from lanes of their own they go out one by one as well), at some 90 cycles each
+            const uint32_t dst = stages + f_stage * 2 * S::TILE_BYTES;
+            const int plane = g.block * 2 * Hk + wf.kvh;
+            for (int p = 0; p < per_unit; ++p) {
+                const int pageu = __shfl_sync(FULL_WARP, page, p), slot0 = (wf.unit * KEYS + p * box_rows) & (b.page_size - 1);
+                if (elect_one()) {
+                    if (g.whole_boxes) {
+                        tma_load_5d(dst + p * box_bytes, &map_kv, 0, slot0, 0, 0, pageu == b.n_pages ? g.planes : pageu * (g.planes / b.n_pages) + plane, full(f_stage));
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 2 * HALVES; ++x)
+                            tma_load_4d(dst + p * box_bytes + x * box_half, &map_kv, 64 * (x % HALVES), slot0, plane + (x / HALVES) * Hk, pageu, full(f_stage));
+                    }
+                }
+            }
+            if (wf.unit == 0 || wf.unit + 1 == wf.units) {
+                if (wf.unit == 0) g.item_first[wf.item] = me;             // (all lanes write the same)
                 if (wf.unit + 1 == wf.units) g.item_last[wf.item] = me;
             }
             if (++f_stage == S::STAGES) { f_stage = 0; f_turn ^= 1u; }
-            if (++asked < count) bd_next<KEYS>(b, g, wf);
+            if (++asked < count) {
+                bd_next<KEYS>(b, g, wf);
+                look_up();
+            }
         };
         if (mt == 0) {
-            next_page = look_up();
+            look_up();
             for (int i = 0; i < S::STAGES && asked < count; ++i) ask();
         }
+        // This lane's rows in a unit: ldmatrix takes 8 rows of 8 lanes each; the eight-row groups of K and of V it starts from.
+        const uint32_t k_lane = (lane & 7) * 128, k_piece = (lane >> 3) & 1, v_piece = lane >> 4;
+        uint32_t k_grp[MT], v_grp[MT];
+#pragma unroll
+        for (int n = 0; n < MT; ++n) {
+            const int kr = 16 * n + ((lane >> 4) << 3), vr = 16 * n + (((lane >> 3) & 1) << 3);
+            k_grp[n] = (kr >> box_shift) * box_bytes + (kr & (box_rows - 1)) * 128 + k_lane;
+            v_grp[n] = (vr >> box_shift) * box_bytes + (vr & (box_rows - 1)) * 128 + k_lane + box_v;
+        }
+        auto piece_at = [&](uint32_t piece) { return (piece >> 3) * box_half + (((piece & 7) ^ (lane & 7)) << 4); };
 
         uint32_t turn = 0;
         int stage = 0;
@@ -293,14 +309,15 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
             }
             ok = bt_wait(full(stage), turn, abort_sh);
             if (!ok) break;
-            const uint32_t k_sh = stages + stage * 2 * S::TILE_BYTES, v_sh = k_sh + S::TILE_BYTES;
+            const uint32_t kv_sh = stages + stage * 2 * S::TILE_BYTES;
             const int key0 = w.unit * KEYS, left = w.sp.len - key0;
             if (left < KEYS && (left & (box_rows - 1)) != 0) {
                 // slots behind the end may hold anything: V's become zero before they are read
                 const int end = (left | (box_rows - 1)) + 1;
                 for (int i = lane; i < (end - left) * 8 * HALVES; i += 32) {
                     const int row = left + i / (8 * HALVES), piece = i % (8 * HALVES);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_sh + swizzled(row, piece, KEYS)), "r"(0) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"      // whole rows: the swizzle stays inside
+                                 ::"r"(kv_sh + (row >> box_shift) * box_bytes + box_v + (piece >> 3) * box_half + (row & (box_rows - 1)) * 128 + (piece & 7) * 16), "r"(0) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -313,7 +330,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
 #pragma unroll
                 for (int n = 0; n < KEYS / 16; ++n) {
                     uint32_t kf[4];                                       // keys 16 n .. + 15 x dims 16 ks .. + 15
-                    ldsm4(kf, k_sh + swizzled(16 * n + (lane & 7) + ((lane >> 4) << 3), 2 * ks + ((lane >> 3) & 1), KEYS));
+                    ldsm4(kf, kv_sh + k_grp[n] + piece_at(2 * ks + k_piece));
                     mma16816(s[2 * n], qf[ks], kf[0], kf[1], T());
                     mma16816(s[2 * n + 1], qf[ks], kf[2], kf[3], T());
                 }
@@ -376,7 +393,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
 #pragma unroll
                 for (int d = 0; d < 4 * HALVES; ++d) {                    // keys 16 n .. + 15 x dims 16 d .. + 15
                     uint32_t vf[4];
-                    ldsm4_trans(vf, v_sh + swizzled(16 * n + (lane & 15), 2 * d + (lane >> 4), KEYS));
+                    ldsm4_trans(vf, kv_sh + v_grp[n] + piece_at(2 * d + v_piece));
                     mma16816(o[2 * d], pf, vf[0], vf[1], T());
                     mma16816(o[2 * d + 1], pf, vf[2], vf[3], T());
                 }
