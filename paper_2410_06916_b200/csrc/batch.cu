@@ -358,11 +358,11 @@ cudaError_t launch_dec_any(const PrefixPlan& p, const CUtensorMap& kv_map, const
 template <typename T>
 cudaError_t launch_join(const PrefixPlan& p, const BatchView& bv, const BjArgs& j, cudaStream_t s)
 {
-    // An item has about (workers / items + 1) parts of the few-row kernel: with more than eight of them the four warps of a block
+    // An item has about (workers / items + 1) parts of the few-row kernel: with more than eight of them the eight warps of a block
     // share a head, else each takes one.
     const bool cut = p.few && (long long)p.grid * (BD_WARPS / p.mt) > 8 * p.items;
-    return cut ? launch(attn_join_kernel<T, 4>, dim3(bv.n_rows, j.a.n_heads), 128, 0, s, true, bv, j)
-               : launch(attn_join_kernel<T, 1>, dim3(bv.n_rows, ceil_div(j.a.n_heads, 4)), 128, 0, s, true, bv, j);
+    return cut ? launch(attn_join_kernel<T, 8>, dim3(bv.n_rows, j.a.n_heads), 256, 0, s, true, bv, j)
+               : launch(attn_join_kernel<T, 1>, dim3(bv.n_rows, ceil_div(j.a.n_heads, 8)), 256, 0, s, true, bv, j);
 }
 
 swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, int block, const PrefixPlan& p, unsigned char* ws, cudaStream_t s)

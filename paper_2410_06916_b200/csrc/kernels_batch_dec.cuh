@@ -354,21 +354,20 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
                 top[0] = max3(top[0], s[n][0], s[n][1]);
                 top[1] = max3(top[1], s[n][2], s[n][3]);
             }
-            bool moved = false;
+            // as in the many-row kernel, a row's sums are rescaled when its maximum has grown by more than 2^8
+            bool moved[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 top[e] = fmaxf(top[e], __shfl_xor_sync(FULL_WARP, top[e], 1));
                 top[e] = fmaxf(top[e], __shfl_xor_sync(FULL_WARP, top[e], 2));
-                // as in the many-row kernel, sums are rescaled when the maximum has grown by more than 2^8
-                moved = moved || (top[e] > m[e] && (m[e] == -INFINITY || (top[e] - m[e]) * c > BT_GROW));
+                moved[e] = bt_outgrown(top[e], m[e], c);
             }
-            if (__any_sync(FULL_WARP, moved)) {
+            if (__any_sync(FULL_WARP, moved[0] || moved[1])) {
                 float shrink[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float m_new = fmaxf(m[e], top[e]);
-                    shrink[e] = m_new == m[e] ? 1.f : ex2((m[e] - m_new) * c);
-                    m[e] = m_new;
+                    shrink[e] = moved[e] ? ex2((m[e] - top[e]) * c) : 1.f;
+                    if (moved[e]) m[e] = top[e];
                     l[e] *= shrink[e];
                 }
 #pragma unroll
@@ -449,99 +448,107 @@ struct BjArgs {
 
 // out[row][h] = sum_i 2^(M_i - M) O_i / sum_i 2^(M_i - M) l_i over the parts of a row, in a fixed order: the many-row
 // kernel's parts, then the prefix item's, then the own item's.
-struct BjHead {                                           // where the parts of one (row, head) are
-    int first[2], n[2], item[2], rho[2];
+struct BjSum {
+    float M, l;
+    float4 acc;
 };
-__device__ __forceinline__ BjHead bj_head(const BatchView& b, const BjArgs& g, int row, int seq, const SeqSpan& sp, int h)
-{
-    const int Hk = g.a.n_kv_heads, G = g.a.n_heads / Hk, kvh = h / G, hg = h - kvh * G;
-    BjHead p = {{0, 0}, {0, 0}, {kvh, (g.prefix_here ? Hk : 0) + seq * Hk + kvh}, {row * G + hg, (row - sp.r0) * G + hg}};
-    if (g.prefix_here) { p.first[0] = g.item_first[p.item[0]]; p.n[0] = g.item_last[p.item[0]] - p.first[0] + 1; }
-    if (g.own_here && sp.len > 0) { p.first[1] = g.item_first[p.item[1]]; p.n[1] = g.item_last[p.item[1]] - p.first[1] + 1; }
-    return p;
-}
-__device__ __forceinline__ size_t bj_place(const BatchView& b, const BjArgs& g, const BjHead& p, int row, int h, int i)   // part i's (maximum, sum); its sums times dp
-{
-    if (i < g.splits) return ((size_t)i * b.n_rows + row) * g.a.n_heads + h;
-    const int j = i - g.splits < p.n[0] ? 0 : 1;
-    return (size_t)(p.item[j] + p.first[j] + i - g.splits - (j ? p.n[0] : 0)) * g.item_rows + p.rho[j];
-}
-// WARPS warps per (row, head), each taking every WARPS-th part.  The sums of eight parts are fetched at once and along with
-// their maxima, so that a head costs four dependent trips to memory (its sequence, its items' first and last worker, its
-// parts, the store) and one more for every 8 WARPS further parts.  Four warps are for few rows, whose items are cut into many
-// parts (one row, 64 heads, 148 parts each).  grid = (rows, ceil(heads / (4 / WARPS))), block = 128.
+// Adds parts at, at + step, ... below n of one kind; part i's sums start at o + i * stride_o.  Eight parts' sums and maxima are
+// fetched at once.
 constexpr int BJ_PARTS = 8;
+__device__ __forceinline__ void bj_add(BjSum& s, const float* o, const float2* ml, size_t stride_o, size_t stride_ml, int n, int at, int step, bool mine)
+{
+    if (at >= n) return;
+    o += at * stride_o;
+    ml += at * stride_ml;
+    stride_o *= step;
+    stride_ml *= step;
+    for (; at < n; at += BJ_PARTS * step) {
+        float2 x[BJ_PARTS];
+        float4 v[BJ_PARTS];
+#pragma unroll
+        for (int i = 0; i < BJ_PARTS; ++i) {
+            x[i] = make_float2(-INFINITY, 0.f);
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (at + i * step < n) {
+                x[i] = *ml;
+                if (mine) v[i] = *reinterpret_cast<const float4*>(o);
+            }
+            ml += stride_ml;
+            o += stride_o;
+        }
+        float top = s.M;
+#pragma unroll
+        for (int i = 0; i < BJ_PARTS; ++i) top = x[i].y != 0.f ? fmaxf(top, x[i].x) : top;
+        const float shrink = s.M == top ? 1.f : ex2(s.M - top);
+        s.l *= shrink;
+        s.acc.x *= shrink; s.acc.y *= shrink; s.acc.z *= shrink; s.acc.w *= shrink;
+        s.M = top;
+#pragma unroll
+        for (int i = 0; i < BJ_PARTS; ++i) {
+            if (x[i].y == 0.f) continue;                  // an empty part: its sums were not written
+            const float f = ex2(x[i].x - top);
+            s.l += x[i].y * f;
+            s.acc.x += f * v[i].x; s.acc.y += f * v[i].y; s.acc.z += f * v[i].z; s.acc.w += f * v[i].w;
+        }
+    }
+}
 
+// WARPS warps per (row, head), each taking every WARPS-th part, lanes over dims.  A head costs four dependent trips to memory (its
+// sequence, its items' first and last worker, its parts, the store) and one more for every 8 WARPS further parts.  Eight warps
+// are for few rows, whose items are cut into many parts (one row, 64 heads, 148 parts each).
+// grid = (rows, ceil(heads / (8 / WARPS))), block = 256.
 template <typename T, int WARPS>
-__global__ void __launch_bounds__(128) attn_join_kernel(BatchView b, BjArgs g)
+__global__ void __launch_bounds__(256) attn_join_kernel(BatchView b, BjArgs g)
 {
     pdl_wait();
-    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y * (4 / WARPS) + warp / WARPS;
-    if (h >= g.a.n_heads) return;                         // (WARPS 4: all or none of a block)
+    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y * (8 / WARPS) + warp / WARPS, turn = warp % WARPS;
+    if (h >= g.a.n_heads) return;                         // (WARPS 8: all or none of a block)
+    const int Hk = g.a.n_kv_heads, G = g.a.n_heads / Hk, kvh = h / G, hg = h - kvh * G;
+    int f0 = 0, n0 = 0;
+    if (g.prefix_here) { f0 = g.item_first[kvh]; n0 = g.item_last[kvh] - f0 + 1; }
     SeqSpan sp;
     const int seq = find_seq(b, row, sp);
     if (seq < 0 || row - sp.r0 >= g.a.max_rows) return;   // the same for the whole block
     const bool mine = 4 * lane < g.dp;
-    const BjHead p = bj_head(b, g, row, seq, sp, h);
-    const int parts = g.splits + p.n[0] + p.n[1];
-    float M = -INFINITY, l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p0 = warp % WARPS; p0 < parts; p0 += BJ_PARTS * WARPS) {
-        float2 ml[BJ_PARTS];
-        float4 v[BJ_PARTS];
-        float top = M;
-#pragma unroll
-        for (int i = 0; i < BJ_PARTS; ++i) {
-            ml[i] = make_float2(-INFINITY, 0.f);
-            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            const int part = p0 + i * WARPS;
-            if (part < parts) {
-                const size_t at = bj_place(b, g, p, row, h, part);
-                const bool many = part < g.splits;
-                ml[i] = (many ? g.many_ml : g.few_ml)[at];
-                if (mine) v[i] = *reinterpret_cast<const float4*>((many ? g.many_o : g.few_o) + at * g.dp + 4 * lane);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < BJ_PARTS; ++i)
-            if (ml[i].y != 0.f) top = fmaxf(top, ml[i].x);
-        const float shrink = M == top ? 1.f : exp2f(M - top);
-        l *= shrink;
-        acc.x *= shrink; acc.y *= shrink; acc.z *= shrink; acc.w *= shrink;
-        M = top;
-#pragma unroll
-        for (int i = 0; i < BJ_PARTS; ++i) {
-            if (ml[i].y == 0.f) continue;                 // an empty part: its sums were not written
-            const float f = exp2f(ml[i].x - M);
-            l += ml[i].y * f;
-            acc.x += f * v[i].x; acc.y += f * v[i].y; acc.z += f * v[i].z; acc.w += f * v[i].w;
-        }
+    BjSum s = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    if (g.splits > 0) {
+        const size_t at = (size_t)row * g.a.n_heads + h, slot = (size_t)b.n_rows * g.a.n_heads;
+        bj_add(s, g.many_o + at * g.dp + 4 * lane, g.many_ml + at, slot * g.dp, slot, g.splits, turn, WARPS, mine);
+    }
+    const int own_item = (g.prefix_here ? Hk : 0) + seq * Hk + kvh;
+    int f1 = 0, n1 = 0;
+    if (g.own_here && sp.len > 0) { f1 = g.item_first[own_item]; n1 = g.item_last[own_item] - f1 + 1; }
+    if (n0 > 0) {
+        const size_t at = (size_t)(kvh + f0) * g.item_rows + row * G + hg;
+        bj_add(s, g.few_o + at * g.dp + 4 * lane, g.few_ml + at, (size_t)g.item_rows * g.dp, g.item_rows, n0, turn, WARPS, mine);
+    }
+    if (n1 > 0) {
+        const size_t at = (size_t)(own_item + f1) * g.item_rows + (row - sp.r0) * G + hg;
+        bj_add(s, g.few_o + at * g.dp + 4 * lane, g.few_ml + at, (size_t)g.item_rows * g.dp, g.item_rows, n1, turn, WARPS, mine);
     }
     if (WARPS > 1) {
-        __shared__ float4 acc_sh[4][32];
-        __shared__ float2 ml_sh[4];
-        acc_sh[warp][lane] = acc;
-        if (lane == 0) ml_sh[warp] = make_float2(M, l);
+        __shared__ float4 acc_sh[8][32];
+        __shared__ float2 ml_sh[8];
+        acc_sh[warp][lane] = s.acc;
+        if (lane == 0) ml_sh[warp] = make_float2(s.M, s.l);
         __syncthreads();
         if (warp > 0) return;
-        M = ml_sh[0].x;
+        s = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll
-        for (int w = 1; w < WARPS; ++w) M = fmaxf(M, ml_sh[w].x);
-        l = 0.f;
-        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < WARPS; ++w) s.M = fmaxf(s.M, ml_sh[w].x);
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
             if (ml_sh[w].y == 0.f) continue;
-            const float f = exp2f(ml_sh[w].x - M);
+            const float f = ex2(ml_sh[w].x - s.M);
             const float4 v = acc_sh[w][lane];
-            l += f * ml_sh[w].y;
-            acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+            s.l += f * ml_sh[w].y;
+            s.acc.x += f * v.x; s.acc.y += f * v.y; s.acc.z += f * v.z; s.acc.w += f * v.w;
         }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;           // 0: the row sees nothing
+    const float inv = s.l == 0.f ? 0.f : 1.f / s.l;       // 0: the row sees nothing
     if (4 * lane < g.a.head_dim) {
         T* out = reinterpret_cast<T*>(g.a.out) + ((size_t)row * g.a.n_heads + h) * g.a.head_dim + 4 * lane;
-        *reinterpret_cast<uint2*>(out) = make_uint2(pack2(acc.x * inv, acc.y * inv, T()), pack2(acc.z * inv, acc.w * inv, T()));
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack2(s.acc.x * inv, s.acc.y * inv, T()), pack2(s.acc.z * inv, s.acc.w * inv, T()));
     }
 }
 

@@ -336,10 +336,14 @@ __device__ __forceinline__ void bt_hand_over(uint32_t p_bar, int h)
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(p_bar + 8u * h);
 }
-// Rows whose maximum has outgrown what their sums are scaled by: new maximum, sums and (behind the first tile) O rescaled.
-template <int DP> __device__ __forceinline__ void bt_rescale(uint32_t o_at, float c, float top, bool first, float& m, float& l)
+// Whether a row's maximum has outgrown what its sums are scaled by.
+__device__ __forceinline__ bool bt_outgrown(float top, float m, float c) { return top > m && (m == -INFINITY || (top - m) * c > BT_GROW); }
+
+// Such rows get the new maximum, their sums and (behind the first tile) O rescaled.  The others of the warp keep theirs: a row's
+// bits depend on its own scores alone, not on its neighbours' nor on the unused rows of a tile, which hold anything.
+template <int DP> __device__ __forceinline__ void bt_rescale(uint32_t o_at, float c, float top, bool mine, bool first, float& m, float& l)
 {
-    const float m_new = fmaxf(m, top), shrink = m == m_new ? 1.f : ex2((m - m_new) * c);
+    const float m_new = mine ? top : m, shrink = mine ? ex2((m - m_new) * c) : 1.f;
     l *= shrink;
     m = m_new;
     if (first) return;
@@ -353,11 +357,6 @@ template <int DP> __device__ __forceinline__ void bt_rescale(uint32_t o_at, floa
         tmem_st8(o_at + i, o);
     }
 }
-__device__ __forceinline__ bool bt_outgrown(float top, float m, float c)
-{
-    return __any_sync(FULL_WARP, top > m && (m == -INFINITY || (top - m) * c > BT_GROW));
-}
-
 // The softmax warps' part of one key tile: S in, P out (over the upper half of S), the row's maximum m and sum l brought up to
 // date.  s_at, o_at: this warp's lanes of S and O; p_bar: the two hand-over barriers.  Scores come a quarter (32 keys) at a
 // time; the upper half of the keys goes first.
@@ -391,7 +390,8 @@ __device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_
     tmem_wait_ld(s3);
     hide(3, s3);
     top = fmaxf(top, bt_highest(s3));
-    if (bt_outgrown(top, m, c)) bt_rescale<DP>(o_at, c, top, first, m, l);
+    const bool grown = bt_outgrown(top, m, c);
+    if (__any_sync(FULL_WARP, grown)) bt_rescale<DP>(o_at, c, top, grown, first, m, l);
     const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
     const f32x2 c2 = pair2(c, c), off2 = pair2(off, off);
     f32x2 sum[2] = {0ull, 0ull};

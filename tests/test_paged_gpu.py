@@ -204,6 +204,23 @@ def test_attention(case, form):
 
 
 @pytest.mark.parametrize("form", ["prompt", "prefix"])
+@pytest.mark.parametrize("heads,kv_heads,each", [(14, 2, 9), (14, 2, 1), (56, 8, 40), (9, 3, 40)])
+def test_bits_do_not_depend_on_what_ran_before(form, heads, kv_heads, each):
+    """Groups that leave rows of a tile unused: what an earlier call left in shared memory for those rows must not show."""
+    b = Batch([each] * 5, [300 + each] * 5, heads, kv_heads, 128, 16, BF16, prefix_len=500)
+    pool, batch = setup(b)
+    q = b.q.cuda()
+    before = []
+    for scale in (1.0, 1e3, 1e-3, 30.0):
+        other = Batch([64, 33], [400, 90], 8, 1, 128, 16, BF16, prefix_len=70, seed=7)   # fills whole tiles
+        opool, obatch = setup(other)
+        (obatch.prompt_attention if form == "prompt" else obatch.prefix_attention)(0, other.q.cuda() * scale)
+        before.append((batch.prompt_attention if form == "prompt" else batch.prefix_attention)(0, q))
+    for o in before[1:]:
+        assert torch.equal(o, before[0])
+
+
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
 @pytest.mark.parametrize("dim,dt", [(128, BF16), (64, F16), (128, F32)])
 def test_attention_with_strided_queries_and_a_scale(form, dim, dt):
     b = Batch([37, 3], [50, 400], 8, 2, dim, 16, dt, prefix_len=50)
