@@ -287,21 +287,21 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
         if (bv.prefix_len > 0 && !p->prefix_few && !p->prompt) {
             // The prefix is tensor work, the sequences' own parts are HBM work: both kernels run at once, on SMs of their own, and
             // the share of SMs and the cuts of the prefix are chosen for the earliest common end.  Costs in microseconds: a key
-            // tile of a pair of query tiles 1.75, a piece's set-up and write-back 4; own parts at 44 GB/s per SM up to 6 TB/s, 4 an item,
-            // their lengths (which only the device knows) taken as 0.6 of the page table's width, and never more than 3/4 of the
+            // tile of a pair of query tiles 1.75, a piece's set-up and write-back 8; own parts at 44 GB/s per SM up to 6 TB/s, 4 an item,
+            // their lengths (which only the device knows) taken as 0.6 of the page table's width, and never more than 5/6 of the
             // SMs for them.  (64 continuations of 8192 positions, 64 heads on 8, about 750 own positions: 86 us one after the other.)
             const int tiles = ceil_div(bv.prefix_len, BT_KEYS), TQ = BT_ROWS / p->group;
             const long long pairs = (long long)ceil_div(bv.n_rows, 2 * TQ) * Hk;
             const double own_bytes = 0.6 * bv.n_seqs * bv.max_len * Hk * kv->head_dim * 4.0;
             const int own_mt = own <= 16 ? 1 : own <= 32 ? 2 : 4;
             double best = 0;
-            for (int g = p->few ? sms / 4 : sms; g <= sms; g += sms / 37 > 0 ? sms / 37 : 1) {
+            for (int g = p->few ? sms / 6 : sms; g <= sms; g += sms / 37 > 0 ? sms / 37 : 1) {
                 const int rest = g == sms ? sms : sms - g;
                 const double stream_us = own_bytes / (rest * 44e3 < 6e6 ? rest * 44e3 : 6e6), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * (BD_WARPS / own_mt));
                 const double own_us = p->few ? 3.0 + (stream_us > item_us ? stream_us : item_us) : 0.0;
                 for (int c = 1; c <= 64 && c <= tiles; ++c) {
-                    const double pre_us = ceil_div(pairs * c, g) * (ceil_div(tiles, c) * 1.75 + 4.0);
-                    const double cost = (g == sms ? pre_us + own_us : pre_us > own_us ? pre_us : own_us) + 0.5 * c;   // every cut is read again by the join
+                    const double pre_us = ceil_div(pairs * c, g) * (ceil_div(tiles, c) * 1.75 + 8.0);
+                    const double cost = (g == sms ? pre_us + own_us : pre_us > own_us ? pre_us : own_us) + c;         // every cut is read again by the join
                     if (p->splits == 0 || cost < best) {
                         best = cost;
                         p->splits = c;

@@ -452,29 +452,57 @@ struct BjSum {
     float M, l;
     float4 acc;
 };
-// Adds parts at, at + step, ... below n of one kind; part i's sums start at o + i * stride_o.  Eight parts' sums and maxima are
-// fetched at once.
-constexpr int BJ_PARTS = 8;
-__device__ __forceinline__ void bj_add(BjSum& s, const float* o, const float2* ml, size_t stride_o, size_t stride_ml, int n, int at, int step, bool mine)
+struct BjKind {                                           // one kind of parts: how many, where the first one's sums and maximum are, what lies between two
+    const float* o;
+    const float2* ml;
+    int n;
+    long long stride;                                     // in (row, head)s
+};
+
+// WARPS warps per (row, head), each taking every WARPS-th part, lanes over dims.  A head costs four dependent trips to memory (its
+// sequence, its items' first and last worker, its parts, the store) and one more for every batch of further parts.  Eight warps
+// are for few rows, whose items are cut into many parts (one row, 64 heads, 148 parts each).
+// grid = (rows, ceil(heads / (8 / WARPS))), block = 256.
+template <typename T, int WARPS>
+__global__ void __launch_bounds__(256) attn_join_kernel(BatchView b, BjArgs g)
 {
-    if (at >= n) return;
-    o += at * stride_o;
-    ml += at * stride_ml;
-    stride_o *= step;
-    stride_ml *= step;
-    for (; at < n; at += BJ_PARTS * step) {
+    constexpr int BJ_PARTS = WARPS == 1 ? 4 : 8;          // parts whose sums and maxima are fetched at once
+    pdl_wait();
+    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y * (8 / WARPS) + warp / WARPS, turn = warp % WARPS;
+    if (h >= g.a.n_heads) return;                         // (WARPS 8: all or none of a block)
+    const int Hk = g.a.n_kv_heads, G = g.a.n_heads / Hk, kvh = h / G, hg = h - kvh * G;
+    int f0 = 0, n0 = 0;
+    if (g.prefix_here) { f0 = g.item_first[kvh]; n0 = g.item_last[kvh] - f0 + 1; }
+    SeqSpan sp;
+    const int seq = find_seq(b, row, sp);
+    if (seq < 0 || row - sp.r0 >= g.a.max_rows) return;   // the same for the whole block
+    const int own_item = (g.prefix_here ? Hk : 0) + seq * Hk + kvh;
+    int f1 = 0, n1 = 0;
+    if (g.own_here && sp.len > 0) { f1 = g.item_first[own_item]; n1 = g.item_last[own_item] - f1 + 1; }
+    BjKind kinds[3];
+    const size_t at[3] = {(size_t)row * g.a.n_heads + h, (size_t)(kvh + f0) * g.item_rows + row * G + hg, (size_t)(own_item + f1) * g.item_rows + (row - sp.r0) * G + hg};
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+        kinds[j] = {(j ? g.few_o : g.many_o) + at[j] * g.dp + 4 * lane, (j ? g.few_ml : g.many_ml) + at[j], j == 0 ? g.splits : j == 1 ? n0 : n1,
+                    j ? (long long)g.item_rows : (long long)b.n_rows * g.a.n_heads};
+    const bool mine = 4 * lane < g.dp;
+    const int parts = g.splits + n0 + n1;
+    BjSum s = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int p0 = turn; p0 < parts; p0 += BJ_PARTS * WARPS) {
         float2 x[BJ_PARTS];
         float4 v[BJ_PARTS];
 #pragma unroll
         for (int i = 0; i < BJ_PARTS; ++i) {
+            int part = p0 + i * WARPS;
             x[i] = make_float2(-INFINITY, 0.f);
             v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (at + i * step < n) {
-                x[i] = *ml;
-                if (mine) v[i] = *reinterpret_cast<const float4*>(o);
+            if (part < parts) {
+                const bool many = part < kinds[0].n, prefix = !many && part < kinds[0].n + kinds[1].n;
+                const BjKind& k = many ? kinds[0] : prefix ? kinds[1] : kinds[2];
+                const long long off = (part - (many ? 0 : prefix ? kinds[0].n : kinds[0].n + kinds[1].n)) * k.stride;
+                x[i] = k.ml[off];
+                if (mine) v[i] = *reinterpret_cast<const float4*>(k.o + off * g.dp);
             }
-            ml += stride_ml;
-            o += stride_o;
         }
         float top = s.M;
 #pragma unroll
@@ -490,41 +518,6 @@ __device__ __forceinline__ void bj_add(BjSum& s, const float* o, const float2* m
             s.l += x[i].y * f;
             s.acc.x += f * v[i].x; s.acc.y += f * v[i].y; s.acc.z += f * v[i].z; s.acc.w += f * v[i].w;
         }
-    }
-}
-
-// WARPS warps per (row, head), each taking every WARPS-th part, lanes over dims.  A head costs four dependent trips to memory (its
-// sequence, its items' first and last worker, its parts, the store) and one more for every 8 WARPS further parts.  Eight warps
-// are for few rows, whose items are cut into many parts (one row, 64 heads, 148 parts each).
-// grid = (rows, ceil(heads / (8 / WARPS))), block = 256.
-template <typename T, int WARPS>
-__global__ void __launch_bounds__(256) attn_join_kernel(BatchView b, BjArgs g)
-{
-    pdl_wait();
-    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y * (8 / WARPS) + warp / WARPS, turn = warp % WARPS;
-    if (h >= g.a.n_heads) return;                         // (WARPS 8: all or none of a block)
-    const int Hk = g.a.n_kv_heads, G = g.a.n_heads / Hk, kvh = h / G, hg = h - kvh * G;
-    int f0 = 0, n0 = 0;
-    if (g.prefix_here) { f0 = g.item_first[kvh]; n0 = g.item_last[kvh] - f0 + 1; }
-    SeqSpan sp;
-    const int seq = find_seq(b, row, sp);
-    if (seq < 0 || row - sp.r0 >= g.a.max_rows) return;   // the same for the whole block
-    const bool mine = 4 * lane < g.dp;
-    BjSum s = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-    if (g.splits > 0) {
-        const size_t at = (size_t)row * g.a.n_heads + h, slot = (size_t)b.n_rows * g.a.n_heads;
-        bj_add(s, g.many_o + at * g.dp + 4 * lane, g.many_ml + at, slot * g.dp, slot, g.splits, turn, WARPS, mine);
-    }
-    const int own_item = (g.prefix_here ? Hk : 0) + seq * Hk + kvh;
-    int f1 = 0, n1 = 0;
-    if (g.own_here && sp.len > 0) { f1 = g.item_first[own_item]; n1 = g.item_last[own_item] - f1 + 1; }
-    if (n0 > 0) {
-        const size_t at = (size_t)(kvh + f0) * g.item_rows + row * G + hg;
-        bj_add(s, g.few_o + at * g.dp + 4 * lane, g.few_ml + at, (size_t)g.item_rows * g.dp, g.item_rows, n0, turn, WARPS, mine);
-    }
-    if (n1 > 0) {
-        const size_t at = (size_t)(own_item + f1) * g.item_rows + (row - sp.r0) * G + hg;
-        bj_add(s, g.few_o + at * g.dp + 4 * lane, g.few_ml + at, (size_t)g.item_rows * g.dp, g.item_rows, n1, turn, WARPS, mine);
     }
     if (WARPS > 1) {
         __shared__ float4 acc_sh[8][32];
