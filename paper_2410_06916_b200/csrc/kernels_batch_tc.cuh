@@ -34,7 +34,7 @@
 
 namespace swk {
 
-constexpr int BT_THREADS = 320;     // 2 x 4 softmax warps, the TMA warp, the MMA warp
+constexpr int BT_THREADS = 352;     // 2 x 4 softmax warps, a TMA warp for Q and K, the MMA warp, a TMA warp for V
 constexpr int BT_KEYS = 128;        // keys per tile
 constexpr int BT_ROWS = 128;        // packed query rows per tile
 constexpr int BT_PAGE_RING = 16;    // page-validity words kept (more than the key tiles ever in flight)
@@ -447,7 +447,7 @@ template <typename T, int COLS> __device__ __noinline__ void bt_store_out(uint32
 }
 
 // ------------------------------------------------------------------------------ the kernel
-// grid = persistent CTAs (at most one per SM), each taking pieces blockIdx.x, + gridDim.x, ...; block = 320.
+// grid = persistent CTAs (at most one per SM), each taking pieces blockIdx.x, + gridDim.x, ...; block = 352.
 // PART: leaves parts in the workspace (BT_PREFIX, BT_OWN) rather than results (BT_PROMPT).
 template <typename T, int HALVES, bool PART>
 __global__ void __launch_bounds__(BT_THREADS, 1)
@@ -507,81 +507,86 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
     auto s_col = [&](int x) { return tmem + 128u * x; };              // S, then P, of tile x
     auto o_col = [&](int x) { return tmem + 256u + 128u * x; };
 
-    if (warp == 8) {
-        // ---------------------------------------------------------------- TMA: queries, then K and V tiles in turn
+    if (warp == 8 || warp == 10) {
+        // ---------------------------------------------------------------- TMA: one warp for the queries and K tiles, one for V tiles
+        // The ring holds K and V tiles in turn.  A box costs its issuing lane some 90 cycles: with pages of 16, the 32 boxes of a
+        // key tile's K and V would take one warp about as long as the products.
+        const int kv = warp == 10;
         const int per_tile = BT_KEYS >> b.page_shift;                 // pages per key tile, 1..16
-        const int pg = lane / HALVES, half = lane % HALVES;           // this lane's box of a tile
-        const bool boxed = pg < per_tile;
-        const uint32_t box_at = half * (BT_KEYS * 128) + (pg << b.page_shift) * 128;
-        uint32_t slot = 0, turn = 0, q_turn[2] = {0, 0}, landed_turn = 0;   // turn: parity of the ring's current pass
+        uint32_t slot = kv, turn = 0, q_turn[2] = {0, 0}, landed_turn = 0;   // turn: parity of the ring's current pass
         int tile_no = 0;
         bool ok = true;
         BtItem it;
         for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
             const int n_tiles = max(it.tiles[0], it.tiles[1]);
-            const int plane_k = (g.block * 2) * g.a.n_kv_heads + it.kvh, plane_v = plane_k + g.a.n_kv_heads;
-            if (lane == 0) {
-                for (int x = 0; ok && x < 2; ++x) {
-                    if (it.tiles[x] == 0) continue;
+            const int plane = (g.block * 2 + kv) * g.a.n_kv_heads + it.kvh;
+            if (kv == 0) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (!ok || it.tiles[x] == 0) continue;
                     ok = bt_wait(q_empty(x), q_turn[x] ^ 1u, abort_sh);
-                    if (!ok) break;
-                    mbar_expect_tx(q_full(x), (uint32_t)(TQ * G * 128 * HALVES));
-                    for (int hf = 0; hf < HALVES; ++hf)
-                        tma_load_3d(q_sh + x * S::Q_BYTES + hf * (BT_ROWS * 128), &map_q, 64 * hf, it.kvh * G, it.r0 + it.t0 + x * TQ, q_full(x));
+                    q_turn[x] ^= 1u;
+                    if (ok && elect_one()) {
+                        mbar_expect_tx(q_full(x), (uint32_t)(TQ * G * 128 * HALVES));
+                        for (int hf = 0; hf < HALVES; ++hf)
+                            tma_load_3d(q_sh + x * S::Q_BYTES + hf * (BT_ROWS * 128), &map_q, 64 * hf, it.kvh * G, it.r0 + it.t0 + x * TQ, q_full(x));
+                    }
                 }
             }
-            for (int x = 0; x < 2; ++x)
-                if (it.tiles[x]) q_turn[x] ^= 1u;
-            ok = __shfl_sync(FULL_WARP, ok ? 1 : 0, 0) != 0;
-            for (int j = 0; ok && j < n_tiles; ++j, ++tile_no) {
+            // lane p: page p of the next tile, looked up a tile ahead
+            auto look_up = [&](int j) {
                 const bool shared_part = j < it.np;
                 const int key0 = (shared_part ? it.first_tile + j : j - it.np) * BT_KEYS;
-                const int left = (shared_part ? b.prefix_len : it.len) - key0;            // keys of this tile that exist
-                int page = b.n_pages;                                 // beyond the last page: zeros
-                if (boxed && (pg << b.page_shift) < left) {
-                    const int at = (key0 >> b.page_shift) + pg;
+                const int left = (shared_part ? b.prefix_len : it.len) - key0;
+                int page = -1;
+                if (j < n_tiles && lane < per_tile && (lane << b.page_shift) < left) {
+                    const int at = (key0 >> b.page_shift) + lane;
                     page = shared_part ? b.prefix_pages[at] : b.page_table[(size_t)it.seq * b.table_stride + at];
                 }
-                const bool good = (unsigned)page < (unsigned)b.n_pages;
-                if (!good) page = b.n_pages;
-                const unsigned bits = __ballot_sync(FULL_WARP, boxed && good && half == 0);
-                unsigned pages = 0;
-#pragma unroll
-                for (int p = 0; p < 32 / HALVES; ++p) pages |= ((bits >> (p * HALVES)) & 1u) << p;
+                return page;
+            };
+            int next_page = look_up(0);
+            for (int j = 0; ok && j < n_tiles; ++j, ++tile_no) {
+                const bool good = (unsigned)next_page < (unsigned)b.n_pages;
+                const int page = good ? next_page : b.n_pages;        // beyond the last page: zeros
+                const unsigned pages = __ballot_sync(FULL_WARP, good);
+                next_page = look_up(j + 1);
+                const bool shared_part = j < it.np;
+                const int left = (shared_part ? b.prefix_len - (it.first_tile + j) * BT_KEYS : it.len - (j - it.np) * BT_KEYS);   // keys of this tile that exist
                 const int tail = left & (b.page_size - 1);            // slots of the last page that hold something
-                const bool cut = left < BT_KEYS && tail != 0 && ((pages >> (left >> b.page_shift)) & 1u);
-#pragma unroll 1
-                for (int kv = 0; kv < 2; ++kv) {
-                    const bool mend = kv == 1 && cut;                 // V tile with unwritten slots: zeroed before the product may read them
-                    if (lane == 0) {
-                        ok = bt_wait(empty(slot), turn ^ 1u, abort_sh);
-                        if (ok) {
-                            if (kv == 0) page_bits[tile_no & (BT_PAGE_RING - 1)] = pages;
-                            mbar_expect_tx(mend ? landed : full(slot), (uint32_t)S::SLOT_BYTES);
-                        }
-                    }
-                    ok = __shfl_sync(FULL_WARP, ok ? 1 : 0, 0) != 0;
-                    if (!ok) break;
-                    const uint32_t dst = ring + slot * S::SLOT_BYTES;
-                    if (boxed) tma_load_4d(dst + box_at, &map_kv, 64 * half, 0, kv ? plane_v : plane_k, page, mend ? landed : full(slot));
-                    if (mend) {
-                        bool here = true;
-                        if (lane == 0) here = bt_wait(landed, landed_turn, abort_sh);
-                        landed_turn ^= 1u;
-                        ok = __shfl_sync(FULL_WARP, here ? 1 : 0, 0) != 0;
-                        if (!ok) break;
-                        const int row1 = ((left >> b.page_shift) + 1) << b.page_shift;
-                        for (int i = lane; i < (row1 - left) * 8 * HALVES; i += 32) {
-                            const int row = left + i / (8 * HALVES), piece = i % (8 * HALVES);
-                            const uint32_t a = dst + (piece >> 3) * (BT_KEYS * 128) + row * 128 + (piece & 7) * 16;    // whole rows: the swizzle stays inside
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a), "r"(0) : "memory");
-                        }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(full(slot));
-                    }
-                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                // a V tile with unwritten slots: they are zeroed before the product may read them
+                const bool mend = kv == 1 && left < BT_KEYS && tail != 0 && ((pages >> (left >> b.page_shift)) & 1u);
+                ok = bt_wait(empty(slot), turn ^ 1u, abort_sh);
+                if (!ok) break;
+                const uint32_t bar = mend ? landed : full(slot), dst = ring + slot * S::SLOT_BYTES;
+                if (elect_one()) {
+                    if (kv == 0) page_bits[tile_no & (BT_PAGE_RING - 1)] = pages;
+                    mbar_expect_tx(bar, (uint32_t)S::SLOT_BYTES);
                 }
+                __syncwarp();
+                for (int p = 0; p < per_tile; ++p) {
+                    const int pg = __shfl_sync(FULL_WARP, page, p);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int hf = 0; hf < HALVES; ++hf) tma_load_4d(dst + hf * (BT_KEYS * 128) + (p << b.page_shift) * 128, &map_kv, 64 * hf, 0, plane, pg, bar);
+                    }
+                }
+                if (mend) {
+                    ok = bt_wait(landed, landed_turn, abort_sh);
+                    landed_turn ^= 1u;
+                    if (!ok) break;
+                    const int row1 = ((left >> b.page_shift) + 1) << b.page_shift;
+                    for (int i = lane; i < (row1 - left) * 8 * HALVES; i += 32) {
+                        const int row = left + i / (8 * HALVES), piece = i % (8 * HALVES);
+                        const uint32_t a = dst + (piece >> 3) * (BT_KEYS * 128) + row * 128 + (piece & 7) * 16;    // whole rows: the swizzle stays inside
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a), "r"(0) : "memory");
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(full(slot));
+                }
+                slot += 2;
+                if (slot >= S::SLOTS) { slot -= S::SLOTS; turn ^= 1u; }
             }
         }
         // After a wait that ran out: the copies still on their way must land before the block's shared memory is given back.
@@ -669,7 +674,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 }
             }
         }
-    } else {
+    } else if (warp < 8) {
         // ---------------------------------------------------------------- softmax: a thread owns one packed query row
         const int x = warp >> 2, rho = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
