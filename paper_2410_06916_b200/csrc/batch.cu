@@ -226,7 +226,7 @@ swift_status run_tc(const swift_paged_kv* kv, const BatchView& bv, const BtArgs&
     swift_status st = make_kv_map(kv, BT_KEYS, &kv_map);
     if (st == SWIFT_OK) st = make_q_map(kv, bv, g.a, g.rows_per_tile, &q_map);
     if (st != SWIFT_OK) return st;
-    const int grid = (int)(items < most ? items : most);
+    const int grid = (int)(items < most ? items : most);          // prompts: `most` does not limit, blocks take over one another's pieces
     const bool wide = kv->head_dim > 64, bf16 = kv->dtype == SWIFT_BF16;
     const cudaError_t e = g.mode == BT_PROMPT ? launch_tc_any<false>(bf16, wide, kv_map, q_map, bv, g, grid, s, after_previous)
                                               : launch_tc_any<true>(bf16, wide, kv_map, q_map, bv, g, grid, s, after_previous);
@@ -253,7 +253,7 @@ swift_status run_prompt(const swift_paged_kv* kv, const BatchView& bv, const Att
     // A pair of tiles takes little longer than one tile (each works while the other waits), so pieces are pairs unless even
     // single tiles leave no SM more than one.
     g.tiles = piece_bound(bv, av.n_kv_heads, g.rows_per_tile) <= multiprocessors() ? 1 : 2;
-    return run_tc(kv, bv, g, piece_bound(bv, av.n_kv_heads, g.tiles * g.rows_per_tile), multiprocessors(), s, false);
+    return run_tc(kv, bv, g, piece_bound(bv, av.n_kv_heads, g.tiles * g.rows_per_tile), 0x7FFFFFFF, s, false);
 }
 
 // ------------------------------------------------------------------------------ few rows per sequence

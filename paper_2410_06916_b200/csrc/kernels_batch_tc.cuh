@@ -254,6 +254,62 @@ __device__ __forceinline__ bool bt_wait(uint32_t bar, uint32_t parity, volatile 
     return bt_wait_long(bar, parity, abort_sh);
 }
 
+// ------------------------------------------------------------------------------ which piece next
+// Pieces differ in length (causal edges, ragged sequences), so whole prompts are launched one block per piece and a block that
+// is done takes over the next block not yet launched (cluster launch control): pieces go out in order, to whoever is free,
+// with the pipeline kept full.  (Dealt out in turn: 5003 ragged rows 158 us, 8192 rows 915.)  The K warp asks for the next piece
+// while the current one runs; the answer is read by every warp at its own pace from a ring of two.
+__device__ __forceinline__ void bt_ask_piece(uint32_t answer, uint32_t bar)
+{
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar) : "memory");
+}
+__device__ __forceinline__ int bt_answer(uint32_t answer)             // the block taken over, or -1: none is left
+{
+    uint32_t taken, x = 0;
+    asm volatile("{\n\t.reg .b128 h;\n\t.reg .pred p;\n\t.reg .b32 y, z, w;\n\t"
+                 "ld.shared.b128 h, [%2];\n\t"
+                 "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
+                 "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, h;\n\t}"
+                 : "=r"(taken), "=&r"(x) : "r"(answer) : "memory");
+    return taken ? (int)x : -1;
+}
+template <bool PART> struct BtPieces {
+    uint32_t answers, full, empty;                                    // two answers of 16 bytes, their barriers
+    volatile int* abort_sh;
+    int idx, n;
+    __device__ __forceinline__ void begin() { idx = blockIdx.x; n = 0; }
+    // K warp, before it starts on a piece
+    __device__ __forceinline__ bool ask()
+    {
+        if (PART) return true;
+        const uint32_t at = n & 1, turn = (n >> 1) & 1;
+        if (!bt_wait(empty + 8u * at, turn ^ 1u, abort_sh)) return false;
+        if (elect_one()) {
+            mbar_expect_tx(full + 8u * at, 16u);
+            bt_ask_piece(answers + 16u * at, full + 8u * at);
+        }
+        return true;
+    }
+    // every warp, behind a piece: false when there is none left (or a wait ran out: ok becomes false)
+    __device__ __forceinline__ bool next(bool& ok)
+    {
+        if (PART) {
+            idx += gridDim.x;
+            return true;
+        }
+        const uint32_t at = n & 1, turn = (n >> 1) & 1;
+        ok = bt_wait(full + 8u * at, turn, abort_sh);
+        if (!ok) return false;
+        idx = bt_answer(answers + 16u * at);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(empty + 8u * at);
+        ++n;
+        return idx >= 0;
+    }
+};
+
 // Bit i: key 32 q + i of a tile is shown to a row that sees the tile's keys below `seen`, and lies on a page of the pool.
 __device__ __forceinline__ unsigned bt_shown(unsigned pages, int page_shift, int seen, int q)
 {
@@ -447,7 +503,7 @@ template <typename T, int COLS> __device__ __noinline__ void bt_store_out(uint32
 }
 
 // ------------------------------------------------------------------------------ the kernel
-// grid = persistent CTAs (at most one per SM), each taking pieces blockIdx.x, + gridDim.x, ...; block = 352.
+// grid: one block per piece (PART: persistent blocks that take pieces blockIdx.x, + gridDim.x, ...); block = 352.
 // PART: leaves parts in the workspace (BT_PREFIX, BT_OWN) rather than results (BT_PROMPT).
 template <typename T, int HALVES, bool PART>
 __global__ void __launch_bounds__(BT_THREADS, 1)
@@ -474,6 +530,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
     auto p_ready = [&](int x, int h) { return b2 + 48u + 8u * (2 * x + h); };
     auto o_full = [&](int x) { return b2 + 80u + 8u * x; };
     const uint32_t landed = b2 + 96u;
+    const uint32_t piece_bars = b2 + 104u, answers = bars + S::BAR_BYTES - 32u;   // answers: 16-byte aligned
     __shared__ uint32_t tmem_base_sh;
     __shared__ int abort_flag;
     __shared__ unsigned page_bits[BT_PAGE_RING];                      // bit p: page p of that key tile lies in the pool
@@ -489,6 +546,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 mbar_init(p_ready(x, 0), 4); mbar_init(p_ready(x, 1), 4);
             }
             mbar_init(landed, 1);
+            for (int i = 0; i < 2; ++i) { mbar_init(piece_bars + 8u * i, 1); mbar_init(piece_bars + 16u + 8u * i, 11); }
             abort_flag = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -504,6 +562,9 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base_sh;
+    BtPieces<PART> pieces = {answers, piece_bars, piece_bars + 16u, abort_sh, 0, 0};
+    pieces.begin();
+    bool more_pieces = true;
     auto s_col = [&](int x) { return tmem + 128u * x; };              // S, then P, of tile x
     auto o_col = [&](int x) { return tmem + 256u + 128u * x; };
 
@@ -517,7 +578,10 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
         int tile_no = 0;
         bool ok = true;
         BtItem it;
-        for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
+        for (; ok && more_pieces; more_pieces = ok && pieces.next(ok)) {
+            if (kv == 0) ok = pieces.ask();
+            if (!ok) break;
+            if (!bt_locate(b, g, pieces.idx, it)) { if (PART) break; continue; }
             const int n_tiles = max(it.tiles[0], it.tiles[1]);
             const int plane = (g.block * 2 + kv) * g.a.n_kv_heads + it.kvh;
             if (kv == 0) {
@@ -599,7 +663,8 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
         uint32_t slot = 0, turn = 0, q_turn[2] = {0, 0}, p_turn[2] = {0, 0};
         bool ok = true;
         BtItem it;
-        for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
+        for (; ok && more_pieces; more_pieces = ok && pieces.next(ok)) {
+            if (!bt_locate(b, g, pieces.idx, it)) { if (PART) break; continue; }
             const int n_tiles = max(it.tiles[0], it.tiles[1]);
             auto commit = [&](uint32_t bar) { if (elect_one()) tc_commit(bar); };
             auto scores = [&](int x, uint32_t k_sh) {                 // S(x) = Q(x) K^T
@@ -686,7 +751,8 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
         int tile_no = 0;
         bool ok = true;
         BtItem it;
-        for (int idx = blockIdx.x; ok && bt_locate(b, g, idx, it); idx += gridDim.x) {
+        for (; ok && more_pieces; more_pieces = ok && pieces.next(ok)) {
+            if (!bt_locate(b, g, pieces.idx, it)) { if (PART) break; continue; }
             const int n_tiles = max(it.tiles[0], it.tiles[1]), mine = it.tiles[x];
             const int t = it.t0 + x * TQ + tok;                       // token within the sequence
             const bool live = x < g.tiles && tok < TQ && t < it.n && (g.mode == BT_PREFIX || t < g.a.max_rows);
