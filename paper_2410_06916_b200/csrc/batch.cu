@@ -295,16 +295,19 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
             const double own_bytes = 0.6 * bv.n_seqs * bv.max_len * Hk * kv->head_dim * 4.0;
             const int own_mt = own <= 16 ? 1 : own <= 32 ? 2 : 4;
             double best = 0;
-            for (int g = p->few ? sms / 6 : sms; g <= sms; g += sms / 37 > 0 ? sms / 37 : 1) {
-                const int rest = g == sms ? sms : sms - g;
+            for (int share = 2; share <= 12; ++share) {               // twelfths of the SMs
+                const int g = sms * share / 12, rest = g == sms ? sms : sms - g;
+                if (!p->few && g < sms) continue;
                 const double stream_us = own_bytes / (rest * 44e3 < 6e6 ? rest * 44e3 : 6e6), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * (BD_WARPS / own_mt));
                 const double own_us = p->few ? 3.0 + (stream_us > item_us ? stream_us : item_us) : 0.0;
-                for (int c = 1; c <= 64 && c <= tiles; ++c) {
+                for (int waves = 1; waves <= 4; ++waves) {            // as many cuts as fill that many waves
+                    long long c = (long long)waves * g / pairs;
+                    c = c < 1 ? 1 : c > tiles ? tiles : c > 64 ? 64 : c;
                     const double pre_us = ceil_div(pairs * c, g) * (ceil_div(tiles, c) * 1.75 + 8.0);
-                    const double cost = (g == sms ? pre_us + own_us : pre_us > own_us ? pre_us : own_us) + c;         // every cut is read again by the join
+                    const double cost = (g == sms ? pre_us + own_us : pre_us > own_us ? pre_us : own_us) + c;    // every cut is read again by the join
                     if (p->splits == 0 || cost < best) {
                         best = cost;
-                        p->splits = c;
+                        p->splits = (int)c;
                         p->pre_grid = g;
                     }
                 }
