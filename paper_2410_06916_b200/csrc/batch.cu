@@ -102,7 +102,7 @@ swift_status check_attention(const swift_paged_kv* kv, const swift_row_batch* b,
     if (a->block < 0 || a->block >= kv->n_blocks) return fail_batch(SWIFT_EINVAL, "block %d outside 0..%d", a->block, kv->n_blocks - 1);
     if (a->n_heads < 1 || a->n_heads > MAX_HEADS || a->n_heads % kv->n_kv_heads)
         return fail_batch(SWIFT_EINVAL, "n_heads %d is not a multiple of the cache's %d (at most %d)", a->n_heads, kv->n_kv_heads, MAX_HEADS);
-    if (!(a->scale > 0.f) || std::isinf(a->scale)) return fail_batch(SWIFT_EINVAL, "scale must be positive and finite");
+    if (!(a->scale > 0.f) || !std::isfinite(a->scale * 2.f)) return fail_batch(SWIFT_EINVAL, "scale must be positive and below 2^127");
     if (b->n_rows > 0) {
         const int es = type_size(kv->dtype);
         if (!a->q.ptr || !a->out) return fail_batch(SWIFT_EINVAL, "null q or out");
