@@ -86,7 +86,7 @@ swift_status check_batch(const swift_paged_kv* kv, const swift_row_batch* b, Bat
     return SWIFT_OK;
 }
 
-// what the tensor-core kernels take; the rest runs row by row
+// what the tensor-core kernels take; the rest is computed in fp32 arithmetic
 inline bool tensor_core_shape(const swift_paged_kv* kv) { return kv->dtype != SWIFT_F32 && kv->head_dim % 8 == 0 && kv->head_dim <= 128; }
 inline long long kv_elems(const swift_paged_kv* kv) { return (long long)kv->n_kv_heads * kv->page_size * kv->head_dim; }
 inline const char* block_base(const swift_paged_kv* kv, int block)
@@ -259,7 +259,7 @@ swift_status run_prompt(const swift_paged_kv* kv, const BatchView& bv, const Att
 // ------------------------------------------------------------------------------ few rows per sequence
 // How swift_prefix_attention runs a batch, from sizes the host knows.
 struct PrefixPlan {
-    bool rows;                  // row by row: no tensor-core form
+    bool rows;                  // fp32 arithmetic: no tensor-core form
     bool prompt;                // each sequence by itself, no prefix to share and too many rows for the few-row kernel
     bool few, prefix_few;       // the few-row kernel takes the sequences' own parts; and the prefix
     int group, dp, mt, grid, pre_grid;   // grid: CTAs of the few-row kernel; pre_grid: of the prefix's
@@ -428,13 +428,22 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
     return SWIFT_OK;
 }
 
+template <typename T> cudaError_t launch_fp32(const BatchView& bv, const AttnView& av, cudaStream_t s)
+{
+    static std::atomic<unsigned long long> done{0};
+    const cudaError_t e = allow_smem(attn_fp32_kernel<T>, af_smem_bytes(256), done);
+    if (e != cudaSuccess) return e;
+    const long long group = av.n_heads / av.n_kv_heads, some = bv.n_seqs < bv.n_rows ? bv.n_seqs : bv.n_rows;
+    const long long pieces = (bv.n_rows * group / AF_ROWS + some) * av.n_kv_heads;         // at most
+    if (pieces > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+    return launch(attn_fp32_kernel<T>, dim3((unsigned)pieces), 128, af_smem_bytes(av.head_dim), s, false, bv, av);
+}
 cudaError_t launch_rows(const swift_paged_kv* kv, const BatchView& bv, const AttnView& av, cudaStream_t s)
 {
-    const dim3 grid(bv.n_rows, ceil_div(av.n_heads, 4));
     switch (kv->dtype) {
-    case SWIFT_F32: return launch(attn_rows_kernel<float>, grid, 128, 0, s, false, bv, av);
-    case SWIFT_BF16: return launch(attn_rows_kernel<__nv_bfloat16>, grid, 128, 0, s, false, bv, av);
-    default: return launch(attn_rows_kernel<__half>, grid, 128, 0, s, false, bv, av);
+    case SWIFT_F32: return launch_fp32<float>(bv, av, s);
+    case SWIFT_BF16: return launch_fp32<__nv_bfloat16>(bv, av, s);
+    default: return launch_fp32<__half>(bv, av, s);
     }
 }
 

@@ -1,6 +1,6 @@
 // Batches of sequences over one paged cache: the shared row and page arithmetic, the rotary table, the pass between a
-// layer's projection and its attention (norm + rotation + append), and attention row by row for the types and head sizes
-// the tensor-core kernels next door do not take.
+// layer's projection and its attention (norm + rotation + append), and attention in fp32 arithmetic for the types and head
+// sizes the tensor-core kernels next door do not take.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(AP_THREADS) append_any_kernel(BatchView b, App
     }
 }
 
-// ------------------------------------------------------------------------------ attention, row by row
+// ------------------------------------------------------------------------------ attention in fp32 arithmetic
 struct AttnView {
     const void* q;
     long long q_row_stride, q_head_stride;
@@ -376,64 +376,153 @@ struct AttnView {
     float scale;
 };
 
-// One warp per (row, query head), any type and head size: 32 positions at a time, a lane computes one position's score
-// (q from shared memory, K from the cache in order), the running maximum and sum are joined across lanes, and the
-// weighted sum of V runs with lanes over dims.  fp32 throughout.  grid = (rows, ceil(n_heads / 4)), block = 128.
+// Any type and head size: fp32 caches, whose products the matrix instructions would round, and the sizes the tensor-core
+// kernels do not take.  A block takes 16 query rows of a kv head (tokens x heads of the group, so that a group shares its
+// keys) and goes through the keys 32 at a time, widened to fp32 in shared memory.  Eight threads share a row's scores and
+// its running maximum and sum; the weighted sum of V runs with lanes over dims, four rows per warp.  Bound by shared-memory
+// loads (about one per two multiply-adds).  grid = pieces, block = 128, dynamic smem = af_smem_bytes(head_dim).
+constexpr int AF_ROWS = 16, AF_KEYS = 32;
+__host__ __device__ inline int af_stride(int head_dim) { return (head_dim + 3) / 4 * 4 + 4; }   // floats per staged row: 16-byte loads of eight rows fall into different banks
+__host__ __device__ inline int af_smem_bytes(int head_dim) { return ((AF_ROWS + 2 * AF_KEYS) * af_stride(head_dim) + AF_ROWS * (AF_KEYS + 1)) * 4 + AF_KEYS * 8; }
+
 template <typename T>
-__global__ void __launch_bounds__(128) attn_rows_kernel(BatchView b, AttnView a)
+__global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
 {
-    __shared__ float q_sh[4][256];
-    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y * 4 + warp;
-    if (h >= a.n_heads) return;
-    SeqSpan sp;
-    const int seq = find_seq(b, row, sp);
-    if (seq < 0 || row - sp.r0 >= a.max_rows) return;
-    const int D = a.head_dim, kvh = h / (a.n_heads / a.n_kv_heads);
-    const T* q = reinterpret_cast<const T*>(a.q) + row * a.q_row_stride + h * a.q_head_stride;
-    for (int d = lane; d < D; d += 32) q_sh[warp][d] = to_float(q[d]) * a.scale;
-    __syncwarp();
-    const int own = max(0, sp.len - sp.n + (row - sp.r0) + 1), total = b.prefix_len + own;    // visible positions
-    const T* head = reinterpret_cast<const T*>(a.pool) + (size_t)kvh * b.page_size * D;
-    float m = -INFINITY, l = 0.f, o[8];
+    extern __shared__ __align__(16) float af_smem[];
+    const int D = a.head_dim, ld = af_stride(D), G = a.n_heads / a.n_kv_heads, Hk = a.n_kv_heads, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    float* q_sh = af_smem;
+    float* k_sh = q_sh + AF_ROWS * ld;
+    float* v_sh = k_sh + AF_KEYS * ld;
+    float* p_sh = v_sh + AF_KEYS * ld;                    // [row][AF_KEYS + 1]
+    long long* at_sh = reinterpret_cast<long long*>(af_smem + (AF_ROWS + 2 * AF_KEYS) * ld + AF_ROWS * (AF_KEYS + 1));   // element offset of each key's K, -1: nothing there
+    // ---- this block's piece
+    int idx = blockIdx.x, seq = -1;
+    SeqSpan sp = {0, 0, 0};
+    for (int base = 0; base < b.n_seqs && seq < 0; base += 32) {
+        SeqSpan mine = {0, 0, 0};
+        if (base + lane < b.n_seqs) mine = seq_span(b, base + lane);
+        const int pieces = (mine.n * G + AF_ROWS - 1) / AF_ROWS * Hk;
+        int upto = pieces;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = 0.f;
-    for (int p0 = 0; p0 < total; p0 += 32) {
-        const int p = p0 + lane;
-        long long at = -1;                                // element offset of the position's K, -1: nothing there
-        if (p < total) {
-            const int own_p = p - b.prefix_len, pp = own_p < 0 ? p : own_p;
-            const int page = own_p < 0 ? b.prefix_pages[pp >> b.page_shift] : b.page_table[(size_t)seq * b.table_stride + (pp >> b.page_shift)];
-            if ((unsigned)page < (unsigned)b.n_pages) at = (long long)page * a.page_elems + (long long)(pp & (b.page_size - 1)) * D;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(FULL_WARP, upto, o);
+            if (lane >= o) upto += v;
         }
-        float s = -INFINITY;
-        if (at >= 0) {
-            const T* k = head + at;
-            s = 0.f;
-            for (int d = 0; d < D; ++d) s = fmaf(q_sh[warp][d], to_float(k[d]), s);
+        const unsigned m = __ballot_sync(FULL_WARP, idx < upto);
+        if (m == 0) {
+            idx -= __shfl_sync(FULL_WARP, upto, 31);
+            continue;
         }
-        if (!__any_sync(FULL_WARP, at >= 0)) continue;    // nothing here
-        const float m_new = fmaxf(m, warp_max(s));
-        const float shrink = expf(m - m_new), e_s = at >= 0 ? expf(s - m_new) : 0.f;
-        l = l * shrink + warp_sum(e_s);
-        m = m_new;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] *= shrink;
-        const int n = min(32, total - p0);
-        for (int j = 0; j < n; ++j) {
-            const float pj = __shfl_sync(FULL_WARP, e_s, j);
-            const long long aj = __shfl_sync(FULL_WARP, at, j);
-            if (aj < 0) continue;
-            const T* v = head + aj + a.kv_elems;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (lane + 32 * e < D) o[e] = fmaf(pj, to_float(v[lane + 32 * e]), o[e]);
-        }
+        const int at = __ffs(m) - 1;
+        idx -= __shfl_sync(FULL_WARP, upto - pieces, at);
+        seq = base + at;
+        sp = {__shfl_sync(FULL_WARP, mine.r0, at), __shfl_sync(FULL_WARP, mine.n, at), __shfl_sync(FULL_WARP, mine.len, at)};
     }
-    T* out = reinterpret_cast<T*>(a.out) + ((size_t)row * a.n_heads + h) * D;
-    const float inv = l == 0.f ? 0.f : 1.f / l;           // 0: the row sees nothing
+    if (seq < 0) return;                                  // the same for the whole block
+    const int kvh = idx % Hk, rho0 = idx / Hk * AF_ROWS, rows = min(AF_ROWS, sp.n * G - rho0);
+    const T* head = reinterpret_cast<const T*>(a.pool) + (size_t)kvh * b.page_size * D;
+    // ---- queries, scaled; dead rows and the dims behind the last are zero
+    for (int i = tid; i < AF_ROWS * ld; i += 128) {
+        const int r = i / ld, d = i - r * ld, tok = (rho0 + r) / G;
+        float v = 0.f;
+        if (r < rows && d < D)
+            v = to_float(reinterpret_cast<const T*>(a.q)[(long long)(sp.r0 + tok) * a.q_row_stride + (long long)(kvh * G + rho0 + r - tok * G) * a.q_head_stride + d]) * a.scale;
+        q_sh[i] = v;
+    }
+    for (int i = tid; i < 2 * AF_KEYS * (ld - D); i += 128) k_sh[i / (ld - D) * ld + D + i % (ld - D)] = 0.f;
+    const int row = tid >> 3, sub = tid & 7;              // this thread's row of scores; rows 4 warp .. + 3 are the warp's
+    const int tok = min(rho0 + row, sp.n * G - 1) / G, seen = b.prefix_len + max(0, sp.len - sp.n + tok + 1);
+    const int last = min(rho0 + rows - 1, sp.n * G - 1) / G, total = b.prefix_len + max(0, sp.len - sp.n + last + 1);   // what the last row sees
+    float m = -INFINITY, l = 0.f, o[4][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (lane + 32 * e < D) store_val(out + lane + 32 * e, o[e] * inv);
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[r][e] = 0.f;
+    for (int p0 = 0; p0 < total; p0 += AF_KEYS) {
+        __syncthreads();                                  // the tile before is used up
+        if (tid < AF_KEYS) {
+            long long at = -1;
+            const int p = p0 + tid, own = p - b.prefix_len, pp = own < 0 ? p : own;
+            if (p < total) {
+                const int page = own < 0 ? b.prefix_pages[pp >> b.page_shift] : b.page_table[(size_t)seq * b.table_stride + (pp >> b.page_shift)];
+                if ((unsigned)page < (unsigned)b.n_pages) at = (long long)page * a.page_elems + (long long)(pp & (b.page_size - 1)) * D;
+            }
+            at_sh[tid] = at;
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int i = tid; i < AF_KEYS * D; i += 128) {
+            const int j = i / D, d = i - j * D;
+            const long long at = at_sh[j];
+            k_sh[j * ld + d] = at >= 0 ? to_float(head[at + d]) : 0.f;
+            v_sh[j * ld + d] = at >= 0 ? to_float(head[at + a.kv_elems + d]) : 0.f;
+        }
+        __syncthreads();
+        float s[4] = {0.f, 0.f, 0.f, 0.f};                // keys sub, sub + 8, sub + 16, sub + 24
+        const float4* qr = reinterpret_cast<const float4*>(q_sh + row * ld);
+        for (int d = 0; d < (D + 3) / 4; ++d) {
+            const float4 x = qr[d];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 y = reinterpret_cast<const float4*>(k_sh + (sub + 8 * i) * ld)[d];
+                s[i] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[i]))));
+            }
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = sub + 8 * i;
+            if (p0 + j >= seen || at_sh[j] < 0) s[i] = -INFINITY;
+            top = fmaxf(top, s[i]);
+        }
+#pragma unroll
+        for (int x = 4; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_WARP, top, x));
+        const float shrink = m == top ? 1.f : expf(m - top), from = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float e = expf(s[i] - from);
+            p_sh[row * (AF_KEYS + 1) + sub + 8 * i] = e;
+            sum += e;
+        }
+#pragma unroll
+        for (int x = 4; x > 0; x >>= 1) sum += __shfl_xor_sync(FULL_WARP, sum, x);
+        l = l * shrink + sum;
+        m = top;
+        __syncwarp();
+        float f[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            f[r] = __shfl_sync(FULL_WARP, shrink, 8 * r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[r][e] *= f[r];
+        }
+        const int n = min(AF_KEYS, total - p0);
+        for (int j = 0; j < n; ++j) {
+            float pj[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) pj[r] = p_sh[(4 * warp + r) * (AF_KEYS + 1) + j];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (32 * e >= D) break;
+                const float v = lane + 32 * e < D ? v_sh[j * ld + lane + 32 * e] : 0.f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r][e] = fmaf(pj[r], v, o[r][e]);
+            }
+        }
+        __syncwarp();
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float sum = __shfl_sync(FULL_WARP, l, 8 * r);
+        const int rr = 4 * warp + r, t = (rho0 + rr) / G;
+        if (rr >= rows || t >= a.max_rows) continue;
+        T* out = reinterpret_cast<T*>(a.out) + ((size_t)(sp.r0 + t) * a.n_heads + kvh * G + rho0 + rr - t * G) * D;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;   // 0: the row sees nothing
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (lane + 32 * e < D) store_val(out + lane + 32 * e, o[r][e] * inv);
+    }
 }
 
 } // namespace swk

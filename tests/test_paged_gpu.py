@@ -344,6 +344,37 @@ def test_a_cache_beyond_32_bit_offsets():
     assert torch.equal(pool[int(where[int(small.page_table[0, pos // page])]), 15, 0, :, pos % page], k[2])
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(128, 1), (65, 1), (160, 1), (100, 2)])
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_large_groups(heads, kv_heads, dt):
+    b = Batch([5, 2], [70, 200], heads, kv_heads, 64, 16, dt, prefix_len=40)
+    pool, batch = setup(b)
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    close(batch.prompt_attention(0, b.q.cuda()), want, tol)
+    close(batch.prefix_attention(0, b.q.cuda()), want, tol)
+
+
+def test_as_many_sequences_as_a_batch_takes():
+    n = 4096
+    b = Batch([1 if i % 3 else 0 for i in range(n)], [1 + i % 40 for i in range(n)], 4, 2, 64, 8, BF16, prefix_len=9, poison=False)
+    pool, batch = setup(b)
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    close(batch.prompt_attention(0, b.q.cuda()), want, tol)
+    close(batch.prefix_attention(0, b.q.cuda()), want, tol)
+
+
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+def test_broadcast_queries(form):
+    """Strides of zero: one head's or one row's queries for all."""
+    for pick in (lambda q: q[:, :1], lambda q: q[:1]):
+        b = Batch([40, 3], [50, 60], 8, 2, 128, 16, BF16, prefix_len=30)
+        one = pick(b.q).clone()
+        b.q[:] = one
+        pool, batch = setup(b)
+        want, tol = attention(b, b.pool, b.q, dev="cuda")
+        close((batch.prompt_attention if form == "prompt" else batch.prefix_attention)(0, one.cuda().expand(43, 8, 128)), want, tol)
+
+
 # ----------------------------------------------------------------------------------------------- as a program uses them
 def step_reference(pool, rows, spans, table, prefix_pages, prefix_len, freq, gains, D, H, Hk, page, dtype):
     """One layer's append + attention in 64 bits on a host pool; q, K and V rounded to the cache's type as the cache holds them."""
@@ -474,6 +505,56 @@ def test_captured_steps_follow_their_tensors(rows, dt):
                 assert torch.isfinite(w).all(), (turn, name, (~torch.isfinite(w)).nonzero()[:5].tolist())
                 assert torch.equal(o, w), (turn, name, (o != w).nonzero()[:5].tolist(), float((o - w).abs().max()))
             assert torch.equal(torch.nan_to_num(pool, nan=-1.0), torch.nan_to_num(want[3], nan=-1.0))
+
+
+def test_a_process_may_capture_its_first_calls():
+    """No warm-up: kernels, attributes and tensor maps are set up inside the capture."""
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = """
+import sys
+sys.path[:0] = [%r, %r]
+import torch
+from paged_reference import Batch, attention
+from test_paged_gpu import close, setup
+from paper_2410_06916_b200 import rope_table
+b = Batch([40, 3], [50, 60], 8, 2, 128, 16, torch.bfloat16, prefix_len=300)
+pool, batch = setup(b)
+want, tol = attention(b, b.pool, b.q, dev="cuda")
+q = b.q.cuda()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    t, x, y = rope_table(400, 128), batch.prompt_attention(0, q), batch.prefix_attention(0, q)
+g.replay()
+torch.cuda.synchronize()
+close(x, want, tol)
+close(y, want, tol)
+print("fine")
+""" % (here, os.path.dirname(here))
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "fine" in done.stdout, done.stderr[-2000:]
+
+
+def test_calls_side_by_side_on_two_streams():
+    """Eager calls of two batches on two streams at once: nothing is shared but the code."""
+    made = []
+    for seed in range(2):
+        b = Batch([600, 33, 1], [700, 500, 900], 16, 4, 128, 16, BF16, prefix_len=200, seed=seed)
+        pool, batch = setup(b)
+        q = b.q.cuda()
+        made.append((pool, batch, q, batch.prompt_attention(0, q), batch.prefix_attention(0, q), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for j, (_, batch, q, _, _, s) in enumerate(made):
+            got[j] += [(batch.prompt_attention(0, q, stream=s), batch.prefix_attention(0, q, stream=s))]
+    torch.cuda.synchronize()
+    for j, (_, _, _, p, x, _) in enumerate(made):
+        for a, c in got[j]:
+            assert torch.equal(a, p) and torch.equal(c, x)
 
 
 def test_calls_on_a_given_stream_and_sync():
