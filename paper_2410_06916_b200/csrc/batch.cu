@@ -260,7 +260,7 @@ swift_status run_prompt(const swift_paged_kv* kv, const BatchView& bv, const Att
 // How swift_prefix_attention runs a batch, from sizes the host knows.
 struct PrefixPlan {
     bool rows;                  // fp32 arithmetic: no tensor-core form
-    bool prompt;                // each sequence by itself, no prefix to share and too many rows for the few-row kernel
+    bool prompt;                // too many rows for the few-row kernel, and no prefix or none worth sharing: each sequence by itself
     bool few, prefix_few;       // the few-row kernel takes the sequences' own parts; and the prefix
     int group, dp, mt, grid, pre_grid;   // grid: CTAs of the few-row kernel; pre_grid: of the prefix's
     long long items;
@@ -282,7 +282,10 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
     if (!p->rows) {
         const long long own = (long long)max_rows * p->group, all = (long long)bv.n_rows * p->group;
         p->few = own <= BD_MAX_ROWS;
-        p->prefix_few = p->few && bv.prefix_len > 0 && all <= BD_MAX_ROWS;
+        p->mt = own <= 16 ? 1 : own <= 32 ? 2 : 4;
+        // the prefix too, if the rows of all sequences fit the same tile (a larger tile for the prefix alone slows the own parts: 10
+        // sequences x 5 rows, 40 heads: 43 us against 27 with the many-row kernel beside it)
+        p->prefix_few = p->few && bv.prefix_len > 0 && all <= 16 * p->mt;
         p->prompt = !p->few && bv.prefix_len == 0;
         if (bv.prefix_len > 0 && !p->prefix_few && !p->prompt) {
             // The prefix is tensor work, the sequences' own parts are HBM work: both kernels run at once, on SMs of their own, and
@@ -293,12 +296,11 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
             const int tiles = ceil_div(bv.prefix_len, BT_KEYS), TQ = BT_ROWS / p->group;
             const long long pairs = (long long)ceil_div(bv.n_rows, 2 * TQ) * Hk;
             const double own_bytes = 0.6 * bv.n_seqs * bv.max_len * Hk * kv->head_dim * 4.0;
-            const int own_mt = own <= 16 ? 1 : own <= 32 ? 2 : 4;
             double best = 0;
             for (int share = 2; share <= 12; ++share) {               // twelfths of the SMs
                 const int g = sms * share / 12, rest = g == sms ? sms : sms - g;
                 if (!p->few && g < sms) continue;
-                const double stream_us = own_bytes / (rest * 44e3 < 6e6 ? rest * 44e3 : 6e6), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * (BD_WARPS / own_mt));
+                const double stream_us = own_bytes / (rest * 44e3 < 6e6 ? rest * 44e3 : 6e6), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * (BD_WARPS / p->mt));
                 const double own_us = p->few ? 3.0 + (stream_us > item_us ? stream_us : item_us) : 0.0;
                 for (int waves = 1; waves <= 4; ++waves) {            // as many cuts as fill that many waves
                     long long c = (long long)waves * g / pairs;
@@ -313,13 +315,24 @@ swift_status plan_prefix(const swift_paged_kv* kv, const BatchView& bv, int n_he
                 }
             }
         }
+        if (!p->few && !p->prompt) {
+            // Rows that fill tiles anyway gain nothing from a shared prefix but a better split over the SMs, and pay for writing and
+            // joining parts: by the same costs, whichever form ends earlier.
+            const int TQ2 = 2 * (BT_ROWS / p->group), own_tiles = ceil_div((long long)(0.6 * bv.max_len), BT_KEYS), tiles = ceil_div(bv.prefix_len, BT_KEYS);
+            const long long seqs = bv.n_seqs < bv.n_rows ? bv.n_seqs : bv.n_rows, own_pieces = seqs * ceil_div(max_rows, TQ2) * Hk;
+            const double one = ceil_div(own_pieces, sms) * ((tiles + own_tiles) * 1.75 + 8.0);
+            const double shared = ceil_div((long long)ceil_div(bv.n_rows, TQ2) * Hk * p->splits, sms) * (ceil_div(tiles, p->splits) * 1.75 + 8.0) +
+                                  ceil_div(own_pieces, sms) * (own_tiles * 1.75 + 8.0) + 5.0 + (double)bv.n_rows * n_heads * (p->splits + 1.5) * p->dp * 4 / 5e6;
+            if (one < shared) {
+                p->prompt = true;
+                p->splits = 0;
+            }
+        }
         p->slots = p->splits + (!p->few && !p->prompt ? 1 : 0);
         const size_t many = (size_t)p->slots * bv.n_rows * n_heads;
         p->many_o = take(many * p->dp * 4);
         p->many_ml = take(many * 8);
         if (p->few) {
-            const long long rows = p->prefix_few ? (all > own ? all : own) : own;
-            p->mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
             p->items = (long long)(bv.n_seqs + (p->prefix_few ? 1 : 0)) * Hk;
             p->grid = p->splits > 0 && p->pre_grid < sms ? sms - p->pre_grid : sms;
             const int keys = 16 * p->mt;

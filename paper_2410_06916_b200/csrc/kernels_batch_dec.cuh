@@ -464,7 +464,7 @@ struct BjKind {                                           // one kind of parts: 
 // are for few rows, whose items are cut into many parts (one row, 64 heads, 148 parts each).
 // grid = (rows, ceil(heads / (8 / WARPS))), block = 256.
 template <typename T, int WARPS>
-__global__ void __launch_bounds__(256) attn_join_kernel(BatchView b, BjArgs g)
+__global__ void __launch_bounds__(256, WARPS == 1 ? 4 : 3) attn_join_kernel(BatchView b, BjArgs g)
 {
     constexpr int BJ_PARTS = WARPS == 1 ? 4 : 8;          // parts whose sums and maxima are fetched at once
     pdl_wait();
