@@ -448,8 +448,9 @@ swift_status swift_kv_append(const swift_paged_kv* kv, const swift_row_batch* ba
  *
  * swift_prompt_attention takes each sequence by itself: prompts, chunks of prompts, any number of rows.
  * swift_prefix_attention is for few rows per sequence (decoding steps, verification, scoring windows): the scores against
- * the prefix are computed once for the rows of all sequences together and joined with each sequence's own part.  max_rows
- * bounds the rows of one sequence; rows beyond it are left out.  Both compute the same function.
+ * the prefix are computed once for the rows of all sequences together and joined with each sequence's own part (sequences
+ * with enough rows to fill tiles are taken by themselves where that ends earlier).  max_rows bounds the rows of one
+ * sequence; rows beyond it are left out.  Both compute the same function.
  * 16-bit caches with head_dim a multiple of 8 up to 128 run on the tensor cores; fp32 caches and other head sizes are
  * computed in fp32 arithmetic by either call, each sequence by itself.
  * workspace: device memory of at least swift_prefix_workspace_bytes (0 on invalid arguments), 256-byte aligned,

@@ -180,7 +180,7 @@ class RowBatch:
         self._c = _Batch(n_seqs, n_rows, row_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), page_table.shape[1],
                          prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len)
         self._kv_p, self._c_p = C.byref(kv._c), C.byref(self._c)
-        self._lib, self._types, self._scale = lib(), (kv.dtype,), kv.head_dim ** -0.5
+        self._lib, self._types, self._x_types, self._scale = lib(), (kv.dtype,), (kv.dtype, torch.float32), kv.head_dim ** -0.5
         self._ws_bytes = {}
 
     # ------------------------------------------------------------------ checks shared by the calls
@@ -198,6 +198,12 @@ class RowBatch:
             raise ValueError(f"the dims of {name} must be contiguous")
         # a stride over a single row or head means nothing
         return _Rows(t.data_ptr(), row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2])
+
+    def _gain(self, name: str, g: torch.Tensor) -> int:
+        _cuda_tensor(name, g, self.kv.device)
+        if g.dtype != torch.float32 or g.shape != (self.kv.head_dim,) or not g.is_contiguous():
+            raise ValueError(f"{name} must be contiguous float32 [{self.kv.head_dim}]")
+        return g.data_ptr()
 
     def _out(self, out: Optional[torch.Tensor], heads: int) -> torch.Tensor:
         kv = self.kv
@@ -219,27 +225,25 @@ class RowBatch:
         views (slices of a fused projection), fp32 or the cache's type.  Rows left out (padding, pages or positions out of
         range) keep what `out` held.  positions: int32 [n_rows], instead of prefix_len + own position."""
         kv = self.kv
-        types = (kv.dtype, torch.float32)
-        a = _Append()
-        a.q, a.k, a.v = self._rows("q", q, None, types), self._rows("k", k, kv.n_kv_heads, types), self._rows("v", v, kv.n_kv_heads, types)
+        heads = kv.n_kv_heads
+        rows = (self._rows("q", q, None, self._x_types), self._rows("k", k, heads, self._x_types), self._rows("v", v, heads, self._x_types))
         if q.dtype != k.dtype or q.dtype != v.dtype:
             raise TypeError("q, k and v must have one type")
-        a.block, a.n_heads, a.x_dtype, a.eps, a.interleaved = block, q.shape[1], _TYPES[q.dtype], eps, 1 if interleaved else 0
-        for name, g in (("q_gain", q_gain), ("k_gain", k_gain)):
-            if g is not None:
-                _cuda_tensor(name, g, kv.device)
-                if g.dtype != torch.float32 or tuple(g.shape) != (kv.head_dim,) or not g.is_contiguous():
-                    raise ValueError(f"{name} must be contiguous float32 [{kv.head_dim}]")
-                setattr(a, name, g.data_ptr())
+        q_gain_p = None if q_gain is None else self._gain("q_gain", q_gain)
+        k_gain_p = None if k_gain is None else self._gain("k_gain", k_gain)
+        rope_p, rope_rows, pairs = None, 0, 0
         if rope is not None:
             _cuda_tensor("rope", rope, kv.device)
-            if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or 2 * rope.shape[1] > kv.head_dim:
+            shape = rope.shape
+            if rope.dtype != torch.float32 or len(shape) != 3 or shape[2] != 2 or not rope.is_contiguous() or 2 * shape[1] > kv.head_dim:
                 raise ValueError("rope must be a rope_table of at most head_dim dims")
-            a.rope, a.rope_positions, a.rotary_dim = rope.data_ptr(), rope.shape[0], 2 * rope.shape[1]
+            rope_p, rope_rows, pairs = rope.data_ptr(), shape[0], shape[1]
+        positions_p = None
         if positions is not None:
             if tuple(_int32("positions", positions, kv.device).shape) != (self.n_rows,):
                 raise ValueError(f"positions must be [{self.n_rows}]")
-            a.positions = positions.data_ptr()
+            positions_p = positions.data_ptr()
+        a = _Append(block, q.shape[1], _TYPES[q.dtype], *rows, q_gain_p, k_gain_p, eps, rope_p, rope_rows, 2 * pairs, 1 if interleaved else 0, positions_p, None)
         return _on(kv.device, stream, self._append, a, out)
 
     def _append(self, s: int, a: _Append, out: Optional[torch.Tensor]) -> torch.Tensor:
