@@ -344,6 +344,26 @@ def test_a_cache_beyond_32_bit_offsets():
     assert torch.equal(pool[int(where[int(small.page_table[0, pos // page])]), 15, 0, :, pos % page], k[2])
 
 
+@pytest.mark.parametrize("dim,dt", [(128, BF16), (128, F16), (64, BF16), (64, F16), (96, BF16)])
+@pytest.mark.parametrize("n,kv,heads,kv_heads,prefix,parts", [
+    ([2, 1, 2], [300, 40, 900], 8, 2, 0, True),             # own parts only
+    ([1, 1], [300, 40], 8, 2, 500, True),                   # few rows: the prefix beside them in the same kernel
+    ([3] * 12, [300] * 12, 8, 2, 900, True),                # the prefix by the many-row kernel, own parts by the few-row kernel
+    ([7] * 5, [100, 7, 300, 64, 900], 16, 2, 2000, True),   # the same at 56 packed rows
+    ([24, 40], [1500, 40], 8, 1, 20000, True),              # both by the many-row kernel
+    ([200, 190], [200, 300], 8, 1, 130, False),             # each sequence by itself
+], ids=["own", "few", "beside", "beside56", "many", "alone"])
+def test_every_form_of_the_prefix_call(dim, dt, n, kv, heads, kv_heads, prefix, parts):
+    """The forms a batch's sizes can select; those that leave parts to be joined need a workspace that holds them."""
+    import ctypes
+    b = Batch(n, kv, heads, kv_heads, dim, 32, dt, prefix_len=prefix, padding=1)
+    pool, batch = setup(b)
+    need = batch._lib.swift_prefix_workspace_bytes(ctypes.byref(batch.kv._c), ctypes.byref(batch._c), heads, batch.max_rows)
+    assert (need > 4096) == parts, need
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    close(batch.prefix_attention(0, b.q.cuda())[:b.start[-1]], want[:b.start[-1]], tol[:b.start[-1]])
+
+
 @pytest.mark.parametrize("heads,kv_heads", [(128, 1), (65, 1), (160, 1), (100, 2)])
 @pytest.mark.parametrize("dt", [BF16, F32])
 def test_large_groups(heads, kv_heads, dt):
