@@ -38,7 +38,8 @@ constexpr int BT_THREADS = 352;     // 2 x 4 softmax warps, a TMA warp for Q and
 constexpr int BT_KEYS = 128;        // keys per tile
 constexpr int BT_ROWS = 128;        // packed query rows per tile
 constexpr int BT_PAGE_RING = 16;    // page-validity words kept (more than the key tiles ever in flight)
-constexpr unsigned BT_POLY = 0x1111u;   // pairs of every 16 whose exponentials are polynomials: 4 of 16
+// Pairs of every 16 whose exponentials are polynomials: 4 of 16 (8192 tokens: 909 us; 2 of 16 922, 5 of 16 920, none 2 % more).
+constexpr unsigned BT_POLY = 0x1111u;
 constexpr float BT_GROW = 8.f;      // growth of the maximum (in powers of two) that triggers a rescaling
 
 enum { BT_PROMPT = 0, BT_PREFIX = 1, BT_OWN = 2 };
@@ -257,8 +258,10 @@ __device__ __forceinline__ bool bt_wait(uint32_t bar, uint32_t parity, volatile 
 // ------------------------------------------------------------------------------ which piece next
 // Pieces differ in length (causal edges, ragged sequences), so whole prompts are launched one block per piece and a block that
 // is done takes over the next block not yet launched (cluster launch control): pieces go out in order, to whoever is free,
-// with the pipeline kept full.  (Dealt out in turn: 5003 ragged rows 158 us, 8192 rows 915.)  The K warp asks for the next piece
-// while the current one runs; the answer is read by every warp at its own pace from a ring of two.
+// with the pipeline kept full.  (Dealt out in turn: 5003 ragged rows 158 us, 8192 rows 915.)  A call with a shared prefix splits
+// the SMs between two launches instead (taking over there: 8 x 32 rows behind 3000 124 -> 112 us, 20 x 16 behind 1000 63 -> 73).
+// The K warp asks for the next piece while the current one runs; the answer is read by every warp at its own pace from a ring of
+// two.
 __device__ __forceinline__ void bt_ask_piece(uint32_t answer, uint32_t bar)
 {
     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar) : "memory");
