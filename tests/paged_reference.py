@@ -96,7 +96,7 @@ def attention(b: Batch, pool: torch.Tensor, q: torch.Tensor, scale: Optional[flo
         s = torch.einsum("rhd,nhd->hrn", x, k) * scale
         mag = torch.einsum("rhd,nhd->hrn", x.abs(), k.abs()) * scale
         last = torch.arange(n, device=dev) + (b.kv[i] - n)
-        hidden = own[None, :] > last[:, None]
+        hidden = (own[None, :] >= 0) & (own[None, :] > last[:, None])      # every row sees the whole prefix
         s = s.masked_fill(hidden[None], -math.inf)
         top = s.amax(-1, keepdim=True)
         e = torch.exp(s - torch.where(top.isinf(), torch.zeros_like(top), top))

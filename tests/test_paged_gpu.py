@@ -203,6 +203,17 @@ def test_attention(case, form):
     assert torch.equal(again[:b.start[-1]], out[:b.start[-1]])       # the same bits, whatever order the blocks ran in
 
 
+@pytest.mark.parametrize("case", [
+    ([5, 9, 1], [2, 0, 30], 4, 2, 128, 16, BF16, 100),              # the few-row kernel beside the many-row kernel
+    ([5, 2], [2, 0], 2, 2, 64, 16, F16, 70),                        # the few-row kernel alone
+    ([70, 33], [60, 2], 8, 2, 128, 32, BF16, 300),                  # the many-row kernel
+    ([5, 9], [2, 0], 4, 2, 36, 16, F32, 40),
+], ids=IDS)
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+def test_rows_before_their_sequences_first_position_see_the_prefix(case, form):
+    test_attention(case, form)
+
+
 @pytest.mark.parametrize("form", ["prompt", "prefix"])
 @pytest.mark.parametrize("heads,kv_heads,each", [(14, 2, 9), (14, 2, 1), (56, 8, 40), (9, 3, 40)])
 def test_bits_do_not_depend_on_what_ran_before(form, heads, kv_heads, each):
