@@ -377,31 +377,46 @@ struct AttnView {
 };
 
 // Any type and head size: fp32 caches, whose products the matrix instructions would round, and the sizes the tensor-core
-// kernels do not take.  A block takes 16 query rows of a kv head (tokens x heads of the group, so that a group shares its
-// keys) and goes through the keys 32 at a time, widened to fp32 in shared memory.  Eight threads share a row's scores and
-// its running maximum and sum; the weighted sum of V runs with lanes over dims, four rows per warp.  Bound by shared-memory
-// loads (about one per two multiply-adds).  grid = pieces, block = 128, dynamic smem = af_smem_bytes(head_dim).
-constexpr int AF_ROWS = 16, AF_KEYS = 32;
+// kernels do not take.  A block of four warps takes 4 RPW query rows of a kv head (tokens x heads of the group, so that a group
+// shares its keys) and goes through the keys 32 at a time, widened to fp32 in shared memory.  Eight lanes share a row's scores
+// and its running maximum and sum (RPW / 4 rows x 4 keys a lane); for the weighted sum of V a lane holds four dims (NV times) of
+// all its warp's rows.  With RPW 16 both products make 8 multiply-adds per 16-byte load from shared memory, so the multiply-add
+// rate bounds them (5003 ragged rows of 56 heads on 8, fp32: 3.9 ms, 25 TFLOP/s of the 96 GFLOP that count; keys staged one float
+// at a time and 16 rows a block 10.9); RPW 4 is for batches too small to fill the SMs with that.  grid = pieces, block = 128.
+constexpr int AF_KEYS = 32;
 __host__ __device__ inline int af_stride(int head_dim) { return (head_dim + 3) / 4 * 4 + 4; }   // floats per staged row: 16-byte loads of eight rows fall into different banks
-__host__ __device__ inline int af_smem_bytes(int head_dim) { return ((AF_ROWS + 2 * AF_KEYS) * af_stride(head_dim) + AF_ROWS * (AF_KEYS + 1)) * 4 + AF_KEYS * 8; }
+__host__ __device__ constexpr int af_p_stride(int rpw) { return rpw == 4 ? 4 : rpw + 4; }       // floats per key of a warp's weights: no bank conflicts
+__host__ __device__ inline int af_smem_bytes(int head_dim, int rpw)
+{
+    return ((4 * rpw + 2 * AF_KEYS) * af_stride(head_dim) + 4 * AF_KEYS * af_p_stride(rpw)) * 4 + AF_KEYS * 8;
+}
 
-template <typename T>
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+template <typename T> __device__ __forceinline__ float4 load4(const T* p)      // 16-bit types: 8 bytes
+{
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    const T* e = reinterpret_cast<const T*>(&v);
+    return make_float4(to_float(e[0]), to_float(e[1]), to_float(e[2]), to_float(e[3]));
+}
+
+template <typename T, int RPW, int NV>
 __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
 {
+    constexpr int ROWS = 4 * RPW, RT = RPW / 4, PS = af_p_stride(RPW);
     extern __shared__ __align__(16) float af_smem[];
     const int D = a.head_dim, ld = af_stride(D), G = a.n_heads / a.n_kv_heads, Hk = a.n_kv_heads, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     float* q_sh = af_smem;
-    float* k_sh = q_sh + AF_ROWS * ld;
+    float* k_sh = q_sh + ROWS * ld;
     float* v_sh = k_sh + AF_KEYS * ld;
-    float* p_sh = v_sh + AF_KEYS * ld;                    // [row][AF_KEYS + 1]
-    long long* at_sh = reinterpret_cast<long long*>(af_smem + (AF_ROWS + 2 * AF_KEYS) * ld + AF_ROWS * (AF_KEYS + 1));   // element offset of each key's K, -1: nothing there
+    float* p_sh = v_sh + AF_KEYS * ld + warp * AF_KEYS * PS;          // this warp's weights, [key][row]
+    long long* at_sh = reinterpret_cast<long long*>(af_smem + (ROWS + 2 * AF_KEYS) * ld + 4 * AF_KEYS * PS);   // element offset of each key's K, -1: nothing there
     // ---- this block's piece
     int idx = blockIdx.x, seq = -1;
     SeqSpan sp = {0, 0, 0};
     for (int base = 0; base < b.n_seqs && seq < 0; base += 32) {
         SeqSpan mine = {0, 0, 0};
         if (base + lane < b.n_seqs) mine = seq_span(b, base + lane);
-        const int pieces = (mine.n * G + AF_ROWS - 1) / AF_ROWS * Hk;
+        const int pieces = (mine.n * G + ROWS - 1) / ROWS * Hk;
         int upto = pieces;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -419,25 +434,29 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
         sp = {__shfl_sync(FULL_WARP, mine.r0, at), __shfl_sync(FULL_WARP, mine.n, at), __shfl_sync(FULL_WARP, mine.len, at)};
     }
     if (seq < 0) return;                                  // the same for the whole block
-    const int kvh = idx % Hk, rho0 = idx / Hk * AF_ROWS, rows = min(AF_ROWS, sp.n * G - rho0);
+    const int kvh = idx % Hk, rho0 = idx / Hk * ROWS, rows = min(ROWS, sp.n * G - rho0);
     const T* head = reinterpret_cast<const T*>(a.pool) + (size_t)kvh * b.page_size * D;
     // ---- queries, scaled; dead rows and the dims behind the last are zero
-    for (int i = tid; i < AF_ROWS * ld; i += 128) {
-        const int r = i / ld, d = i - r * ld, tok = (rho0 + r) / G;
-        float v = 0.f;
-        if (r < rows && d < D)
-            v = to_float(reinterpret_cast<const T*>(a.q)[(long long)(sp.r0 + tok) * a.q_row_stride + (long long)(kvh * G + rho0 + r - tok * G) * a.q_head_stride + d]) * a.scale;
-        q_sh[i] = v;
+    for (int r = warp; r < ROWS; r += 4) {
+        const int tok = (rho0 + r) / G;
+        const T* src = reinterpret_cast<const T*>(a.q) + (long long)(sp.r0 + tok) * a.q_row_stride + (long long)(kvh * G + rho0 + r - tok * G) * a.q_head_stride;
+        for (int d = lane; d < ld; d += 32) q_sh[r * ld + d] = r < rows && d < D ? to_float(src[d]) * a.scale : 0.f;
     }
     for (int i = tid; i < 2 * AF_KEYS * (ld - D); i += 128) k_sh[i / (ld - D) * ld + D + i % (ld - D)] = 0.f;
-    const int row = tid >> 3, sub = tid & 7;              // this thread's row of scores; rows 4 warp .. + 3 are the warp's
-    const int tok = min(rho0 + row, sp.n * G - 1) / G, seen = b.prefix_len + max(0, sp.len - sp.n + tok + 1);
+    const int grp = lane >> 3, sub = lane & 7, row0 = warp * RPW;     // this lane's rows of scores: row0 + grp + 4 r
+    int seen[RT];
+    float m[RT], l[RT], o[RPW][4 * NV];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        seen[r] = b.prefix_len + max(0, sp.len - sp.n + min(rho0 + row0 + grp + 4 * r, sp.n * G - 1) / G + 1);
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+    }
     const int last = min(rho0 + rows - 1, sp.n * G - 1) / G, total = b.prefix_len + max(0, sp.len - sp.n + last + 1);   // what the last row sees
-    float m = -INFINITY, l = 0.f, o[4][8];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < RPW; ++r)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[r][e] = 0.f;
+        for (int e = 0; e < 4 * NV; ++e) o[r][e] = 0.f;
     for (int p0 = 0; p0 < total; p0 += AF_KEYS) {
         __syncthreads();                                  // the tile before is used up
         if (tid < AF_KEYS) {
@@ -450,78 +469,124 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
             at_sh[tid] = at;
         }
         __syncthreads();
+        if (D % 4 == 0) {                                 // 16 (or 8) bytes a lane: pages and rows start on multiples of that
 #pragma unroll 4
-        for (int i = tid; i < AF_KEYS * D; i += 128) {
-            const int j = i / D, d = i - j * D;
-            const long long at = at_sh[j];
-            k_sh[j * ld + d] = at >= 0 ? to_float(head[at + d]) : 0.f;
-            v_sh[j * ld + d] = at >= 0 ? to_float(head[at + a.kv_elems + d]) : 0.f;
+            for (int j = warp; j < AF_KEYS; j += 4) {
+                const long long at = at_sh[j];
+#pragma unroll
+                for (int e = 0; e < NV; ++e) {
+                    const int d = 4 * lane + 128 * e;
+                    if (d >= D) break;
+                    float4 kx = make_float4(0.f, 0.f, 0.f, 0.f), vx = kx;
+                    if (at >= 0) {
+                        kx = load4(head + at + d);
+                        vx = load4(head + at + a.kv_elems + d);
+                    }
+                    *reinterpret_cast<float4*>(k_sh + j * ld + d) = kx;
+                    *reinterpret_cast<float4*>(v_sh + j * ld + d) = vx;
+                }
+            }
+        } else {
+            for (int j = warp; j < AF_KEYS; j += 4) {
+                const long long at = at_sh[j];
+                for (int d = lane; d < D; d += 32) {
+                    k_sh[j * ld + d] = at >= 0 ? to_float(head[at + d]) : 0.f;
+                    v_sh[j * ld + d] = at >= 0 ? to_float(head[at + a.kv_elems + d]) : 0.f;
+                }
+            }
         }
         __syncthreads();
-        float s[4] = {0.f, 0.f, 0.f, 0.f};                // keys sub, sub + 8, sub + 16, sub + 24
-        const float4* qr = reinterpret_cast<const float4*>(q_sh + row * ld);
-        for (int d = 0; d < (D + 3) / 4; ++d) {
-            const float4 x = qr[d];
+        if (row0 >= rows) continue;                       // the same for the whole warp
+        float s[RT][4];                                   // keys sub, sub + 8, sub + 16, sub + 24
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[r][i] = 0.f;
+#pragma unroll 2
+        for (int d = 0; d < ld - 4; d += 4) {
+            float4 y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = *reinterpret_cast<const float4*>(k_sh + (sub + 8 * i) * ld + d);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float4 x = *reinterpret_cast<const float4*>(q_sh + (row0 + grp + 4 * r) * ld + d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[r][i] = fmaf(x.x, y[i].x, fmaf(x.y, y[i].y, fmaf(x.z, y[i].z, fmaf(x.w, y[i].w, s[r][i]))));
+            }
+        }
+        bool there[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) there[i] = at_sh[sub + 8 * i] >= 0;
+        float shrink[RT];
+        __syncwarp();                                     // the weights before are used up
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float top = m[r];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float4 y = reinterpret_cast<const float4*>(k_sh + (sub + 8 * i) * ld)[d];
-                s[i] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[i]))));
+                if (p0 + sub + 8 * i >= seen[r] || !there[i]) s[r][i] = -INFINITY;
+                top = fmaxf(top, s[r][i]);
             }
+#pragma unroll
+            for (int x = 4; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_WARP, top, x));
+            shrink[r] = m[r] == top ? 1.f : expf(m[r] - top);
+            const float from = top == -INFINITY ? 0.f : top;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = expf(s[r][i] - from);
+                p_sh[(sub + 8 * i) * PS + grp + 4 * r] = e;
+                sum += e;
+            }
+#pragma unroll
+            for (int x = 4; x > 0; x >>= 1) sum += __shfl_xor_sync(FULL_WARP, sum, x);
+            l[r] = l[r] * shrink[r] + sum;
+            m[r] = top;
         }
-        float top = m;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = sub + 8 * i;
-            if (p0 + j >= seen || at_sh[j] < 0) s[i] = -INFINITY;
-            top = fmaxf(top, s[i]);
-        }
-#pragma unroll
-        for (int x = 4; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_WARP, top, x));
-        const float shrink = m == top ? 1.f : expf(m - top), from = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float e = expf(s[i] - from);
-            p_sh[row * (AF_KEYS + 1) + sub + 8 * i] = e;
-            sum += e;
-        }
-#pragma unroll
-        for (int x = 4; x > 0; x >>= 1) sum += __shfl_xor_sync(FULL_WARP, sum, x);
-        l = l * shrink + sum;
-        m = top;
         __syncwarp();
-        float f[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            f[r] = __shfl_sync(FULL_WARP, shrink, 8 * r);
+        for (int r = 0; r < RPW; ++r) {
+            const float f = __shfl_sync(FULL_WARP, shrink[r >> 2], 8 * (r & 3));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[r][e] *= f[r];
+            for (int e = 0; e < 4 * NV; ++e) o[r][e] *= f;
         }
         const int n = min(AF_KEYS, total - p0);
+#pragma unroll 2
         for (int j = 0; j < n; ++j) {
-            float pj[4];
+            float4 v[NV];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) pj[r] = p_sh[(4 * warp + r) * (AF_KEYS + 1) + j];
+            for (int e = 0; e < NV; ++e) {
+                const int d = 4 * lane + 128 * e;
+                v[e] = d < D ? *reinterpret_cast<const float4*>(v_sh + j * ld + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (32 * e >= D) break;
-                const float v = lane + 32 * e < D ? v_sh[j * ld + lane + 32 * e] : 0.f;
+            for (int r = 0; r < RPW; r += 4) {
+                const float4 w = *reinterpret_cast<const float4*>(p_sh + j * PS + r);
+                const float wr[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[r][e] = fmaf(pj[r], v, o[r][e]);
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < NV; ++e) {
+                        o[r + i][4 * e] = fmaf(wr[i], v[e].x, o[r + i][4 * e]);
+                        o[r + i][4 * e + 1] = fmaf(wr[i], v[e].y, o[r + i][4 * e + 1]);
+                        o[r + i][4 * e + 2] = fmaf(wr[i], v[e].z, o[r + i][4 * e + 2]);
+                        o[r + i][4 * e + 3] = fmaf(wr[i], v[e].w, o[r + i][4 * e + 3]);
+                    }
             }
         }
-        __syncwarp();
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float sum = __shfl_sync(FULL_WARP, l, 8 * r);
-        const int rr = 4 * warp + r, t = (rho0 + rr) / G;
+    for (int r = 0; r < RPW; ++r) {
+        const float sum = __shfl_sync(FULL_WARP, l[r >> 2], 8 * (r & 3));
+        const int rr = row0 + r, t = (rho0 + rr) / G;
         if (rr >= rows || t >= a.max_rows) continue;
         T* out = reinterpret_cast<T*>(a.out) + ((size_t)(sp.r0 + t) * a.n_heads + kvh * G + rho0 + rr - t * G) * D;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;   // 0: the row sees nothing
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (lane + 32 * e < D) store_val(out + lane + 32 * e, o[r][e] * inv);
+        for (int e = 0; e < 4 * NV; ++e) {
+            const int d = 4 * lane + 128 * (e >> 2) + (e & 3);
+            if (d < D) store_val(out + d, o[r][e] * inv);
+        }
     }
 }
 

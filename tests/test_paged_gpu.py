@@ -214,6 +214,40 @@ def test_rows_before_their_sequences_first_position_see_the_prefix(case, form):
     test_attention(case, form)
 
 
+# enough rows for blocks of 64 in fp32 arithmetic: at least 148 of them
+FP32_MANY = [
+    ([300, 0, 40], [300, 7, 333], 32, 8, 128, 16, F32, 0),
+    ([700, 1, 650], [700, 90, 1000], 8, 8, 36, 16, F32, 40),
+    ([1300, 60], [1300, 61], 8, 8, 66, 8, BF16, 0),                 # 4-byte rows: elements are staged one by one
+    ([640, 30], [650, 25], 16, 8, 256, 32, F16, 33),                # two chunks of dims; rows with nothing of their own
+    ([1300, 50], [1290, 70], 8, 8, 130, 64, F32, 0),                # rows that see nothing; an odd second chunk
+]
+
+
+@pytest.mark.parametrize("case", FP32_MANY, ids=IDS)
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+def test_attention_in_fp32_arithmetic_with_many_rows(case, form):
+    test_attention(case, form)
+
+
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+def test_fp32_arithmetic_with_many_rows_leaves_out_rows_and_pages(form):
+    """Pages outside the pool, a sequence of NaN, rows beyond max_rows: 700 rows of 8 heads each, in fp32."""
+    b = Batch([700, 650], [700, 800], 8, 8, 64, 16, F32, prefix_len=90)
+    q = b.q.clone()
+    q[:700] = float("nan")
+    b.page_table[1, 3] = b.n_pages
+    b.page_table[1, 20] = -1
+    pool, batch = setup(b, max_rows=640)
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    out = torch.full((b.n_rows, 8, 64), 5.0, device="cuda", dtype=F32)
+    (batch.prompt_attention if form == "prompt" else batch.prefix_attention)(0, q.cuda(), out=out)
+    kept = 650 if form == "prompt" else 640
+    close(out[700:700 + kept], want[700:700 + kept], tol[700:700 + kept])
+    assert (out[700 + kept:] == 5).all()
+    assert torch.isnan(out[:640]).all()
+
+
 @pytest.mark.parametrize("form", ["prompt", "prefix"])
 @pytest.mark.parametrize("heads,kv_heads,each", [(14, 2, 9), (14, 2, 1), (56, 8, 40), (9, 3, 40)])
 def test_bits_do_not_depend_on_what_ran_before(form, heads, kv_heads, each):
