@@ -381,8 +381,10 @@ typedef struct {
  * kv_len[i] - n + r.  Own position p lives in slot p % page_size of page page_table[i * table_stride + p / page_size].
  * With prefix_len > 0, all sequences continue the same prefix of prefix_len positions in prefix_pages[0 ..
  * ceil(prefix_len / page_size) - 1], and own position p is position prefix_len + p of the sequence.  Pages are looked up
- * in [0, n_pages): the positions of a page id outside it hold nothing and are neither read nor written.  kv_len is
- * clipped to 0 .. table_stride * page_size.  Slots at and behind kv_len may hold anything, NaN included.
+ * in [0, n_pages): the positions of a page id outside it hold nothing and are neither read nor written.  Positions outside
+ * 0 .. table_stride * page_size - 1 hold nothing either: where kv_len (or row_start) reaches further, the rows keep their
+ * positions, and what lies outside the table or the packed tensors is left out.  Slots at and behind kv_len may hold
+ * anything, NaN included.
  */
 typedef struct {
     int32_t n_seqs, n_rows;

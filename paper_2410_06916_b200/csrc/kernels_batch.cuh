@@ -19,7 +19,7 @@ struct BatchView {
     const int* page_table;
     const int* prefix_pages;
 };
-struct SeqSpan { int r0, n, len; };                       // first row, rows, cached positions (own)
+struct SeqSpan { int r0, n, len, pos0; };                 // first row, rows, cached positions that can be read (own), own position of row r0
 
 __device__ __forceinline__ SeqSpan make_span(const BatchView& b, int start, int end, int len)
 {
@@ -27,12 +27,24 @@ __device__ __forceinline__ SeqSpan make_span(const BatchView& b, int start, int 
     s.r0 = min(max(start, 0), b.n_rows);
     s.n = min(max(end, s.r0), b.n_rows) - s.r0;
     s.len = min(max(len, 0), b.max_len);
+    // From the lengths as given: a sequence longer than its table keeps its rows' positions, and those behind the table are left
+    // out.  Positions behind max_len or far below 0 are alike, so the 64-bit difference may be clamped to an int.
+    const long long pos0 = (long long)len - end + s.r0;
+    s.pos0 = (int)max(-0x80000000ll, min(pos0, (long long)b.max_len));
     return s;
 }
 __device__ __forceinline__ SeqSpan seq_span(const BatchView& b, int i)
 {
     return make_span(b, b.row_start[i], b.row_start[i + 1], b.kv_len[i]);
 }
+
+// lane `at`'s span, for the whole warp
+__device__ __forceinline__ SeqSpan span_of(const SeqSpan& s, int at)
+{
+    return {__shfl_sync(FULL_WARP, s.r0, at), __shfl_sync(FULL_WARP, s.n, at), __shfl_sync(FULL_WARP, s.len, at), __shfl_sync(FULL_WARP, s.pos0, at)};
+}
+// how many of its sequence's cached positions row t sees
+__device__ __forceinline__ int seen_own(const SeqSpan& s, int t) { return min(max(s.pos0 + t + 1, 0), s.len); }
 
 // The sequence that holds row `row`, found by a whole warp: 32 row starts per step are compared at once, so a batch of up
 // to 32 sequences costs one trip to memory (the spans' three numbers come with it) and one of 1024 two.  Returns -1 for
@@ -196,8 +208,8 @@ __device__ __forceinline__ bool place_row(const BatchView& b, const AppendView& 
     const int given = a.positions ? a.positions[row] : 0;
     const int seq = find_seq(b, row, sp);
     if (seq < 0) return false;
-    const int own = sp.len - sp.n + (row - sp.r0);
-    if (own < 0) return false;                            // own < len <= max_len
+    const int own = sp.pos0 + (row - sp.r0);
+    if (own < 0 || own >= b.max_len) return false;        // before the first position, or behind the page table
     const int page = b.page_table[(size_t)seq * b.table_stride + (own >> b.page_shift)];
     p.rope_row = a.positions ? given : b.prefix_len + own;
     if ((unsigned)page >= (unsigned)b.n_pages) return false;
@@ -412,9 +424,9 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
     long long* at_sh = reinterpret_cast<long long*>(af_smem + (ROWS + 2 * AF_KEYS) * ld + 4 * AF_KEYS * PS);   // element offset of each key's K, -1: nothing there
     // ---- this block's piece
     int idx = blockIdx.x, seq = -1;
-    SeqSpan sp = {0, 0, 0};
+    SeqSpan sp = {};
     for (int base = 0; base < b.n_seqs && seq < 0; base += 32) {
-        SeqSpan mine = {0, 0, 0};
+        SeqSpan mine = {};
         if (base + lane < b.n_seqs) mine = seq_span(b, base + lane);
         const int pieces = (mine.n * G + ROWS - 1) / ROWS * Hk;
         int upto = pieces;
@@ -431,7 +443,7 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
         const int at = __ffs(m) - 1;
         idx -= __shfl_sync(FULL_WARP, upto - pieces, at);
         seq = base + at;
-        sp = {__shfl_sync(FULL_WARP, mine.r0, at), __shfl_sync(FULL_WARP, mine.n, at), __shfl_sync(FULL_WARP, mine.len, at)};
+        sp = span_of(mine, at);
     }
     if (seq < 0) return;                                  // the same for the whole block
     const int kvh = idx % Hk, rho0 = idx / Hk * ROWS, rows = min(ROWS, sp.n * G - rho0);
@@ -448,11 +460,11 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
     float m[RT], l[RT], o[RPW][4 * NV];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        seen[r] = b.prefix_len + max(0, sp.len - sp.n + min(rho0 + row0 + grp + 4 * r, sp.n * G - 1) / G + 1);
+        seen[r] = b.prefix_len + seen_own(sp, min(rho0 + row0 + grp + 4 * r, sp.n * G - 1) / G);
         m[r] = -INFINITY;
         l[r] = 0.f;
     }
-    const int last = min(rho0 + rows - 1, sp.n * G - 1) / G, total = b.prefix_len + max(0, sp.len - sp.n + last + 1);   // what the last row sees
+    const int last = min(rho0 + rows - 1, sp.n * G - 1) / G, total = b.prefix_len + seen_own(sp, last);   // what the last row sees
 #pragma unroll
     for (int r = 0; r < RPW; ++r)
 #pragma unroll

@@ -61,11 +61,11 @@ __device__ __forceinline__ SeqSpan bd_span(const BatchView& b, BdWalk& w, int se
     if (seq < w.base || seq >= w.base + 32) {
         const int i = seq + (threadIdx.x & 31);
         w.base = seq;
-        w.ahead = {0, 0, 0};
+        w.ahead = {};
         if (i < b.n_seqs) w.ahead = seq_span(b, i);
     }
     const int at = seq - w.base;
-    return {__shfl_sync(FULL_WARP, w.ahead.r0, at), __shfl_sync(FULL_WARP, w.ahead.n, at), __shfl_sync(FULL_WARP, w.ahead.len, at)};
+    return span_of(w.ahead, at);
 }
 template <int KEYS> __device__ __forceinline__ void bd_enter(const BatchView& b, const BdArgs& g, BdWalk& w)
 {
@@ -87,16 +87,14 @@ template <int KEYS> __device__ __forceinline__ void bd_start(const BatchView& b,
         w.unit = (int)(u - (long long)w.kvh * prefix_units);
         w.units = prefix_units;
         w.item = w.kvh;
-        w.sp.r0 = 0;
-        w.sp.n = min(max(b.row_start[b.n_seqs], 0), b.n_rows);
-        w.sp.len = b.prefix_len;
+        w.sp = {0, min(max(b.row_start[b.n_seqs], 0), b.n_rows), b.prefix_len, 0};
         return;
     }
     u -= (long long)prefix_units * Hk;
     w.seq = 0;
     for (int base = 0; base < b.n_seqs; base += 32) {
         w.base = base;
-        w.ahead = {0, 0, 0};
+        w.ahead = {};
         if (base + lane < b.n_seqs) w.ahead = seq_span(b, base + lane);
         const int mine = bd_units<KEYS>(w.ahead) * Hk;
         int upto = mine;
@@ -339,7 +337,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
             // own part: rows see keys up to their own position; the prefix: all rows see all of it
             int seen[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) seen[e] = w.seq < 0 ? left : min(left, w.sp.len - w.sp.n + tok[e] + 1 - key0);
+            for (int e = 0; e < 2; ++e) seen[e] = w.seq < 0 ? left : min(left, w.sp.pos0 + tok[e] + 1 - key0);
             if (__any_sync(FULL_WARP, min(seen[0], seen[1]) < KEYS) || pages != all_boxes) {
 #pragma unroll
                 for (int n = 0; n < KEYS / 8; ++n)

@@ -65,7 +65,8 @@ struct BtArgs {
 };
 
 struct BtItem {
-    int seq, r0, n, len, t0, kvh;                                     // t0: first token of the pair within the sequence
+    int seq, kvh, t0;                                                 // t0: first token of the pair within the sequence
+    SeqSpan sp;                                                       // (the prefix: all rows, nothing of its own)
     int first_tile, np, slot;                                         // np: prefix tiles counted from first_tile on (then own tiles)
     int tiles[2];                                                     // key tiles of tile A and of tile B
 };
@@ -82,9 +83,7 @@ __device__ __forceinline__ bool bt_locate(const BatchView& b, const BtArgs& g, i
         if (idx >= pairs * Hk * g.splits) return false;
         const int s = idx % g.splits, rest = idx / g.splits;
         it.seq = -1;
-        it.r0 = 0;
-        it.n = n;
-        it.len = 0;
+        it.sp = {0, n, 0, 0};
         it.kvh = rest % Hk;
         it.t0 = rest / Hk * pair_rows;
         it.slot = s;
@@ -95,7 +94,7 @@ __device__ __forceinline__ bool bt_locate(const BatchView& b, const BtArgs& g, i
         return true;
     }
     for (int base = 0; base < b.n_seqs; base += 32) {
-        SeqSpan sp = {0, 0, 0};
+        SeqSpan sp = {};
         if (base + lane < b.n_seqs) sp = seq_span(b, base + lane);
         const int mine = (sp.n + pair_rows - 1) / pair_rows * Hk;
         int upto = mine;
@@ -111,19 +110,17 @@ __device__ __forceinline__ bool bt_locate(const BatchView& b, const BtArgs& g, i
         }
         const int at = __ffs(m) - 1;
         it.seq = base + at;
-        it.r0 = __shfl_sync(FULL_WARP, sp.r0, at);
-        it.n = __shfl_sync(FULL_WARP, sp.n, at);
-        it.len = __shfl_sync(FULL_WARP, sp.len, at);
+        it.sp = span_of(sp, at);
         idx -= __shfl_sync(FULL_WARP, upto - mine, at);
-        const int pairs = (it.n + pair_rows - 1) / pair_rows;
+        const int pairs = (it.sp.n + pair_rows - 1) / pair_rows;
         it.kvh = idx % Hk;
         it.t0 = (pairs - 1 - idx / Hk) * pair_rows;                   // the longest pieces of a sequence first
         it.np = g.mode == BT_OWN ? 0 : prefix_tiles;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const int t_end = min(it.n, it.t0 + (x + 1) * TQ);        // tokens of this tile end here
-            const bool some = x < g.tiles && it.t0 + x * TQ < it.n;
-            const int seen = min(max(it.len - it.n + t_end, 0), it.len);
+            const int t_end = min(it.sp.n, it.t0 + (x + 1) * TQ);     // tokens of this tile end here
+            const bool some = x < g.tiles && it.t0 + x * TQ < it.sp.n;
+            const int seen = seen_own(it.sp, t_end - 1);
             it.tiles[x] = some ? it.np + (seen + BT_KEYS - 1) / BT_KEYS : 0;
         }
         return true;
@@ -596,7 +593,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                     if (ok && elect_one()) {
                         mbar_expect_tx(q_full(x), (uint32_t)(TQ * G * 128 * HALVES));
                         for (int hf = 0; hf < HALVES; ++hf)
-                            tma_load_3d(q_sh + x * S::Q_BYTES + hf * (BT_ROWS * 128), &map_q, 64 * hf, it.kvh * G, it.r0 + it.t0 + x * TQ, q_full(x));
+                            tma_load_3d(q_sh + x * S::Q_BYTES + hf * (BT_ROWS * 128), &map_q, 64 * hf, it.kvh * G, it.sp.r0 + it.t0 + x * TQ, q_full(x));
                     }
                 }
             }
@@ -604,7 +601,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             auto look_up = [&](int j) {
                 const bool shared_part = j < it.np;
                 const int key0 = (shared_part ? it.first_tile + j : j - it.np) * BT_KEYS;
-                const int left = (shared_part ? b.prefix_len : it.len) - key0;
+                const int left = (shared_part ? b.prefix_len : it.sp.len) - key0;
                 int page = -1;
                 if (j < n_tiles && lane < per_tile && (lane << b.page_shift) < left) {
                     const int at = (key0 >> b.page_shift) + lane;
@@ -619,7 +616,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 const unsigned pages = __ballot_sync(FULL_WARP, good);
                 next_page = look_up(j + 1);
                 const bool shared_part = j < it.np;
-                const int left = (shared_part ? b.prefix_len - (it.first_tile + j) * BT_KEYS : it.len - (j - it.np) * BT_KEYS);   // keys of this tile that exist
+                const int left = (shared_part ? b.prefix_len - (it.first_tile + j) * BT_KEYS : it.sp.len - (j - it.np) * BT_KEYS);   // keys of this tile that exist
                 const int tail = left & (b.page_size - 1);            // slots of the last page that hold something
                 // a V tile with unwritten slots: they are zeroed before the product may read them
                 const bool mend = kv == 1 && left < BT_KEYS && tail != 0 && ((pages >> (left >> b.page_shift)) & 1u);
@@ -758,9 +755,9 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             if (!bt_locate(b, g, pieces.idx, it)) { if (PART) break; continue; }
             const int n_tiles = max(it.tiles[0], it.tiles[1]), mine = it.tiles[x];
             const int t = it.t0 + x * TQ + tok;                       // token within the sequence
-            const bool live = x < g.tiles && tok < TQ && t < it.n && (g.mode == BT_PREFIX || t < g.a.max_rows);
-            const int own = it.len - it.n + t;                        // own position: keys 0 .. own are seen
-            const int all_see = it.len - it.n + it.t0 + x * TQ + 1;    // own keys that every row of the tile sees
+            const bool live = x < g.tiles && tok < TQ && t < it.sp.n && (g.mode == BT_PREFIX || t < g.a.max_rows);
+            const int own_seen = seen_own(it.sp, t);                  // own keys that this row sees
+            const int all_see = seen_own(it.sp, it.t0 + x * TQ);      // ... that every row of the tile sees
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < mine; ++j) {
                 ok = bt_wait(s_full(x), s_turn, abort_sh);
@@ -768,7 +765,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 s_turn ^= 1u;
                 tc_fence_after();
                 const int key0 = (j < it.np ? it.first_tile + j : j - it.np) * BT_KEYS;
-                const int seen = j < it.np ? b.prefix_len - key0 : own + 1 - key0;        // this row sees keys below this
+                const int seen = j < it.np ? b.prefix_len - key0 : own_seen - key0;       // this row sees keys below this
                 const unsigned pages = page_bits[(tile_no + j) & (BT_PAGE_RING - 1)];
                 const bool masked = key0 + BT_KEYS > (j < it.np ? b.prefix_len : all_see) || pages != all_pages;
                 if (masked) bt_softmax<T, DP, true>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
@@ -782,7 +779,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 o_turn ^= 1u;
                 tc_fence_after();
             }
-            const int row = it.r0 + t, head = it.kvh * G + head_in;
+            const int row = it.sp.r0 + t, head = it.kvh * G + head_in;
             if (PART) {
                 const size_t at = ((size_t)it.slot * b.n_rows + row) * g.a.n_heads + head;
                 if (live) g.part_ml[at] = make_float2(m * c - BIAS, l);

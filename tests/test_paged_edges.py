@@ -1,0 +1,154 @@
+"""The paged-batch operators at the edges of what their interface allows: plans that reach further than their tables, scores
+that are not finite or far from zero, waits that run out, tensors of other streams (bounds as in paged_reference.py)."""
+import pytest
+import torch
+
+from paged_reference import F64, Batch, append_tolerance, attention, finish_heads, frequencies, half_step
+from test_paged_gpu import close, setup
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def call(batch, form):
+    return batch.prompt_attention if form == "prompt" else batch.prefix_attention
+
+
+# ----------------------------------------------------------------------------------------------- plans that reach too far
+class Long(Batch):
+    """A batch whose kv_len reach beyond the page table: the positions behind it hold nothing."""
+    def longer(self, kv):
+        self.capacity = self.page_table.shape[1] * self.page
+        self.kv = kv
+        return self
+
+    def visible(self, i):
+        kv, self.kv = self.kv, [min(max(l, 0), self.capacity) for l in self.kv]
+        try:
+            return super().visible(i)
+        finally:
+            self.kv = kv
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt,x_dtype,dim,heads", [(BF16, BF16, 128, 8), (F16, F32, 64, 4), (F32, F32, 34, 2)])
+def test_append_leaves_out_rows_behind_the_page_table(dt, x_dtype, dim, heads):
+    """kv_len one, three and 2^31 - 1 beyond a full table, just full, below zero: rows keep their positions, and of those behind
+    the table nothing is written."""
+    from paper_2410_06916_b200 import PagedKV, RowBatch, rope_table
+    page, width, B = 16, 4, 7
+    cap = page * width
+    n = [1, 3, 5, 2, 4, 2, 1]
+    kv = [cap + 1, cap + 3, cap + 3, cap, (1 << 31) - 1, -3, 40]
+    T, kv_heads = sum(n), 2
+    g = torch.Generator().manual_seed(2)
+    x = [torch.randn(T, h, dim, generator=g).to(x_dtype) for h in (heads, kv_heads, kv_heads)]
+    start = [0]
+    for a in n:
+        start.append(start[-1] + a)
+    table = torch.randperm(B * width, generator=g).to(torch.int32).view(B, width)
+    before = torch.randn(B * width, 1, 2, kv_heads, page, dim, generator=g).to(dt)
+    pool = before.cuda()
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    batch = RowBatch(PagedKV(pool), i32(start), i32(kv), table.cuda(), n_rows=T)
+    out = torch.full((T, heads, dim), 3.0, device="cuda", dtype=dt)
+    xd = [t.cuda() for t in x]
+    batch.append(0, *xd, rope=rope_table(2 * cap, dim), out=out)
+    want_pool, tol_pool = before.to(F64), torch.zeros(before.shape, dtype=F64)
+    want_q, tol_q = torch.full((T, heads, dim), 3.0, dtype=F64), torch.zeros(T, heads, dim, dtype=F64)
+    written = 0
+    for i in range(B):
+        for j in range(n[i]):
+            own, row = kv[i] - n[i] + j, start[i] + j
+            if not 0 <= own < cap:
+                continue
+            written += 1
+            pos = torch.tensor([own])
+            (yq, mq), (yk, mk) = (finish_heads(t[row:row + 1], pos, frequencies(dim), False, None, 1e-5) for t in x[:2])
+            want_q[row], tol_q[row] = yq[0], append_tolerance(yq, mq, dim, dt)[0]
+            at = int(table[i, own // page])
+            want_pool[at, 0, 0, :, own % page], tol_pool[at, 0, 0, :, own % page] = yk[0], append_tolerance(yk, mk, dim, dt)[0]
+            v = x[2][row].to(F64)
+            want_pool[at, 0, 1, :, own % page], tol_pool[at, 0, 1, :, own % page] = v, half_step(dt) * v.abs() + (2.0 ** -25 if dt == F16 else 0.0)
+    assert written == 2 + 2 + 1
+    close(out, want_q, tol_q)
+    close(pool, want_pool, tol_pool)
+
+
+LONG = [
+    # rows, cached (the first fills the table), beyond, heads, kv heads, dim, type, prefix
+    ([1, 1, 1], [64, 20, 64], [65, 20, 70], 8, 2, 128, BF16, 0),
+    ([5, 9, 3], [64, 64, 30], [66, 67, 30], 8, 2, 128, F16, 100),
+    ([9, 9, 9], [640, 640, 30], [641, 700, 30], 14, 2, 64, BF16, 700),
+    ([40, 130, 50], [512, 512, 300], [530, 513, 300], 8, 2, 128, BF16, 0),
+    ([40, 130, 50], [512, 512, 300], [530, 800, 300], 4, 4, 96, F16, 90),
+    ([40, 5, 50], [512, 512, 300], [530, 514, -7], 4, 2, 36, F32, 90),
+    ([700, 650], [704, 704], [720, 710], 8, 8, 64, F32, 0),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", LONG, ids=lambda c: "-".join(str(x).replace("torch.", "") for x in c[3:]))
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+def test_attention_keeps_the_positions_of_sequences_beyond_their_table(case, form):
+    n, kv, longer, H, Hk, dim, dt, prefix = case
+    b = Long(n, kv, H, Hk, dim, 16, dt, prefix_len=prefix).longer(longer)
+    pool, batch = setup(b)
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    close(call(batch, form)(0, b.q.cuda()), want, tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+@pytest.mark.parametrize("each,dt", [(4, BF16), (60, BF16), (4, F32)])
+def test_row_starts_behind_the_packed_rows_move_no_row(form, each, dt):
+    """The last sequence claims two rows more than the tensors have: its first rows stay at their positions."""
+    from paper_2410_06916_b200 import PagedKV, RowBatch
+    b = Batch([each, each], [200, 170], 8, 2, 64, 16, dt)
+    (start, kv, table), kw = b.device_args()
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    pool = b.pool.cuda()
+    kw["n_rows"] -= 2
+    batch = RowBatch(PagedKV(pool), start, kv, table, **kw)
+    q = b.q[:-2].cuda()
+    close(call(batch, form)(0, q), want[:-2], tol[:-2])
+    k = torch.randn(2 * each - 2, 2, 64, device="cuda").to(dt)
+    before = pool.clone()
+    batch.append(0, q, k, k)
+    for i in range(2):
+        for j in range(each):
+            own, row = b.kv[i] - each + j, i * each + j
+            at = (int(b.page_table[i, own // 16]), 0, slice(None), slice(None), own % 16)
+            before[at] = k[row] if row < len(k) else before[at]
+    assert torch.equal(torch.nan_to_num(pool, nan=-1.0), torch.nan_to_num(before, nan=-1.0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+@pytest.mark.parametrize("each,dt", [(4, BF16), (60, F16), (3, F32)])
+def test_lengths_below_zero_and_row_starts_that_descend(form, each, dt):
+    """A length below zero is an empty cache: such rows see nothing and append nothing.  Row starts that descend hold no rows."""
+    from paper_2410_06916_b200 import PagedKV, RowBatch
+    b = Batch([each, each], [200, 170], 8, 2, 64, 16, dt)
+    (start, kv, table), kw = b.device_args()
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    pool, q = b.pool.cuda(), b.q.cuda()
+    before = pool.clone()
+    batch = RowBatch(PagedKV(pool), start, torch.tensor([200, -3], dtype=torch.int32, device="cuda"), table, **kw)
+    got = call(batch, form)(0, q)
+    close(got[:each], want[:each], tol[:each])
+    assert (got[each:] == 0).all()
+    rows = torch.full_like(q, 2.0)
+    k = torch.ones(2 * each, 2, 64, device="cuda", dtype=dt)
+    assert (batch.append(0, q, k, k, out=rows)[each:] == 2).all()
+    own = set(range(200 - each, 200))
+    for p in range(200):
+        at = (int(b.page_table[0, p // 16]), 0, slice(None), slice(None), p % 16)
+        before[at] = 1.0 if p in own else before[at]
+    assert torch.equal(torch.nan_to_num(pool, nan=-1.0), torch.nan_to_num(before, nan=-1.0))
+    backwards = torch.tensor([2 * each, each, -2], dtype=torch.int32, device="cuda")
+    batch = RowBatch(PagedKV(pool), backwards, kv, table, **kw)
+    out = torch.full_like(q, 9.0)
+    call(batch, form)(0, q, out=out)
+    batch.append(0, q, k + 1, k + 1, out=rows.fill_(9.0))
+    assert (out == 9).all() and (rows == 9).all()
+    assert torch.equal(torch.nan_to_num(pool, nan=-1.0), torch.nan_to_num(before, nan=-1.0))
