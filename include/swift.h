@@ -471,6 +471,13 @@ swift_status swift_prefix_attention(const swift_paged_kv* kv, const swift_row_ba
                                     int32_t max_rows, swift_devbuf workspace, void* cuda_stream);
 const char* swift_batch_error(void);
 
+/* Exercises the path a wait that runs out takes, in a harmless form: swift_prefix_attention with these arguments (max_rows 0:
+ * swift_prompt_attention, which needs no workspace), whose blocks never ask for the first copy that they wait for and give up
+ * after limit_us microseconds (1..100000).  Enqueues and returns SWIFT_OK; swift_batch_sync then reports SWIFT_ETIMEOUT, out holds
+ * anything, and the calls after it work normally.  SWIFT_EUNSUPPORTED where the call is computed in fp32 arithmetic (no waits). */
+swift_status swift_probe_batch_wait_limit(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args,
+                                          int32_t max_rows, swift_devbuf workspace, int32_t limit_us, void* cuda_stream);
+
 /* Waits for the stream's work and reports what only the device knows: SWIFT_ETIMEOUT when a bounded device-side wait of
  * one of the attention calls above ran out on this device since the last report (the outputs of that call are then not
  * complete), SWIFT_ECUDA when the work failed, else SWIFT_OK.  Not inside a stream capture. */

@@ -123,6 +123,8 @@ swift_status check_attention(const swift_paged_kv* kv, const swift_row_batch* b,
     av->head_dim = kv->head_dim;
     av->max_rows = b->n_rows;
     av->scale = a->scale;
+    av->wait_kcycles = (int)(TC_WAIT_CYCLES >> 10);
+    av->withhold = 0;
     return SWIFT_OK;
 }
 
@@ -412,6 +414,7 @@ swift_status run_prefix(const swift_paged_kv* kv, const BatchView& bv, const Att
     j.few_ml = reinterpret_cast<float2*>(ws + p.few_ml);
     j.item_first = reinterpret_cast<int*>(ws + p.first);
     j.item_last = reinterpret_cast<int*>(ws + p.last);
+    j.workers = p.grid * (BD_WARPS / p.mt);
     cudaError_t e = cudaSuccess;
     if (p.few) {
         BdArgs g = {};
@@ -490,6 +493,55 @@ cudaError_t launch_append(const BatchView& b, const AppendView& a, bool vec, cud
     case 8: return launch(append_vec_kernel<TX, TC, 8>, grid, AP_THREADS, 0, s, false, b, a, per_warp, chunks);
     default: return launch(append_vec_kernel<TX, TC, 16>, grid, AP_THREADS, 0, s, false, b, a, per_warp, chunks);
     }
+}
+
+// limit_us > 0: the probe of swift_probe_batch_wait_limit.
+void set_probe(AttnView* av, int limit_us)
+{
+    if (limit_us <= 0) return;
+    av->wait_kcycles = 2 * limit_us;                      // about 2 cycles per nanosecond
+    av->withhold = 1;
+}
+
+swift_status prompt_attention(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args, int probe_us, cudaStream_t s)
+{
+    BatchView bv;
+    AttnView av;
+    swift_status st = check_attention(kv, batch, args, &bv, &av);
+    if (st != SWIFT_OK) return st;
+    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
+    set_probe(&av, probe_us);
+    if (!tensor_core_shape(kv) || av.n_heads / av.n_kv_heads > BT_ROWS) {
+        const cudaError_t e = launch_rows(kv, bv, av, s);
+        if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+        return SWIFT_OK;
+    }
+    return run_prompt(kv, bv, av, args->block, s);
+}
+
+swift_status prefix_attention(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args, int max_rows,
+                              swift_devbuf workspace, int probe_us, cudaStream_t s)
+{
+    BatchView bv;
+    AttnView av;
+    swift_status st = check_attention(kv, batch, args, &bv, &av);
+    if (st != SWIFT_OK) return st;
+    if (max_rows < 1) return fail_batch(SWIFT_EINVAL, "max_rows %d", max_rows);
+    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
+    PrefixPlan p;
+    st = plan_prefix(kv, bv, av.n_heads, max_rows, &p);
+    if (st != SWIFT_OK) return st;
+    if (!workspace.dptr || !aligned(workspace.dptr, 256)) return fail_batch(SWIFT_EINVAL, "the workspace must be 256-byte aligned device memory");
+    if (workspace.bytes < p.bytes) return fail_batch(SWIFT_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace.bytes, p.bytes);
+    av.max_rows = max_rows;
+    set_probe(&av, probe_us);
+    if (p.rows) {
+        const cudaError_t e = launch_rows(kv, bv, av, s);
+        if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+        return SWIFT_OK;
+    }
+    if (p.prompt) return run_prompt(kv, bv, av, args->block, s);
+    return run_prefix(kv, bv, av, args->block, p, reinterpret_cast<unsigned char*>(workspace.dptr), s);
 }
 
 } // namespace
@@ -583,18 +635,7 @@ swift_status swift_kv_append(const swift_paged_kv* kv, const swift_row_batch* ba
 
 swift_status swift_prompt_attention(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args, void* cuda_stream)
 {
-    BatchView bv;
-    AttnView av;
-    swift_status st = check_attention(kv, batch, args, &bv, &av);
-    if (st != SWIFT_OK) return st;
-    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
-    cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (!tensor_core_shape(kv) || av.n_heads / av.n_kv_heads > BT_ROWS) {
-        const cudaError_t e = launch_rows(kv, bv, av, s);
-        if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
-        return SWIFT_OK;
-    }
-    return run_prompt(kv, bv, av, args->block, s);
+    return prompt_attention(kv, batch, args, 0, (cudaStream_t)cuda_stream);
 }
 
 size_t swift_prefix_workspace_bytes(const swift_paged_kv* kv, const swift_row_batch* batch, int32_t n_heads, int32_t max_rows)
@@ -612,26 +653,18 @@ size_t swift_prefix_workspace_bytes(const swift_paged_kv* kv, const swift_row_ba
 swift_status swift_prefix_attention(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args, int32_t max_rows,
                                     swift_devbuf workspace, void* cuda_stream)
 {
-    BatchView bv;
-    AttnView av;
-    swift_status st = check_attention(kv, batch, args, &bv, &av);
-    if (st != SWIFT_OK) return st;
-    if (max_rows < 1) return fail_batch(SWIFT_EINVAL, "max_rows %d", max_rows);
-    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
-    PrefixPlan p;
-    st = plan_prefix(kv, bv, av.n_heads, max_rows, &p);
-    if (st != SWIFT_OK) return st;
-    if (!workspace.dptr || !aligned(workspace.dptr, 256)) return fail_batch(SWIFT_EINVAL, "the workspace must be 256-byte aligned device memory");
-    if (workspace.bytes < p.bytes) return fail_batch(SWIFT_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace.bytes, p.bytes);
-    av.max_rows = max_rows;
-    cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (p.rows) {
-        const cudaError_t e = launch_rows(kv, bv, av, s);
-        if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
-        return SWIFT_OK;
-    }
-    if (p.prompt) return run_prompt(kv, bv, av, args->block, s);
-    return run_prefix(kv, bv, av, args->block, p, reinterpret_cast<unsigned char*>(workspace.dptr), s);
+    return prefix_attention(kv, batch, args, max_rows, workspace, 0, (cudaStream_t)cuda_stream);
+}
+
+swift_status swift_probe_batch_wait_limit(const swift_paged_kv* kv, const swift_row_batch* batch, const swift_attention_args* args, int32_t max_rows,
+                                          swift_devbuf workspace, int32_t limit_us, void* cuda_stream)
+{
+    if (limit_us < 1 || limit_us > 100000) return fail_batch(SWIFT_EINVAL, "limit_us must be in 1..100000");
+    if (max_rows < 0) return fail_batch(SWIFT_EINVAL, "max_rows %d", max_rows);
+    if (kv && args && kv->n_kv_heads > 0 && (!tensor_core_shape(kv) || args->n_heads / kv->n_kv_heads > BT_ROWS))
+        return fail_batch(SWIFT_EUNSUPPORTED, "fp32 arithmetic has no waits");
+    if (max_rows == 0) return prompt_attention(kv, batch, args, limit_us, (cudaStream_t)cuda_stream);
+    return prefix_attention(kv, batch, args, max_rows, workspace, limit_us, (cudaStream_t)cuda_stream);
 }
 
 swift_status swift_batch_sync(void* cuda_stream)

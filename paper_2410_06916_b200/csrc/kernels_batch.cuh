@@ -386,6 +386,7 @@ struct AttnView {
     void* out;
     int n_heads, n_kv_heads, head_dim, max_rows;
     float scale;
+    int wait_kcycles, withhold;                           // limit of the tensor-core kernels' waits in 1024 cycles; withhold: a copy is never asked for
 };
 
 // Any type and head size: fp32 caches, whose products the matrix instructions would round, and the sizes the tensor-core

@@ -167,8 +167,8 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
     __shared__ __align__(8) unsigned long long bars[S::WORKERS * S::STAGES * 2];
     __shared__ unsigned page_bits[S::WORKERS * S::STAGES];
     __shared__ int sums[BD_THREADS / 32];
-    __shared__ int abort_flag;
-    volatile int* abort_sh = &abort_flag;
+    __shared__ int waits_sh[2];
+    volatile int* waits = waits_sh;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, Hk = g.a.n_kv_heads, G = g.a.n_heads / Hk;
     const int wk = warp / MT, mt = warp % MT, gq = lane >> 2, t = lane & 3;
@@ -176,7 +176,8 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
     auto empty = [&](int s) { return smem_u32(&bars[(S::WORKERS + wk) * S::STAGES + s]); };
     if (tid == 0) {
         for (int s = 0; s < S::WORKERS * S::STAGES; ++s) { mbar_init(smem_u32(&bars[s]), 1); mbar_init(smem_u32(&bars[S::WORKERS * S::STAGES + s]), MT); }
-        abort_flag = 0;
+        waits[0] = 0;
+        waits[1] = g.a.wait_kcycles;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_kv) : "memory");
     }
@@ -223,15 +224,16 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
             const bool good = (unsigned)next_page < (unsigned)b.n_pages;
             const int page = good ? next_page : b.n_pages;                // beyond the last page: zeros
             const unsigned pages = __ballot_sync(FULL_WARP, good) & all_boxes;
+            const bool asks = !(g.a.withhold && asked == 0);
             if (elect_one()) {
                 page_bits[wk * S::STAGES + f_stage] = pages;
-                mbar_expect_tx(full(f_stage), 2u * S::TILE_BYTES);
+                if (asks) mbar_expect_tx(full(f_stage), 2u * S::TILE_BYTES);
             }
             __syncwarp();
             // one lane asks for all boxes in turn (from lanes of their own they go out one by one as well), at some 90 cycles each
             const uint32_t dst = stages + f_stage * 2 * S::TILE_BYTES;
             const int plane = g.block * 2 * Hk + wf.kvh;
-            for (int p = 0; p < per_unit; ++p) {
+            for (int p = 0; asks && p < per_unit; ++p) {
                 const int pageu = __shfl_sync(FULL_WARP, page, p), slot0 = (wf.unit * KEYS + p * box_rows) & (b.page_size - 1);
                 if (elect_one()) {
                     if (g.whole_boxes) {
@@ -306,7 +308,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
                 m[0] = m[1] = -INFINITY;
                 l[0] = l[1] = 0.f;
             }
-            ok = bt_wait(full(stage), turn, abort_sh);
+            ok = bt_wait(full(stage), turn, waits);
             if (!ok) break;
             const uint32_t kv_sh = stages + stage * 2 * S::TILE_BYTES;
             const int key0 = w.unit * KEYS, left = w.sp.len - key0;
@@ -400,7 +402,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
             __syncwarp();
             if (MT > 1 && lane == 0) mbar_arrive(empty(stage));
             if (mt == 0 && asked < count) {
-                if (MT > 1) ok = bt_wait(empty(f_stage), f_turn ^ 1u, abort_sh);
+                if (MT > 1) ok = bt_wait(empty(f_stage), f_turn ^ 1u, waits);
                 if (!ok) break;
                 ask();
             }
@@ -423,11 +425,9 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
             }
             if (k + 1 < count) bd_next<KEYS>(b, g, w);
         }
-        if (!ok && lane == 0) {                                           // copies still on their way land before the block ends
-            const long long t0 = clock64();
-            while (clock64() - t0 < 2000000LL) { }
-        }
     }
+    __syncthreads();
+    bt_give_up(waits);
     pdl_wait();                                           // the launch before this one ends first: what follows waits for both
 }
 
@@ -443,6 +443,7 @@ struct BjArgs {
     const float2* few_ml;
     const int* item_first;
     const int* item_last;
+    int workers;                                          // of the few-row kernel, at most
 };
 
 // out[row][h] = sum_i 2^(M_i - M) O_i / sum_i 2^(M_i - M) l_i over the parts of a row, in a fixed order: the many-row
@@ -451,6 +452,15 @@ struct BjSum {
     float M, l;
     float4 acc;
 };
+// The first worker that left a part of an item, and how many did; none where a wait ran out before the entries were written (they
+// are then whatever the workspace held).
+__device__ __forceinline__ int bj_parts(const BjArgs& g, int item, int& first)
+{
+    const int f = g.item_first[item], l = g.item_last[item];
+    const bool good = f >= 0 && f <= l && l < g.workers;
+    first = good ? f : 0;
+    return good ? l - f + 1 : 0;
+}
 struct BjKind {                                           // one kind of parts: how many, where the first one's sums and maximum are, what lies between two
     const float* o;
     const float2* ml;
@@ -471,13 +481,13 @@ __global__ void __launch_bounds__(256, WARPS == 1 ? 4 : 3) attn_join_kernel(Batc
     if (h >= g.a.n_heads) return;                         // (WARPS 8: all or none of a block)
     const int Hk = g.a.n_kv_heads, G = g.a.n_heads / Hk, kvh = h / G, hg = h - kvh * G;
     int f0 = 0, n0 = 0;
-    if (g.prefix_here) { f0 = g.item_first[kvh]; n0 = g.item_last[kvh] - f0 + 1; }
+    if (g.prefix_here) n0 = bj_parts(g, kvh, f0);
     SeqSpan sp;
     const int seq = find_seq(b, row, sp);
     if (seq < 0 || row - sp.r0 >= g.a.max_rows) return;   // the same for the whole block
     const int own_item = (g.prefix_here ? Hk : 0) + seq * Hk + kvh;
     int f1 = 0, n1 = 0;
-    if (g.own_here && sp.len > 0) { f1 = g.item_first[own_item]; n1 = g.item_last[own_item] - f1 + 1; }
+    if (g.own_here && sp.len > 0) n1 = bj_parts(g, own_item, f1);
     BjKind kinds[3];
     const size_t at[3] = {(size_t)row * g.a.n_heads + h, (size_t)(kvh + f0) * g.item_rows + row * G + hg, (size_t)(own_item + f1) * g.item_rows + (row - sp.r0) * G + hg};
 #pragma unroll

@@ -222,7 +222,12 @@ __device__ __forceinline__ float ex2(float x)
 
 __device__ int batch_wait_error;                                      // set when a bounded wait ran out; swift_batch_sync reports it
 
-// A wait of one role: bounded, and over at once when another role has given up.
+// A wait of one role, by a whole warp: bounded, and over when another role has given up.  waits[0]: a role has given up;
+// waits[1]: the limit, in 1024 cycles.  The lanes must take the same answer (the warp goes on to shuffles and barriers of its
+// own) although each looks for itself: a lane leaves without success only BT_QUIET cycles after the giving up was
+// known, by when nothing on the SM moves any more, and with a last look that then shows all lanes the same.  A block that gave
+// up keeps its memory until what it asked for has landed (bt_give_up).
+constexpr long long BT_QUIET = 2000000LL;                             // about a millisecond
 __device__ __forceinline__ bool bt_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
@@ -230,26 +235,38 @@ __device__ __forceinline__ bool bt_try(uint32_t bar, uint32_t parity)
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __noinline__ bool bt_wait_long(uint32_t bar, uint32_t parity, volatile int* abort_sh)
+__device__ __noinline__ bool bt_wait_long(uint32_t bar, uint32_t parity, volatile int* waits)
 {
-    const long long t0 = clock64();
+    const long long t0 = clock64(), limit = (long long)waits[1] << 10;
+    long long over = 0;                                               // when this lane knew
     for (uint32_t it = 0;; ++it) {
         if (bt_try(bar, parity)) return true;
-        if ((it & 63u) == 63u) {
-            if (*abort_sh) return false;
-            if (clock64() - t0 > TC_WAIT_CYCLES) {
-                *abort_sh = 1;
-                atomicExch(&batch_wait_error, TC_ERR_TIMEOUT);
-                return false;
-            }
+        if ((it & 63u) != 63u) continue;
+        const long long now = clock64();
+        if (over) {
+            if (now - over > BT_QUIET) return bt_try(bar, parity);
+        } else if (waits[0]) {
+            over = now;
+        } else if (now - t0 > limit) {
+            over = now;
+            waits[0] = 1;
+            atomicExch(&batch_wait_error, TC_ERR_TIMEOUT);
         }
     }
 }
-__device__ __forceinline__ bool bt_wait(uint32_t bar, uint32_t parity, volatile int* abort_sh)
+__device__ __forceinline__ bool bt_wait(uint32_t bar, uint32_t parity, volatile int* waits)
 {
     for (int it = 0; it < 4; ++it)
         if (bt_try(bar, parity)) return true;
-    return bt_wait_long(bar, parity, abort_sh);
+    return bt_wait_long(bar, parity, waits);
+}
+// The end of a block, behind a barrier of all its threads: copies, products and answers still on their way after a wait that
+// ran out land before its memory is given back.
+__device__ __forceinline__ void bt_give_up(volatile int* waits)
+{
+    if (!waits[0]) return;
+    const long long t0 = clock64();
+    while (clock64() - t0 < BT_QUIET) { }
 }
 
 // ------------------------------------------------------------------------------ which piece next
@@ -276,7 +293,7 @@ __device__ __forceinline__ int bt_answer(uint32_t answer)             // the blo
 }
 template <bool PART> struct BtPieces {
     uint32_t answers, full, empty;                                    // two answers of 16 bytes, their barriers
-    volatile int* abort_sh;
+    volatile int* waits;
     int idx, n;
     __device__ __forceinline__ void begin() { idx = blockIdx.x; n = 0; }
     // K warp, before it starts on a piece
@@ -284,7 +301,7 @@ template <bool PART> struct BtPieces {
     {
         if (PART) return true;
         const uint32_t at = n & 1, turn = (n >> 1) & 1;
-        if (!bt_wait(empty + 8u * at, turn ^ 1u, abort_sh)) return false;
+        if (!bt_wait(empty + 8u * at, turn ^ 1u, waits)) return false;
         if (elect_one()) {
             mbar_expect_tx(full + 8u * at, 16u);
             bt_ask_piece(answers + 16u * at, full + 8u * at);
@@ -299,7 +316,7 @@ template <bool PART> struct BtPieces {
             return true;
         }
         const uint32_t at = n & 1, turn = (n >> 1) & 1;
-        ok = bt_wait(full + 8u * at, turn, abort_sh);
+        ok = bt_wait(full + 8u * at, turn, waits);
         if (!ok) return false;
         idx = bt_answer(answers + 16u * at);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -532,9 +549,9 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
     const uint32_t landed = b2 + 96u;
     const uint32_t piece_bars = b2 + 104u, answers = bars + S::BAR_BYTES - 32u;   // answers: 16-byte aligned
     __shared__ uint32_t tmem_base_sh;
-    __shared__ int abort_flag;
+    __shared__ int waits_sh[2];
     __shared__ unsigned page_bits[BT_PAGE_RING];                      // bit p: page p of that key tile lies in the pool
-    volatile int* abort_sh = &abort_flag;
+    volatile int* waits = waits_sh;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = g.a.n_heads / g.a.n_kv_heads, TQ = g.rows_per_tile;
@@ -547,7 +564,8 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             }
             mbar_init(landed, 1);
             for (int i = 0; i < 2; ++i) { mbar_init(piece_bars + 8u * i, 1); mbar_init(piece_bars + 16u + 8u * i, 11); }
-            abort_flag = 0;
+            waits[0] = 0;
+            waits[1] = g.a.wait_kcycles;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
@@ -562,7 +580,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base_sh;
-    BtPieces<PART> pieces = {answers, piece_bars, piece_bars + 16u, abort_sh, 0, 0};
+    BtPieces<PART> pieces = {answers, piece_bars, piece_bars + 16u, waits, 0, 0};
     pieces.begin();
     bool more_pieces = true;
     auto s_col = [&](int x) { return tmem + 128u * x; };              // S, then P, of tile x
@@ -588,7 +606,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (!ok || it.tiles[x] == 0) continue;
-                    ok = bt_wait(q_empty(x), q_turn[x] ^ 1u, abort_sh);
+                    ok = bt_wait(q_empty(x), q_turn[x] ^ 1u, waits);
                     q_turn[x] ^= 1u;
                     if (ok && elect_one()) {
                         mbar_expect_tx(q_full(x), (uint32_t)(TQ * G * 128 * HALVES));
@@ -620,15 +638,16 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 const int tail = left & (b.page_size - 1);            // slots of the last page that hold something
                 // a V tile with unwritten slots: they are zeroed before the product may read them
                 const bool mend = kv == 1 && left < BT_KEYS && tail != 0 && ((pages >> (left >> b.page_shift)) & 1u);
-                ok = bt_wait(empty(slot), turn ^ 1u, abort_sh);
+                ok = bt_wait(empty(slot), turn ^ 1u, waits);
                 if (!ok) break;
                 const uint32_t bar = mend ? landed : full(slot), dst = ring + slot * S::SLOT_BYTES;
+                const bool asks = !(g.a.withhold && kv == 0 && tile_no == 0);
                 if (elect_one()) {
                     if (kv == 0) page_bits[tile_no & (BT_PAGE_RING - 1)] = pages;
-                    mbar_expect_tx(bar, (uint32_t)S::SLOT_BYTES);
+                    if (asks) mbar_expect_tx(bar, (uint32_t)S::SLOT_BYTES);
                 }
                 __syncwarp();
-                for (int p = 0; p < per_tile; ++p) {
+                for (int p = 0; asks && p < per_tile; ++p) {
                     const int pg = __shfl_sync(FULL_WARP, page, p);
                     if (elect_one()) {
 #pragma unroll
@@ -636,7 +655,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                     }
                 }
                 if (mend) {
-                    ok = bt_wait(landed, landed_turn, abort_sh);
+                    ok = bt_wait(landed, landed_turn, waits);
                     landed_turn ^= 1u;
                     if (!ok) break;
                     const int row1 = ((left >> b.page_shift) + 1) << b.page_shift;
@@ -652,11 +671,6 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 slot += 2;
                 if (slot >= S::SLOTS) { slot -= S::SLOTS; turn ^= 1u; }
             }
-        }
-        // After a wait that ran out: the copies still on their way must land before the block's shared memory is given back.
-        if (!ok && lane == 0) {
-            const long long t0 = clock64();
-            while (clock64() - t0 < 2000000LL) { }                    // about a millisecond
         }
     } else if (warp == 9) {
         // ---------------------------------------------------------------- tensor pipe
@@ -684,7 +698,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 const uint64_t vd = tc_smem_desc_mn(v_sh);
 #pragma unroll
                 for (int h = 1; h >= 0; --h) {                        // the upper half of the keys is ready first
-                    if (!bt_wait(p_ready(x, h), p_turn[x], abort_sh)) return false;
+                    if (!bt_wait(p_ready(x, h), p_turn[x], waits)) return false;
                     tc_fence_after();
                     if (elect_one()) {
 #pragma unroll
@@ -697,9 +711,9 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             };
 #pragma unroll
             for (int x = 0; x < 2; ++x)
-                if (ok && it.tiles[x]) { ok = bt_wait(q_full(x), q_turn[x], abort_sh); q_turn[x] ^= 1u; }
+                if (ok && it.tiles[x]) { ok = bt_wait(q_full(x), q_turn[x], waits); q_turn[x] ^= 1u; }
             if (ok && n_tiles > 0) {
-                ok = bt_wait(full(slot), turn, abort_sh);
+                ok = bt_wait(full(slot), turn, waits);
                 tc_fence_after();
                 if (ok) {
 #pragma unroll
@@ -715,7 +729,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             for (int j = 0; ok && j < n_tiles; ++j) {
                 const uint32_t v_slot = slot, v_turn = turn;
                 if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
-                ok = bt_wait(full(v_slot), v_turn, abort_sh);
+                ok = bt_wait(full(v_slot), v_turn, waits);
                 const bool more = j + 1 < n_tiles;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -725,7 +739,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                     }
                     if (ok && x == 1) commit(empty(v_slot));
                     if (ok && j + 1 < it.tiles[x]) {
-                        ok = bt_wait(full(slot), turn, abort_sh);
+                        ok = bt_wait(full(slot), turn, waits);
                         if (ok) {
                             tc_fence_after();
                             scores(x, ring + slot * S::SLOT_BYTES);
@@ -760,7 +774,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             const int all_see = seen_own(it.sp, it.t0 + x * TQ);      // ... that every row of the tile sees
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < mine; ++j) {
-                ok = bt_wait(s_full(x), s_turn, abort_sh);
+                ok = bt_wait(s_full(x), s_turn, waits);
                 if (!ok) break;
                 s_turn ^= 1u;
                 tc_fence_after();
@@ -774,7 +788,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             tile_no += n_tiles;
             if (!ok) break;
             if (mine > 0) {
-                ok = bt_wait(o_full(x), o_turn, abort_sh);
+                ok = bt_wait(o_full(x), o_turn, waits);
                 if (!ok) break;
                 o_turn ^= 1u;
                 tc_fence_after();
@@ -806,6 +820,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
         }
     }
     __syncthreads();
+    bt_give_up(waits);
     pdl_wait();                                           // (a launch before this one in the same call ends first)
     if (warp == 9) {
         tc_fence_after();

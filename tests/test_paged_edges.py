@@ -152,3 +152,86 @@ def test_lengths_below_zero_and_row_starts_that_descend(form, each, dt):
     batch.append(0, q, k + 1, k + 1, out=rows.fill_(9.0))
     assert (out == 9).all() and (rows == 9).all()
     assert torch.equal(torch.nan_to_num(pool, nan=-1.0), torch.nan_to_num(before, nan=-1.0))
+
+
+# ----------------------------------------------------------------------------------------------- waits that run out
+WAITS = [
+    # rows of each of four sequences, cached, heads, kv heads, dim, type, prefix, form
+    (130, 500, 8, 2, 128, BF16, 0, "prompt"), (3, 300, 4, 4, 64, F16, 40, "prompt"),
+    (1, 3000, 8, 2, 128, BF16, 0, "prefix"), (2, 700, 8, 2, 64, F16, 500, "prefix"),            # the few-row kernel, its prefix too
+    (9, 900, 14, 2, 128, F16, 2000, "prefix"),                                                 # ... beside the many-row kernel
+    (40, 100, 8, 1, 128, BF16, 20000, "prefix"),                                                # the many-row kernel alone
+]
+
+
+def waits_run_out(case):
+    """In a process of its own: the probe gives up, the report comes once, the next call on the same workspace is right."""
+    import ctypes as C
+    import time
+    from paper_2410_06916_b200 import SwiftError, batch_sync, lib
+    from paper_2410_06916_b200.binding import _DevBuf
+    each, kv, H, Hk, dim, dt, prefix, form = case
+    b = Batch([each] * 4, [kv, kv - 9, kv // 2, kv], H, Hk, dim, 16, dt, prefix_len=prefix)
+    pool, batch = setup(b)
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    q = b.q.cuda()
+    rows = 0 if form == "prompt" else batch.max_rows
+    need = lib().swift_prefix_workspace_bytes(C.byref(batch.kv._c), C.byref(batch._c), H, max(rows, 1))
+    out = torch.empty_like(q)
+    a = batch._attention(0, q, None)
+    a.out = out.data_ptr()
+    stream = torch.cuda.current_stream().cuda_stream
+    for fill in (0, 0x7F, 0xFF, 0x01):
+        ws = torch.full((need,), fill, dtype=torch.uint8, device="cuda")       # what an entry no one wrote may hold
+        where = _DevBuf(ws.data_ptr(), need)
+        torch.cuda.synchronize()
+        t0 = time.monotonic()
+        assert lib().swift_probe_batch_wait_limit(C.byref(batch.kv._c), C.byref(batch._c), C.byref(a), rows, where, 1000, stream) == 0
+        try:
+            batch_sync()
+            raise AssertionError("no report")
+        except SwiftError as e:
+            assert "ETIMEOUT" in str(e), e
+        assert time.monotonic() - t0 < 5.0
+        batch_sync()
+        if form == "prefix":
+            assert lib().swift_prefix_attention(C.byref(batch.kv._c), C.byref(batch._c), C.byref(a), rows, where, stream) == 0
+        else:
+            assert lib().swift_prompt_attention(C.byref(batch.kv._c), C.byref(batch._c), C.byref(a), stream) == 0
+        batch_sync()
+        close(out, want, tol)
+
+
+def in_its_own_process(function, *args):
+    """Runs a function of this file in a fresh process: what it leaves behind on the device is no other test's."""
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = (f"import sys; sys.path[:0] = [{here!r}, {os.path.dirname(here)!r}]\nimport torch\nimport test_paged_edges as t\n"
+            f"t.{function}(*{args!r})\ntorch.cuda.synchronize()\nprint('fine')\n")
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "fine" in done.stdout, done.stderr[-2000:]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", WAITS, ids=lambda c: "-".join(str(x).replace("torch.", "") for x in c))
+def test_a_wait_that_runs_out_is_a_status(case):
+    """Copies that are never asked for: every block gives up within its limit, swift_batch_sync reports it once, and entries
+    of the workspace that were never written lead nowhere."""
+    in_its_own_process("waits_run_out", case)
+
+
+def test_the_wait_probe_refuses_what_has_no_waits():
+    import ctypes as C
+    from paper_2410_06916_b200 import lib, paged
+    from paper_2410_06916_b200.binding import _DevBuf
+    at = 1 << 20
+    batch = paged._Batch(2, 4, at, at, at, 4, None, 0)
+    args = paged._Attention(0, 4, paged._Rows(at, 256, 64), 0.125, at)
+    probe = lambda dtype, rows, ws, us: lib().swift_probe_batch_wait_limit(
+        C.byref(paged._Kv(at, dtype, 8, 1, 2, 16, 64)), C.byref(batch), C.byref(args), rows, ws, us, None)
+    ws = _DevBuf(at, 1 << 40)
+    assert probe(0, 4, ws, 100) == 6 and probe(0, 0, ws, 100) == 6
+    assert probe(1, 4, ws, 0) == 1 and probe(1, 4, ws, 100001) == 1 and probe(1, -1, ws, 100) == 1
+    assert probe(1, 4, _DevBuf(at, 16), 100) == 3 and probe(1, 4, _DevBuf(None, 0), 100) == 1
