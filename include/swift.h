@@ -445,6 +445,8 @@ swift_status swift_kv_append(const swift_paged_kv* kv, const swift_row_batch* ba
  * reads kv head h / (n_heads / n_kv_heads).  out[row][h][:] = softmax(scale * q k^T) v, the softmax and the sums in fp32;
  * a row that sees nothing gives 0.  q and out are of the cache's type, out [n_rows][n_heads][head_dim] contiguous;
  * where the tensor cores compute (below), both and q's strides are multiples of 16 bytes.  scale > 0.
+ * A score of NaN or +infinity makes its row NaN; one of -infinity (an overflowed key) counts as hidden, and a row all of whose
+ * scores are -infinity gives 0.
  * Cached values of visible positions must be finite for the rows that do not see them yet to stay so: a row's result may
  * be spoilt by a NaN or infinity in V of a later row of its own sequence, never by another sequence's.
  *

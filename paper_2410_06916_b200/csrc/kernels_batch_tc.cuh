@@ -208,6 +208,8 @@ __device__ __forceinline__ void split2(f32x2 v, float& a, float& b) { asm("mov.b
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+__device__ __forceinline__ float max2_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }   // NaN if any is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 // 32 bytes at once: a full sector per lane, where lanes write rows of their own (p 32-byte aligned)
 __device__ __forceinline__ void store32(void* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h)
 {
@@ -344,7 +346,7 @@ __device__ __forceinline__ unsigned bt_shown(unsigned pages, int page_shift, int
     return n >= 32 ? w : n <= 0 ? 0u : w & ((1u << n) - 1u);
 }
 
-// 2^x for two values on the multiply-add pipe, x in about [-126, 127] (below: 2^-126): x = n + f with n the nearest integer,
+// 2^x for two values on the multiply-add pipe, x in about [-126, 127] (below, and for NaN: 2^-126): x = n + f with n the nearest integer,
 // 2^f as a polynomial, n added to its exponent.  The coefficients minimise the largest relative error on [-1/2, 1/2] (a linear
 // programme over 2001 Chebyshev points): 7.5e-5 for degree 3, which is a fiftieth of half a step of bf16; 2.6e-6 for degree 4, with
 // which fp16's half step is 180 times as large.
@@ -391,15 +393,15 @@ __device__ __forceinline__ void bt_weights(const float (&s)[32], f32x2 c2, f32x2
         p[i] = pack2(p0, p1, T());
     }
 }
-__device__ __forceinline__ float bt_highest(const float (&s)[32])
+__device__ __forceinline__ float bt_highest(const float (&s)[32])      // NaN if any is
 {
     float x0 = s[0], x1 = s[1];
 #pragma unroll
     for (int i = 2; i < 30; i += 4) {
-        x0 = max3(x0, s[i], s[i + 1]);
-        x1 = max3(x1, s[i + 2], s[i + 3]);
+        x0 = max3_nan(x0, s[i], s[i + 1]);
+        x1 = max3_nan(x1, s[i + 2], s[i + 3]);
     }
-    return fmaxf(max3(x0, s[30], s[31]), x1);
+    return max2_nan(max3_nan(x0, s[30], s[31]), x1);
 }
 // P of half h of the keys is in TMEM: the MMA warp may use it.
 __device__ __forceinline__ void bt_hand_over(uint32_t p_bar, int h)
@@ -437,7 +439,7 @@ template <int DP> __device__ __forceinline__ void bt_rescale(uint32_t o_at, floa
 template <typename T, int DP, bool MASKED>
 __device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, int seen, unsigned pages, int page_shift, bool first, float& m, float& l)
 {
-    constexpr unsigned POLY = MASKED ? 0u : BT_POLY;                  // (the polynomial does not give 0 for a hidden key)
+    constexpr unsigned POLY = MASKED ? 0u : BT_POLY;                  // (the polynomial gives a hidden key 2^-126, not 0)
     auto hide = [&](int q, float (&s)[32]) {
         if (!MASKED) return;
         const unsigned shown = bt_shown(pages, page_shift, seen, q);
@@ -455,14 +457,17 @@ __device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_
     tmem_wait_ld(s1);
     tmem_ld32(s_at + 64, s2);
     hide(1, s1);
-    top = fmaxf(top, bt_highest(s1));
+    top = max2_nan(top, bt_highest(s1));
     tmem_wait_ld(s2);
     tmem_ld32(s_at + 96, s3);
     hide(2, s2);
-    top = fmaxf(top, bt_highest(s2));
+    top = max2_nan(top, bt_highest(s2));
     tmem_wait_ld(s3);
     hide(3, s3);
-    top = fmaxf(top, bt_highest(s3));
+    top = max2_nan(top, bt_highest(s3));
+    // A score of NaN or +infinity makes the row NaN, through l: the polynomial below would give such a key, and every key beside an
+    // infinite score, a weight near zero.
+    if (!(top < INFINITY)) l = __int_as_float(0x7FFFFFFF);
     const bool grown = bt_outgrown(top, m, c);
     if (__any_sync(FULL_WARP, grown)) bt_rescale<DP>(o_at, c, top, grown, first, m, l);
     const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
@@ -793,6 +798,7 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 o_turn ^= 1u;
                 tc_fence_after();
             }
+            if (m == -INFINITY && l == l) l = 0.f;                    // no score but -infinity: what the polynomial made of them does not count
             const int row = it.sp.r0 + t, head = it.kvh * G + head_in;
             if (PART) {
                 const size_t at = ((size_t)it.slot * b.n_rows + row) * g.a.n_heads + head;

@@ -235,3 +235,74 @@ def test_the_wait_probe_refuses_what_has_no_waits():
     assert probe(0, 4, ws, 100) == 6 and probe(0, 0, ws, 100) == 6
     assert probe(1, 4, ws, 0) == 1 and probe(1, 4, ws, 100001) == 1 and probe(1, -1, ws, 100) == 1
     assert probe(1, 4, _DevBuf(at, 16), 100) == 3 and probe(1, 4, _DevBuf(None, 0), 100) == 1
+
+
+# ----------------------------------------------------------------------------------------------- scores that are not finite
+SHAPES = [
+    # rows of each of two sequences, cached, heads, kv heads, dim, type, prefix: every kernel and form
+    (130, 400, 8, 2, 128, BF16, 0), (130, 400, 8, 2, 64, F16, 0),               # many rows
+    (40, 300, 8, 2, 128, F16, 300), (24, 300, 8, 1, 128, BF16, 2000),           # ... and a shared prefix
+    (3, 300, 8, 2, 128, BF16, 0), (9, 300, 8, 2, 64, F16, 0),                   # few rows
+    (200, 400, 8, 8, 36, F16, 0), (3, 200, 8, 2, 64, F32, 0),                   # fp32 arithmetic
+]
+SHAPE_IDS = lambda s: "-".join(str(x).replace("torch.", "") for x in s) if isinstance(s, tuple) else str(s)
+
+
+def edge_batch(shape):
+    each, kv, H, Hk, dim, dt, prefix = shape
+    b = Batch([each, each], [kv, kv - 7], H, Hk, dim, 32, dt, prefix_len=prefix)
+    b.q[:, :, 0] = b.q[:, :, 0].abs() + 0.25
+    return b
+
+
+def key_slot(b, i, p, head):
+    """Index of own position p of sequence i in K of a kv head, all dims."""
+    return int(b.page_table[i, p // b.page]), b.block, 0, head, p % b.page
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("shape", SHAPES, ids=SHAPE_IDS)
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+def test_a_visible_key_without_a_finite_score_shows_wherever_it_lies(form, shape, value):
+    """One dim of one cached key of sequence 0 is NaN or infinite, at 32 positions in turn that every row sees: the rows of its
+    group are NaN in every dim, those of the other sequence and the other kv head stay what they were."""
+    b = edge_batch(shape)
+    pool, batch = setup(b)
+    q, each, G = b.q.cuda(), b.n[0], b.heads // b.kv_heads
+    clean = call(batch, form)(0, q)
+    assert torch.isfinite(clean).all()
+    for p in range(64, 96):
+        at = key_slot(b, 0, p, 0)
+        was = pool[at].clone()
+        pool[at][0] = value
+        got = call(batch, form)(0, q)
+        pool[at] = was
+        assert torch.isnan(got[:each, :G]).all(), p
+        assert torch.equal(got[each:], clean[each:]) and torch.equal(got[:each, G:], clean[:each, G:]), p
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", SHAPES, ids=SHAPE_IDS)
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+def test_scores_of_minus_infinity_weigh_nothing(form, shape):
+    """Keys whose score is -infinity (a whole page of them, its first and last keys next to finite ones) count as hidden; rows that
+    see no other key give 0, as rows that see nothing."""
+    b = edge_batch(shape)
+    pool, batch = setup(b)
+    q = b.q.cuda()
+    hidden = edge_batch(shape)
+    hidden.page_table[0, 2] = hidden.n_pages
+    want, tol = attention(hidden, b.pool, b.q, dev="cuda")
+    low = -float("inf")
+    for p in range(64, 96):
+        for h in range(b.kv_heads):
+            pool[key_slot(b, 0, p, h)][0] = low
+    close(call(batch, form)(0, q), want, tol)
+    if b.prefix_len == 0:
+        for p in range(b.kv[0]):
+            pool[key_slot(b, 0, p, 0)][0] = low
+        got, G = call(batch, form)(0, q), b.heads // b.kv_heads
+        assert (got[:b.n[0], :G] == 0).all()
+        close(got[b.n[0]:], want[b.n[0]:], tol[b.n[0]:])
+        close(got[:b.n[0], G:], want[:b.n[0], G:], tol[:b.n[0], G:])
