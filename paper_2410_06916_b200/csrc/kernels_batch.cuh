@@ -449,11 +449,11 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
     if (seq < 0) return;                                  // the same for the whole block
     const int kvh = idx % Hk, rho0 = idx / Hk * ROWS, rows = min(ROWS, sp.n * G - rho0);
     const T* head = reinterpret_cast<const T*>(a.pool) + (size_t)kvh * b.page_size * D;
-    // ---- queries, scaled; dead rows and the dims behind the last are zero
+    // ---- queries; dead rows and the dims behind the last are zero
     for (int r = warp; r < ROWS; r += 4) {
         const int tok = (rho0 + r) / G;
         const T* src = reinterpret_cast<const T*>(a.q) + (long long)(sp.r0 + tok) * a.q_row_stride + (long long)(kvh * G + rho0 + r - tok * G) * a.q_head_stride;
-        for (int d = lane; d < ld; d += 32) q_sh[r * ld + d] = r < rows && d < D ? to_float(src[d]) * a.scale : 0.f;
+        for (int d = lane; d < ld; d += 32) q_sh[r * ld + d] = r < rows && d < D ? to_float(src[d]) : 0.f;
     }
     for (int i = tid; i < 2 * AF_KEYS * (ld - D); i += 128) k_sh[i / (ld - D) * ld + D + i % (ld - D)] = 0.f;
     const int grp = lane >> 3, sub = lane & 7, row0 = warp * RPW;     // this lane's rows of scores: row0 + grp + 4 r
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
             float top = m[r];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (p0 + sub + 8 * i >= seen[r] || !there[i]) s[r][i] = -INFINITY;
+                s[r][i] = p0 + sub + 8 * i >= seen[r] || !there[i] ? -INFINITY : s[r][i] * a.scale;     // scaled behind the sum, as the other kernels do
                 top = fmaxf(top, s[r][i]);
             }
 #pragma unroll

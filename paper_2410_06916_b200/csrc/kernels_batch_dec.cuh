@@ -377,8 +377,20 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch_dec_kernel(const __g
                     o[nt][2] *= shrink[1]; o[nt][3] *= shrink[1];
                 }
             }
+            bool far[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) off[e] = BIAS - (m[e] == -INFINITY ? 0.f : m[e] * c);
+            for (int e = 0; e < 2; ++e) {
+                off[e] = BIAS - (m[e] == -INFINITY ? 0.f : m[e] * c);
+                far[e] = fabsf(off[e]) > BT_FAR;
+            }
+            if (__builtin_expect(__any_sync(FULL_WARP, far[0] || far[1]), 0)) {
+                if (far[0]) off[0] = BIAS;
+                if (far[1]) off[1] = BIAS;
+#pragma unroll
+                for (int n = 0; n < KEYS / 8; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[n][e] -= far[e >> 1] ? m[e >> 1] : 0.f;
+            }
 #pragma unroll
             for (int n = 0; n < KEYS / 8; ++n)
 #pragma unroll

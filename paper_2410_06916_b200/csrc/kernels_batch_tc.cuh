@@ -411,6 +411,46 @@ __device__ __forceinline__ void bt_hand_over(uint32_t p_bar, int h)
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(p_bar + 8u * h);
 }
+// Scores are weighed as 2^(c s + off), off = BIAS - c m rounded once, in one multiply-add.  Where c m is large its rounding is too
+// (half a step of 2^30 is 32: a factor of 2^32 on all weights of the row, which no 16 bits hold), so beyond BT_FAR a row subtracts m
+// from its scores first, an addition per score.  Below it the factor is at most 2^(2^-11).
+constexpr float BT_FAR = 16384.f;
+// The weights of a key tile with such rows, from the scores in TMEM on: their sum.  Rare; called from one place outside the
+// softmax's common path, which keeps its registers (two calls inside it: 512 tokens 13.1 -> 13.8 us; in line: 8192 tokens 3 % more).
+template <typename T>
+__device__ __noinline__ float bt_weights_far(uint32_t s_at, uint32_t p_bar, float c, float m, int seen, unsigned pages, int page_shift)
+{
+    constexpr float BIAS = std::is_same<T, __half>::value ? 7.f : 0.f;
+    float off = BIAS - (m == -INFINITY ? 0.f : m * c);
+    const bool far = fabsf(off) > BT_FAR;
+    const float by = far ? m : 0.f;
+    if (far) off = BIAS;
+    const f32x2 c2 = pair2(c, c), off2 = pair2(off, off);
+    f32x2 sum[2] = {0ull, 0ull};
+#pragma unroll 1
+    for (int h = 1; h >= 0; --h) {                                    // the upper half of the keys goes first; both of its quarters are read before P overwrites them
+        float a[32], b[32];
+        uint32_t p[16];
+        tmem_ld32(s_at + 64 * h, a);
+        tmem_ld32(s_at + 64 * h + 32, b);
+        tmem_wait_ld(a);
+        tmem_wait_ld(b);
+        const unsigned shown[2] = {bt_shown(pages, page_shift, seen, 2 * h), bt_shown(pages, page_shift, seen, 2 * h + 1)};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            a[i] = (shown[0] >> i) & 1u ? a[i] - by : -INFINITY;
+            b[i] = (shown[1] >> i) & 1u ? b[i] - by : -INFINITY;
+        }
+        bt_weights<T, 0u>(a, c2, off2, sum, p);
+        tmem_st16(s_at + 64 + 32 * h, p);
+        bt_weights<T, 0u>(b, c2, off2, sum, p);
+        tmem_st16(s_at + 80 + 32 * h, p);
+        bt_hand_over(p_bar, h);
+    }
+    float l0, l1;
+    split2(add2(sum[0], sum[1]), l0, l1);
+    return l0 + l1;
+}
 // Whether a row's maximum has outgrown what its sums are scaled by.
 __device__ __forceinline__ bool bt_outgrown(float top, float m, float c) { return top > m && (m == -INFINITY || (top - m) * c > BT_GROW); }
 
@@ -435,9 +475,9 @@ template <int DP> __device__ __forceinline__ void bt_rescale(uint32_t o_at, floa
 // The softmax warps' part of one key tile: S in, P out (over the upper half of S), the row's maximum m and sum l brought up to
 // date.  s_at, o_at: this warp's lanes of S and O; p_bar: the two hand-over barriers.  Scores come a quarter (32 keys) at a
 // time; the upper half of the keys goes first.
-// MASKED: some keys are hidden from some rows.
+// MASKED: some keys are hidden from some rows.  False: m and O are up to date, but the weights are bt_weights_far's to make.
 template <typename T, int DP, bool MASKED>
-__device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, int seen, unsigned pages, int page_shift, bool first, float& m, float& l)
+__device__ __forceinline__ bool bt_softmax(uint32_t s_at, uint32_t o_at, uint32_t p_bar, float c, int seen, unsigned pages, int page_shift, bool first, float& m, float& l)
 {
     constexpr unsigned POLY = MASKED ? 0u : BT_POLY;                  // (the polynomial gives a hidden key 2^-126, not 0)
     auto hide = [&](int q, float (&s)[32]) {
@@ -471,6 +511,7 @@ __device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_
     const bool grown = bt_outgrown(top, m, c);
     if (__any_sync(FULL_WARP, grown)) bt_rescale<DP>(o_at, c, top, grown, first, m, l);
     const float off = BIAS - (m == -INFINITY ? 0.f : m * c);
+    if (__any_sync(FULL_WARP, fabsf(off) > BT_FAR)) return false;
     const f32x2 c2 = pair2(c, c), off2 = pair2(off, off);
     f32x2 sum[2] = {0ull, 0ull};
     uint32_t p[16];
@@ -493,6 +534,7 @@ __device__ __forceinline__ void bt_softmax(uint32_t s_at, uint32_t o_at, uint32_
     float l0, l1;
     split2(add2(sum[0], sum[1]), l0, l1);
     l += l0 + l1;
+    return true;
 }
 
 // A row's result to the output (a function of its own: inlined, its registers crowd out the softmax's).  Every lane takes
@@ -764,7 +806,6 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = s_col(x) + lanes, o_at = o_col(x) + lanes;
         const int tok = rho / G, head_in = rho - tok * G;
-        const float c = g.a.scale * 1.4426950408889634f;              // scores in powers of two
         const unsigned all_pages = 0xFFFFu >> (16 - (BT_KEYS >> b.page_shift));
         uint32_t s_turn = 0, o_turn = 0;
         int tile_no = 0;
@@ -775,6 +816,8 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
             const int n_tiles = max(it.tiles[0], it.tiles[1]), mine = it.tiles[x];
             const int t = it.t0 + x * TQ + tok;                       // token within the sequence
             const bool live = x < g.tiles && tok < TQ && t < it.sp.n && (g.mode == BT_PREFIX || t < g.a.max_rows);
+            // scores in powers of two; rows of the tile that belong to no token hold anything and must not ask for rescaling or the like
+            const float c = live ? g.a.scale * 1.4426950408889634f : 0.f;
             const int own_seen = seen_own(it.sp, t);                  // own keys that this row sees
             const int all_see = seen_own(it.sp, it.t0 + x * TQ);      // ... that every row of the tile sees
             float m = -INFINITY, l = 0.f;
@@ -787,8 +830,9 @@ attn_batch_tc_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_co
                 const int seen = j < it.np ? b.prefix_len - key0 : own_seen - key0;       // this row sees keys below this
                 const unsigned pages = page_bits[(tile_no + j) & (BT_PAGE_RING - 1)];
                 const bool masked = key0 + BT_KEYS > (j < it.np ? b.prefix_len : all_see) || pages != all_pages;
-                if (masked) bt_softmax<T, DP, true>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
-                else bt_softmax<T, DP, false>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
+                const bool done = masked ? bt_softmax<T, DP, true>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l)
+                                         : bt_softmax<T, DP, false>(s_at, o_at, p_ready(x, 0), c, seen, pages, b.page_shift, j == 0, m, l);
+                if (!done) l += bt_weights_far<T>(s_at, p_ready(x, 0), c, m, seen, pages, b.page_shift);
             }
             tile_no += n_tiles;
             if (!ok) break;

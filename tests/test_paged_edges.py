@@ -306,3 +306,36 @@ def test_scores_of_minus_infinity_weigh_nothing(form, shape):
         assert (got[:b.n[0], :G] == 0).all()
         close(got[b.n[0]:], want[b.n[0]:], tol[b.n[0]:])
         close(got[:b.n[0], G:], want[:b.n[0], G:], tol[:b.n[0], G:])
+
+
+# ----------------------------------------------------------------------------------------------- scores far from zero
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [None, 0.0371, 0.31, 0.77])
+@pytest.mark.parametrize("shape", SHAPES, ids=SHAPE_IDS)
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+def test_scores_far_from_zero(form, shape, scale):
+    """q and K hold +-2^14 (fp32, bf16: +-2^17), so that every product and every partial sum of a score is at most 128 times 2^28
+    (2^34): exact in fp32 in any order.  Two scores are equal or at least 2^29 (2^35) times the scale apart, so the exact
+    weights are equal for the keys with a row's highest score and below 2^-1000 for all others: the result is the mean of those
+    keys' V.  Errors: the weights' common factor cancels but for their rounding (2 h) and that of sums of N terms (2 N u), and
+    the result is rounded once (h)."""
+    b = edge_batch(shape)
+    g = torch.Generator().manual_seed(11)
+    big = 2.0 ** (14 if b.dtype == F16 else 17)
+    signs = lambda t: torch.where(torch.rand(t.shape, generator=g) < 0.5, -big, big).to(t.dtype)
+    b.q[:] = signs(b.q)
+    b.pool[:, :, 0] = torch.where(torch.isnan(b.pool[:, :, 0]), b.pool[:, :, 0], signs(b.pool[:, :, 0]))
+    pool, batch = setup(b)
+    got = call(batch, form)(0, b.q.cuda(), scale=scale).to(F64).cpu()
+    G, h, u = b.heads // b.kv_heads, half_step(b.dtype), 2.0 ** -24
+    assert torch.isfinite(got).all()
+    for i, n in enumerate(b.n):
+        page, slot, own = (torch.tensor([x[j] for x in b.visible(i)]) for j in range(3))
+        kv = b.pool[page, b.block, :, :, slot].to(F64)
+        k, v = (kv[:, j].repeat_interleave(G, dim=1) for j in range(2))
+        s = torch.einsum("rhd,nhd->hrn", b.q[b.start[i]:b.start[i] + n].to(F64), k)
+        last = torch.arange(n) + (b.kv[i] - n)
+        s = s.masked_fill(((own[None] >= 0) & (own[None] > last[:, None]))[None], -float("inf"))
+        best = (s == s.amax(-1, keepdim=True)).to(F64)
+        want, size = (torch.einsum("hrn,nhd->rhd", best, x) / best.sum(-1).T[..., None] for x in (v, v.abs()))
+        close(got[b.start[i]:b.start[i] + n], want, h * want.abs() + (2 * h + 2 * len(page) * u) * size)
