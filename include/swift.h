@@ -481,8 +481,9 @@ swift_status swift_probe_batch_wait_limit(const swift_paged_kv* kv, const swift_
                                           int32_t max_rows, swift_devbuf workspace, int32_t limit_us, void* cuda_stream);
 
 /* Waits for the stream's work and reports what only the device knows: SWIFT_ETIMEOUT when a bounded device-side wait of
- * one of the attention calls above ran out on this device since the last report (the outputs of that call are then not
- * complete), SWIFT_ECUDA when the work failed, else SWIFT_OK.  Not inside a stream capture. */
+ * one of the attention calls above ran out on this device, on whichever stream, since this call last reported for this stream
+ * (for a stream's first report: since the library was loaded); the outputs of some call are then not complete.  SWIFT_ECUDA
+ * when the work failed, else SWIFT_OK.  Not inside a stream capture. */
 swift_status swift_batch_sync(void* cuda_stream);
 
 #ifdef __cplusplus

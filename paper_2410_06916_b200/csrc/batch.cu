@@ -495,6 +495,41 @@ cudaError_t launch_append(const BatchView& b, const AppendView& a, bool vec, cud
     }
 }
 
+// What each stream's last report saw of its device's count of waits that ran out (batch_waits_over): the device's count is never
+// cleared, so a report to one stream takes nothing from another, nor from a wait that runs out meanwhile.  Streams are known by
+// their ids, which a process uses once.  When more streams report than there is room for, the one whose report is the oldest is
+// forgotten and counts from 0 again: told twice rather than never.
+class Reports {
+public:
+    bool changed(int dev, unsigned long long stream, unsigned count)
+    {
+        while (busy.test_and_set(std::memory_order_acquire)) { }      // a few comparisons long
+        Entry* e = nullptr;
+        for (int i = 0; i < ENTRIES; ++i)
+            if (entries[i].age != 0 && entries[i].dev == dev && entries[i].stream == stream) e = &entries[i];
+        if (!e) {
+            e = &entries[0];
+            for (int i = 1; i < ENTRIES; ++i)
+                if (entries[i].age < e->age) e = &entries[i];
+            e->dev = dev;
+            e->stream = stream;
+            e->seen = 0;
+        }
+        const bool news = e->seen != count;
+        e->seen = count;
+        e->age = ++clock;
+        busy.clear(std::memory_order_release);
+        return news;
+    }
+private:
+    static constexpr int ENTRIES = 256;
+    struct Entry { unsigned long long age, stream; int dev; unsigned seen; };     // age 0: free
+    Entry entries[ENTRIES] = {};
+    unsigned long long clock = 0;
+    std::atomic_flag busy = ATOMIC_FLAG_INIT;
+};
+Reports g_reports;
+
 // limit_us > 0: the probe of swift_probe_batch_wait_limit.
 void set_probe(AttnView* av, int limit_us)
 {
@@ -669,17 +704,16 @@ swift_status swift_probe_batch_wait_limit(const swift_paged_kv* kv, const swift_
 
 swift_status swift_batch_sync(void* cuda_stream)
 {
-    int error = 0;
+    unsigned count = 0;
+    int dev = 0;
+    unsigned long long id = 0;
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(&error, batch_wait_error, sizeof error, 0, cudaMemcpyDeviceToHost, s);
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaStreamGetId(s, &id);
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbolAsync(&count, batch_waits_over, sizeof count, 0, cudaMemcpyDeviceToHost, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "the stream's work failed: %s", cudaGetErrorString(e));
-    if (error) {
-        const int none = 0;
-        e = cudaMemcpyToSymbolAsync(batch_wait_error, &none, sizeof none, 0, cudaMemcpyHostToDevice, s);
-        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-        return fail_batch(SWIFT_ETIMEOUT, "a device-side wait of an attention call ran out of time");
-    }
+    if (g_reports.changed(dev, id, count)) return fail_batch(SWIFT_ETIMEOUT, "a device-side wait of an attention call ran out of time");
     return SWIFT_OK;
 }
 

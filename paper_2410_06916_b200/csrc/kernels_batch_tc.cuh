@@ -222,7 +222,7 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-__device__ int batch_wait_error;                                      // set when a bounded wait ran out; swift_batch_sync reports it
+__device__ unsigned batch_waits_over;                                 // bounded waits that ran out since the library was loaded (modulo 2^32); never cleared
 
 // A wait of one role, by a whole warp: bounded, and over when another role has given up.  waits[0]: a role has given up;
 // waits[1]: the limit, in 1024 cycles.  The lanes must take the same answer (the warp goes on to shuffles and barriers of its
@@ -252,7 +252,7 @@ __device__ __noinline__ bool bt_wait_long(uint32_t bar, uint32_t parity, volatil
         } else if (now - t0 > limit) {
             over = now;
             waits[0] = 1;
-            atomicExch(&batch_wait_error, TC_ERR_TIMEOUT);
+            atomicAdd(&batch_waits_over, 1u);
         }
     }
 }

@@ -214,6 +214,47 @@ def in_its_own_process(function, *args):
     assert done.returncode == 0 and "fine" in done.stdout, done.stderr[-2000:]
 
 
+def every_stream_is_told():
+    """A wait that runs out is reported once to every stream that asks, whoever asks first, and to threads side by side."""
+    import ctypes as C
+    import threading
+    from paper_2410_06916_b200 import SwiftError, batch_sync, lib
+    from paper_2410_06916_b200.binding import _DevBuf
+    b = Batch([40], [300], 8, 2, 128, 16, BF16)
+    pool, batch = setup(b)
+    q = b.q.cuda()
+    out = torch.empty_like(q)
+    a = batch._attention(0, q, None)
+    a.out = out.data_ptr()
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    torch.cuda.synchronize()
+
+    def told(s):
+        try:
+            batch_sync(stream=s)
+            return False
+        except SwiftError as e:
+            assert "ETIMEOUT" in str(e), e
+            return True
+    assert not any(told(s) for s in streams)
+    for _ in range(3):
+        assert lib().swift_probe_batch_wait_limit(C.byref(batch.kv._c), C.byref(batch._c), C.byref(a), 0, _DevBuf(None, 0), 500,
+                                                  streams[1].cuda_stream) == 0
+        streams[1].synchronize()
+        got = [None] * 4
+        threads = [threading.Thread(target=lambda i=i: got.__setitem__(i, told(streams[i]))) for i in range(4)]
+        [t.start() for t in threads], [t.join() for t in threads]
+        assert got == [True] * 4, got
+        assert not any(told(s) for s in streams)
+    assert told(torch.cuda.current_stream())                             # its first report
+    assert not told(torch.cuda.current_stream())
+
+
+@pytest.mark.gpu
+def test_a_report_takes_nothing_from_other_streams():
+    in_its_own_process("every_stream_is_told")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("case", WAITS, ids=lambda c: "-".join(str(x).replace("torch.", "") for x in c))
 def test_a_wait_that_runs_out_is_a_status(case):
