@@ -81,12 +81,19 @@ class _Target:
             g.__exit__(*exc)
 
 
-def _on(device: torch.device, stream: Optional[torch.cuda.Stream], call, *args):
-    """call(raw stream, *args) with `device` current, on `stream` or else the device's current stream."""
+def _on(device: torch.device, stream: Optional[torch.cuda.Stream], used, call, *args):
+    """call(raw stream, *args) with `device` current, on `stream` or else the device's current stream.  used: the caller's tensors
+    the call's work touches (or None); those lent to another stream are marked, so that the allocator does not hand out the memory
+    of one that is freed while that stream still works on it."""
     if stream is None and torch.cuda.current_device() == device.index:
         return call(_raw_stream(device.index), *args)
     with _Target(device, stream):
-        return call(_raw_stream(device.index), *args)
+        result = call(_raw_stream(device.index), *args)
+    if stream is not None:
+        for t in used:
+            if t is not None:
+                t.record_stream(stream)
+    return result
 
 
 def _cuda_tensor(name: str, t: torch.Tensor, device: Optional[torch.device] = None) -> torch.Tensor:
@@ -120,7 +127,7 @@ def rope_table(n_positions: int, rotary_dim: int, theta: float = 10000.0, factor
     desc = _RopeDesc(n_positions, rotary_dim, theta, factor, original_positions, low_turns, high_turns, magnitude)
     if n_positions < 0 or rotary_dim < 2:
         raise ValueError("n_positions >= 0 and rotary_dim >= 2")
-    return _on(device, stream, _rope_table, desc, device, out)
+    return _on(device, stream, (out,), _rope_table, desc, device, out)
 
 
 def _rope_table(s: int, desc: _RopeDesc, device: torch.device, out: Optional[torch.Tensor]) -> torch.Tensor:
@@ -155,7 +162,8 @@ class RowBatch:
     prefix_pages, prefix_len: a prefix that all sequences continue (its pages, its length in positions)
 
     The tensors are read on the device when a call's work runs; they may be rewritten between calls, and between replays
-    of a captured graph.
+    of a captured graph.  Calls work on the device's current stream, or on `stream`, which the caller has made wait for what its
+    tensors still wait for; tensors lent to it may be freed at any time.
     """
 
     def __init__(self, kv: PagedKV, row_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, n_rows: int,
@@ -177,6 +185,7 @@ class RowBatch:
         self.kv, self.n_seqs, self.n_rows = kv, n_seqs, n_rows
         self.max_rows = max(1, n_rows if max_rows is None else min(max_rows, n_rows))
         self._keep = (row_start, kv_len, page_table, prefix_pages)
+        self._tensors = (kv.pool, *self._keep)
         self._c = _Batch(n_seqs, n_rows, row_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), page_table.shape[1],
                          prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len)
         self._kv_p, self._c_p = C.byref(kv._c), C.byref(self._c)
@@ -244,7 +253,7 @@ class RowBatch:
                 raise ValueError(f"positions must be [{self.n_rows}]")
             positions_p = positions.data_ptr()
         a = _Append(block, q.shape[1], _TYPES[q.dtype], *rows, q_gain_p, k_gain_p, eps, rope_p, rope_rows, 2 * pairs, 1 if interleaved else 0, positions_p, None)
-        return _on(kv.device, stream, self._append, a, out)
+        return _on(kv.device, stream, (q, k, v, rope, q_gain, k_gain, positions, out, *self._tensors), self._append, a, out)
 
     def _append(self, s: int, a: _Append, out: Optional[torch.Tensor]) -> torch.Tensor:
         out = self._out(out, a.n_heads)
@@ -260,7 +269,7 @@ class RowBatch:
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Causal attention of every row over the prefix and its sequence's own positions up to its own; [n_rows, heads,
         head_dim] in the cache's type.  scale defaults to head_dim ** -0.5.  Padding rows keep what `out` held."""
-        return _on(self.kv.device, stream, self._prompt, self._attention(block, q, scale), out)
+        return _on(self.kv.device, stream, (q, out, *self._tensors), self._prompt, self._attention(block, q, scale), out)
 
     def _prompt(self, s: int, a: _Attention, out: Optional[torch.Tensor]) -> torch.Tensor:
         out = self._out(out, a.n_heads)
@@ -272,7 +281,7 @@ class RowBatch:
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The same function for few rows per sequence: what all rows share of the prefix is computed once for all of them.
         Rows of a sequence beyond max_rows are left out."""
-        return _on(self.kv.device, stream, self._prefix, self._attention(block, q, scale), out)
+        return _on(self.kv.device, stream, (q, out, *self._tensors), self._prefix, self._attention(block, q, scale), out)
 
     def _prefix(self, s: int, a: _Attention, out: Optional[torch.Tensor]) -> torch.Tensor:
         need = self._ws_bytes.get(a.n_heads)
@@ -295,4 +304,4 @@ def batch_sync(device="cuda", stream: Optional[torch.cuda.Stream] = None) -> Non
         raise ValueError("batch_sync needs a CUDA device")
     if device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
-    _on(device, stream, lambda s: _check(lib().swift_batch_sync(s)))
+    _on(device, stream, (), lambda s: _check(lib().swift_batch_sync(s)))

@@ -380,3 +380,57 @@ def test_scores_far_from_zero(form, shape, scale):
         best = (s == s.amax(-1, keepdim=True)).to(F64)
         want, size = (torch.einsum("hrn,nhd->rhd", best, x) / best.sum(-1).T[..., None] for x in (v, v.abs()))
         close(got[b.start[i]:b.start[i] + n], want, h * want.abs() + (2 * h + 2 * len(page) * u) * size)
+
+
+# ----------------------------------------------------------------------------------------------- tensors of other streams
+@pytest.mark.gpu
+def test_tensors_freed_behind_a_call_on_another_stream_stay_until_it_is_done():
+    """Everything a call takes is dropped right behind it and its sizes are asked for again on the tensors' own stream, while the
+    given stream still waits in front of the call: the call reads and writes what it was given."""
+    from paper_2410_06916_b200 import PagedKV, RowBatch, rope_table
+    b = Batch([70, 5], [200, 150], 8, 2, 128, 16, BF16, prefix_len=40)
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    g = torch.Generator().manual_seed(3)
+    host = [b.q] + [torch.randn(75, 2, 128, generator=g).to(BF16) for _ in range(2)]
+    gain = 1 + 0.1 * torch.randn(128, generator=g)
+    rope = rope_table(300, 128)
+    s = torch.cuda.Stream()
+
+    def fresh():
+        (start, kv, table), kw = b.device_args()
+        pool = b.pool.cuda()
+        return pool, RowBatch(PagedKV(pool), start, kv, table, **kw)
+
+    def overwrite(sizes):
+        return [torch.full((n,), 0x7B, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(8)]
+
+    def nbytes(*tensors):
+        return [t.numel() * t.element_size() for t in tensors]
+    pool, batch = fresh()
+    plain = batch.append(0, *(t.cuda() for t in host), rope=rope, q_gain=gain.cuda(), k_gain=gain.cuda()), pool.clone()
+    for form in ("prompt", "prefix", "append"):
+        pool, batch = fresh()
+        x, gains = [t.cuda() for t in host], gain.cuda()
+        sizes = nbytes(*x, gains, *batch._keep)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(40_000_000)                                # about 20 ms
+        if form == "append":
+            table = rope.clone()
+            s.wait_stream(torch.cuda.current_stream())
+            sizes += nbytes(table)
+            got = batch.append(0, *x, rope=table, q_gain=gains, k_gain=gains, stream=s)
+            del table
+        else:
+            got = call(batch, form)(0, x[0], stream=s)
+            sizes += nbytes(pool)
+        assert not s.query()
+        kept = pool if form == "append" else None
+        del x, gains, pool, batch
+        taken = overwrite(sizes)
+        torch.cuda.synchronize()
+        if form == "append":
+            assert torch.equal(got, plain[0]) and torch.equal(torch.nan_to_num(kept, nan=-1.0), torch.nan_to_num(plain[1], nan=-1.0))
+        else:
+            close(got, want, tol)
+        del taken, kept, got
