@@ -104,6 +104,12 @@ def _cuda_tensor(name: str, t: torch.Tensor, device: Optional[torch.device] = No
     return t
 
 
+def _gradient(name: str) -> None:
+    """For a tensor that requires a gradient: the calls have no backward pass, and a result that silently drops it is wrong."""
+    if torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which these calls do not have: detach it, or call under torch.no_grad()")
+
+
 def _int32(name: str, t: torch.Tensor, device: torch.device) -> torch.Tensor:
     _cuda_tensor(name, t, device)
     if t.dtype != torch.int32 or not t.is_contiguous():
@@ -122,6 +128,8 @@ def rope_table(n_positions: int, rotary_dim: int, theta: float = 10000.0, factor
         raise ValueError("rope_table needs a CUDA device")
     if device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
+    if out is not None and out.requires_grad:
+        _gradient("out")
     if out is not None and (out.dtype != torch.float32 or not out.is_contiguous() or tuple(out.shape) != (n_positions, rotary_dim // 2, 2)):
         raise ValueError("out must be contiguous float32 [n_positions, rotary_dim / 2, 2]")
     desc = _RopeDesc(n_positions, rotary_dim, theta, factor, original_positions, low_turns, high_turns, magnitude)
@@ -144,6 +152,8 @@ class PagedKV:
 
     def __init__(self, pool: torch.Tensor):
         _cuda_tensor("pool", pool)
+        if pool.requires_grad:
+            _gradient("pool")
         if pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_contiguous() or pool.dtype not in _TYPES:
             raise ValueError("pool must be contiguous [n_pages, n_blocks, 2, n_kv_heads, page_size, head_dim] in fp32, bf16 or fp16")
         self.pool, self.device, self.dtype = pool, pool.device, pool.dtype
@@ -200,6 +210,8 @@ class RowBatch:
         shape = t.shape
         if len(shape) != 3 or shape[0] != self.n_rows or shape[2] != kv.head_dim or (heads is not None and shape[1] != heads):
             raise ValueError(f"{name} must be [{self.n_rows}, {heads if heads is not None else 'heads'}, {kv.head_dim}], got {tuple(shape)}")
+        if t.requires_grad:
+            _gradient(name)
         if t.dtype not in dtypes:
             raise TypeError(f"{name} must be one of {dtypes}, got {t.dtype}")
         row, head, dim = t.stride()
@@ -210,6 +222,8 @@ class RowBatch:
 
     def _gain(self, name: str, g: torch.Tensor) -> int:
         _cuda_tensor(name, g, self.kv.device)
+        if g.requires_grad:
+            _gradient(name)
         if g.dtype != torch.float32 or g.shape != (self.kv.head_dim,) or not g.is_contiguous():
             raise ValueError(f"{name} must be contiguous float32 [{self.kv.head_dim}]")
         return g.data_ptr()
@@ -220,6 +234,8 @@ class RowBatch:
             return torch.empty(self.n_rows, heads, kv.head_dim, dtype=kv.dtype, device=kv.device)
         if not isinstance(out, torch.Tensor) or out.device != kv.device:
             _cuda_tensor("out", out, kv.device)
+        if out.requires_grad:
+            _gradient("out")
         if out.shape != (self.n_rows, heads, kv.head_dim) or out.dtype != kv.dtype or not out.is_contiguous():
             raise ValueError(f"out must be contiguous {(self.n_rows, heads, kv.head_dim)} of {kv.dtype}")
         return out
@@ -243,6 +259,8 @@ class RowBatch:
         rope_p, rope_rows, pairs = None, 0, 0
         if rope is not None:
             _cuda_tensor("rope", rope, kv.device)
+            if rope.requires_grad:
+                _gradient("rope")
             shape = rope.shape
             if rope.dtype != torch.float32 or len(shape) != 3 or shape[2] != 2 or not rope.is_contiguous() or 2 * shape[1] > kv.head_dim:
                 raise ValueError("rope must be a rope_table of at most head_dim dims")
@@ -253,7 +271,7 @@ class RowBatch:
                 raise ValueError(f"positions must be [{self.n_rows}]")
             positions_p = positions.data_ptr()
         a = _Append(block, q.shape[1], _TYPES[q.dtype], *rows, q_gain_p, k_gain_p, eps, rope_p, rope_rows, 2 * pairs, 1 if interleaved else 0, positions_p, None)
-        return _on(kv.device, stream, (q, k, v, rope, q_gain, k_gain, positions, out, *self._tensors), self._append, a, out)
+        return _on(kv.device, stream, () if stream is None else (q, k, v, rope, q_gain, k_gain, positions, out, *self._tensors), self._append, a, out)
 
     def _append(self, s: int, a: _Append, out: Optional[torch.Tensor]) -> torch.Tensor:
         out = self._out(out, a.n_heads)
@@ -269,7 +287,7 @@ class RowBatch:
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Causal attention of every row over the prefix and its sequence's own positions up to its own; [n_rows, heads,
         head_dim] in the cache's type.  scale defaults to head_dim ** -0.5.  Padding rows keep what `out` held."""
-        return _on(self.kv.device, stream, (q, out, *self._tensors), self._prompt, self._attention(block, q, scale), out)
+        return _on(self.kv.device, stream, () if stream is None else (q, out, *self._tensors), self._prompt, self._attention(block, q, scale), out)
 
     def _prompt(self, s: int, a: _Attention, out: Optional[torch.Tensor]) -> torch.Tensor:
         out = self._out(out, a.n_heads)
@@ -281,7 +299,7 @@ class RowBatch:
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The same function for few rows per sequence: what all rows share of the prefix is computed once for all of them.
         Rows of a sequence beyond max_rows are left out."""
-        return _on(self.kv.device, stream, (q, out, *self._tensors), self._prefix, self._attention(block, q, scale), out)
+        return _on(self.kv.device, stream, () if stream is None else (q, out, *self._tensors), self._prefix, self._attention(block, q, scale), out)
 
     def _prefix(self, s: int, a: _Attention, out: Optional[torch.Tensor]) -> torch.Tensor:
         need = self._ws_bytes.get(a.n_heads)

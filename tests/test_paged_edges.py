@@ -434,3 +434,33 @@ def test_tensors_freed_behind_a_call_on_another_stream_stay_until_it_is_done():
         else:
             close(got, want, tol)
         del taken, kept, got
+
+
+# ----------------------------------------------------------------------------------------------- refusals of the torch side
+@pytest.mark.gpu
+def test_tensors_that_require_gradients_are_refused():
+    """No call has a backward pass: what autograd would follow is refused, and taken under no_grad."""
+    from paper_2410_06916_b200 import rope_table
+    b = Batch([3, 2], [3, 9], 4, 2, 64, 16, BF16)
+    pool, batch = setup(b)
+    q = b.q.cuda()
+    k = q[:, :2].contiguous()
+    rope, gain = rope_table(16, 64), torch.ones(64, device="cuda")
+    leaf = lambda t: t.clone().requires_grad_()
+    calls = [lambda: batch.append(0, leaf(q), k, k), lambda: batch.append(0, q, leaf(k), k), lambda: batch.append(0, q, k, leaf(k)),
+             lambda: batch.append(0, q, k, k, q_gain=leaf(gain)), lambda: batch.append(0, q, k, k, k_gain=leaf(gain)),
+             lambda: batch.append(0, q, k, k, rope=leaf(rope)), lambda: batch.append(0, q, k, k, out=leaf(q)),
+             lambda: batch.append(0, leaf(q.float()) * 1.0, k.float(), k.float()),
+             lambda: batch.prompt_attention(0, leaf(q)), lambda: batch.prefix_attention(0, leaf(q)),
+             lambda: batch.prompt_attention(0, q, out=leaf(q)), lambda: batch.prefix_attention(0, q, out=leaf(q)),
+             lambda: rope_table(16, 64, out=leaf(rope))]
+    before = pool.clone()
+    for f in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            f()
+    assert torch.equal(torch.nan_to_num(pool, nan=-1.0), torch.nan_to_num(before, nan=-1.0))
+    with torch.no_grad():
+        for f in calls:
+            assert not f().requires_grad or f is calls[6] or f in calls[10:]
+    with torch.inference_mode():
+        assert torch.equal(batch.prompt_attention(0, q), batch.prompt_attention(0, leaf(q)))
