@@ -104,6 +104,13 @@ def _cuda_tensor(name: str, t: torch.Tensor, device: Optional[torch.device] = No
     return t
 
 
+def _number(name: str, value: int) -> int:
+    """An integer that fits the C structures' 32 bits (ctypes would cut it to them)."""
+    if not -(1 << 31) <= value < 1 << 31:
+        raise ValueError(f"{name} {value} does not fit 32 bits")
+    return value
+
+
 def _gradient(name: str) -> None:
     """For a tensor that requires a gradient: the calls have no backward pass, and a result that silently drops it is wrong."""
     if torch.is_grad_enabled():
@@ -123,6 +130,8 @@ def rope_table(n_positions: int, rotary_dim: int, theta: float = 10000.0, factor
     """fp32 [n_positions, rotary_dim / 2, 2]: (cos, sin) of every position and pair.  factor > 1 stretches the positions: all
     alike (original_positions 0), or by parts with low_turns / high_turns as the ramp (LLaMA 3: 1 and 4; YaRN: 1 and 32,
     with magnitude = 0.1 ln(factor) + 1)."""
+    for name, value in (("n_positions", n_positions), ("rotary_dim", rotary_dim), ("original_positions", original_positions)):
+        _number(name, value)
     device = torch.device(device) if out is None else _cuda_tensor("out", out).device
     if device.type != "cuda":
         raise ValueError("rope_table needs a CUDA device")
@@ -189,6 +198,7 @@ class RowBatch:
             raise ValueError("row_start [n_seqs + 1], kv_len [n_seqs], page_table [n_seqs, stride]")
         if n_rows < 0 or prefix_len < 0 or (max_rows is not None and max_rows < 1):
             raise ValueError("n_rows and prefix_len must not be negative, max_rows at least 1")
+        _number("n_rows", n_rows), _number("prefix_len", prefix_len)
         if prefix_len > 0:
             if prefix_pages is None or _int32("prefix_pages", prefix_pages, dev).numel() * kv.page_size < prefix_len:
                 raise ValueError("prefix_pages must hold prefix_len positions")
@@ -270,7 +280,7 @@ class RowBatch:
             if tuple(_int32("positions", positions, kv.device).shape) != (self.n_rows,):
                 raise ValueError(f"positions must be [{self.n_rows}]")
             positions_p = positions.data_ptr()
-        a = _Append(block, q.shape[1], _TYPES[q.dtype], *rows, q_gain_p, k_gain_p, eps, rope_p, rope_rows, 2 * pairs, 1 if interleaved else 0, positions_p, None)
+        a = _Append(_number("block", block), q.shape[1], _TYPES[q.dtype], *rows, q_gain_p, k_gain_p, eps, rope_p, rope_rows, 2 * pairs, 1 if interleaved else 0, positions_p, None)
         return _on(kv.device, stream, () if stream is None else (q, k, v, rope, q_gain, k_gain, positions, out, *self._tensors), self._append, a, out)
 
     def _append(self, s: int, a: _Append, out: Optional[torch.Tensor]) -> torch.Tensor:
@@ -281,7 +291,7 @@ class RowBatch:
 
     def _attention(self, block: int, q: torch.Tensor, scale: Optional[float]) -> _Attention:
         rows = self._rows("q", q, None, self._types)
-        return _Attention(block, q.shape[1], rows, self._scale if scale is None else scale, None)
+        return _Attention(_number("block", block), q.shape[1], rows, self._scale if scale is None else scale, None)
 
     def prompt_attention(self, block: int, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:

@@ -464,3 +464,31 @@ def test_tensors_that_require_gradients_are_refused():
             assert not f().requires_grad or f is calls[6] or f in calls[10:]
     with torch.inference_mode():
         assert torch.equal(batch.prompt_attention(0, q), batch.prompt_attention(0, leaf(q)))
+
+
+@pytest.mark.parametrize("kw", [dict(n_positions=(1 << 32) + 8), dict(n_positions=1 << 31), dict(rotary_dim=(1 << 32) + 64),
+                                dict(original_positions=1 << 32), dict(n_positions=-(1 << 32) + 8)], ids=str)
+def test_numbers_beyond_32_bits_are_refused(kw):
+    """... rather than cut to their low bits: a table of 2^32 + 8 positions had 8."""
+    from paper_2410_06916_b200 import rope_table
+    args = dict(n_positions=8, rotary_dim=64, device="cuda:0")
+    args.update(kw)
+    with pytest.raises(ValueError, match="32 bits"):
+        rope_table(**args)
+
+
+@pytest.mark.gpu
+def test_blocks_and_lengths_beyond_32_bits_are_refused():
+    from paper_2410_06916_b200 import PagedKV, RowBatch
+    b = Batch([3, 2], [3, 9], 4, 2, 64, 16, BF16)
+    pool, batch = setup(b)
+    q = b.q.cuda()
+    k = q[:, :2].contiguous()
+    for f in (lambda x: batch.append(x, q, k, k), lambda x: batch.prompt_attention(x, q), lambda x: batch.prefix_attention(x, q)):
+        for block in (1 << 32, -(1 << 32), 1 << 31):
+            with pytest.raises(ValueError, match="32 bits"):
+                f(block)
+    (start, kv, table), kw = b.device_args()
+    for more in (dict(n_rows=(1 << 32) + 5), dict(prefix_len=1 << 32, prefix_pages=table[0].contiguous())):
+        with pytest.raises(ValueError):
+            RowBatch(PagedKV(pool), start, kv, table, **{**kw, **more})
