@@ -357,7 +357,8 @@ const char* swift_gemm_static_error(void);
  * per-layer steps of a program that runs many at once (several continuations of a prompt, candidates that share a long
  * prefix, packed prompts) with its own projections in between.  They need no context: every buffer is the caller's, work
  * is enqueued on cuda_stream (a cudaStream_t; NULL = default stream) of the current device and the calls return without
- * synchronising.  They allocate nothing, keep nothing from one call for the next, and may be captured into a CUDA graph;
+ * synchronising.  They allocate nothing, keep nothing from one call for the next (but a count of waits that ran out, which
+ * swift_batch_sync reads), and may be captured into a CUDA graph;
  * row_start, kv_len, the page tables and the positions are read on the device when the work runs, so a replayed graph
  * follows their new values.  Calls on different streams do not share state (a workspace belongs to one call at a time).
  * On error nothing is enqueued; swift_batch_error() gives the text of the calling thread's last failure.
@@ -376,9 +377,9 @@ typedef struct {
 
 /*
  * Rows of several sequences, packed.  Sequence i holds rows row_start[i] .. row_start[i+1] - 1 (ascending; a sequence may
- * be empty); rows from row_start[n_seqs] to n_rows are padding, which no call reads or writes.  kv_len[i] counts the
- * cached positions of sequence i, its rows of this batch included: with n rows, row r is at own position
- * kv_len[i] - n + r.  Own position p lives in slot p % page_size of page page_table[i * table_stride + p / page_size].
+ * be empty); rows from row_start[n_seqs] to n_rows are padding: no call writes them, and what they hold shows nowhere.
+ * kv_len[i] counts the cached positions of sequence i, its rows of this batch included: with n rows, row r is at own
+ * position kv_len[i] - n + r.  Own position p lives in slot p % page_size of page page_table[i * table_stride + p / page_size].
  * With prefix_len > 0, all sequences continue the same prefix of prefix_len positions in prefix_pages[0 ..
  * ceil(prefix_len / page_size) - 1], and own position p is position prefix_len + p of the sequence.  Pages are looked up
  * in [0, n_pages): the positions of a page id outside it hold nothing and are neither read nor written.  Positions outside
@@ -442,8 +443,9 @@ swift_status swift_kv_append(const swift_paged_kv* kv, const swift_row_batch* ba
 
 /*
  * Attention of the batch's rows over what they see: the whole prefix and own positions 0 .. the row's own.  Query head h
- * reads kv head h / (n_heads / n_kv_heads).  out[row][h][:] = softmax(scale * q k^T) v, the softmax and the sums in fp32;
- * a row that sees nothing gives 0.  q and out are of the cache's type, out [n_rows][n_heads][head_dim] contiguous;
+ * reads kv head h / (n_heads / n_kv_heads).  out[row][h][:] = softmax(scale * q k^T) v; scores, maxima, sums and outputs are
+ * held in fp32, and where the tensor cores compute, each probability is rounded to the cache's type for its product with v.
+ * A row that sees nothing gives 0.  q and out are of the cache's type, out [n_rows][n_heads][head_dim] contiguous;
  * where the tensor cores compute (below), both and q's strides are multiples of 16 bytes.  scale > 0.
  * A score of NaN or +infinity makes its row NaN; one of -infinity (an overflowed key) counts as hidden, and a row all of whose
  * scores are -infinity gives 0.
@@ -454,7 +456,10 @@ swift_status swift_kv_append(const swift_paged_kv* kv, const swift_row_batch* ba
  * swift_prefix_attention is for few rows per sequence (decoding steps, verification, scoring windows): the scores against
  * the prefix are computed once for the rows of all sequences together and joined with each sequence's own part (sequences
  * with enough rows to fill tiles are taken by themselves where that ends earlier).  max_rows bounds the rows of one
- * sequence; rows beyond it are left out.  Both compute the same function.
+ * sequence; rows beyond it are left out, and the kernels are chosen by it: a bound far above the sequences' rows costs time.
+ * So does a page table much wider than the sequences, whose lengths are taken for 0.6 of its width when the SMs are divided.
+ * Both calls compute the same function.  The same batch gives the same bits whatever ran before or beside it; another batch
+ * may group a row's sums differently.
  * 16-bit caches with head_dim a multiple of 8 up to 128 run on the tensor cores; fp32 caches and other head sizes are
  * computed in fp32 arithmetic by either call, each sequence by itself.
  * workspace: device memory of at least swift_prefix_workspace_bytes (0 on invalid arguments), 256-byte aligned,

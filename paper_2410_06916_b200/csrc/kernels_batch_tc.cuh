@@ -455,7 +455,8 @@ __device__ __noinline__ float bt_weights_far(uint32_t s_at, uint32_t p_bar, floa
 __device__ __forceinline__ bool bt_outgrown(float top, float m, float c) { return top > m && (m == -INFINITY || (top - m) * c > BT_GROW); }
 
 // Such rows get the new maximum, their sums and (behind the first tile) O rescaled.  The others of the warp keep theirs: a row's
-// bits depend on its own scores alone, not on its neighbours' nor on the unused rows of a tile, which hold anything.
+// bits do not depend on its neighbours' scores nor on the unused rows of a tile, which hold anything.  (They do depend on where the
+// tile's causal edge lies: a tile with hidden keys takes no polynomials.)
 template <int DP> __device__ __forceinline__ void bt_rescale(uint32_t o_at, float c, float top, bool mine, bool first, float& m, float& l)
 {
     const float m_new = mine ? top : m, shrink = mine ? ex2((m - m_new) * c) : 1.f;

@@ -129,7 +129,8 @@ def rope_table(n_positions: int, rotary_dim: int, theta: float = 10000.0, factor
                out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """fp32 [n_positions, rotary_dim / 2, 2]: (cos, sin) of every position and pair.  factor > 1 stretches the positions: all
     alike (original_positions 0), or by parts with low_turns / high_turns as the ramp (LLaMA 3: 1 and 4; YaRN: 1 and 32,
-    with magnitude = 0.1 ln(factor) + 1)."""
+    with magnitude = 0.1 ln(factor) + 1).  The ramp runs over the turns, as the paper defines it; common
+    implementations let it run over the pair's index between the same two ends, and checkpoints made with those need that table."""
     for name, value in (("n_positions", n_positions), ("rotary_dim", rotary_dim), ("original_positions", original_positions)):
         _number(name, value)
     device = torch.device(device) if out is None else _cuda_tensor("out", out).device
@@ -177,12 +178,18 @@ class RowBatch:
     kv_len     int32 [n_seqs]: cached positions of each sequence, its rows of this batch included
     page_table int32 [n_seqs, stride]: pages of each sequence's own positions
     n_rows     rows of the packed tensors (rows from row_start[-1] on are padding)
-    max_rows   upper bound of the rows of one sequence (default n_rows); prefix_attention leaves out rows beyond it
+    max_rows   upper bound of the rows of one sequence; prefix_attention leaves out rows beyond it, and chooses its kernels by
+               it.  The default, n_rows, is right for any batch but slow for many sequences of few rows: give the bound
+               (64 one-token continuations of 8192 positions, 64 heads on 8: 59 us with max_rows 1, 102 without)
     prefix_pages, prefix_len: a prefix that all sequences continue (its pages, its length in positions)
 
     The tensors are read on the device when a call's work runs; they may be rewritten between calls, and between replays
     of a captured graph.  Calls work on the device's current stream, or on `stream`, which the caller has made wait for what its
     tensors still wait for; tensors lent to it may be freed at any time.
+
+    prefix_attention divides the SMs between the prefix and the sequences' own parts before it knows their lengths: it takes
+    them for 0.6 of the page table's width.  A table much wider than its sequences (the same 64 continuations with about 750 own
+    positions, in a table of 4096) costs up to twice the time; one cut to the columns in use does not.
     """
 
     def __init__(self, kv: PagedKV, row_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, n_rows: int,

@@ -124,6 +124,22 @@ def test_row_starts_behind_the_packed_rows_move_no_row(form, each, dt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("form", ["prompt", "prefix"])
+@pytest.mark.parametrize("each,dt,prefix", [(1, BF16, 0), (4, F16, 0), (4, BF16, 50), (60, BF16, 0), (3, F32, 0)])
+def test_a_sequence_that_claims_every_row_there_can_be(form, each, dt, prefix):
+    """row_start ends at 2^31 - 1: the rows that exist lie far before the sequence's first position and see the prefix alone."""
+    from paper_2410_06916_b200 import PagedKV, RowBatch
+    b = Batch([each, each], [200, 700], 8, 2, 64, 16, dt, prefix_len=prefix)
+    (start, kv, table), kw = b.device_args()
+    start[2] = (1 << 31) - 1
+    got = call(RowBatch(PagedKV(b.pool.cuda()), start, kv, table, **kw), form)(0, b.q.cuda())
+    b.kv[1] = 0
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    assert prefix or not want[each:].any()
+    close(got, want, tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
 @pytest.mark.parametrize("each,dt", [(4, BF16), (60, F16), (3, F32)])
 def test_lengths_below_zero_and_row_starts_that_descend(form, each, dt):
     """A length below zero is an empty cache: such rows see nothing and append nothing.  Row starts that descend hold no rows."""
