@@ -508,3 +508,35 @@ def test_blocks_and_lengths_beyond_32_bits_are_refused():
     for more in (dict(n_rows=(1 << 32) + 5), dict(prefix_len=1 << 32, prefix_pages=table[0].contiguous())):
         with pytest.raises(ValueError):
             RowBatch(PagedKV(pool), start, kv, table, **{**kw, **more})
+
+
+@pytest.mark.gpu
+def test_captured_calls_on_a_given_stream_whose_inputs_are_dropped():
+    """stream= inside a capture, on the capturing stream and on one forked from it, with inputs freed during the capture; the two
+    graphs share one memory pool and are replayed in turn."""
+    b = Batch([40, 3], [50, 60], 8, 2, 128, 16, BF16, prefix_len=300)
+    pool, batch = setup(b)
+    want, tol = attention(b, b.pool, b.q, dev="cuda")
+    q, main, side = b.q.cuda(), torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graphs, share = [], None
+    for forked in (False, True):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=main, pool=share):
+            lent = q.clone()
+            on = side if forked else main
+            if forked:
+                side.wait_stream(main)
+            got = [call(batch, form)(0, lent, stream=on) for form in ("prompt", "prefix", "prefix")]
+            if forked:
+                main.wait_stream(side)
+            del lent
+            got = [t.clone() for t in got] + [batch.prefix_attention(0, q)]
+        share = g.pool()
+        graphs.append((g, got))
+    for _ in range(3):
+        for g, got in graphs:
+            g.replay()
+            torch.cuda.synchronize()
+            for t in got:
+                close(t, want, tol)
