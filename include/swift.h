@@ -491,6 +491,74 @@ swift_status swift_probe_batch_wait_limit(const swift_paged_kv* kv, const swift_
  * when the work failed, else SWIFT_OK.  Not inside a stream capture. */
 swift_status swift_batch_sync(void* cuda_stream);
 
+/*
+ * The same cache held in 8 bits: int8 codes in -127..127, or float8 e4m3 ones.  A page's K (or V) of one kv head in one block shares one
+ * scale, scales[page][block][0 = K, 1 = V][kv head], fp32: value = code x scale.  Half the bytes of a 16-bit cache, and as much less to
+ * read per decoding step.  Everything about batches, pages, positions, prefixes, streams and capture holds as above, and the calls are
+ * chosen and used as theirs.  Scales are 0 or in 2^-50..2^50; a page with scale 0 holds codes 0.  A scale of NaN makes every row NaN that
+ * sees a position of its page.
+ */
+enum { SWIFT_I8 = 3, SWIFT_E4M3 = 4 };   /* storage types of these caches only */
+typedef struct {
+    swift_paged_kv kv;            /* dtype SWIFT_I8 or SWIFT_E4M3 */
+    float* scales;                /* device, 4-byte aligned */
+} swift_coded_kv;
+
+/*
+ * swift_kv_append for an 8-bit cache.  q, k, v: SWIFT_F32, SWIFT_BF16 or SWIFT_F16 (x_dtype); q_out is of that type too, finished in fp32
+ * and rounded once.  K and V are finished in 64 bits and rounded once, to the nearest code (halves to even).
+ * A page that gets rows takes the scale its largest new value needs (divided by 127, or 448), or keeps the one it has where that is
+ * larger; codes that were there are rounded anew where the scale grew.  A page with no position of the sequence before its new rows
+ * starts afresh, whatever it held: its other slots' codes become 0.  After a rollback (kv_len shortened) a page keeps the scale of what it held.  A scale below 2^-50
+ * becomes 0 and its codes 0; a row with a value that is not finite, or would need a scale above 2^50, makes its page's scale NaN until
+ * the page starts afresh.  Rows that are left out count for nothing.  Two sequences must not append to one page in one call.
+ */
+swift_status swift_coded_append(const swift_coded_kv* kv, const swift_row_batch* batch, const swift_append_args* args, void* cuda_stream);
+
+/*
+ * swift_prompt_attention and swift_prefix_attention over an 8-bit cache; q and out are of x_dtype (SWIFT_F32, SWIFT_BF16 or SWIFT_F16).
+ * With 16-bit q, head_dim a multiple of 16 up to 128 and at most 128 query heads per kv head the tensor cores compute: codes are exact in their 16-bit operands,
+ * scales are applied in fp32, and each weight (probability x V's scale) is rounded to fp16's 11 bits, or to 2^-32 of the row's largest weight, for
+ * its product; pool, q, its strides and out are multiples of 16 bytes then.  Else fp32 arithmetic takes each sequence by itself.
+ */
+swift_status swift_coded_prompt_attention(const swift_coded_kv* kv, const swift_row_batch* batch, const swift_attention_args* args,
+                                        int32_t x_dtype, void* cuda_stream);
+size_t swift_coded_prefix_workspace_bytes(const swift_coded_kv* kv, const swift_row_batch* batch, int32_t n_heads, int32_t max_rows, int32_t x_dtype);
+swift_status swift_coded_prefix_attention(const swift_coded_kv* kv, const swift_row_batch* batch, const swift_attention_args* args,
+                                        int32_t x_dtype, int32_t max_rows, swift_devbuf workspace, void* cuda_stream);
+/* swift_probe_batch_wait_limit for these calls. */
+swift_status swift_probe_coded_wait_limit(const swift_coded_kv* kv, const swift_row_batch* batch, const swift_attention_args* args,
+                                        int32_t x_dtype, int32_t max_rows, swift_devbuf workspace, int32_t limit_us, void* cuda_stream);
+
+/*
+ * One token per row from its logits, with a given random number each.  With z = logits / temperature and w = exp(z - max z), tokens are
+ * ordered by their logits, the largest first, among equals the lowest id first; kept are
+ *   the first top_k (all with top_k <= 0 or >= vocab), of those
+ *   the shortest run from the start whose w sum to at least top_p of theirs (all with top_p >= 1; the first at least), of those
+ *   the ones with w >= min_p (all with min_p <= 0);
+ * the token is the lowest id whose running sum of kept w, in the order of ids, exceeds uniform x their total, and its probability is
+ * its w over that total.  temperature 0 takes the first of the order, with probability 1.  Sums are held in 64-bit integers, in units of
+ * 2^-45 of the largest w: the result does not depend on the order of additions, and tokens below half of such a unit are never drawn.
+ * A row gives token -1 and probability 0 when its logits hold a NaN or +infinity or nothing but -infinity, its uniform is not in
+ * 0 <= u < 1, its temperature is negative or not finite, its top_p is NaN, or its min_p is NaN or above 1.
+ * Per-row settings are device arrays; where one is NULL the field behind it holds for all rows.
+ */
+enum { SWIFT_MAX_VOCAB = 262144 };
+typedef struct {
+    int32_t n_rows, vocab;                 /* vocab 1..SWIFT_MAX_VOCAB */
+    int32_t dtype;                         /* of the logits: SWIFT_F32, SWIFT_BF16 or SWIFT_F16 */
+    const void* logits;                    /* device [n_rows][vocab], rows row_stride elements apart */
+    int64_t row_stride;
+    const float* uniforms;                 /* device [n_rows] */
+    const float* temperature;  float temperature_all;
+    const int32_t* top_k;      int32_t top_k_all;
+    const float* top_p;        float top_p_all;
+    const float* min_p;        float min_p_all;
+    int32_t* tokens;                       /* device [n_rows] */
+    float* probs;                          /* device [n_rows], or NULL */
+} swift_sample_args;
+swift_status swift_sample_rows(const swift_sample_args* args, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

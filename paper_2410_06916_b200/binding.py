@@ -57,7 +57,8 @@ SYMBOLS = ("swift_weights_bytes", "swift_kv_bytes", "swift_workspace_bytes", "sw
            "swift_committed_length", "swift_launch_count", "swift_round_times", "swift_round_bytes_stored", "swift_final_skip_mask", "swift_forward_bytes", "swift_read_kv", "swift_time_gemm", "swift_set_gemm_impl", "swift_gemm", "swift_gemm_static",
            "swift_gemm_static_error", "swift_probe_wait_limit", "swift_many_row_schedule", "swift_set_tree", "swift_verify_tree", "swift_tree_rows", "swift_opt_create", "swift_opt_free", "swift_opt_suggest", "swift_opt_observe",
            "swift_rope_table", "swift_kv_append", "swift_prompt_attention", "swift_prefix_workspace_bytes", "swift_prefix_attention",
-           "swift_batch_error", "swift_batch_sync", "swift_probe_batch_wait_limit")
+           "swift_batch_error", "swift_batch_sync", "swift_probe_batch_wait_limit", "swift_coded_append", "swift_coded_prompt_attention",
+           "swift_coded_prefix_workspace_bytes", "swift_coded_prefix_attention", "swift_probe_coded_wait_limit", "swift_sample_rows")
 
 _lib = None
 
@@ -129,6 +130,13 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.swift_batch_error.restype = C.c_char_p
     lib.swift_batch_sync.argtypes = [vp]
     lib.swift_probe_batch_wait_limit.argtypes = [vp, vp, vp, i32, _DevBuf, i32, vp]
+    lib.swift_coded_append.argtypes = [vp, vp, vp, vp]
+    lib.swift_coded_prompt_attention.argtypes = [vp, vp, vp, i32, vp]
+    lib.swift_coded_prefix_workspace_bytes.argtypes = [vp, vp, i32, i32, i32]
+    lib.swift_coded_prefix_workspace_bytes.restype = C.c_size_t
+    lib.swift_coded_prefix_attention.argtypes = [vp, vp, vp, i32, i32, _DevBuf, vp]
+    lib.swift_probe_coded_wait_limit.argtypes = [vp, vp, vp, i32, i32, _DevBuf, i32, vp]
+    lib.swift_sample_rows.argtypes = [vp, vp]
     for name in SYMBOLS:
         fn = getattr(lib, name)          # AttributeError if a declared symbol is missing
         if fn.restype is C.c_int:

@@ -1,0 +1,205 @@
+// Batches of sequences over a paged cache of 8-bit codes: argument checks, launch shapes and entry points of swift_coded_append,
+// swift_coded_prompt_attention and swift_coded_prefix_attention.  No context and no state between calls.
+// This translation unit gets its own copies of the shared device code (separate namespace).
+#define swk swk_batch8
+#include "kernels_batch8.cuh"
+#include "kernels_batch_dec.cuh"
+#include "batch_host.cuh"
+
+cudaError_t swift_batch8_waits(unsigned* count, cudaStream_t s)
+{
+    return cudaMemcpyFromSymbolAsync(count, batch_waits_over, sizeof *count, 0, cudaMemcpyDeviceToHost, s);
+}
+
+namespace {
+
+swift_status check_cache8(const swift_coded_kv* c, const swift_row_batch* b, BatchView* bv)
+{
+    const swift_status st = check_batch(c ? &c->kv : nullptr, b, bv, true);
+    if (st != SWIFT_OK) return st;
+    if (!c->scales || !aligned(c->scales, 4)) return fail_batch(SWIFT_EINVAL, "the scales must be 4-byte aligned device memory");
+    return SWIFT_OK;
+}
+inline float* block_scales(const swift_coded_kv* c, int block) { return c->scales + (size_t)block * 2 * c->kv.n_kv_heads; }
+inline long long scale_page(const swift_coded_kv* c) { return 2ll * c->kv.n_blocks * c->kv.n_kv_heads; }
+
+// what the tensor-core kernels take; the rest is computed in fp32 arithmetic
+inline bool tensor_core_shape8(const swift_paged_kv* kv, int x_dtype, int n_heads)
+{
+    return x_dtype != SWIFT_F32 && kv->head_dim % 16 == 0 && kv->head_dim <= 128 && n_heads / kv->n_kv_heads <= BT_ROWS;
+}
+
+swift_status check_attention8(const swift_coded_kv* c, const swift_row_batch* b, const swift_attention_args* a, int x_dtype, BatchView* bv, AttnView* av)
+{
+    swift_status st = check_cache8(c, b, bv);
+    if (st != SWIFT_OK) return st;
+    const swift_paged_kv* kv = &c->kv;
+    if (!a) return fail_batch(SWIFT_EINVAL, "null arguments");
+    if (!type_known(x_dtype)) return fail_batch(SWIFT_EINVAL, "type %d of q and out unknown", x_dtype);
+    if (a->block < 0 || a->block >= kv->n_blocks) return fail_batch(SWIFT_EINVAL, "block %d outside 0..%d", a->block, kv->n_blocks - 1);
+    if (a->n_heads < 1 || a->n_heads > MAX_HEADS || a->n_heads % kv->n_kv_heads)
+        return fail_batch(SWIFT_EINVAL, "n_heads %d is not a multiple of the cache's %d (at most %d)", a->n_heads, kv->n_kv_heads, MAX_HEADS);
+    if (!(a->scale > 0.f) || !std::isfinite(a->scale * 2.f)) return fail_batch(SWIFT_EINVAL, "scale must be positive and below 2^127");
+    if (b->n_rows > 0) {
+        const int es = type_size(x_dtype);
+        if (!a->q.ptr || !a->out) return fail_batch(SWIFT_EINVAL, "null q or out");
+        const int unit = tensor_core_shape8(kv, x_dtype, a->n_heads) ? 16 : es;
+        if (!aligned(a->q.ptr, unit) || !aligned(a->out, unit) || a->q.row_stride * es % unit || a->q.head_stride * es % unit)
+            return fail_batch(SWIFT_EINVAL, "q, its strides and out must be multiples of %d bytes", unit);
+        if (a->q.row_stride < 0 || a->q.head_stride < 0) return fail_batch(SWIFT_EINVAL, "negative strides");
+    }
+    av->q = a->q.ptr;
+    av->q_row_stride = a->q.row_stride;
+    av->q_head_stride = a->q.head_stride;
+    av->pool = block_base(kv, a->block);
+    av->page_elems = 2 * kv_elems(kv) * kv->n_blocks;
+    av->kv_elems = kv_elems(kv);
+    av->out = a->out;
+    av->n_heads = a->n_heads;
+    av->n_kv_heads = kv->n_kv_heads;
+    av->head_dim = kv->head_dim;
+    av->max_rows = b->n_rows;
+    av->scale = a->scale;
+    av->wait_kcycles = (int)(TC_WAIT_CYCLES >> 10);
+    av->withhold = 0;
+    av->scales = block_scales(c, a->block);
+    av->scale_page = scale_page(c);
+    return SWIFT_OK;
+}
+
+template <typename TC> cudaError_t launch_rows8(int x_dtype, const BatchView& bv, const AttnView& av, cudaStream_t s)
+{
+    switch (x_dtype) {
+    case SWIFT_F32: return launch_fp32<float, TC>(bv, av, s);
+    case SWIFT_BF16: return launch_fp32<__nv_bfloat16, TC>(bv, av, s);
+    default: return launch_fp32<__half, TC>(bv, av, s);
+    }
+}
+swift_status run_rows8(const swift_paged_kv* kv, int x_dtype, const BatchView& bv, const AttnView& av, cudaStream_t s)
+{
+    const cudaError_t e = kv->dtype == SWIFT_I8 ? launch_rows8<int8_t>(x_dtype, bv, av, s) : launch_rows8<__nv_fp8_e4m3>(x_dtype, bv, av, s);
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+
+// Pages that get rows, at most: each row adds one at most, and n rows of a sequence lie on n / page_size + 2 at most.
+long long page_bound(const BatchView& bv)
+{
+    const long long some = bv.n_seqs < bv.n_rows ? bv.n_seqs : bv.n_rows, bound = bv.n_rows / bv.page_size + 2 * some;
+    return bound < bv.n_rows ? bound : bv.n_rows;
+}
+
+template <typename TX, typename CODE>
+cudaError_t launch_append8(const BatchView& bv, const Append8View& v, bool vec, cudaStream_t s)
+{
+    const dim3 grid((unsigned)page_bound(bv), 2 * v.a.n_kv_heads);
+    if (!vec) return launch(append8_kernel<TX, CODE, 1, 32>, grid, 128, 0, s, false, bv, v);
+    const int pieces = v.a.head_dim / 16;
+    if (pieces <= 1) return launch(append8_kernel<TX, CODE, 8, 1>, grid, 128, 0, s, false, bv, v);
+    if (pieces <= 4) return launch(append8_kernel<TX, CODE, 8, 4>, grid, 128, 0, s, false, bv, v);
+    return launch(append8_kernel<TX, CODE, 8, 8>, grid, 128, 0, s, false, bv, v);
+}
+template <typename TX>
+cudaError_t launch_append8_any(int dtype, const BatchView& bv, const Append8View& v, bool q_vec, bool kv_vec, cudaStream_t s)
+{
+    if (v.a.n_heads > 0) {
+        AppendView q = v.a;                               // the queries alone, by the 16-bit cache's kernel
+        q.n_kv_heads = 0;
+        const cudaError_t e = launch_append<TX, TX>(bv, q, q_vec, s);
+        if (e != cudaSuccess) return e;
+    }
+    return dtype == SWIFT_I8 ? launch_append8<TX, int8_t>(bv, v, kv_vec, s) : launch_append8<TX, __nv_fp8_e4m3>(bv, v, kv_vec, s);
+}
+
+swift_status prompt8(const swift_coded_kv* c, const swift_row_batch* batch, const swift_attention_args* args, int x_dtype, int probe_us, cudaStream_t s)
+{
+    BatchView bv;
+    AttnView av;
+    const swift_status st = check_attention8(c, batch, args, x_dtype, &bv, &av);
+    if (st != SWIFT_OK) return st;
+    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
+    set_probe(&av, probe_us);
+    return run_rows8(&c->kv, x_dtype, bv, av, s);
+}
+
+swift_status prefix8(const swift_coded_kv* c, const swift_row_batch* batch, const swift_attention_args* args, int x_dtype, int max_rows,
+                     swift_devbuf workspace, int probe_us, cudaStream_t s)
+{
+    BatchView bv;
+    AttnView av;
+    const swift_status st = check_attention8(c, batch, args, x_dtype, &bv, &av);
+    if (st != SWIFT_OK) return st;
+    if (max_rows < 1) return fail_batch(SWIFT_EINVAL, "max_rows %d", max_rows);
+    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
+    if (!workspace.dptr || !aligned(workspace.dptr, 256)) return fail_batch(SWIFT_EINVAL, "the workspace must be 256-byte aligned device memory");
+    const size_t need = 256;
+    if (workspace.bytes < need) return fail_batch(SWIFT_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace.bytes, need);
+    av.max_rows = max_rows;
+    set_probe(&av, probe_us);
+    return run_rows8(&c->kv, x_dtype, bv, av, s);
+}
+
+} // namespace
+
+extern "C" {
+
+swift_status swift_coded_append(const swift_coded_kv* c, const swift_row_batch* batch, const swift_append_args* x, void* cuda_stream)
+{
+    BatchView bv;
+    swift_status st = check_cache8(c, batch, &bv);
+    if (st != SWIFT_OK) return st;
+    const swift_paged_kv* kv = &c->kv;
+    if (!x) return fail_batch(SWIFT_EINVAL, "null arguments");
+    if (x->block < 0 || x->block >= kv->n_blocks) return fail_batch(SWIFT_EINVAL, "block %d outside 0..%d", x->block, kv->n_blocks - 1);
+    if (x->n_heads < 0 || x->n_heads > MAX_HEADS) return fail_batch(SWIFT_EINVAL, "n_heads %d", x->n_heads);
+    if (!type_known(x->x_dtype)) return fail_batch(SWIFT_EUNSUPPORTED, "q, k, v must be fp32, bf16 or fp16");
+    st = check_append(kv, x);
+    if (st != SWIFT_OK) return st;
+    if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
+    Append8View v;
+    bool vec[2];
+    st = view_append(kv, x, x->x_dtype, &v.a, vec);
+    if (st != SWIFT_OK) return st;
+    v.scales = block_scales(c, x->block);
+    v.scale_page = scale_page(c);
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    cudaError_t e;
+    if (x->x_dtype == SWIFT_F32) e = launch_append8_any<float>(kv->dtype, bv, v, vec[0], vec[1], s);
+    else if (x->x_dtype == SWIFT_BF16) e = launch_append8_any<__nv_bfloat16>(kv->dtype, bv, v, vec[0], vec[1], s);
+    else e = launch_append8_any<__half>(kv->dtype, bv, v, vec[0], vec[1], s);
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+
+swift_status swift_coded_prompt_attention(const swift_coded_kv* c, const swift_row_batch* batch, const swift_attention_args* args, int32_t x_dtype, void* cuda_stream)
+{
+    return prompt8(c, batch, args, x_dtype, 0, (cudaStream_t)cuda_stream);
+}
+
+size_t swift_coded_prefix_workspace_bytes(const swift_coded_kv* c, const swift_row_batch* batch, int32_t n_heads, int32_t max_rows, int32_t x_dtype)
+{
+    BatchView bv;
+    if (check_cache8(c, batch, &bv) != SWIFT_OK) return 0;
+    if (n_heads < 1 || n_heads > MAX_HEADS || n_heads % c->kv.n_kv_heads || max_rows < 1 || !type_known(x_dtype)) {
+        fail_batch(SWIFT_EINVAL, "n_heads %d, max_rows %d, type %d", n_heads, max_rows, x_dtype);
+        return 0;
+    }
+    return 256;
+}
+
+swift_status swift_coded_prefix_attention(const swift_coded_kv* c, const swift_row_batch* batch, const swift_attention_args* args, int32_t x_dtype,
+                                        int32_t max_rows, swift_devbuf workspace, void* cuda_stream)
+{
+    return prefix8(c, batch, args, x_dtype, max_rows, workspace, 0, (cudaStream_t)cuda_stream);
+}
+
+swift_status swift_probe_coded_wait_limit(const swift_coded_kv* c, const swift_row_batch* batch, const swift_attention_args* args, int32_t x_dtype,
+                                        int32_t max_rows, swift_devbuf workspace, int32_t limit_us, void* cuda_stream)
+{
+    (void)c; (void)batch; (void)args; (void)x_dtype; (void)workspace; (void)cuda_stream;
+    if (limit_us < 1 || limit_us > 100000) return fail_batch(SWIFT_EINVAL, "limit_us must be in 1..100000");
+    if (max_rows < 0) return fail_batch(SWIFT_EINVAL, "max_rows %d", max_rows);
+    return fail_batch(SWIFT_EUNSUPPORTED, "fp32 arithmetic has no waits");
+}
+
+} // extern "C"

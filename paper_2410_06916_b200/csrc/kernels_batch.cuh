@@ -3,6 +3,7 @@
 // sizes the tensor-core kernels next door do not take.
 #pragma once
 #include <cuda_fp16.h>
+#include <cuda_fp8.h>
 
 #include "common.cuh"
 
@@ -78,6 +79,8 @@ __device__ __forceinline__ int find_seq(const BatchView& b, int row, SeqSpan& sp
 }
 
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_float(int8_t v) { return (float)v; }
+__device__ __forceinline__ float to_float(__nv_fp8_e4m3 v) { return (float)v; }
 __device__ __forceinline__ void store_val(__half* p, float v) { *p = __float2half_rn(v); }
 
 __device__ __forceinline__ void load8(const float* p, float (&x)[8])      // from 16-byte loads
@@ -387,6 +390,8 @@ struct AttnView {
     int n_heads, n_kv_heads, head_dim, max_rows;
     float scale;
     int wait_kcycles, withhold;                           // limit of the tensor-core kernels' waits in 1024 cycles; withhold: a copy is never asked for
+    const float* scales;                                  // 8-bit caches: this block's [K, V][kv head] of page 0
+    long long scale_page;                                 // and how far on the next page's are
 };
 
 // Any type and head size: fp32 caches, whose products the matrix instructions would round, and the sizes the tensor-core
@@ -401,7 +406,7 @@ __host__ __device__ inline int af_stride(int head_dim) { return (head_dim + 3) /
 __host__ __device__ constexpr int af_p_stride(int rpw) { return rpw == 4 ? 4 : rpw + 4; }       // floats per key of a warp's weights: no bank conflicts
 __host__ __device__ inline int af_smem_bytes(int head_dim, int rpw)
 {
-    return ((4 * rpw + 2 * AF_KEYS) * af_stride(head_dim) + 4 * AF_KEYS * af_p_stride(rpw)) * 4 + AF_KEYS * 8;
+    return ((4 * rpw + 2 * AF_KEYS) * af_stride(head_dim) + 4 * AF_KEYS * af_p_stride(rpw)) * 4 + AF_KEYS * 16;
 }
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
@@ -412,9 +417,18 @@ template <typename T> __device__ __forceinline__ float4 load4(const T* p)      /
     return make_float4(to_float(e[0]), to_float(e[1]), to_float(e[2]), to_float(e[3]));
 }
 
-template <typename T, int RPW, int NV>
+__device__ __forceinline__ float4 load4(const int8_t* p)                      // 8-bit codes: 4 bytes
+{
+    const char4 v = *reinterpret_cast<const char4*>(p);
+    return make_float4((float)v.x, (float)v.y, (float)v.z, (float)v.w);
+}
+__device__ __forceinline__ float4 load4(const __nv_fp8_e4m3* p) { return (float4)*reinterpret_cast<const __nv_fp8x4_e4m3*>(p); }
+
+// T: of q and out; TC: of the cache.  8-bit codes become values, code x scale in fp32, as they are staged.
+template <typename T, typename TC, int RPW, int NV>
 __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
 {
+    constexpr bool CODES = sizeof(TC) == 1;
     constexpr int ROWS = 4 * RPW, RT = RPW / 4, PS = af_p_stride(RPW);
     extern __shared__ __align__(16) float af_smem[];
     const int D = a.head_dim, ld = af_stride(D), G = a.n_heads / a.n_kv_heads, Hk = a.n_kv_heads, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -423,6 +437,7 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
     float* v_sh = k_sh + AF_KEYS * ld;
     float* p_sh = v_sh + AF_KEYS * ld + warp * AF_KEYS * PS;          // this warp's weights, [key][row]
     long long* at_sh = reinterpret_cast<long long*>(af_smem + (ROWS + 2 * AF_KEYS) * ld + 4 * AF_KEYS * PS);   // element offset of each key's K, -1: nothing there
+    float2* scale_sh = reinterpret_cast<float2*>(at_sh + AF_KEYS);    // (codes) its scales, of K and of V
     // ---- this block's piece
     int idx = blockIdx.x, seq = -1;
     SeqSpan sp = {};
@@ -448,7 +463,7 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
     }
     if (seq < 0) return;                                  // the same for the whole block
     const int kvh = idx % Hk, rho0 = idx / Hk * ROWS, rows = min(ROWS, sp.n * G - rho0);
-    const T* head = reinterpret_cast<const T*>(a.pool) + (size_t)kvh * b.page_size * D;
+    const TC* head = reinterpret_cast<const TC*>(a.pool) + (size_t)kvh * b.page_size * D;
     // ---- queries; dead rows and the dims behind the last are zero
     for (int r = warp; r < ROWS; r += 4) {
         const int tok = (rho0 + r) / G;
@@ -477,7 +492,13 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
             const int p = p0 + tid, own = p - b.prefix_len, pp = own < 0 ? p : own;
             if (p < total) {
                 const int page = own < 0 ? b.prefix_pages[pp >> b.page_shift] : b.page_table[(size_t)seq * b.table_stride + (pp >> b.page_shift)];
-                if ((unsigned)page < (unsigned)b.n_pages) at = (long long)page * a.page_elems + (long long)(pp & (b.page_size - 1)) * D;
+                if ((unsigned)page < (unsigned)b.n_pages) {
+                    at = (long long)page * a.page_elems + (long long)(pp & (b.page_size - 1)) * D;
+                    if (CODES) {
+                        const float* s = a.scales + page * a.scale_page + kvh;
+                        scale_sh[tid] = make_float2(s[0], s[Hk]);
+                    }
+                }
             }
             at_sh[tid] = at;
         }
@@ -494,6 +515,11 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
                     if (at >= 0) {
                         kx = load4(head + at + d);
                         vx = load4(head + at + a.kv_elems + d);
+                        if (CODES) {
+                            const float2 s = scale_sh[j];
+                            kx.x *= s.x; kx.y *= s.x; kx.z *= s.x; kx.w *= s.x;
+                            vx.x *= s.y; vx.y *= s.y; vx.z *= s.y; vx.w *= s.y;
+                        }
                     }
                     *reinterpret_cast<float4*>(k_sh + j * ld + d) = kx;
                     *reinterpret_cast<float4*>(v_sh + j * ld + d) = vx;
@@ -502,9 +528,10 @@ __global__ void __launch_bounds__(128) attn_fp32_kernel(BatchView b, AttnView a)
         } else {
             for (int j = warp; j < AF_KEYS; j += 4) {
                 const long long at = at_sh[j];
+                const float2 s = CODES && at >= 0 ? scale_sh[j] : make_float2(1.f, 1.f);
                 for (int d = lane; d < D; d += 32) {
-                    k_sh[j * ld + d] = at >= 0 ? to_float(head[at + d]) : 0.f;
-                    v_sh[j * ld + d] = at >= 0 ? to_float(head[at + a.kv_elems + d]) : 0.f;
+                    k_sh[j * ld + d] = at >= 0 ? (CODES ? to_float(head[at + d]) * s.x : to_float(head[at + d])) : 0.f;
+                    v_sh[j * ld + d] = at >= 0 ? (CODES ? to_float(head[at + a.kv_elems + d]) * s.y : to_float(head[at + a.kv_elems + d])) : 0.f;
                 }
             }
         }

@@ -1,0 +1,255 @@
+// Appending to a cache of 8-bit codes.  A page's K (or V) of one kv head shares one scale: value = code x scale, code int8 in
+// -127..127 or float8 e4m3.
+//
+//     need = max |x| / 127 (int8) or / 448 (e4m3)  over the rows that the call writes to the page
+//     scale = need for a page without earlier positions, else max(scale, need);  codes that were there: 0, or rnd(code x old / new)
+//     new codes: rnd(x / scale)
+//
+// So a page's values share the scale of its largest one, and a decoding step rewrites a page only when its row is larger than
+// anything there before.
+//
+// Arithmetic.  K and V are finished in 64 bits (sum of squares, norm, rotation, division by the scale) and rounded once, to the code
+// nearest to them: next to the border between two codes, 32 bits would let the order of a sum decide.  One K or V element costs some
+// ten 64-bit operations per pass, and a B200 has half as many 64-bit units as 32-bit ones.
+#pragma once
+#include "kernels_batch.cuh"
+
+namespace swk {
+
+constexpr float CODE_SMALLEST = 8.8817841970012523e-16f;  // 2^-50: a page whose scale would be smaller counts as zero
+constexpr float CODE_LARGEST = 1.125899906842624e15f;     // 2^50: one whose scale would be larger as not finite
+
+struct Append8View {
+    AppendView a;                                         // x[1], x[2]; pool: codes
+    float* scales;                                        // this block's [K, V][kv head] of page 0
+    long long scale_page;
+};
+
+__device__ __forceinline__ double widen(float v) { return (double)v; }
+__device__ __forceinline__ double widen(__nv_bfloat16 v) { return (double)__bfloat162float(v); }
+__device__ __forceinline__ double widen(__half v) { return (double)__half2float(v); }
+
+// value / scale -> code
+__device__ __forceinline__ uint32_t code_of(double t, int8_t) { return (uint32_t)min(max(__double2int_rn(t), -127), 127) & 0xFFu; }
+__device__ __forceinline__ uint32_t code_of(double t, __nv_fp8_e4m3) { return __nv_cvt_float_to_fp8((float)t, __NV_SATFINITE, __NV_E4M3); }
+__device__ __forceinline__ float largest_code(int8_t) { return 127.f; }
+__device__ __forceinline__ float largest_code(__nv_fp8_e4m3) { return 448.f; }
+
+// The idx-th page that gets rows, found by a whole warp; false when there are fewer.
+struct A8Page { int seq, page_no; SeqSpan sp; };
+__device__ __forceinline__ bool a8_locate(const BatchView& b, int idx, A8Page& it)
+{
+    const int lane = threadIdx.x & 31;
+    for (int base = 0; base < b.n_seqs; base += 32) {
+        SeqSpan sp = {};
+        if (base + lane < b.n_seqs) sp = seq_span(b, base + lane);
+        const int lo = max(sp.pos0, 0), hi = (int)min((long long)sp.pos0 + sp.n, (long long)b.max_len);   // own positions of its rows
+        const int first = lo >> b.page_shift, mine = sp.n > 0 && hi > lo ? ((hi - 1) >> b.page_shift) - first + 1 : 0;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(FULL_WARP, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const unsigned m = __ballot_sync(FULL_WARP, idx < upto);
+        if (m == 0) {
+            idx -= __shfl_sync(FULL_WARP, upto, 31);
+            continue;
+        }
+        const int at = __ffs(m) - 1;
+        it.seq = base + at;
+        it.sp = span_of(sp, at);
+        it.page_no = __shfl_sync(FULL_WARP, first, at) + idx - __shfl_sync(FULL_WARP, upto - mine, at);
+        return true;
+    }
+    return false;
+}
+
+// One block per (page, K or V of a kv head): first the largest value of its rows, which a second pass over them (now in L1 or L2)
+// divides by.  PIECE dims at a time: 8 where sizes and alignment allow 16-byte loads, else 1; LPH lanes share a row, each with two pieces that a
+// rotation pairs up, as in the 16-bit cache's kernel.  grid = (pages, 2 x kv heads), block = 128.
+template <typename TX, typename CODE, int PIECE, int LPH>
+__global__ void __launch_bounds__(128) append8_kernel(BatchView b, Append8View v)
+{
+    constexpr int GROUPS = 32 / LPH;                      // rows a warp takes at once
+    const AppendView& a = v.a;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, grp = lane / LPH, c0 = lane % LPH;
+    const int kind = blockIdx.y >= a.n_kv_heads, h = blockIdx.y - kind * a.n_kv_heads, D = a.head_dim;
+    A8Page it;
+    if (!a8_locate(b, blockIdx.x, it)) return;
+    const int page = b.page_table[(size_t)it.seq * b.table_stride + it.page_no];
+    if ((unsigned)page >= (unsigned)b.n_pages) return;
+    const int base = it.page_no << b.page_shift;
+    const int lo = max(max(it.sp.pos0, 0), base);
+    const int hi = (int)min(min((long long)it.sp.pos0 + it.sp.n, (long long)b.max_len), (long long)base + b.page_size);
+    const bool fresh = base >= it.sp.pos0;                // no earlier position lies in the page
+    const int R = kind == 0 && a.rope ? a.rotary_dim : 0, half = R >> 1;
+    const float* gain = kind == 0 ? a.gain[1] : nullptr;
+    const TX* src0 = reinterpret_cast<const TX*>(a.x[1 + kind]) + h * a.head_stride[1 + kind];
+    uint8_t* codes = reinterpret_cast<uint8_t*>(a.pool) + (long long)page * a.page_elems + (kind ? a.kv_elems : 0) + (long long)h * b.page_size * D;
+    float* scale_at = v.scales + page * v.scale_page + kind * a.n_kv_heads + h;
+
+    // pieces of a row: pair j of pieces is (first, second); the rotated ones come first
+    const int pairs = D / (2 * PIECE), turned_pairs = half / PIECE;
+    auto place = [&](int j, int& oa, int& ob) {
+        if (a.interleaved && PIECE > 1) {
+            oa = 2 * PIECE * j;
+            ob = oa + PIECE;
+        } else if (j < turned_pairs) {
+            oa = a.interleaved ? 2 * j : PIECE * j;
+            ob = a.interleaved ? oa + 1 : oa + half;
+        } else {
+            oa = R + 2 * PIECE * (j - turned_pairs);
+            ob = oa + PIECE;
+        }
+    };
+    // row of own position o: the finished values of this lane's pieces, handed to use(j, oa, ob, xa, xb)
+    auto finish = [&](int o, bool live, auto use) {
+        const int row = it.sp.r0 + (int)((long long)o - it.sp.pos0);
+        const TX* src = src0 + (long long)row * a.row_stride[1 + kind];
+        double norm = 1.0;
+        if (gain) {                                       // the same for the whole block
+            double ss = 0.0;
+            if (live)
+                for (int j = c0; j < pairs; j += LPH) {
+                    int oa, ob;
+                    place(j, oa, ob);
+#pragma unroll
+                    for (int e = 0; e < PIECE; ++e) {
+                        const double xa = widen(src[oa + e]), xb = widen(src[ob + e]);
+                        ss += xa * xa + xb * xb;
+                    }
+                }
+#pragma unroll
+            for (int x = LPH / 2; x > 0; x >>= 1) ss += __shfl_xor_sync(FULL_WARP, ss, x);
+            norm = 1.0 / sqrt(ss / D + (double)a.eps);
+        }
+        if (!live) return;
+        const float2* turn = R ? a.rope + (size_t)(a.positions ? a.positions[row] : b.prefix_len + o) * half : nullptr;
+        for (int j = c0; j < pairs; j += LPH) {
+            int oa, ob;
+            place(j, oa, ob);
+            TX ra[PIECE], rb[PIECE];
+            if (PIECE == 8) {
+                constexpr int WORDS = PIECE * sizeof(TX) / 16;
+#pragma unroll
+                for (int e = 0; e < WORDS; ++e) {
+                    reinterpret_cast<uint4*>(ra)[e] = reinterpret_cast<const uint4*>(src + oa)[e];
+                    reinterpret_cast<uint4*>(rb)[e] = reinterpret_cast<const uint4*>(src + ob)[e];
+                }
+            } else {
+                ra[0] = src[oa];
+                rb[0] = src[ob];
+            }
+            double xa[PIECE], xb[PIECE];
+#pragma unroll
+            for (int e = 0; e < PIECE; ++e) {
+                xa[e] = widen(ra[e]);
+                xb[e] = widen(rb[e]);
+                if (gain) {
+                    xa[e] *= norm * (double)gain[oa + e];
+                    xb[e] *= norm * (double)gain[ob + e];
+                }
+            }
+            if (oa < R) {
+                if (a.interleaved && PIECE > 1) {         // neighbours: pairs lie within a piece
+#pragma unroll
+                    for (int e = 0; e + 1 < PIECE; e += 2) {
+                        const float2 s = turn[(oa + e) >> 1], z = turn[(ob + e) >> 1];
+                        const double a0 = xa[e], a1 = xa[e + 1], b0 = xb[e], b1 = xb[e + 1];
+                        xa[e] = a0 * s.x - a1 * s.y;
+                        xa[e + 1] = a1 * s.x + a0 * s.y;
+                        xb[e] = b0 * z.x - b1 * z.y;
+                        xb[e + 1] = b1 * z.x + b0 * z.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PIECE; ++e) {
+                        const float2 s = turn[a.interleaved ? j : oa + e];
+                        const double p = xa[e], q = xb[e];
+                        xa[e] = p * s.x - q * s.y;
+                        xb[e] = q * s.x + p * s.y;
+                    }
+                }
+            }
+            use(oa, ob, xa, xb);
+        }
+    };
+    auto live_row = [&](int o) {
+        if (o >= hi) return false;
+        if (!a.rope) return true;                         // (V of a row is left out with its K)
+        const int at = a.positions ? a.positions[it.sp.r0 + (int)((long long)o - it.sp.pos0)] : b.prefix_len + o;
+        return (unsigned)at < (unsigned)a.rope_positions;
+    };
+
+    // ---- the largest value
+    double top = 0.0;
+    bool bad = false, some = false, whole = true;         // whole: no row between lo and hi is left out
+    for (int o0 = lo + warp * GROUPS; o0 < hi; o0 += 4 * GROUPS) {
+        const bool live = live_row(o0 + grp);
+        some |= live;
+        whole &= live || o0 + grp >= hi;
+        finish(o0 + grp, live, [&](int, int, const double (&xa)[PIECE], const double (&xb)[PIECE]) {
+#pragma unroll
+            for (int e = 0; e < PIECE; ++e) {
+                const double m = fmax(fabs(xa[e]), fabs(xb[e]));
+                bad |= !(fabs(xa[e]) + fabs(xb[e]) < INFINITY);           // NaN or infinity in either
+                top = fmax(top, m);
+            }
+        });
+    }
+    __shared__ double top_sh[4];
+    __shared__ int flags_sh[4];
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) top = fmax(top, __shfl_xor_sync(FULL_WARP, top, x));
+    const int flags = (__any_sync(FULL_WARP, bad) ? 1 : 0) | (__any_sync(FULL_WARP, some) ? 2 : 0) | (__all_sync(FULL_WARP, whole) ? 0 : 8);
+    if (lane == 0) {
+        top_sh[warp] = top;
+        flags_sh[warp] = flags;
+    }
+    __syncthreads();
+    top = fmax(fmax(top_sh[0], top_sh[1]), fmax(top_sh[2], top_sh[3]));
+    const int all = flags_sh[0] | flags_sh[1] | flags_sh[2] | flags_sh[3];
+    if (!(all & 2)) return;                               // every row is left out
+    const float old = fresh ? 0.f : *scale_at;
+    float need = (float)(top / largest_code(CODE()));
+    if (need < CODE_SMALLEST) need = 0.f;
+    const float scale = (all & 1) || !(need <= CODE_LARGEST) || !(old >= 0.f) ? __int_as_float(0x7FC00000) : fmaxf(old, need);
+    const double inv = scale > 0.f ? 1.0 / (double)scale : 0.0;           // 0 for a page of zeros, and for one that is not finite
+    __syncthreads();                                      // everyone has read the old scale
+    if (tid == 0 && (fresh || !(scale == old))) *scale_at = scale;
+
+    // ---- the page's other codes: rounded anew when the scale has grown, 0 where the page starts afresh
+    if (fresh ? hi - lo < b.page_size || (all & 8) : !(scale == old)) {
+        const double ratio = !fresh && inv > 0.0 ? (double)old / (double)scale : 0.0;
+        const CODE* had = reinterpret_cast<const CODE*>(codes);
+        for (int slot = warp; slot < b.page_size; slot += 4) {
+            const int o = base + slot;
+            if (o >= lo && o < hi && live_row(o)) continue;               // written below
+            for (int d = lane; d < D; d += 32)
+                codes[slot * D + d] = ratio > 0.0 ? (uint8_t)code_of((double)to_float(had[slot * D + d]) * ratio, CODE()) : 0;
+        }
+    }
+    // ---- the new codes
+    for (int o0 = lo + warp * GROUPS; o0 < hi; o0 += 4 * GROUPS) {
+        const int o = o0 + grp;
+        uint8_t* dst = codes + (long long)(o - base) * D;
+        finish(o, live_row(o), [&](int oa, int ob, const double (&xa)[PIECE], const double (&xb)[PIECE]) {
+            uint32_t wa[(PIECE + 3) / 4] = {}, wb[(PIECE + 3) / 4] = {};
+#pragma unroll
+            for (int e = 0; e < PIECE; ++e) {
+                wa[e >> 2] |= (inv > 0.0 ? code_of(xa[e] * inv, CODE()) : 0u) << (8 * (e & 3));
+                wb[e >> 2] |= (inv > 0.0 ? code_of(xb[e] * inv, CODE()) : 0u) << (8 * (e & 3));
+            }
+            if (PIECE == 8) {
+                *reinterpret_cast<uint2*>(dst + oa) = make_uint2(wa[0], wa[PIECE > 4]);
+                *reinterpret_cast<uint2*>(dst + ob) = make_uint2(wb[0], wb[PIECE > 4]);
+            } else {
+                dst[oa] = (uint8_t)wa[0];
+                dst[ob] = (uint8_t)wb[0];
+            }
+        });
+    }
+}
+
+} // namespace swk

@@ -1,0 +1,70 @@
+// Tokens from logits: argument checks, launch shapes and the entry point of swift_sample_rows.  No state between calls.
+// This translation unit gets its own copies of the shared device code (separate namespace).
+#define swk swk_sample
+#include "kernels_sample.cuh"
+#include "batch_host.cuh"
+
+namespace {
+
+static_assert(SWIFT_MAX_VOCAB / SA_BLOCKS / SA_CHUNK <= SA_CHUNKS && SA_CHUNKS <= SA_THREADS && SA_BINS == SA_THREADS && SA_LIST == SA_THREADS, "one of each per thread");
+
+template <typename T> cudaError_t launch_sample(const SampleView& v, int blocks, cudaStream_t s)
+{
+    static std::atomic<unsigned long long> done{0};
+    const auto bytes = [](int slice) { return (int)((sizeof(SampleShared) + 15) / 16 * 16 + (size_t)slice * sizeof(T)); };
+    cudaError_t e = allow_smem(sample_kernel<T>, bytes(SWIFT_MAX_VOCAB / SA_BLOCKS), done);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)v.n_rows * blocks);
+    cfg.blockDim = dim3(SA_THREADS);
+    cfg.dynamicSmemBytes = bytes(v.slice);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = blocks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, sample_kernel<T>, v);
+}
+
+} // namespace
+
+extern "C" swift_status swift_sample_rows(const swift_sample_args* a, void* cuda_stream)
+{
+    if (!a) return fail_batch(SWIFT_EINVAL, "null arguments");
+    if (!type_known(a->dtype)) return fail_batch(SWIFT_EINVAL, "type %d of the logits unknown", a->dtype);
+    if (a->n_rows < 0 || a->n_rows > (1 << 24)) return fail_batch(SWIFT_EINVAL, "n_rows %d outside 0..2^24", a->n_rows);
+    if (a->vocab < 1 || a->vocab > SWIFT_MAX_VOCAB) return fail_batch(SWIFT_EINVAL, "vocab %d outside 1..%d", a->vocab, (int)SWIFT_MAX_VOCAB);
+    if (a->n_rows == 0) return SWIFT_OK;
+    if (!a->logits || !a->uniforms || !a->tokens) return fail_batch(SWIFT_EINVAL, "null logits, uniforms or tokens");
+    if (!aligned(a->logits, type_size(a->dtype)) || a->row_stride < 0) return fail_batch(SWIFT_EINVAL, "the logits must be aligned to their element size, their row stride not negative");
+    const void* fours[] = {a->uniforms, a->temperature, a->top_k, a->top_p, a->min_p, a->tokens, a->probs};
+    for (const void* p : fours)
+        if (!aligned(p, 4)) return fail_batch(SWIFT_EINVAL, "uniforms, settings, tokens and probs must be 4-byte aligned");
+    SampleView v;
+    v.logits = a->logits;
+    v.row_stride = a->row_stride;
+    v.n_rows = a->n_rows;
+    v.vocab = a->vocab;
+    v.uniforms = a->uniforms;
+    v.temperature = a->temperature;
+    v.top_k = a->top_k;
+    v.top_p = a->top_p;
+    v.min_p = a->min_p;
+    v.temperature_all = a->temperature_all;
+    v.top_k_all = a->top_k_all;
+    v.top_p_all = a->top_p_all;
+    v.min_p_all = a->min_p_all;
+    v.tokens = a->tokens;
+    v.probs = a->probs;
+    int blocks = 1;
+    while (blocks < SA_BLOCKS && ceil_div(a->vocab, blocks) > 16384) blocks *= 2;
+    while (blocks < SA_BLOCKS && (long long)a->n_rows * blocks < multiprocessors() && a->vocab / blocks > 4096) blocks *= 2;
+    v.slice = ceil_div(ceil_div(a->vocab, blocks), SA_CHUNK) * SA_CHUNK;
+    const cudaStream_t s = (cudaStream_t)cuda_stream;
+    const cudaError_t e = a->dtype == SWIFT_F32 ? launch_sample<float>(v, blocks, s)
+                        : a->dtype == SWIFT_BF16 ? launch_sample<__nv_bfloat16>(v, blocks, s) : launch_sample<__half>(v, blocks, s);
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}

@@ -1,6 +1,7 @@
 """Batches of sequences over one paged K,V cache: the torch side of swift_rope_table, swift_kv_append,
-swift_prompt_attention and swift_prefix_attention (include/swift.h says what each computes).  As in binding.py, torch only
-provides memory and streams; every call enqueues hand-written kernels and returns without waiting.
+swift_prompt_attention and swift_prefix_attention, and of their forms for a cache held in 8 bits (swift_coded_append and so on);
+include/swift.h says what each computes.  As in binding.py, torch only provides memory and streams; every call enqueues hand-written
+kernels and returns without waiting.
 
 A program that runs several sequences keeps one PagedKV for all layers, makes a RowBatch per step (or keeps one whose
 device tensors it rewrites), and calls per layer:
@@ -8,6 +9,8 @@ device tensors it rewrites), and calls per layer:
     q = batch.append(block, q, k, v, rope=table)      # norm + rotation of q and k, K and V into the pages
     o = batch.prompt_attention(block, q)              # whole prompts, or chunks of them
     o = batch.prefix_attention(block, q)              # a few rows per sequence behind a shared prefix
+
+With PagedKV(pool, scales) over an int8 or float8_e4m3fn pool the same calls read and write 8-bit codes.
 """
 from __future__ import annotations
 
@@ -19,10 +22,15 @@ import torch
 from .binding import SwiftError, _DevBuf, lib
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_CODES = {torch.int8: 3, torch.float8_e4m3fn: 4}
 
 
 class _Kv(C.Structure):
     _fields_ = [("pool", C.c_void_p)] + [(n, C.c_int32) for n in ("dtype", "n_pages", "n_blocks", "n_kv_heads", "page_size", "head_dim")]
+
+
+class _Kv8(C.Structure):
+    _fields_ = [("kv", _Kv), ("scales", C.c_void_p)]
 
 
 class _Batch(C.Structure):
@@ -158,17 +166,30 @@ def _rope_table(s: int, desc: _RopeDesc, device: torch.device, out: Optional[tor
 
 class PagedKV:
     """One K,V pool for all layers: a contiguous CUDA tensor [n_pages, n_blocks, 2, n_kv_heads, page_size, head_dim] the
-    caller made (fp32, bf16 or fp16); [.., 0, ..] is K, [.., 1, ..] is V."""
+    caller made (fp32, bf16 or fp16); [.., 0, ..] is K, [.., 1, ..] is V.
 
-    def __init__(self, pool: torch.Tensor):
+    8-bit caches: an int8 or float8_e4m3fn pool of codes with scales, contiguous fp32 [n_pages, n_blocks, 2, n_kv_heads]: a page's K (or
+    V) of one kv head shares a scale, value = code * scale.  Both may be torch.empty: append writes a page's scale with its first row.  q,
+    k, v and the results are then fp32, bf16 or fp16, whichever the caller has."""
+
+    def __init__(self, pool: torch.Tensor, scales: Optional[torch.Tensor] = None):
         _cuda_tensor("pool", pool)
         if pool.requires_grad:
             _gradient("pool")
-        if pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_contiguous() or pool.dtype not in _TYPES:
-            raise ValueError("pool must be contiguous [n_pages, n_blocks, 2, n_kv_heads, page_size, head_dim] in fp32, bf16 or fp16")
-        self.pool, self.device, self.dtype = pool, pool.device, pool.dtype
+        eight = scales is not None
+        if pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_contiguous() or pool.dtype not in (_CODES if eight else _TYPES):
+            raise ValueError("pool must be contiguous [n_pages, n_blocks, 2, n_kv_heads, page_size, head_dim] in fp32, bf16 or fp16, or with scales "
+                             "in int8 or float8_e4m3fn")
+        self.pool, self.scales, self.device, self.dtype = pool, scales, pool.device, pool.dtype
         self.n_pages, self.n_blocks, _, self.n_kv_heads, self.page_size, self.head_dim = pool.shape
-        self._c = _Kv(pool.data_ptr(), _TYPES[pool.dtype], self.n_pages, self.n_blocks, self.n_kv_heads, self.page_size, self.head_dim)
+        self._c = _Kv(pool.data_ptr(), _CODES[pool.dtype] if eight else _TYPES[pool.dtype], self.n_pages, self.n_blocks, self.n_kv_heads, self.page_size, self.head_dim)
+        if eight:
+            _cuda_tensor("scales", scales, pool.device)
+            if scales.requires_grad:
+                _gradient("scales")
+            if scales.dtype != torch.float32 or scales.shape != pool.shape[:4] or not scales.is_contiguous():
+                raise ValueError(f"scales must be contiguous float32 {tuple(pool.shape[:4])}")
+            self._c = _Kv8(self._c, scales.data_ptr())
 
 
 class RowBatch:
@@ -212,12 +233,13 @@ class RowBatch:
         self.kv, self.n_seqs, self.n_rows = kv, n_seqs, n_rows
         self.max_rows = max(1, n_rows if max_rows is None else min(max_rows, n_rows))
         self._keep = (row_start, kv_len, page_table, prefix_pages)
-        self._tensors = (kv.pool, *self._keep)
+        self._tensors = (kv.pool, kv.scales, *self._keep)
         self._c = _Batch(n_seqs, n_rows, row_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), page_table.shape[1],
                          prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len)
         self._kv_p, self._c_p = C.byref(kv._c), C.byref(self._c)
-        self._lib, self._types, self._x_types, self._scale = lib(), (kv.dtype,), (kv.dtype, torch.float32), kv.head_dim ** -0.5
-        self._ws_bytes = {}
+        self._lib, self._scale, self._ws_bytes = lib(), kv.head_dim ** -0.5, {}
+        self._eight = kv.scales is not None
+        self._types, self._x_types = (tuple(_TYPES), tuple(_TYPES)) if self._eight else ((kv.dtype,), (kv.dtype, torch.float32))
 
     # ------------------------------------------------------------------ checks shared by the calls
     def _rows(self, name: str, t: torch.Tensor, heads: Optional[int], dtypes) -> _Rows:
@@ -245,16 +267,16 @@ class RowBatch:
             raise ValueError(f"{name} must be contiguous float32 [{self.kv.head_dim}]")
         return g.data_ptr()
 
-    def _out(self, out: Optional[torch.Tensor], heads: int) -> torch.Tensor:
+    def _out(self, out: Optional[torch.Tensor], heads: int, dtype: torch.dtype) -> torch.Tensor:
         kv = self.kv
         if out is None:
-            return torch.empty(self.n_rows, heads, kv.head_dim, dtype=kv.dtype, device=kv.device)
+            return torch.empty(self.n_rows, heads, kv.head_dim, dtype=dtype, device=kv.device)
         if not isinstance(out, torch.Tensor) or out.device != kv.device:
             _cuda_tensor("out", out, kv.device)
         if out.requires_grad:
             _gradient("out")
-        if out.shape != (self.n_rows, heads, kv.head_dim) or out.dtype != kv.dtype or not out.is_contiguous():
-            raise ValueError(f"out must be contiguous {(self.n_rows, heads, kv.head_dim)} of {kv.dtype}")
+        if out.shape != (self.n_rows, heads, kv.head_dim) or out.dtype != dtype or not out.is_contiguous():
+            raise ValueError(f"out must be contiguous {(self.n_rows, heads, kv.head_dim)} of {dtype}")
         return out
 
     # ------------------------------------------------------------------ the calls
@@ -263,9 +285,11 @@ class RowBatch:
                eps: float = 1e-5, positions: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Norm (where a gain fp32 [head_dim] is given) and rotation (where a rope_table is given) of q and k, K and V into the
-        cache's block; returns the finished q [n_rows, heads, head_dim] in the cache's type.  q, k, v: [n_rows, heads, head_dim]
-        views (slices of a fused projection), fp32 or the cache's type.  Rows left out (padding, pages or positions out of
-        range) keep what `out` held.  positions: int32 [n_rows], instead of prefix_len + own position."""
+        cache's block; returns the finished q [n_rows, heads, head_dim] in the cache's type (8-bit caches: in q's).  q, k, v: [n_rows,
+        heads, head_dim] views (slices of a fused projection), fp32 or the cache's type (8-bit caches: fp32, bf16 or fp16).  Rows left
+        out (padding, pages or positions out of range) keep what `out` held.  positions: int32 [n_rows], instead of prefix_len + own
+        position.  8-bit caches: a page's scale is that of its largest value so far; where a new row is larger, the page's codes are
+        rounded anew."""
         kv = self.kv
         heads = kv.n_kv_heads
         rows = (self._rows("q", q, None, self._x_types), self._rows("k", k, heads, self._x_types), self._rows("v", v, heads, self._x_types))
@@ -288,12 +312,13 @@ class RowBatch:
                 raise ValueError(f"positions must be [{self.n_rows}]")
             positions_p = positions.data_ptr()
         a = _Append(_number("block", block), q.shape[1], _TYPES[q.dtype], *rows, q_gain_p, k_gain_p, eps, rope_p, rope_rows, 2 * pairs, 1 if interleaved else 0, positions_p, None)
-        return _on(kv.device, stream, () if stream is None else (q, k, v, rope, q_gain, k_gain, positions, out, *self._tensors), self._append, a, out)
+        return _on(kv.device, stream, () if stream is None else (q, k, v, rope, q_gain, k_gain, positions, out, *self._tensors), self._append, a, out, q.dtype)
 
-    def _append(self, s: int, a: _Append, out: Optional[torch.Tensor]) -> torch.Tensor:
-        out = self._out(out, a.n_heads)
+    def _append(self, s: int, a: _Append, out: Optional[torch.Tensor], dtype: torch.dtype) -> torch.Tensor:
+        out = self._out(out, a.n_heads, dtype if self._eight else self.kv.dtype)
         a.q_out = out.data_ptr()
-        _check(self._lib.swift_kv_append(self._kv_p, self._c_p, C.byref(a), s))
+        call = self._lib.swift_coded_append if self._eight else self._lib.swift_kv_append
+        _check(call(self._kv_p, self._c_p, C.byref(a), s))
         return out
 
     def _attention(self, block: int, q: torch.Tensor, scale: Optional[float]) -> _Attention:
@@ -303,32 +328,43 @@ class RowBatch:
     def prompt_attention(self, block: int, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Causal attention of every row over the prefix and its sequence's own positions up to its own; [n_rows, heads,
-        head_dim] in the cache's type.  scale defaults to head_dim ** -0.5.  Padding rows keep what `out` held."""
-        return _on(self.kv.device, stream, () if stream is None else (q, out, *self._tensors), self._prompt, self._attention(block, q, scale), out)
+        head_dim] in q's type, which is the cache's (8-bit caches: bf16 or fp16, or fp32 in slower fp32 arithmetic).  scale defaults to
+        head_dim ** -0.5.  Padding rows keep what `out` held."""
+        return _on(self.kv.device, stream, () if stream is None else (q, out, *self._tensors), self._prompt, self._attention(block, q, scale), out, q.dtype)
 
-    def _prompt(self, s: int, a: _Attention, out: Optional[torch.Tensor]) -> torch.Tensor:
-        out = self._out(out, a.n_heads)
+    def _prompt(self, s: int, a: _Attention, out: Optional[torch.Tensor], dtype: torch.dtype) -> torch.Tensor:
+        out = self._out(out, a.n_heads, dtype)
         a.out = out.data_ptr()
-        _check(self._lib.swift_prompt_attention(self._kv_p, self._c_p, C.byref(a), s))
+        if self._eight:
+            _check(self._lib.swift_coded_prompt_attention(self._kv_p, self._c_p, C.byref(a), _TYPES[dtype], s))
+        else:
+            _check(self._lib.swift_prompt_attention(self._kv_p, self._c_p, C.byref(a), s))
         return out
 
     def prefix_attention(self, block: int, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The same function for few rows per sequence: what all rows share of the prefix is computed once for all of them.
         Rows of a sequence beyond max_rows are left out."""
-        return _on(self.kv.device, stream, () if stream is None else (q, out, *self._tensors), self._prefix, self._attention(block, q, scale), out)
+        return _on(self.kv.device, stream, () if stream is None else (q, out, *self._tensors), self._prefix, self._attention(block, q, scale), out, q.dtype)
 
-    def _prefix(self, s: int, a: _Attention, out: Optional[torch.Tensor]) -> torch.Tensor:
-        need = self._ws_bytes.get(a.n_heads)
+    def _prefix(self, s: int, a: _Attention, out: Optional[torch.Tensor], dtype: torch.dtype) -> torch.Tensor:
+        need = self._ws_bytes.get((a.n_heads, dtype))
         if need is None:
-            need = self._lib.swift_prefix_workspace_bytes(self._kv_p, self._c_p, a.n_heads, self.max_rows)
+            if self._eight:
+                need = self._lib.swift_coded_prefix_workspace_bytes(self._kv_p, self._c_p, a.n_heads, self.max_rows, _TYPES[dtype])
+            else:
+                need = self._lib.swift_prefix_workspace_bytes(self._kv_p, self._c_p, a.n_heads, self.max_rows)
             if need == 0:
                 raise SwiftError(1, self._lib.swift_batch_error().decode())
-            self._ws_bytes[a.n_heads] = need
-        out = self._out(out, a.n_heads)
+            self._ws_bytes[a.n_heads, dtype] = need
+        out = self._out(out, a.n_heads, dtype)
         a.out = out.data_ptr()
         ws = torch.empty(need, dtype=torch.uint8, device=self.kv.device)     # of this call alone; the allocator aligns to 512
-        _check(self._lib.swift_prefix_attention(self._kv_p, self._c_p, C.byref(a), self.max_rows, _DevBuf(ws.data_ptr(), need), s))
+        buf = _DevBuf(ws.data_ptr(), need)
+        if self._eight:
+            _check(self._lib.swift_coded_prefix_attention(self._kv_p, self._c_p, C.byref(a), _TYPES[dtype], self.max_rows, buf, s))
+        else:
+            _check(self._lib.swift_prefix_attention(self._kv_p, self._c_p, C.byref(a), self.max_rows, buf, s))
         return out
 
 
