@@ -2,8 +2,7 @@
 // swift_coded_prompt_attention and swift_coded_prefix_attention.  No context and no state between calls.
 // This translation unit gets its own copies of the shared device code (separate namespace).
 #define swk swk_batch8
-#include "kernels_batch8.cuh"
-#include "kernels_batch_dec.cuh"
+#include "kernels_batch8_dec.cuh"
 #include "batch_host.cuh"
 
 cudaError_t swift_batch8_waits(unsigned* count, cudaStream_t s)
@@ -111,6 +110,130 @@ cudaError_t launch_append8_any(int dtype, const BatchView& bv, const Append8View
     return dtype == SWIFT_I8 ? launch_append8<TX, int8_t>(bv, v, kv_vec, s) : launch_append8<TX, __nv_fp8_e4m3>(bv, v, kv_vec, s);
 }
 
+// ------------------------------------------------------------------------------ few rows per sequence
+// [page][block, K/V, kv head][slot][dim] bytes, seen as [plane][K, V][slot][dim] with overlapping planes (plane + n_kv_heads holds the V
+// of plane's K): one box brings a page's K and V for a kv head.  dp: bytes of a row in shared memory, 64 or 128; what lies beyond head_dim is 0.
+swift_status make_codes_map(const swift_paged_kv* kv, int dp, int most_slots, CUtensorMap* out)
+{
+    const EncodeTiled encode = encoder();
+    if (!encode) return fail_batch(SWIFT_ECUDA, "cuTensorMapEncodeTiled not available from the driver");
+    const cuuint64_t row = kv->head_dim, plane = row * kv->page_size;
+    const cuuint64_t dims[4] = {row, (cuuint64_t)kv->page_size, 2, 2ull * kv->n_blocks * kv->n_kv_heads * kv->n_pages};
+    const cuuint64_t strides[3] = {row, plane * kv->n_kv_heads, plane};
+    const cuuint32_t box[4] = {(cuuint32_t)dp, (cuuint32_t)(kv->page_size < most_slots ? kv->page_size : most_slots), 2, 1}, one[4] = {1, 1, 1, 1};
+    const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, kv->pool, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              dp == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail_batch(SWIFT_EINVAL, "cuTensorMapEncodeTiled refused the tensor (code %d): a cache of odd size", (int)r);
+    return SWIFT_OK;
+}
+
+struct Plan8 {
+    bool rows;                  // fp32 arithmetic: no tensor-core form
+    bool few, prefix_few;       // the few-row kernel takes the sequences' own parts; and the prefix
+    int group, dp, mt, grid;
+    long long items;
+    size_t few_o, few_ml, first, last, bytes;             // offsets in the workspace
+};
+inline int unit_keys8(int mt) { return mt == 1 ? 32 : 64; }
+
+swift_status plan_prefix8(const swift_coded_kv* c, const BatchView& bv, int n_heads, int max_rows, int x_dtype, Plan8* p)
+{
+    *p = Plan8();
+    const swift_paged_kv* kv = &c->kv;
+    const int Hk = kv->n_kv_heads, sms = multiprocessors();
+    if (max_rows > bv.n_rows) max_rows = bv.n_rows;
+    p->group = n_heads / Hk;
+    p->dp = kv->head_dim > 64 ? 128 : 64;
+    size_t at = 0;
+    auto take = [&](size_t n) { const size_t o = at; at += (n + 255) / 256 * 256; return o; };
+    p->rows = !tensor_core_shape8(kv, x_dtype, n_heads);
+    if (!p->rows) {
+        const long long own = (long long)max_rows * p->group, all = (long long)bv.n_rows * p->group;
+        p->few = own <= BD_MAX_ROWS;
+        p->mt = own <= 16 ? 1 : own <= 32 ? 2 : 4;
+        p->prefix_few = p->few && bv.prefix_len > 0 && all <= 16 * p->mt;
+        if (!p->few || (bv.prefix_len > 0 && !p->prefix_few)) p->rows = true;
+    }
+    if (!p->rows) {
+        p->items = (long long)(bv.n_seqs + (p->prefix_few ? 1 : 0)) * Hk;
+        p->grid = sms;
+        const int keys = unit_keys8(p->mt);
+        const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, keys) + ceil_div(bv.prefix_len, keys)) * Hk;
+        if (units > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a page table of %d x %d for %d kv heads is beyond 2^31 units of work", bv.n_seqs, bv.table_stride, Hk);
+        if (2ll * kv->n_blocks * Hk * kv->n_pages > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a pool of %d pages of %d heads is beyond 2^31 planes", kv->n_pages, 2 * kv->n_blocks * Hk);
+        const size_t rows_all = (size_t)(p->items + (long long)p->grid * (BD_WARPS / p->mt)) * 16 * p->mt;
+        p->few_o = take(rows_all * p->dp * 4);
+        p->few_ml = take(rows_all * 8);
+        p->first = take((size_t)p->items * 4);
+        p->last = take((size_t)p->items * 4);
+    }
+    p->bytes = at > 256 ? at : 256;
+    return SWIFT_OK;
+}
+
+template <typename QT, typename CODE, int DP, int MT>
+cudaError_t launch_dec8(const CUtensorMap& map, const BatchView& bv, const BdArgs& g, int grid, cudaStream_t s, bool after_previous)
+{
+    static std::atomic<unsigned long long> done{0};
+    const cudaError_t e = allow_smem(attn_batch8_dec_kernel<QT, CODE, DP, MT>, B8Shape<DP, MT>::SMEM_BYTES, done);
+    if (e != cudaSuccess) return e;
+    return launch(attn_batch8_dec_kernel<QT, CODE, DP, MT>, dim3(grid), BD_THREADS, B8Shape<DP, MT>::SMEM_BYTES, s, after_previous, map, bv, g);
+}
+template <typename QT, typename CODE>
+cudaError_t launch_dec8_any(const Plan8& p, const CUtensorMap& map, const BatchView& bv, const BdArgs& g, cudaStream_t s, bool after)
+{
+    if (p.dp == 128) {
+        if (p.mt == 1) return launch_dec8<QT, CODE, 128, 1>(map, bv, g, p.grid, s, after);
+        if (p.mt == 2) return launch_dec8<QT, CODE, 128, 2>(map, bv, g, p.grid, s, after);
+        return launch_dec8<QT, CODE, 128, 4>(map, bv, g, p.grid, s, after);
+    }
+    if (p.mt == 1) return launch_dec8<QT, CODE, 64, 1>(map, bv, g, p.grid, s, after);
+    if (p.mt == 2) return launch_dec8<QT, CODE, 64, 2>(map, bv, g, p.grid, s, after);
+    return launch_dec8<QT, CODE, 64, 4>(map, bv, g, p.grid, s, after);
+}
+
+template <typename T>
+cudaError_t launch_join8(const Plan8& p, const BatchView& bv, const BjArgs& j, cudaStream_t s)
+{
+    const bool cut = p.few && (long long)p.grid * (BD_WARPS / p.mt) > 8 * p.items;       // as for the 16-bit cache
+    return cut ? launch(attn_join_kernel<T, 8>, dim3(bv.n_rows, j.a.n_heads), 256, 0, s, true, bv, j)
+               : launch(attn_join_kernel<T, 1>, dim3(bv.n_rows, ceil_div(j.a.n_heads, 8)), 256, 0, s, true, bv, j);
+}
+
+template <typename QT>
+swift_status run_prefix8(const swift_coded_kv* c, const BatchView& bv, const AttnView& av, int block, const Plan8& p, unsigned char* ws, cudaStream_t s)
+{
+    const swift_paged_kv* kv = &c->kv;
+    BdArgs g = {};
+    g.a = av;
+    g.block = block;
+    g.prefix_here = p.prefix_few;
+    g.planes = 2 * kv->n_blocks * kv->n_kv_heads * kv->n_pages;
+    g.part_o = reinterpret_cast<float*>(ws + p.few_o);
+    g.part_ml = reinterpret_cast<float2*>(ws + p.few_ml);
+    g.item_first = reinterpret_cast<int*>(ws + p.first);
+    g.item_last = reinterpret_cast<int*>(ws + p.last);
+    CUtensorMap map;
+    const swift_status st = make_codes_map(kv, p.dp, unit_keys8(p.mt), &map);
+    if (st != SWIFT_OK) return st;
+    cudaError_t e = kv->dtype == SWIFT_I8 ? launch_dec8_any<QT, int8_t>(p, map, bv, g, s, false) : launch_dec8_any<QT, __nv_fp8_e4m3>(p, map, bv, g, s, false);
+    BjArgs j = {};
+    j.a = av;
+    j.dp = p.dp;
+    j.item_rows = 16 * p.mt;
+    j.prefix_here = p.prefix_few;
+    j.own_here = p.few;
+    j.many_o = j.few_o = g.part_o;
+    j.many_ml = j.few_ml = g.part_ml;
+    j.item_first = g.item_first;
+    j.item_last = g.item_last;
+    j.workers = p.grid * (BD_WARPS / p.mt);
+    if (e == cudaSuccess) e = launch_join8<QT>(p, bv, j, s);
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+
 swift_status prompt8(const swift_coded_kv* c, const swift_row_batch* batch, const swift_attention_args* args, int x_dtype, int probe_us, cudaStream_t s)
 {
     BatchView bv;
@@ -127,16 +250,20 @@ swift_status prefix8(const swift_coded_kv* c, const swift_row_batch* batch, cons
 {
     BatchView bv;
     AttnView av;
-    const swift_status st = check_attention8(c, batch, args, x_dtype, &bv, &av);
+    swift_status st = check_attention8(c, batch, args, x_dtype, &bv, &av);
     if (st != SWIFT_OK) return st;
     if (max_rows < 1) return fail_batch(SWIFT_EINVAL, "max_rows %d", max_rows);
     if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
+    Plan8 p;
+    st = plan_prefix8(c, bv, av.n_heads, max_rows, x_dtype, &p);
+    if (st != SWIFT_OK) return st;
     if (!workspace.dptr || !aligned(workspace.dptr, 256)) return fail_batch(SWIFT_EINVAL, "the workspace must be 256-byte aligned device memory");
-    const size_t need = 256;
-    if (workspace.bytes < need) return fail_batch(SWIFT_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace.bytes, need);
+    if (workspace.bytes < p.bytes) return fail_batch(SWIFT_ECAPACITY, "workspace of %zu bytes, %zu needed", workspace.bytes, p.bytes);
     av.max_rows = max_rows;
     set_probe(&av, probe_us);
-    return run_rows8(&c->kv, x_dtype, bv, av, s);
+    if (p.rows) return run_rows8(&c->kv, x_dtype, bv, av, s);
+    unsigned char* ws = reinterpret_cast<unsigned char*>(workspace.dptr);
+    return x_dtype == SWIFT_BF16 ? run_prefix8<__nv_bfloat16>(c, bv, av, args->block, p, ws, s) : run_prefix8<__half>(c, bv, av, args->block, p, ws, s);
 }
 
 } // namespace
@@ -184,7 +311,8 @@ size_t swift_coded_prefix_workspace_bytes(const swift_coded_kv* c, const swift_r
         fail_batch(SWIFT_EINVAL, "n_heads %d, max_rows %d, type %d", n_heads, max_rows, x_dtype);
         return 0;
     }
-    return 256;
+    Plan8 p;
+    return plan_prefix8(c, bv, n_heads, max_rows, x_dtype, &p) == SWIFT_OK ? p.bytes : 0;
 }
 
 swift_status swift_coded_prefix_attention(const swift_coded_kv* c, const swift_row_batch* batch, const swift_attention_args* args, int32_t x_dtype,

@@ -1,0 +1,391 @@
+// Attention of few query rows per sequence over a cache of 8-bit codes: the few-row kernel of the 16-bit cache (kernels_batch_dec.cuh:
+// items, units, workers, parts and their joining are its own), with half the bytes per key, which must then be turned into operands at
+// twice the rate.
+//
+// Operands.  Products are fp16 mma.sync.m16n8k16 with fp32 sums, whatever q's type: int8 and e4m3 codes are exact in fp16, and q is too
+// once each row is brought to [2^14, 2^15) by a power of two (elements below 2^-38 of the row's largest lose bits).  The instruction takes its
+// 16 dims in any order that both operands share: lane t of four takes dims 4 t .. 4 t + 3, so that the 4 bytes that ldmatrix gives it are its
+// operand's 4 elements.  For the second product ldmatrix.trans gives a lane 2 keys x 2 dims; one byte permutation makes two
+// operands of them, of the even and the odd dims, and a lane's results are 4 neighbouring dims again.
+// int8: bytes with 128 added become the low bytes of 1024 + code + 128 in fp16, one subtraction makes that the code: 5 instructions for 4
+// codes.  e4m3: one conversion for two.
+//
+// Scales.  A score's scale is its page's; V's must be applied to the weights, before the sum over keys.  With t = c s + log2 sv (c: scale x
+// sk x log2 e) a weight is w = 2^(t - r), r a running maximum of t, the sum of probabilities is that of w / sv, and no multiplication per
+// weight is needed.  Weights carry a factor 2^7 against subnormals and are rounded to fp16.  t - r is exact where it matters, so scores
+// far from zero need no path of their own.
+#pragma once
+#include "kernels_batch8.cuh"
+#include "kernels_batch_dec.cuh"
+
+namespace swk {
+
+constexpr float B8_BIAS = 7.f;                            // weights are at most 2^(BT_GROW + 7)
+
+template <int DP_, int MT> struct B8Shape {               // DP: bytes of a staged row, 64 or 128
+    static constexpr int DP = DP_;
+    static constexpr int KEYS = MT == 1 ? 32 : 64;        // per unit
+    static constexpr int WORKERS = BD_WARPS / MT;
+    static constexpr int UNIT_BYTES = 2 * KEYS * DP;
+    static constexpr int STAGES = 192 * 1024 / (WORKERS * UNIT_BYTES);
+    static constexpr int RING_BYTES = WORKERS * STAGES * UNIT_BYTES;
+    static constexpr int Q_BYTES = 16 * 2 * DP;           // a warp's queries, 16 bits
+    static constexpr int BOXES = KEYS / 8;                // most pages of a unit
+    static constexpr int SCALE_BYTES = WORKERS * STAGES * BOXES * 8;
+    static constexpr int SMEM_BYTES = 1024 + RING_BYTES + BD_WARPS * Q_BYTES + SCALE_BYTES;
+};
+
+// What a key group needs of its page's scales.  0 stands for a page of zeros, whose codes are 0.
+struct B8Scale { float c, lv, inv; };                     // scale sk log2 e; log2 sv; 1 / sv
+__device__ __forceinline__ B8Scale b8_scale(float sk, float sv, float c)
+{
+    const float nan = __int_as_float(0x7FC00000);
+    const float v = sv == 0.f ? 1.f : fmaxf(sv, CODE_SMALLEST);
+    const bool good = sv >= 0.f && sv <= CODE_LARGEST;
+    return {sk >= 0.f ? c * sk : nan, good ? __log2f(v) : nan, __frcp_rn(v)};
+}
+
+// 4 codes -> 2 operand registers: of bytes 0 and 1, 2 and 3 (NEXT), or of bytes 0 and 2, 1 and 3
+template <bool NEXT> __device__ __forceinline__ void b8_operands(uint32_t x, uint32_t& a, uint32_t& b, int8_t)
+{
+    x ^= 0x80808080u;
+    const uint32_t p = __byte_perm(x, 0x64646464u, NEXT ? 0x4140 : 0x4240), q = __byte_perm(x, 0x64646464u, NEXT ? 0x4342 : 0x4341);
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(a) : "r"(p), "r"(0x64806480u));
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(b) : "r"(q), "r"(0x64806480u));
+}
+template <bool NEXT> __device__ __forceinline__ void b8_operands(uint32_t x, uint32_t& a, uint32_t& b, __nv_fp8_e4m3)
+{
+    if (!NEXT) x = __byte_perm(x, 0, 0x3120);
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(a), "=r"(b) : "r"(x));
+}
+
+// A power of two that brings a largest magnitude to [2^14, 2^15), and its inverse
+__device__ __forceinline__ float b8_lift(float top, float& inverse)
+{
+    const int e = top > 0.f ? min(max(141 - (int)(__float_as_uint(top) >> 23), -126), 126) : 0;      // 14 - (exponent - 127)
+    inverse = __uint_as_float((uint32_t)(127 - e) << 23);
+    return __uint_as_float((uint32_t)(127 + e) << 23);
+}
+
+// QT: q's type; CODE: the codes'; the rest as attn_batch_dec_kernel.
+template <typename QT, typename CODE, int DPT, int MT>
+__global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __grid_constant__ CUtensorMap map_kv, BatchView b, BdArgs g)
+{
+    typedef B8Shape<DPT, MT> S;
+    constexpr int DP = DPT, KEYS = S::KEYS, R = 16 * MT, CHUNKS = DP / 16;
+    constexpr bool MAY_BE_NAN = !std::is_same<CODE, int8_t>::value;
+    pdl_trigger();
+
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    __shared__ __align__(8) unsigned long long bars[S::WORKERS * S::STAGES * 2];
+    __shared__ unsigned page_bits[S::WORKERS * S::STAGES];
+    __shared__ int sums[BD_THREADS / 32];
+    __shared__ int waits_sh[2];
+    volatile int* waits = waits_sh;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, Hk = g.a.n_kv_heads, G = g.a.n_heads / Hk;
+    const int wk = warp / MT, mt = warp % MT, gq = lane >> 2, t = lane & 3;
+    auto full = [&](int s) { return smem_u32(&bars[wk * S::STAGES + s]); };
+    auto empty = [&](int s) { return smem_u32(&bars[(S::WORKERS + wk) * S::STAGES + s]); };
+    const uint32_t scales_sh = base + S::RING_BYTES + BD_WARPS * S::Q_BYTES + wk * S::STAGES * S::BOXES * 8;
+    if (tid == 0) {
+        // a stage is full when its boxes have landed (one arrival and their bytes) and the lanes' copies of its scales (an arrival each)
+        for (int s = 0; s < S::WORKERS * S::STAGES; ++s) { mbar_init(smem_u32(&bars[s]), 33); mbar_init(smem_u32(&bars[S::WORKERS * S::STAGES + s]), MT); }
+        waits[0] = 0;
+        waits[1] = g.a.wait_kcycles;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_kv) : "memory");
+    }
+    // units of the whole batch (the host has made sure that they fit an int)
+    const int prefix_units = g.prefix_here ? (b.prefix_len + KEYS - 1) / KEYS : 0;
+    int own = 0;
+    for (int i = tid; i < b.n_seqs; i += BD_THREADS) own += bd_units<KEYS>(seq_span(b, i));
+    own = __reduce_add_sync(FULL_WARP, own);
+    if (lane == 0) sums[warp] = own;
+    __syncthreads();
+    long long U = prefix_units;
+#pragma unroll
+    for (int w = 0; w < BD_THREADS / 32; ++w) U += sums[w];
+    U *= Hk;
+    const int all = gridDim.x * S::WORKERS, workers = (int)(U < (long long)all ? U : (long long)all), me = blockIdx.x * S::WORKERS + wk;
+    const long long u0 = me < workers ? U * me / workers : 0, u1 = me < workers ? U * (me + 1) / workers : 0;
+    const int count = (int)(u1 - u0);
+
+    if (count > 0) {
+        const uint32_t stages = base + wk * S::STAGES * S::UNIT_BYTES;
+        const float c = g.a.scale * 1.4426950408889634f;
+        const int box_rows = min(b.page_size, KEYS), box_shift = min(b.page_shift, 31 - __clz(KEYS));
+        const int per_unit = KEYS >> box_shift;                           // boxes (pages, or part of one) per unit, 1..8
+        const unsigned all_boxes = (1u << per_unit) - 1u;
+        BdWalk w;
+        bd_start<KEYS>(b, g, prefix_units, u0, w);
+
+        // ---- the fetching side, by the worker's first warp.  Shared memory: box after box [K, V][slot][dim]
+        const uint32_t box_v = box_rows * DP, box_bytes = 2 * box_v;
+        BdWalk wf = w;
+        int asked = 0, f_stage = 0, next_page = 0;                        // next_page: lane p: page of box p of unit `asked`
+        uint32_t f_turn = 0;
+        auto look_up = [&]() {
+            next_page = -1;                                               // beyond the end: no page
+            const int key0 = wf.unit * KEYS;
+            if (lane < per_unit && lane * box_rows < wf.sp.len - key0) {
+                const int at = (key0 + lane * box_rows) >> b.page_shift;
+                next_page = wf.seq < 0 ? b.prefix_pages[at] : b.page_table[(size_t)wf.seq * b.table_stride + at];
+            }
+        };
+        auto ask = [&]() {                                                // asks for unit `asked`; its stage is free
+            const bool good = (unsigned)next_page < (unsigned)b.n_pages;
+            const int page = good ? next_page : b.n_pages;                // beyond the last page: zeros
+            const unsigned pages = __ballot_sync(FULL_WARP, good) & all_boxes;
+            const bool asks = !(g.a.withhold && asked == 0);
+            if (elect_one()) {
+                page_bits[wk * S::STAGES + f_stage] = pages;
+                if (asks) mbar_expect_tx(full(f_stage), (uint32_t)S::UNIT_BYTES);
+            }
+            __syncwarp();
+            const uint32_t dst = stages + f_stage * S::UNIT_BYTES;
+            const int plane = g.block * 2 * Hk + wf.kvh;
+            for (int p = 0; asks && p < per_unit; ++p) {
+                const int pageu = __shfl_sync(FULL_WARP, page, p), slot0 = (wf.unit * KEYS + p * box_rows) & (b.page_size - 1);
+                if (elect_one()) tma_load_4d(dst + p * box_bytes, &map_kv, 0, slot0, 0, pageu == b.n_pages ? g.planes : pageu * (g.planes / b.n_pages) + plane, full(f_stage));
+            }
+            if (lane < per_unit && good) {                                // its scales; those of no page are not looked at
+                const float* s = g.a.scales + page * g.a.scale_page + wf.kvh;
+                const uint32_t at = scales_sh + (f_stage * S::BOXES + lane) * 8;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at), "l"(s) : "memory");
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at + 4u), "l"(s + Hk) : "memory");
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full(f_stage)) : "memory");
+            if (wf.unit == 0 || wf.unit + 1 == wf.units) {
+                if (wf.unit == 0) g.item_first[wf.item] = me;             // (all lanes write the same)
+                if (wf.unit + 1 == wf.units) g.item_last[wf.item] = me;
+            }
+            if (++f_stage == S::STAGES) { f_stage = 0; f_turn ^= 1u; }
+            if (++asked < count) {
+                bd_next<KEYS>(b, g, wf);
+                look_up();
+            }
+        };
+        if (mt == 0) {
+            look_up();
+            for (int i = 0; i < S::STAGES && asked < count; ++i) ask();
+        }
+        // ldmatrix: lane l names row l & 7 of matrix l >> 3.  K: a matrix is 8 keys x 16 dims, V: too, of keys 0..7 and 8..15 in turn
+        const uint32_t swz = DP == 128 ? lane & 7 : (lane & 7) >> 1, row_at = (lane & 7) * DP;
+        auto group_at = [&](int key) { return (uint32_t)((key >> box_shift) * box_bytes + (key & (box_rows - 1)) * DP); };   // of 8 keys
+        const uint32_t v_key = ((lane >> 3) & 1) * 8, v_chunk = lane >> 4, k_chunk = lane >> 3;
+
+        uint32_t turn = 0;
+        int stage = 0;
+        bool ok = true, fresh = true;                                     // fresh: first unit of an item here
+        uint32_t qf[CHUNKS][4];
+        float lower[2] = {1.f, 1.f};                                      // undo the rows' powers of two
+        float o[2 * CHUNKS][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        const int rho[2] = {16 * mt + gq, 16 * mt + gq + 8};              // this thread's two packed rows, their tokens
+        const int tok[2] = {rho[0] / G, rho[1] / G};
+        unsigned char* q_mem = smem_raw + (base - smem_u32(smem_raw)) + S::RING_BYTES + warp * S::Q_BYTES;
+        const uint32_t q_sh = base + S::RING_BYTES + warp * S::Q_BYTES;
+        auto fetch_q = [&](const BdWalk& item) {                          // this warp's 16 rows of an item's queries; dead rows zero
+#pragma unroll
+            for (int i = 0; i < CHUNKS; ++i) {
+                const int row = (i * 32 + lane) / (2 * CHUNKS), piece = (i * 32 + lane) % (2 * CHUNKS), r = 16 * mt + row, tk = r / G;
+                const bool live = r < item.sp.n * G && 8 * piece < g.a.head_dim;
+                const QT* q = reinterpret_cast<const QT*>(g.a.q) + (size_t)(item.sp.r0 + (live ? tk : 0)) * g.a.q_row_stride +
+                              (size_t)(item.kvh * G + (live ? r - tk * G : 0)) * g.a.q_head_stride + (live ? 8 * piece : 0);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(q_sh + row * 2 * DP + ((piece ^ (row & 7)) << 4)), "l"(q), "r"(live ? 16 : 0) : "memory");
+            }
+        };
+        fetch_q(w);
+        for (int k = 0; k < count; ++k) {
+            if (fresh) {
+                // queries into fragments: 4 dims of each 16, fp16, every row at its power of two
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                __syncwarp();
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x[CHUNKS][4], top = 0.f;
+#pragma unroll
+                    for (int ks = 0; ks < CHUNKS; ++ks) {
+                        const int row = gq + 8 * e, piece = 2 * ks + (t >> 1);
+                        const uint2 v = *reinterpret_cast<const uint2*>(q_mem + row * 2 * DP + ((piece ^ (row & 7)) << 4) + (t & 1) * 8);
+                        const QT* h = reinterpret_cast<const QT*>(&v);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            x[ks][i] = to_float(h[i]);
+                            if (fabsf(x[ks][i]) < INFINITY) top = fmaxf(top, fabsf(x[ks][i]));
+                        }
+                    }
+                    top = fmaxf(top, __shfl_xor_sync(FULL_WARP, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(FULL_WARP, top, 2));
+                    const float lift = b8_lift(top, lower[e]);
+#pragma unroll
+                    for (int ks = 0; ks < CHUNKS; ++ks) {
+                        qf[ks][e] = pack2(x[ks][0] * lift, x[ks][1] * lift, __half());
+                        qf[ks][2 + e] = pack2(x[ks][2] * lift, x[ks][3] * lift, __half());
+                    }
+                }
+                __syncwarp();
+                if (count - k > w.units - w.unit) {
+                    BdWalk wn = w;
+                    wn.unit = wn.units - 1;
+                    bd_next<KEYS>(b, g, wn);
+                    fetch_q(wn);
+                }
+#pragma unroll
+                for (int nt = 0; nt < 2 * CHUNKS; ++nt) o[nt][0] = o[nt][1] = o[nt][2] = o[nt][3] = 0.f;
+                m[0] = m[1] = -INFINITY;
+                l[0] = l[1] = 0.f;
+            }
+            ok = bt_wait(full(stage), turn, waits);
+            if (!ok) break;
+            const uint32_t kv_sh = stages + stage * S::UNIT_BYTES;
+            const int key0 = w.unit * KEYS, left = w.sp.len - key0;
+            if (MAY_BE_NAN && left < KEYS && (left & (box_rows - 1)) != 0) {
+                // slots behind the end may hold anything: V's become zero before they are read
+                const int end = (left | (box_rows - 1)) + 1;
+                for (int i = lane; i < (end - left) * CHUNKS; i += 32) {
+                    const int row = left + i / CHUNKS;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"      // whole rows: the swizzle stays inside
+                                 ::"r"(kv_sh + (row >> box_shift) * box_bytes + box_v + (row & (box_rows - 1)) * DP + (i % CHUNKS) * 16), "r"(0) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
+            float s[KEYS / 8][4];
+#pragma unroll
+            for (int n = 0; n < KEYS / 8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+            for (int h = 0; h < CHUNKS / 4; ++h)
+#pragma unroll
+                for (int n = 0; n < KEYS / 8; ++n) {
+                    uint32_t kf[4];                                       // keys 8 n .. + 7 x dims 64 h .. + 63
+                    ldsm4(kf, kv_sh + group_at(8 * n) + row_at + (((4 * h + k_chunk) ^ swz) << 4));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t b0, b1;
+                        b8_operands<true>(kf[j], b0, b1, CODE());
+                        mma16816(s[n], qf[4 * h + j], b0, b1, __half());
+                    }
+                }
+            const unsigned pages = page_bits[wk * S::STAGES + stage];
+            // ---- t = c s + log2 sv, hidden keys -infinity
+            float2 raw = make_float2(1.f, 1.f);
+            if (lane < per_unit) raw = *reinterpret_cast<const float2*>(smem_raw + (scales_sh - smem_u32(smem_raw)) + (stage * S::BOXES + lane) * 8);
+            const B8Scale mine = b8_scale(raw.x, raw.y, c);               // lane p: box p's
+            float inv[KEYS / 8];
+#pragma unroll
+            for (int n = 0; n < KEYS / 8; ++n) {
+                const int box = (8 * n) >> box_shift;
+                const float cn = __shfl_sync(FULL_WARP, mine.c, box), lv = __shfl_sync(FULL_WARP, mine.lv, box);
+                inv[n] = __shfl_sync(FULL_WARP, mine.inv, box);
+                const float c0 = cn * lower[0], c1 = cn * lower[1];
+                s[n][0] = fmaf(s[n][0], c0, lv);
+                s[n][1] = fmaf(s[n][1], c0, lv);
+                s[n][2] = fmaf(s[n][2], c1, lv);
+                s[n][3] = fmaf(s[n][3], c1, lv);
+            }
+            int seen[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) seen[e] = w.seq < 0 ? left : min(left, w.sp.pos0 + tok[e] + 1 - key0);
+            if (__any_sync(FULL_WARP, min(seen[0], seen[1]) < KEYS) || pages != all_boxes) {
+#pragma unroll
+                for (int n = 0; n < KEYS / 8; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = 8 * n + 2 * t + (e & 1);
+                        if (key >= seen[e >> 1] || !((pages >> (key >> box_shift)) & 1u)) s[n][e] = -INFINITY;
+                    }
+            }
+            float top[2] = {-INFINITY, -INFINITY}, off[2];
+#pragma unroll
+            for (int n = 0; n < KEYS / 8; ++n) {
+                top[0] = max3(top[0], s[n][0], s[n][1]);
+                top[1] = max3(top[1], s[n][2], s[n][3]);
+            }
+            // a row's sums are rescaled when its maximum has grown by more than 2^8
+            bool moved[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                top[e] = fmaxf(top[e], __shfl_xor_sync(FULL_WARP, top[e], 1));
+                top[e] = fmaxf(top[e], __shfl_xor_sync(FULL_WARP, top[e], 2));
+                moved[e] = bt_outgrown(top[e], m[e], 1.f);
+            }
+            if (__any_sync(FULL_WARP, moved[0] || moved[1])) {
+                float shrink[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float from = m[e] - B8_BIAS, to = top[e] - B8_BIAS;     // (as the weights are made: both rounded)
+                    shrink[e] = moved[e] ? ex2(from - to) : 1.f;
+                    if (moved[e]) m[e] = top[e];
+                    l[e] *= shrink[e];
+                }
+#pragma unroll
+                for (int nt = 0; nt < 2 * CHUNKS; ++nt) {
+                    o[nt][0] *= shrink[0]; o[nt][1] *= shrink[0];
+                    o[nt][2] *= shrink[1]; o[nt][3] *= shrink[1];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) off[e] = m[e] == -INFINITY ? 0.f : m[e] - B8_BIAS;
+#pragma unroll
+            for (int n = 0; n < KEYS / 8; ++n) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] = ex2(s[n][e] - off[e >> 1]);
+                l[0] = fmaf(s[n][0] + s[n][1], inv[n], l[0]);
+                l[1] = fmaf(s[n][2] + s[n][3], inv[n], l[1]);
+            }
+#pragma unroll
+            for (int n = 0; n < KEYS / 16; ++n) {
+                const uint32_t pf[4] = {pack2(s[2 * n][0], s[2 * n][1], __half()), pack2(s[2 * n][2], s[2 * n][3], __half()),
+                                        pack2(s[2 * n + 1][0], s[2 * n + 1][1], __half()), pack2(s[2 * n + 1][2], s[2 * n + 1][3], __half())};
+                const uint32_t v_at = kv_sh + box_v + group_at(16 * n + v_key) + row_at;
+#pragma unroll
+                for (int d = 0; d < CHUNKS / 2; ++d) {                    // keys 16 n .. + 15 x dims 32 d .. + 31
+                    uint32_t vf[4], even[2], odd[2];                      // matrices: keys 0..7 and 8..15 of 16 dims, then of the next 16
+                    ldsm4_trans(vf, v_at + (((2 * d + v_chunk) ^ swz) << 4));
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        b8_operands<false>(vf[2 * x], even[0], odd[0], CODE());
+                        b8_operands<false>(vf[2 * x + 1], even[1], odd[1], CODE());
+                        mma16816(o[2 * (2 * d + x)], pf, even[0], even[1], __half());
+                        mma16816(o[2 * (2 * d + x) + 1], pf, odd[0], odd[1], __half());
+                    }
+                }
+            }
+            // ---- the stage is used up: ask for the unit that takes its place
+            __syncwarp();
+            if (MT > 1 && lane == 0) mbar_arrive(empty(stage));
+            if (mt == 0 && asked < count) {
+                if (MT > 1) ok = bt_wait(empty(f_stage), f_turn ^ 1u, waits);
+                if (!ok) break;
+                ask();
+            }
+            if (++stage == S::STAGES) { stage = 0; turn ^= 1u; }
+            fresh = w.unit + 1 == w.units || k + 1 == count;
+            if (fresh) {
+                // ---- the item, or this worker's share of it, ends
+                const size_t slot = (size_t)(w.item + me) * R;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    l[e] += __shfl_xor_sync(FULL_WARP, l[e], 1);
+                    l[e] += __shfl_xor_sync(FULL_WARP, l[e], 2);
+                    if (rho[e] < w.sp.n * G) {
+                        float* out = g.part_o + (slot + rho[e]) * DP + 4 * t;
+#pragma unroll
+                        for (int ch = 0; ch < CHUNKS; ++ch)
+                            *reinterpret_cast<float4*>(out + 16 * ch) = make_float4(o[2 * ch][2 * e], o[2 * ch + 1][2 * e], o[2 * ch][2 * e + 1], o[2 * ch + 1][2 * e + 1]);
+                        if (t == 0) g.part_ml[slot + rho[e]] = make_float2(off[e], l[e]);
+                    }
+                }
+            }
+            if (k + 1 < count) bd_next<KEYS>(b, g, w);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+    __syncthreads();
+    bt_give_up(waits);
+    pdl_wait();                                           // the launch before this one ends first: what follows waits for both
+}
+
+} // namespace swk
