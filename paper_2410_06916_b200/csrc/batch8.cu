@@ -2,7 +2,7 @@
 // swift_coded_prompt_attention and swift_coded_prefix_attention.  No context and no state between calls.
 // This translation unit gets its own copies of the shared device code (separate namespace).
 #define swk swk_batch8
-#include "kernels_batch8_dec.cuh"
+#include "kernels_batch8_tc.cuh"
 #include "batch_host.cuh"
 
 cudaError_t swift_batch8_waits(unsigned* count, cudaStream_t s)
@@ -128,12 +128,17 @@ swift_status make_codes_map(const swift_paged_kv* kv, int dp, int most_slots, CU
     return SWIFT_OK;
 }
 
+// How swift_coded_prefix_attention runs a batch, from sizes the host knows: the choices of the 16-bit cache's plan, with this cache's
+// bytes and rates.
 struct Plan8 {
     bool rows;                  // fp32 arithmetic: no tensor-core form
+    bool prompt;                // too many rows for the few-row kernel, and no prefix or none worth sharing: each sequence by itself
     bool few, prefix_few;       // the few-row kernel takes the sequences' own parts; and the prefix
-    int group, dp, mt, grid;
+    int group, dp, mt, grid, pre_grid;                    // grid: CTAs of the few-row kernel; pre_grid: of the prefix's
     long long items;
-    size_t few_o, few_ml, first, last, bytes;             // offsets in the workspace
+    int splits;                 // cuts of the prefix by the many-row kernel (0: it has no prefix work)
+    int slots;                  // parts per row that the many-row kernel leaves: splits, and the own part if it takes it
+    size_t many_o, many_ml, few_o, few_ml, first, last, bytes;   // offsets in the workspace
 };
 inline int unit_keys8(int mt) { return mt == 1 ? 32 : 64; }
 
@@ -149,27 +154,104 @@ swift_status plan_prefix8(const swift_coded_kv* c, const BatchView& bv, int n_he
     auto take = [&](size_t n) { const size_t o = at; at += (n + 255) / 256 * 256; return o; };
     p->rows = !tensor_core_shape8(kv, x_dtype, n_heads);
     if (!p->rows) {
+        // Costs in microseconds: a key tile of a pair of query tiles, a piece's set-up and write-back; own parts per SM and in all.
+        constexpr double TILE = 1.9, PIECE = 9.0, SM_RATE = 30e3, RATE = 4.5e6;
         const long long own = (long long)max_rows * p->group, all = (long long)bv.n_rows * p->group;
         p->few = own <= BD_MAX_ROWS;
         p->mt = own <= 16 ? 1 : own <= 32 ? 2 : 4;
         p->prefix_few = p->few && bv.prefix_len > 0 && all <= 16 * p->mt;
-        if (!p->few || (bv.prefix_len > 0 && !p->prefix_few)) p->rows = true;
-    }
-    if (!p->rows) {
-        p->items = (long long)(bv.n_seqs + (p->prefix_few ? 1 : 0)) * Hk;
-        p->grid = sms;
-        const int keys = unit_keys8(p->mt);
-        const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, keys) + ceil_div(bv.prefix_len, keys)) * Hk;
-        if (units > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a page table of %d x %d for %d kv heads is beyond 2^31 units of work", bv.n_seqs, bv.table_stride, Hk);
-        if (2ll * kv->n_blocks * Hk * kv->n_pages > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a pool of %d pages of %d heads is beyond 2^31 planes", kv->n_pages, 2 * kv->n_blocks * Hk);
-        const size_t rows_all = (size_t)(p->items + (long long)p->grid * (BD_WARPS / p->mt)) * 16 * p->mt;
-        p->few_o = take(rows_all * p->dp * 4);
-        p->few_ml = take(rows_all * 8);
-        p->first = take((size_t)p->items * 4);
-        p->last = take((size_t)p->items * 4);
+        p->prompt = !p->few && bv.prefix_len == 0;
+        if (bv.prefix_len > 0 && !p->prefix_few && !p->prompt) {
+            // The prefix is tensor work, the sequences' own parts are HBM work: both kernels run at once on SMs of their own, and the share
+            // of SMs and the cuts of the prefix are chosen for the earliest common end; own lengths (which only the device knows) are taken
+            // as 0.6 of the page table's width, and never more than 5/6 of the SMs are for them.
+            const int tiles = ceil_div(bv.prefix_len, BT_KEYS), TQ = BT_ROWS / p->group;
+            const long long pairs = (long long)ceil_div(bv.n_rows, 2 * TQ) * Hk;
+            const double own_bytes = 0.6 * bv.n_seqs * bv.max_len * Hk * kv->head_dim * 2.0;
+            double best = 0;
+            for (int share = 2; share <= 12; ++share) {               // twelfths of the SMs
+                const int g = sms * share / 12, rest = g == sms ? sms : sms - g;
+                if (!p->few && g < sms) continue;
+                const double stream_us = own_bytes / (rest * SM_RATE < RATE ? rest * SM_RATE : RATE), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * (BD_WARPS / p->mt));
+                const double own_us = p->few ? 3.0 + (stream_us > item_us ? stream_us : item_us) : 0.0;
+                for (int waves = 1; waves <= 4; ++waves) {            // as many cuts as fill that many waves
+                    long long n = (long long)waves * g / pairs;
+                    n = n < 1 ? 1 : n > tiles ? tiles : n > 64 ? 64 : n;
+                    const double pre_us = ceil_div(pairs * n, g) * (ceil_div(tiles, n) * TILE + PIECE);
+                    const double cost = (g == sms ? pre_us + own_us : pre_us > own_us ? pre_us : own_us) + n;    // every cut is read again by the join
+                    if (p->splits == 0 || cost < best) {
+                        best = cost;
+                        p->splits = (int)n;
+                        p->pre_grid = g;
+                    }
+                }
+            }
+        }
+        if (!p->few && !p->prompt) {
+            // Rows that fill tiles anyway gain nothing from a shared prefix but a better split over the SMs, and pay for writing and
+            // joining parts: by the same costs, whichever form ends earlier.
+            const int TQ2 = 2 * (BT_ROWS / p->group), own_tiles = ceil_div((long long)(0.6 * bv.max_len), BT_KEYS), tiles = ceil_div(bv.prefix_len, BT_KEYS);
+            const long long seqs = bv.n_seqs < bv.n_rows ? bv.n_seqs : bv.n_rows, own_pieces = seqs * ceil_div(max_rows, TQ2) * Hk;
+            const double one = ceil_div(own_pieces, sms) * ((tiles + own_tiles) * TILE + PIECE);
+            const double shared = ceil_div((long long)ceil_div(bv.n_rows, TQ2) * Hk * p->splits, sms) * (ceil_div(tiles, p->splits) * TILE + PIECE) +
+                                  ceil_div(own_pieces, sms) * (own_tiles * TILE + PIECE) + 5.0 + (double)bv.n_rows * n_heads * (p->splits + 1.5) * p->dp * 4 / 5e6;
+            if (one < shared) {
+                p->prompt = true;
+                p->splits = 0;
+            }
+        }
+        p->slots = p->splits + (!p->few && !p->prompt ? 1 : 0);
+        const size_t many = (size_t)p->slots * bv.n_rows * n_heads;
+        p->many_o = take(many * p->dp * 4);
+        p->many_ml = take(many * 8);
+        if (p->few) {
+            p->items = (long long)(bv.n_seqs + (p->prefix_few ? 1 : 0)) * Hk;
+            p->grid = p->splits > 0 && p->pre_grid < sms ? sms - p->pre_grid : sms;
+            const int keys = unit_keys8(p->mt);
+            const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, keys) + ceil_div(bv.prefix_len, keys)) * Hk;
+            if (units > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a page table of %d x %d for %d kv heads is beyond 2^31 units of work", bv.n_seqs, bv.table_stride, Hk);
+            if (2ll * kv->n_blocks * Hk * kv->n_pages > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a pool of %d pages of %d heads is beyond 2^31 planes", kv->n_pages, 2 * kv->n_blocks * Hk);
+            const size_t rows_all = (size_t)(p->items + (long long)p->grid * (BD_WARPS / p->mt)) * 16 * p->mt;
+            p->few_o = take(rows_all * p->dp * 4);
+            p->few_ml = take(rows_all * 8);
+            p->first = take((size_t)p->items * 4);
+            p->last = take((size_t)p->items * 4);
+        }
     }
     p->bytes = at > 256 ? at : 256;
     return SWIFT_OK;
+}
+
+// ------------------------------------------------------------------------------ many rows
+template <int HALVES, bool PART>
+cudaError_t launch_tc8(const BatchView& bv, const B8TcArgs& g, int grid, cudaStream_t s, bool after_previous)
+{
+    static std::atomic<unsigned long long> done{0};
+    const cudaError_t e = allow_smem(attn_batch8_tc_kernel<HALVES, PART>, B8TcShape<HALVES>::SMEM_BYTES, done);
+    if (e != cudaSuccess) return e;
+    return launch(attn_batch8_tc_kernel<HALVES, PART>, dim3(grid), B8_THREADS, B8TcShape<HALVES>::SMEM_BYTES, s, after_previous, bv, g);
+}
+// The many-row kernel in one of its three modes on at most `most` SMs; items: an upper bound of its pieces of work.
+swift_status run_tc8(const swift_paged_kv* kv, int x_dtype, const BatchView& bv, const BtArgs& t, long long items, int most, cudaStream_t s, bool after)
+{
+    const B8TcArgs g = {t, kv->dtype == SWIFT_E4M3, x_dtype == SWIFT_BF16};
+    const int grid = (int)(items < most ? items : most);          // prompts: `most` does not limit, blocks take over one another's pieces
+    const bool wide = kv->head_dim > 64;
+    const cudaError_t e = t.mode == BT_PROMPT ? (wide ? launch_tc8<2, false>(bv, g, grid, s, after) : launch_tc8<1, false>(bv, g, grid, s, after))
+                                              : (wide ? launch_tc8<2, true>(bv, g, grid, s, after) : launch_tc8<1, true>(bv, g, grid, s, after));
+    if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+    return SWIFT_OK;
+}
+swift_status run_prompt8(const swift_paged_kv* kv, int x_dtype, const BatchView& bv, const AttnView& av, int block, cudaStream_t s)
+{
+    BtArgs g = {};
+    g.a = av;
+    g.mode = BT_PROMPT;
+    g.block = block;
+    g.rows_per_tile = BT_ROWS / (av.n_heads / av.n_kv_heads);
+    g.wide_out = aligned(av.out, 32) && av.head_dim % 16 == 0;
+    g.tiles = piece_bound(bv, av.n_kv_heads, g.rows_per_tile) <= multiprocessors() ? 1 : 2;     // as for the 16-bit cache
+    return run_tc8(kv, x_dtype, bv, g, piece_bound(bv, av.n_kv_heads, g.tiles * g.rows_per_tile), 0x7FFFFFFF, s, false);
 }
 
 template <typename QT, typename CODE, int DP, int MT>
@@ -202,33 +284,59 @@ cudaError_t launch_join8(const Plan8& p, const BatchView& bv, const BjArgs& j, c
 }
 
 template <typename QT>
-swift_status run_prefix8(const swift_coded_kv* c, const BatchView& bv, const AttnView& av, int block, const Plan8& p, unsigned char* ws, cudaStream_t s)
+swift_status run_prefix8(const swift_coded_kv* c, int x_dtype, const BatchView& bv, const AttnView& av, int block, const Plan8& p, unsigned char* ws, cudaStream_t s)
 {
     const swift_paged_kv* kv = &c->kv;
-    BdArgs g = {};
-    g.a = av;
-    g.block = block;
-    g.prefix_here = p.prefix_few;
-    g.planes = 2 * kv->n_blocks * kv->n_kv_heads * kv->n_pages;
-    g.part_o = reinterpret_cast<float*>(ws + p.few_o);
-    g.part_ml = reinterpret_cast<float2*>(ws + p.few_ml);
-    g.item_first = reinterpret_cast<int*>(ws + p.first);
-    g.item_last = reinterpret_cast<int*>(ws + p.last);
-    CUtensorMap map;
-    const swift_status st = make_codes_map(kv, p.dp, unit_keys8(p.mt), &map);
-    if (st != SWIFT_OK) return st;
-    cudaError_t e = kv->dtype == SWIFT_I8 ? launch_dec8_any<QT, int8_t>(p, map, bv, g, s, false) : launch_dec8_any<QT, __nv_fp8_e4m3>(p, map, bv, g, s, false);
+    bool before = false;                                  // a kernel of this call has been launched
+    BtArgs t = {};
+    t.a = av;
+    t.block = block;
+    t.rows_per_tile = BT_ROWS / p.group;
+    t.tiles = 2;
+    t.part_o = reinterpret_cast<float*>(ws + p.many_o);
+    t.part_ml = reinterpret_cast<float2*>(ws + p.many_ml);
+    if (p.splits > 0) {
+        t.mode = BT_PREFIX;
+        t.splits = p.splits;
+        const swift_status st = run_tc8(kv, x_dtype, bv, t, (long long)ceil_div(bv.n_rows, 2 * t.rows_per_tile) * av.n_kv_heads * p.splits, p.pre_grid, s, before);
+        if (st != SWIFT_OK) return st;
+        before = true;
+    }
     BjArgs j = {};
     j.a = av;
     j.dp = p.dp;
     j.item_rows = 16 * p.mt;
     j.prefix_here = p.prefix_few;
     j.own_here = p.few;
-    j.many_o = j.few_o = g.part_o;
-    j.many_ml = j.few_ml = g.part_ml;
-    j.item_first = g.item_first;
-    j.item_last = g.item_last;
+    j.splits = p.slots;
+    j.many_o = t.part_o;
+    j.many_ml = t.part_ml;
+    j.few_o = reinterpret_cast<float*>(ws + p.few_o);
+    j.few_ml = reinterpret_cast<float2*>(ws + p.few_ml);
+    j.item_first = reinterpret_cast<int*>(ws + p.first);
+    j.item_last = reinterpret_cast<int*>(ws + p.last);
     j.workers = p.grid * (BD_WARPS / p.mt);
+    cudaError_t e = cudaSuccess;
+    if (p.few) {
+        BdArgs g = {};
+        g.a = av;
+        g.block = block;
+        g.prefix_here = p.prefix_few;
+        g.planes = 2 * kv->n_blocks * kv->n_kv_heads * kv->n_pages;
+        g.part_o = reinterpret_cast<float*>(ws + p.few_o);
+        g.part_ml = reinterpret_cast<float2*>(ws + p.few_ml);
+        g.item_first = reinterpret_cast<int*>(ws + p.first);
+        g.item_last = reinterpret_cast<int*>(ws + p.last);
+        CUtensorMap map;
+        const swift_status st = make_codes_map(kv, p.dp, unit_keys8(p.mt), &map);
+        if (st != SWIFT_OK) return st;
+        e = kv->dtype == SWIFT_I8 ? launch_dec8_any<QT, int8_t>(p, map, bv, g, s, before) : launch_dec8_any<QT, __nv_fp8_e4m3>(p, map, bv, g, s, before);
+    } else {
+        t.mode = BT_OWN;
+        t.part_slot = p.splits;
+        const swift_status st = run_tc8(kv, x_dtype, bv, t, piece_bound(bv, av.n_kv_heads, 2 * t.rows_per_tile), multiprocessors(), s, before);
+        if (st != SWIFT_OK) return st;
+    }
     if (e == cudaSuccess) e = launch_join8<QT>(p, bv, j, s);
     if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
     return SWIFT_OK;
@@ -242,7 +350,8 @@ swift_status prompt8(const swift_coded_kv* c, const swift_row_batch* batch, cons
     if (st != SWIFT_OK) return st;
     if (bv.n_rows == 0 || bv.n_seqs == 0) return SWIFT_OK;
     set_probe(&av, probe_us);
-    return run_rows8(&c->kv, x_dtype, bv, av, s);
+    if (!tensor_core_shape8(&c->kv, x_dtype, av.n_heads)) return run_rows8(&c->kv, x_dtype, bv, av, s);
+    return run_prompt8(&c->kv, x_dtype, bv, av, args->block, s);
 }
 
 swift_status prefix8(const swift_coded_kv* c, const swift_row_batch* batch, const swift_attention_args* args, int x_dtype, int max_rows,
@@ -262,8 +371,10 @@ swift_status prefix8(const swift_coded_kv* c, const swift_row_batch* batch, cons
     av.max_rows = max_rows;
     set_probe(&av, probe_us);
     if (p.rows) return run_rows8(&c->kv, x_dtype, bv, av, s);
+    if (p.prompt) return run_prompt8(&c->kv, x_dtype, bv, av, args->block, s);
     unsigned char* ws = reinterpret_cast<unsigned char*>(workspace.dptr);
-    return x_dtype == SWIFT_BF16 ? run_prefix8<__nv_bfloat16>(c, bv, av, args->block, p, ws, s) : run_prefix8<__half>(c, bv, av, args->block, p, ws, s);
+    return x_dtype == SWIFT_BF16 ? run_prefix8<__nv_bfloat16>(c, x_dtype, bv, av, args->block, p, ws, s)
+                                 : run_prefix8<__half>(c, x_dtype, bv, av, args->block, p, ws, s);
 }
 
 } // namespace
@@ -324,10 +435,12 @@ swift_status swift_coded_prefix_attention(const swift_coded_kv* c, const swift_r
 swift_status swift_probe_coded_wait_limit(const swift_coded_kv* c, const swift_row_batch* batch, const swift_attention_args* args, int32_t x_dtype,
                                         int32_t max_rows, swift_devbuf workspace, int32_t limit_us, void* cuda_stream)
 {
-    (void)c; (void)batch; (void)args; (void)x_dtype; (void)workspace; (void)cuda_stream;
     if (limit_us < 1 || limit_us > 100000) return fail_batch(SWIFT_EINVAL, "limit_us must be in 1..100000");
     if (max_rows < 0) return fail_batch(SWIFT_EINVAL, "max_rows %d", max_rows);
-    return fail_batch(SWIFT_EUNSUPPORTED, "fp32 arithmetic has no waits");
+    if (c && args && c->kv.n_kv_heads > 0 && !tensor_core_shape8(&c->kv, x_dtype, args->n_heads))
+        return fail_batch(SWIFT_EUNSUPPORTED, "fp32 arithmetic has no waits");
+    if (max_rows == 0) return prompt8(c, batch, args, x_dtype, limit_us, (cudaStream_t)cuda_stream);
+    return prefix8(c, batch, args, x_dtype, max_rows, workspace, limit_us, (cudaStream_t)cuda_stream);
 }
 
 } // extern "C"

@@ -1,0 +1,582 @@
+// Attention of many query rows over a cache of 8-bit codes on the 5th-generation tensor cores: the many-row kernel of the 16-bit cache
+// (kernels_batch_tc.cuh: tiles, overlap, rescaling, pieces and modes are its own), whose operands are made on the way.
+//
+// Operands.  Three warps read a key tile's codes from the pages (16 bytes a lane, a tile ahead, in registers), make them fp16, which
+// holds int8 and e4m3 exactly, and store them in the swizzled layout that TMA would have left.  Converting 32768 codes costs these warps
+// some 550 instructions each in the 3100 cycles of a key tile; the first and the last tile of a piece are fetched while its neighbours
+// are still computed.  They stage the queries too, each row at the power of two that brings it to [2^14, 2^15).  So the products are fp16 for every
+// type of q.  (8-bit operands on both sides would round q to 8 bits; a 16-bit copy of the cache would be written and read by every call.)
+//
+// Scales.  As in the few-row kernel: a weight is 2^(c s + log2 sv - r), and a group of 8 keys, which lies in one page, adds its sum times
+// 1 / sv to the sum of probabilities.  Per group of 8 that is one 16-byte load from shared memory and four operations in each of the two
+// passes over the scores.  c s + (log2 sv - r) is one multiply-add; where r is beyond 200 its addend would be rounded too coarsely from group to
+// group, and the row subtracts r last.
+#pragma once
+#include "kernels_batch8_dec.cuh"
+
+namespace swk {
+
+constexpr int B8_THREADS = 384;     // 2 x 4 softmax warps, the MMA warp (9), three warps that make operands (8, 10, 11)
+constexpr int B8_MAKERS = 3;
+constexpr float B8_FAR = 200.f;
+
+template <int HALVES> struct B8TcShape {
+    static constexpr int DP = 64 * HALVES;
+    static constexpr int SLOT_BYTES = BT_KEYS * 128 * HALVES;         // a K or V tile in 16 bits
+    static constexpr int Q_BYTES = BT_ROWS * 128 * HALVES;
+    static constexpr int SLOTS = HALVES == 2 ? 4 : 8;
+    static constexpr int LOWER_BYTES = 2 * 2 * BT_ROWS * 4;           // [piece parity][tile][row]
+    static constexpr int SCALE_BYTES = BT_PAGE_RING * 16 * 16;        // [key tile][group of 8 keys]
+    static constexpr int BAR_BYTES = 512;
+    static constexpr int SMEM_BYTES = 1024 + 2 * Q_BYTES + SLOTS * SLOT_BYTES + LOWER_BYTES + SCALE_BYTES + BAR_BYTES;
+};
+
+struct B8TcArgs {
+    BtArgs t;
+    int e4m3, q_bf16;                                                 // types of the codes, and of q and out
+};
+
+__device__ __forceinline__ float4 b8_group(uint32_t at)               // {scale sk log2 e, log2 sv, 1 / sv}
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ float b8_highest8(const float* s)          // NaN if any is
+{
+    return max2_nan(max3_nan(s[0], s[1], s[2]), max3_nan(max3_nan(s[3], s[4], s[5]), s[6], s[7]));
+}
+// The largest t of a quarter (32 keys); keys that are not shown do not count.
+template <bool MASKED> __device__ __forceinline__ float b8_top(float (&s)[32], uint32_t groups, float lower, unsigned shown)
+{
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 g = b8_group(groups + 16 * i);
+        if (MASKED) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!((shown >> (8 * i + e)) & 1u)) s[8 * i + e] = -INFINITY;
+        }
+        const float t = fmaf(b8_highest8(s + 8 * i), g.x * lower, g.y);
+        top = max2_nan(top, !MASKED || ((shown >> (8 * i)) & 0xFFu) ? t : -INFINITY);
+    }
+    return top;
+}
+// 32 scores -> weights (fp16, two to a register), what they add to the sum of probabilities
+template <bool MASKED> __device__ __forceinline__ void b8_weights(const float (&s)[32], uint32_t groups, float lower, float ref, unsigned shown, f32x2& sum, uint32_t (&p)[16])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 g = b8_group(groups + 16 * i);
+        const float c = g.x * lower, off = g.y - ref;
+        const f32x2 c2 = pair2(c, c), off2 = pair2(off, off);
+        f32x2 part = 0ull;
+#pragma unroll
+        for (int j = 4 * i; j < 4 * i + 4; ++j) {
+            float p0, p1;
+            split2(fma2(pair2(s[2 * j], s[2 * j + 1]), c2, off2), p0, p1);
+            if (!MASKED && ((BT_POLY >> j) & 1u)) {                   // (the polynomial gives a hidden key 2^-126, not 0)
+                ex2_poly<__half>(p0, p1, p0, p1);
+            } else {
+                p0 = ex2(p0);
+                p1 = ex2(p1);
+            }
+            if (MASKED) {                                             // (a hidden score may have met a scale that is 0 or NaN)
+                p0 = (shown >> (2 * j)) & 1u ? p0 : 0.f;
+                p1 = (shown >> (2 * j + 1)) & 1u ? p1 : 0.f;
+            }
+            part = j == 4 * i ? pair2(p0, p1) : add2(part, pair2(p0, p1));
+            p[j] = pack2(p0, p1, __half());
+        }
+        sum = fma2(part, pair2(g.z, g.z), sum);
+    }
+}
+// The weights of a key tile with rows whose maximum is far from zero, from the scores in TMEM on: what they add to the sums.
+__device__ __noinline__ float b8_weights_far(uint32_t s_at, uint32_t p_bar, uint32_t groups, float lower, float ref, int seen, unsigned pages, int page_shift)
+{
+    float l = 0.f;
+#pragma unroll 1
+    for (int h = 1; h >= 0; --h) {                                    // the upper half of the keys goes first; both of its quarters are read before P overwrites them
+        float a[32], b[32];
+        uint32_t p[16];
+        tmem_ld32(s_at + 64 * h, a);
+        tmem_ld32(s_at + 64 * h + 32, b);
+        tmem_wait_ld(a);
+        tmem_wait_ld(b);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            float (&s)[32] = x ? b : a;
+            const unsigned shown = bt_shown(pages, page_shift, seen, 2 * h + x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 g = b8_group(groups + 16 * (8 * h + 4 * x + i));
+                float part = 0.f;
+#pragma unroll
+                for (int e = 8 * i; e < 8 * i + 8; ++e) {
+                    s[e] = (shown >> e) & 1u ? ex2(fmaf(s[e], g.x * lower, g.y) - ref) : 0.f;
+                    part += s[e];
+                }
+                l = fmaf(part, g.z, l);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = pack2(s[2 * i], s[2 * i + 1], __half());
+            tmem_st16(s_at + 64 + 32 * h + 16 * x, p);
+        }
+        bt_hand_over(p_bar, h);
+    }
+    return l;
+}
+
+// The softmax warps' part of one key tile, as bt_softmax's.  m, l: the row's largest t and sum.  False: the weights are
+// b8_weights_far's to make.
+template <int DP, bool MASKED>
+__device__ __forceinline__ bool b8_softmax(uint32_t s_at, uint32_t o_at, uint32_t p_bar, uint32_t groups, float lower, int seen, unsigned pages, int page_shift, bool first,
+                                           float& m, float& l)
+{
+    auto shown = [&](int q) { return MASKED ? bt_shown(pages, page_shift, seen, q) : 0xFFFFFFFFu; };
+    float s0[32], s1[32], s2[32], s3[32];
+    tmem_ld32(s_at, s0);
+    tmem_wait_ld(s0);
+    tmem_ld32(s_at + 32, s1);
+    float top = b8_top<MASKED>(s0, groups, lower, shown(0));
+    tmem_wait_ld(s1);
+    tmem_ld32(s_at + 64, s2);
+    top = max2_nan(top, b8_top<MASKED>(s1, groups + 64, lower, shown(1)));
+    tmem_wait_ld(s2);
+    tmem_ld32(s_at + 96, s3);
+    top = max2_nan(top, b8_top<MASKED>(s2, groups + 128, lower, shown(2)));
+    tmem_wait_ld(s3);
+    top = max2_nan(top, b8_top<MASKED>(s3, groups + 192, lower, shown(3)));
+    if (!(top < INFINITY)) l = __int_as_float(0x7FFFFFFF);            // a score of NaN or +infinity makes the row NaN
+    const bool grown = bt_outgrown(top, m, 1.f);
+    if (__any_sync(FULL_WARP, grown)) bt_rescale<DP>(o_at, 1.f, top, grown, first, m, l);
+    if (__any_sync(FULL_WARP, fabsf(m) > B8_FAR && m != -INFINITY)) return false;
+    const float ref = m == -INFINITY ? 0.f : m - B8_BIAS;
+    f32x2 sum = 0ull;
+    uint32_t p[16];
+    tmem_ld32(s_at, s0);
+    b8_weights<MASKED>(s2, groups + 128, lower, ref, shown(2), sum, p);
+    tmem_st16(s_at + 96, p);
+    b8_weights<MASKED>(s3, groups + 192, lower, ref, shown(3), sum, p);
+    tmem_st16(s_at + 112, p);
+    bt_hand_over(p_bar, 1);
+    tmem_wait_ld(s0);
+    tmem_ld32(s_at + 32, s1);
+    b8_weights<MASKED>(s0, groups, lower, ref, shown(0), sum, p);
+    tmem_st16(s_at + 64, p);
+    tmem_wait_ld(s1);
+    b8_weights<MASKED>(s1, groups + 64, lower, ref, shown(1), sum, p);
+    tmem_st16(s_at + 80, p);
+    bt_hand_over(p_bar, 0);
+    float l0, l1;
+    split2(sum, l0, l1);
+    l += l0 + l1;
+    return true;
+}
+
+// 16 codes -> 16 operands
+__device__ __forceinline__ void b8_widen(const uint4& v, bool e4m3, uint32_t (&r)[8])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if (e4m3) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b8_operands<true>(w[i], r[2 * i], r[2 * i + 1], __nv_fp8_e4m3());
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b8_operands<true>(w[i], r[2 * i], r[2 * i + 1], int8_t());
+    }
+}
+__device__ __forceinline__ void b8_store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// grid: one block per piece (PART: persistent blocks that take pieces blockIdx.x, + gridDim.x, ...); block = 384.
+template <int HALVES, bool PART>
+__global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView b, B8TcArgs ga)
+{
+    typedef B8TcShape<HALVES> S;
+    const BtArgs& g = ga.t;
+    constexpr int DP = S::DP;
+    constexpr uint32_t IDESC_QK = (1u << 4) | ((uint32_t)(BT_KEYS >> 3) << 17) | ((uint32_t)(BT_ROWS >> 4) << 24);          // fp16 operands, fp32 sums
+    constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 16) | ((uint32_t)(DP >> 3) << 17) | ((uint32_t)(BT_ROWS >> 4) << 24);
+
+    pdl_trigger();
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t q_sh = base, ring = base + 2 * S::Q_BYTES, lower_sh = ring + S::SLOTS * S::SLOT_BYTES, scale_sh = lower_sh + S::LOWER_BYTES, bars = scale_sh + S::SCALE_BYTES;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (S::SLOTS + s); };
+    const uint32_t b2 = bars + 16u * S::SLOTS;
+    auto q_full = [&](int x) { return b2 + 8u * x; };
+    auto q_empty = [&](int x) { return b2 + 16u + 8u * x; };
+    auto s_full = [&](int x) { return b2 + 32u + 8u * x; };
+    auto p_ready = [&](int x, int h) { return b2 + 48u + 8u * (2 * x + h); };
+    auto o_full = [&](int x) { return b2 + 80u + 8u * x; };
+    const uint32_t piece_bars = b2 + 96u, answers = bars + S::BAR_BYTES - 32u;   // answers: 16-byte aligned
+    __shared__ uint32_t tmem_base_sh;
+    __shared__ int waits_sh[2];
+    __shared__ unsigned page_bits[BT_PAGE_RING];                      // bit p: page p of that key tile lies in the pool
+    volatile int* waits = waits_sh;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G = g.a.n_heads / g.a.n_kv_heads, TQ = g.rows_per_tile;
+    if (warp == 9) {
+        if (lane == 0) {
+            for (int s = 0; s < S::SLOTS; ++s) { mbar_init(full(s), B8_MAKERS); mbar_init(empty(s), 1); }
+            for (int x = 0; x < 2; ++x) {
+                mbar_init(q_full(x), B8_MAKERS); mbar_init(q_empty(x), 1); mbar_init(s_full(x), 1); mbar_init(o_full(x), 1);
+                mbar_init(p_ready(x, 0), 4); mbar_init(p_ready(x, 1), 4);
+            }
+            for (int i = 0; i < 2; ++i) { mbar_init(piece_bars + 8u * i, 1); mbar_init(piece_bars + 16u + 8u * i, B8_THREADS / 32); }
+            waits[0] = 0;
+            waits[1] = g.a.wait_kcycles;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_sh)), "r"(512));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_sh;
+    BtPieces<PART> pieces = {answers, piece_bars, piece_bars + 16u, waits, 0, 0};
+    pieces.begin();
+    bool more_pieces = true;
+    auto s_col = [&](int x) { return tmem + 128u * x; };              // S, then P, of tile x
+    auto o_col = [&](int x) { return tmem + 256u + 128u * x; };
+
+    if (warp >= 8 && warp != 9) {
+        // ---------------------------------------------------------------- makers of operands: queries, K and V tiles in turn
+        constexpr int LANES = DP / 16, ROWS = 32 / LANES;             // lanes of a row (16 codes each), rows of a step
+        constexpr int STEPS = (BT_KEYS / ROWS + B8_MAKERS - 1) / B8_MAKERS;      // of a maker, per tile
+        const int maker = warp == 8 ? 0 : warp - 9, D = g.a.head_dim;
+        const int j16 = lane % LANES, my_row = lane / LANES;
+        const int per_tile = BT_KEYS >> b.page_shift;                 // pages per key tile, 1..16
+        const uint8_t* pool = reinterpret_cast<const uint8_t*>(g.a.pool);
+        const float c = g.a.scale * 1.4426950408889634f;
+        uint32_t slot = 0, turn = 0, q_turn[2] = {0, 0};
+        int tile_no = 0;
+        bool ok = true;
+        BtItem it;
+        for (; ok && more_pieces; more_pieces = ok && pieces.next(ok)) {
+            if (maker == 0) ok = pieces.ask();
+            if (!ok) break;
+            if (!bt_locate(b, g, pieces.idx, it)) { if (PART) break; continue; }
+            const int n_tiles = max(it.tiles[0], it.tiles[1]);
+            // lane p: page p of a key tile, -1 where there is none
+            auto look_up = [&](int j) {
+                const bool shared_part = j < it.np;
+                const int key0 = (shared_part ? it.first_tile + j : j - it.np) * BT_KEYS;
+                const int left = (shared_part ? b.prefix_len : it.sp.len) - key0;
+                int page = -1;
+                if (j < n_tiles && lane < per_tile && (lane << b.page_shift) < left) {
+                    const int at = (key0 >> b.page_shift) + lane;
+                    page = shared_part ? b.prefix_pages[at] : b.page_table[(size_t)it.seq * b.table_stride + at];
+                    if ((unsigned)page >= (unsigned)b.n_pages) page = -1;
+                }
+                return page;
+            };
+            auto keys_left = [&](int j) { return j < it.np ? b.prefix_len - (it.first_tile + j) * BT_KEYS : it.sp.len - (j - it.np) * BT_KEYS; };
+            uint4 v[STEPS];
+            auto fetch = [&](int i, int page_lane, int left, int kv) {            // step i of a tile of K or V
+                const int row = (i * B8_MAKERS + maker) * ROWS + my_row;
+                const int page = __shfl_sync(FULL_WARP, page_lane, (row & (BT_KEYS - 1)) >> b.page_shift);
+                v[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (row < BT_KEYS && row < left && page >= 0 && 16 * j16 < D)
+                    v[i] = __ldg(reinterpret_cast<const uint4*>(pool + (long long)page * g.a.page_elems + (kv ? g.a.kv_elems : 0) +
+                                                                ((long long)it.kvh * b.page_size + (row & (b.page_size - 1))) * D + 16 * j16));
+            };
+            auto keep = [&](int i, uint32_t dst) {                                // its operands, where the products read them
+                const int row = (i * B8_MAKERS + maker) * ROWS + my_row;
+                if (row >= BT_KEYS) return;
+                uint32_t r[8];
+                b8_widen(v[i], ga.e4m3 != 0, r);
+                const uint32_t p = 2 * (j16 & 3), at = dst + (j16 >> 2) * (BT_KEYS * 128) + row * 128, sw = row & 7;
+                if (j16 & 4) {                                                    // (the order keeps the eight lanes of a row in different banks)
+                    b8_store16(at + (((p + 1) ^ sw) << 4), r[4], r[5], r[6], r[7]);
+                    b8_store16(at + ((p ^ sw) << 4), r[0], r[1], r[2], r[3]);
+                } else {
+                    b8_store16(at + ((p ^ sw) << 4), r[0], r[1], r[2], r[3]);
+                    b8_store16(at + (((p + 1) ^ sw) << 4), r[4], r[5], r[6], r[7]);
+                }
+            };
+            auto group_scales = [&](int page_lane) {                              // lane i < 16: of keys 8 i ..
+                const int page = __shfl_sync(FULL_WARP, page_lane, (8 * (lane & 15)) >> b.page_shift);
+                float2 s = make_float2(1.f, 1.f);
+                if (page >= 0) {
+                    const float* at = g.a.scales + page * g.a.scale_page + it.kvh;
+                    s = make_float2(__ldg(at), __ldg(at + g.a.n_kv_heads));
+                }
+                return s;
+            };
+            int page = look_up(0), next_page = -1;
+            float2 scales = make_float2(1.f, 1.f);
+            if (n_tiles > 0) {
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) fetch(i, page, keys_left(0), 0);
+                if (maker == 0) scales = group_scales(page);
+            }
+            // ---- queries
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (!ok || it.tiles[x] == 0) continue;
+                ok = bt_wait(q_empty(x), q_turn[x] ^ 1u, waits);
+                if (!ok) break;
+                constexpr int QL = DP / 8, QR = 32 / QL, QS = (BT_ROWS / QR + B8_MAKERS - 1) / B8_MAKERS;     // lanes of a row, rows of a step, steps
+                const int piece = lane % QL, q_row = lane / QL;
+                constexpr int AHEAD = 4;
+#pragma unroll 1
+                for (int i0 = 0; i0 < QS; i0 += AHEAD) {
+                    uint4 u[AHEAD];
+#pragma unroll
+                    for (int e = 0; e < AHEAD; ++e) {
+                        const int rho = ((i0 + e) * B8_MAKERS + maker) * QR + q_row, tok = rho / G, tk = it.t0 + x * TQ + tok;
+                        u[e] = make_uint4(0u, 0u, 0u, 0u);
+                        if (rho < BT_ROWS && tok < TQ && tk < it.sp.n && 8 * piece < D)
+                            u[e] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(g.a.q) + (long long)(it.sp.r0 + tk) * g.a.q_row_stride +
+                                                                        (long long)(it.kvh * G + rho - tok * G) * g.a.q_head_stride + 8 * piece));
+                    }
+#pragma unroll
+                    for (int e = 0; e < AHEAD; ++e) {
+                        const int rho = ((i0 + e) * B8_MAKERS + maker) * QR + q_row;
+                        const uint32_t w[4] = {u[e].x, u[e].y, u[e].z, u[e].w};
+                        float y[8], top = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (ga.q_bf16) {
+                                y[2 * i] = __uint_as_float(w[i] << 16);
+                                y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+                            } else {
+                                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                                y[2 * i] = f.x;
+                                y[2 * i + 1] = f.y;
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (fabsf(y[i]) < INFINITY) top = fmaxf(top, fabsf(y[i]));
+#pragma unroll
+                        for (int o = QL / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_WARP, top, o));
+                        float lower;
+                        const float lift = b8_lift(top, lower);
+                        if (rho < BT_ROWS) {
+                            b8_store16(q_sh + x * S::Q_BYTES + (piece >> 3) * (BT_ROWS * 128) + rho * 128 + (((piece & 7) ^ (rho & 7)) << 4),
+                                       pack2(y[0] * lift, y[1] * lift, __half()), pack2(y[2] * lift, y[3] * lift, __half()),
+                                       pack2(y[4] * lift, y[5] * lift, __half()), pack2(y[6] * lift, y[7] * lift, __half()));
+                            if (piece == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(lower_sh + ((q_turn[x] * 2 + x) * BT_ROWS + rho) * 4), "f"(lower) : "memory");
+                        }
+                    }
+                }
+                q_turn[x] ^= 1u;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_full(x));
+            }
+            // ---- key tiles: while one is kept, the next is fetched
+            for (int j = 0; ok && j < n_tiles; ++j, ++tile_no) {
+                const unsigned pages = __ballot_sync(FULL_WARP, page >= 0);
+                const float2 now = scales;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    ok = bt_wait(empty(slot), turn ^ 1u, waits);
+                    if (!ok) break;
+                    const uint32_t dst = ring + slot * S::SLOT_BYTES;
+                    const int left = keys_left(kv ? j + 1 : j), pg = kv ? next_page : page;
+                    const bool more = kv == 0 || j + 1 < n_tiles;
+                    if (kv == 0) next_page = look_up(j + 1);
+#pragma unroll
+                    for (int i = 0; i < STEPS; ++i) {
+                        keep(i, dst);
+                        if (more) fetch(i, pg, left, kv ^ 1);
+                    }
+                    if (maker == 0) {
+                        if (kv == 0) {
+                            if (lane == 0) page_bits[tile_no & (BT_PAGE_RING - 1)] = pages;
+                            if (lane < 16) {
+                                const B8Scale s = b8_scale(now.x, now.y, c);
+                                b8_store16(scale_sh + ((tile_no & (BT_PAGE_RING - 1)) * 16 + lane) * 16, __float_as_uint(s.c), __float_as_uint(s.lv), __float_as_uint(s.inv), 0u);
+                            }
+                        } else if (more) {
+                            scales = group_scales(next_page);
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0 && !(g.a.withhold && maker == 0 && kv == 0 && tile_no == 0)) mbar_arrive(full(slot));
+                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                }
+                page = next_page;
+            }
+        }
+    } else if (warp == 9) {
+        // ---------------------------------------------------------------- tensor pipe (as the 16-bit cache's)
+        uint32_t slot = 0, turn = 0, q_turn[2] = {0, 0}, p_turn[2] = {0, 0};
+        bool ok = true;
+        BtItem it;
+        for (; ok && more_pieces; more_pieces = ok && pieces.next(ok)) {
+            if (!bt_locate(b, g, pieces.idx, it)) { if (PART) break; continue; }
+            const int n_tiles = max(it.tiles[0], it.tiles[1]);
+            auto commit = [&](uint32_t bar) { if (elect_one()) tc_commit(bar); };
+            auto scores = [&](int x, uint32_t k_sh) {                 // S(x) = Q(x) K^T
+                if (elect_one()) {
+                    const uint64_t qd = tc_smem_desc(q_sh + x * S::Q_BYTES), kd = tc_smem_desc(k_sh);
+                    uint32_t q_lo = (uint32_t)qd, k_lo = (uint32_t)kd;
+                    asm volatile("" : "+r"(q_lo), "+r"(k_lo));        // (kept from being precomputed for all steps, slots and tiles)
+#pragma unroll
+                    for (int k = 0; k < 4 * HALVES; ++k) {            // 16 dims a step: 32 bytes, 64 dims a box
+                        const uint32_t step = ((k >> 2) * (BT_KEYS * 128) + (k & 3) * 32) >> 4;
+                        tc_mma(s_col(x), (qd >> 32 << 32) | (q_lo + step), (kd >> 32 << 32) | (k_lo + step), IDESC_QK, k > 0);
+                    }
+                    tc_commit(s_full(x));
+                }
+            };
+            auto weigh = [&](int x, uint32_t v_sh, bool first) {      // O(x) (+)= P(x) V
+                const uint64_t vd = tc_smem_desc_mn(v_sh);
+#pragma unroll
+                for (int h = 1; h >= 0; --h) {                        // the upper half of the keys is ready first
+                    if (!bt_wait(p_ready(x, h), p_turn[x], waits)) return false;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 4 * h; k < 4 * h + 4; ++k)       // 16 keys a step: 8 columns of P, 2048 bytes of V
+                            tc_mma_ts(o_col(x), s_col(x) + 64 + 8 * k, vd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, !first || k != 4);
+                    }
+                }
+                p_turn[x] ^= 1u;
+                return true;
+            };
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                if (ok && it.tiles[x]) { ok = bt_wait(q_full(x), q_turn[x], waits); q_turn[x] ^= 1u; }
+            if (ok && n_tiles > 0) {
+                ok = bt_wait(full(slot), turn, waits);
+                tc_fence_after();
+                if (ok) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (it.tiles[x]) {
+                            scores(x, ring + slot * S::SLOT_BYTES);
+                            if (it.tiles[x] == 1) commit(q_empty(x));
+                        }
+                    commit(empty(slot));
+                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                }
+            }
+            for (int j = 0; ok && j < n_tiles; ++j) {
+                const uint32_t v_slot = slot, v_turn = turn;
+                if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                ok = bt_wait(full(v_slot), v_turn, waits);
+                const bool more = j + 1 < n_tiles;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (ok && j < it.tiles[x]) {
+                        ok = weigh(x, ring + v_slot * S::SLOT_BYTES, j == 0);
+                        if (ok && j + 1 == it.tiles[x]) commit(o_full(x));
+                    }
+                    if (ok && x == 1) commit(empty(v_slot));
+                    if (ok && j + 1 < it.tiles[x]) {
+                        ok = bt_wait(full(slot), turn, waits);
+                        if (ok) {
+                            tc_fence_after();
+                            scores(x, ring + slot * S::SLOT_BYTES);
+                            if (j + 2 == it.tiles[x]) commit(q_empty(x));
+                        }
+                    }
+                }
+                if (ok && more) {
+                    commit(empty(slot));
+                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                }
+            }
+        }
+    } else {
+        // ---------------------------------------------------------------- softmax: a thread owns one packed query row
+        const int x = warp >> 2, rho = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_at = s_col(x) + lanes, o_at = o_col(x) + lanes;
+        const int tok = rho / G, head_in = rho - tok * G;
+        const unsigned all_pages = 0xFFFFu >> (16 - (BT_KEYS >> b.page_shift));
+        uint32_t s_turn = 0, o_turn = 0, q_turn = 0;
+        int tile_no = 0;
+        bool ok = true;
+        BtItem it;
+        for (; ok && more_pieces; more_pieces = ok && pieces.next(ok)) {
+            if (!bt_locate(b, g, pieces.idx, it)) { if (PART) break; continue; }
+            const int n_tiles = max(it.tiles[0], it.tiles[1]), mine = it.tiles[x];
+            const int t = it.t0 + x * TQ + tok;                       // token within the sequence
+            const bool live = x < g.tiles && tok < TQ && t < it.sp.n && (g.mode == BT_PREFIX || t < g.a.max_rows);
+            const int own_seen = seen_own(it.sp, t);                  // own keys that this row sees
+            const int all_see = seen_own(it.sp, it.t0 + x * TQ);      // ... that every row of the tile sees
+            float m = -INFINITY, l = 0.f, lower = 0.f;
+            if (mine > 0) {
+                ok = bt_wait(q_full(x), q_turn, waits);
+                if (!ok) break;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(lower) : "r"(lower_sh + ((q_turn * 2 + x) * BT_ROWS + rho) * 4) : "memory");
+                q_turn ^= 1u;
+            }
+            for (int j = 0; j < mine; ++j) {
+                ok = bt_wait(s_full(x), s_turn, waits);
+                if (!ok) break;
+                s_turn ^= 1u;
+                tc_fence_after();
+                const int key0 = (j < it.np ? it.first_tile + j : j - it.np) * BT_KEYS;
+                const int seen = j < it.np ? b.prefix_len - key0 : own_seen - key0;       // this row sees keys below this
+                const int at = (tile_no + j) & (BT_PAGE_RING - 1);
+                const unsigned pages = page_bits[at];
+                const uint32_t groups = scale_sh + at * 256;
+                const bool masked = key0 + BT_KEYS > (j < it.np ? b.prefix_len : all_see) || pages != all_pages;
+                const bool done = masked ? b8_softmax<DP, true>(s_at, o_at, p_ready(x, 0), groups, lower, seen, pages, b.page_shift, j == 0, m, l)
+                                         : b8_softmax<DP, false>(s_at, o_at, p_ready(x, 0), groups, lower, seen, pages, b.page_shift, j == 0, m, l);
+                if (!done) l += b8_weights_far(s_at, p_ready(x, 0), groups, lower, m == -INFINITY ? 0.f : m - B8_BIAS, seen, pages, b.page_shift);
+            }
+            tile_no += n_tiles;
+            if (!ok) break;
+            if (mine > 0) {
+                ok = bt_wait(o_full(x), o_turn, waits);
+                if (!ok) break;
+                o_turn ^= 1u;
+                tc_fence_after();
+            }
+            if (m == -INFINITY && l == l) l = 0.f;                    // no score but -infinity: what the polynomial made of them does not count
+            const int row = it.sp.r0 + t, head = it.kvh * G + head_in;
+            if (PART) {
+                const size_t at = ((size_t)it.slot * b.n_rows + row) * g.a.n_heads + head;
+                if (live) g.part_ml[at] = make_float2(m - B8_BIAS, l);
+#pragma unroll 1
+                for (int i = 0; i < DP; i += 32) {
+                    float o[32];
+                    if (mine > 0) {
+                        tmem_ld32(o_at + i, o);
+                        tmem_wait_ld(o);
+                    }
+                    if (live && l != 0.f) {
+                        float* dst = g.part_o + at * DP + i;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            store32(dst + e, __float_as_uint(o[e]), __float_as_uint(o[e + 1]), __float_as_uint(o[e + 2]), __float_as_uint(o[e + 3]),
+                                    __float_as_uint(o[e + 4]), __float_as_uint(o[e + 5]), __float_as_uint(o[e + 6]), __float_as_uint(o[e + 7]));
+                    }
+                }
+            } else if (ga.q_bf16) {
+                __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(g.a.out) + ((size_t)row * g.a.n_heads + head) * g.a.head_dim;
+                bt_store_out<__nv_bfloat16, DP>(o_at, dst, g.a.head_dim, mine > 0, live, g.wide_out != 0, l);
+            } else {
+                __half* dst = reinterpret_cast<__half*>(g.a.out) + ((size_t)row * g.a.n_heads + head) * g.a.head_dim;
+                bt_store_out<__half, DP>(o_at, dst, g.a.head_dim, mine > 0, live, g.wide_out != 0, l);
+            }
+            tc_fence_before();                                        // O is read: the next piece's product may overwrite it
+        }
+    }
+    __syncthreads();
+    bt_give_up(waits);
+    pdl_wait();                                           // (a launch before this one in the same call ends first)
+    if (warp == 9) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+    }
+}
+
+} // namespace swk
