@@ -113,16 +113,19 @@ cudaError_t launch_append8_any(int dtype, const BatchView& bv, const Append8View
 // ------------------------------------------------------------------------------ few rows per sequence
 // [page][block, K/V, kv head][slot][dim] bytes, seen as [plane][K, V][slot][dim] with overlapping planes (plane + n_kv_heads holds the V
 // of plane's K): one box brings a page's K and V for a kv head.  dp: bytes of a row in shared memory, 64 or 128; what lies beyond head_dim is 0.
-swift_status make_codes_map(const swift_paged_kv* kv, int dp, int most_slots, CUtensorMap* out)
+// K and V apart (whole = false): for tiles of one of them, not swizzled.
+swift_status make_codes_map(const swift_paged_kv* kv, int dp, int most_slots, bool whole, CUtensorMap* out)
 {
+    if (2ll * kv->n_blocks * kv->n_kv_heads * kv->n_pages > 0x7FFFFFFFll)
+        return fail_batch(SWIFT_EUNSUPPORTED, "a pool of %d pages of %d heads is beyond 2^31 planes", kv->n_pages, 2 * kv->n_blocks * kv->n_kv_heads);
     const EncodeTiled encode = encoder();
     if (!encode) return fail_batch(SWIFT_ECUDA, "cuTensorMapEncodeTiled not available from the driver");
     const cuuint64_t row = kv->head_dim, plane = row * kv->page_size;
     const cuuint64_t dims[4] = {row, (cuuint64_t)kv->page_size, 2, 2ull * kv->n_blocks * kv->n_kv_heads * kv->n_pages};
     const cuuint64_t strides[3] = {row, plane * kv->n_kv_heads, plane};
-    const cuuint32_t box[4] = {(cuuint32_t)dp, (cuuint32_t)(kv->page_size < most_slots ? kv->page_size : most_slots), 2, 1}, one[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {(cuuint32_t)dp, (cuuint32_t)(kv->page_size < most_slots ? kv->page_size : most_slots), whole ? 2u : 1u, 1}, one[4] = {1, 1, 1, 1};
     const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, kv->pool, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              dp == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              !whole ? CU_TENSOR_MAP_SWIZZLE_NONE : dp == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail_batch(SWIFT_EINVAL, "cuTensorMapEncodeTiled refused the tensor (code %d): a cache of odd size", (int)r);
     return SWIFT_OK;
@@ -210,7 +213,6 @@ swift_status plan_prefix8(const swift_coded_kv* c, const BatchView& bv, int n_he
             const int keys = unit_keys8(p->mt);
             const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, keys) + ceil_div(bv.prefix_len, keys)) * Hk;
             if (units > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a page table of %d x %d for %d kv heads is beyond 2^31 units of work", bv.n_seqs, bv.table_stride, Hk);
-            if (2ll * kv->n_blocks * Hk * kv->n_pages > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a pool of %d pages of %d heads is beyond 2^31 planes", kv->n_pages, 2 * kv->n_blocks * Hk);
             const size_t rows_all = (size_t)(p->items + (long long)p->grid * (BD_WARPS / p->mt)) * 16 * p->mt;
             p->few_o = take(rows_all * p->dp * 4);
             p->few_ml = take(rows_all * 8);
@@ -224,21 +226,24 @@ swift_status plan_prefix8(const swift_coded_kv* c, const BatchView& bv, int n_he
 
 // ------------------------------------------------------------------------------ many rows
 template <int HALVES, bool PART>
-cudaError_t launch_tc8(const BatchView& bv, const B8TcArgs& g, int grid, cudaStream_t s, bool after_previous)
+cudaError_t launch_tc8(const CUtensorMap& map, const BatchView& bv, const B8TcArgs& g, int grid, cudaStream_t s, bool after_previous)
 {
     static std::atomic<unsigned long long> done{0};
     const cudaError_t e = allow_smem(attn_batch8_tc_kernel<HALVES, PART>, B8TcShape<HALVES>::SMEM_BYTES, done);
     if (e != cudaSuccess) return e;
-    return launch(attn_batch8_tc_kernel<HALVES, PART>, dim3(grid), B8_THREADS, B8TcShape<HALVES>::SMEM_BYTES, s, after_previous, bv, g);
+    return launch(attn_batch8_tc_kernel<HALVES, PART>, dim3(grid), B8_THREADS, B8TcShape<HALVES>::SMEM_BYTES, s, after_previous, map, bv, g);
 }
 // The many-row kernel in one of its three modes on at most `most` SMs; items: an upper bound of its pieces of work.
 swift_status run_tc8(const swift_paged_kv* kv, int x_dtype, const BatchView& bv, const BtArgs& t, long long items, int most, cudaStream_t s, bool after)
 {
-    const B8TcArgs g = {t, kv->dtype == SWIFT_E4M3, x_dtype == SWIFT_BF16};
-    const int grid = (int)(items < most ? items : most);          // prompts: `most` does not limit, blocks take over one another's pieces
     const bool wide = kv->head_dim > 64;
-    const cudaError_t e = t.mode == BT_PROMPT ? (wide ? launch_tc8<2, false>(bv, g, grid, s, after) : launch_tc8<1, false>(bv, g, grid, s, after))
-                                              : (wide ? launch_tc8<2, true>(bv, g, grid, s, after) : launch_tc8<1, true>(bv, g, grid, s, after));
+    CUtensorMap map;
+    const swift_status st = make_codes_map(kv, wide ? 128 : 64, BT_KEYS, false, &map);
+    if (st != SWIFT_OK) return st;
+    const B8TcArgs g = {t, kv->dtype == SWIFT_E4M3, x_dtype == SWIFT_BF16, 2 * kv->n_blocks * kv->n_kv_heads * kv->n_pages};
+    const int grid = (int)(items < most ? items : most);          // prompts: `most` does not limit, blocks take over one another's pieces
+    const cudaError_t e = t.mode == BT_PROMPT ? (wide ? launch_tc8<2, false>(map, bv, g, grid, s, after) : launch_tc8<1, false>(map, bv, g, grid, s, after))
+                                              : (wide ? launch_tc8<2, true>(map, bv, g, grid, s, after) : launch_tc8<1, true>(map, bv, g, grid, s, after));
     if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
     return SWIFT_OK;
 }
@@ -328,7 +333,7 @@ swift_status run_prefix8(const swift_coded_kv* c, int x_dtype, const BatchView& 
         g.item_first = reinterpret_cast<int*>(ws + p.first);
         g.item_last = reinterpret_cast<int*>(ws + p.last);
         CUtensorMap map;
-        const swift_status st = make_codes_map(kv, p.dp, unit_keys8(p.mt), &map);
+        const swift_status st = make_codes_map(kv, p.dp, unit_keys8(p.mt), true, &map);
         if (st != SWIFT_OK) return st;
         e = kv->dtype == SWIFT_I8 ? launch_dec8_any<QT, int8_t>(p, map, bv, g, s, before) : launch_dec8_any<QT, __nv_fp8_e4m3>(p, map, bv, g, s, before);
     } else {

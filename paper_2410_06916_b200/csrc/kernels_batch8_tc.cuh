@@ -1,11 +1,14 @@
 // Attention of many query rows over a cache of 8-bit codes on the 5th-generation tensor cores: the many-row kernel of the 16-bit cache
 // (kernels_batch_tc.cuh: tiles, overlap, rescaling, pieces and modes are its own), whose operands are made on the way.
 //
-// Operands.  Three warps read a key tile's codes from the pages (16 bytes a lane, a tile ahead, in registers), make them fp16, which
-// holds int8 and e4m3 exactly, and store them in the swizzled layout that TMA would have left.  Converting 32768 codes costs these warps
-// some 550 instructions each in the 3100 cycles of a key tile; the first and the last tile of a piece are fetched while its neighbours
-// are still computed.  They stage the queries too, each row at the power of two that brings it to [2^14, 2^15).  So the products are fp16 for every
-// type of q.  (8-bit operands on both sides would round q to 8 bits; a 16-bit copy of the cache would be written and read by every call.)
+// Operands.  TMA brings a key tile's codes page by page into a ring of raw tiles; six warps make them fp16, which holds int8 and e4m3
+// exactly, and store them in the swizzled layout of the products.  (Three warps that fetched the codes themselves, 16 bytes a lane, took
+// 6300 cycles for a key tile, twice what the products and the softmax need.)  They stage the queries too, each row at the power of two that
+// brings it to [2^14, 2^15), so the products are fp16 for every type of q.  (8-bit operands on both sides would round q to 8 bits; a 16-bit copy
+// of the cache would be written and read by every call.)
+//
+// Registers.  With 16 warps a thread has 128, so a softmax thread holds half a row of scores at a time and reads three quarters of the row from
+// TMEM twice (half of it with 168 registers and 11 warps).
 //
 // Scales.  As in the few-row kernel: a weight is 2^(c s + log2 sv - r), and a group of 8 keys, which lies in one page, adds its sum times
 // 1 / sv to the sum of probabilities.  Per group of 8 that is one 16-byte load from shared memory and four operations in each of the two
@@ -16,24 +19,25 @@
 
 namespace swk {
 
-constexpr int B8_THREADS = 384;     // 2 x 4 softmax warps, the MMA warp (9), three warps that make operands (8, 10, 11)
-constexpr int B8_MAKERS = 3;
+constexpr int B8_THREADS = 512;     // 2 x 4 softmax warps, a TMA warp (8), the MMA warp (9), six warps that make operands (10 .. 15)
+constexpr int B8_MAKERS = 6;
 constexpr float B8_FAR = 200.f;
 
 template <int HALVES> struct B8TcShape {
     static constexpr int DP = 64 * HALVES;
     static constexpr int SLOT_BYTES = BT_KEYS * 128 * HALVES;         // a K or V tile in 16 bits
+    static constexpr int RAW_BYTES = BT_KEYS * DP;                    // ... in codes
     static constexpr int Q_BYTES = BT_ROWS * 128 * HALVES;
-    static constexpr int SLOTS = HALVES == 2 ? 4 : 8;
+    static constexpr int SLOTS = HALVES == 2 ? 3 : 6;                 // and as many raw tiles
     static constexpr int LOWER_BYTES = 2 * 2 * BT_ROWS * 4;           // [piece parity][tile][row]
     static constexpr int SCALE_BYTES = BT_PAGE_RING * 16 * 16;        // [key tile][group of 8 keys]
     static constexpr int BAR_BYTES = 512;
-    static constexpr int SMEM_BYTES = 1024 + 2 * Q_BYTES + SLOTS * SLOT_BYTES + LOWER_BYTES + SCALE_BYTES + BAR_BYTES;
+    static constexpr int SMEM_BYTES = 1024 + 2 * Q_BYTES + SLOTS * (SLOT_BYTES + RAW_BYTES) + LOWER_BYTES + SCALE_BYTES + BAR_BYTES;
 };
 
 struct B8TcArgs {
     BtArgs t;
-    int e4m3, q_bf16;                                                 // types of the codes, and of q and out
+    int e4m3, q_bf16, planes;                                         // types of the codes, and of q and out; planes of the pool
 };
 
 __device__ __forceinline__ float4 b8_group(uint32_t at)               // {scale sk log2 e, log2 sv, 1 / sv}
@@ -135,38 +139,40 @@ __device__ __forceinline__ bool b8_softmax(uint32_t s_at, uint32_t o_at, uint32_
                                            float& m, float& l)
 {
     auto shown = [&](int q) { return MASKED ? bt_shown(pages, page_shift, seen, q) : 0xFFFFFFFFu; };
-    float s0[32], s1[32], s2[32], s3[32];
-    tmem_ld32(s_at, s0);
-    tmem_wait_ld(s0);
-    tmem_ld32(s_at + 32, s1);
-    float top = b8_top<MASKED>(s0, groups, lower, shown(0));
-    tmem_wait_ld(s1);
-    tmem_ld32(s_at + 64, s2);
-    top = max2_nan(top, b8_top<MASKED>(s1, groups + 64, lower, shown(1)));
-    tmem_wait_ld(s2);
-    tmem_ld32(s_at + 96, s3);
-    top = max2_nan(top, b8_top<MASKED>(s2, groups + 128, lower, shown(2)));
-    tmem_wait_ld(s3);
-    top = max2_nan(top, b8_top<MASKED>(s3, groups + 192, lower, shown(3)));
+    float a[32], b[32];
+    tmem_ld32(s_at, a);
+    tmem_wait_ld(a);
+    tmem_ld32(s_at + 32, b);
+    float top = b8_top<MASKED>(a, groups, lower, shown(0));
+    tmem_wait_ld(b);
+    tmem_ld32(s_at + 64, a);
+    top = max2_nan(top, b8_top<MASKED>(b, groups + 64, lower, shown(1)));
+    tmem_wait_ld(a);
+    tmem_ld32(s_at + 96, b);
+    top = max2_nan(top, b8_top<MASKED>(a, groups + 128, lower, shown(2)));
+    tmem_wait_ld(b);
+    tmem_ld32(s_at + 64, a);
+    top = max2_nan(top, b8_top<MASKED>(b, groups + 192, lower, shown(3)));
     if (!(top < INFINITY)) l = __int_as_float(0x7FFFFFFF);            // a score of NaN or +infinity makes the row NaN
     const bool grown = bt_outgrown(top, m, 1.f);
+    tmem_wait_ld(a);
     if (__any_sync(FULL_WARP, grown)) bt_rescale<DP>(o_at, 1.f, top, grown, first, m, l);
     if (__any_sync(FULL_WARP, fabsf(m) > B8_FAR && m != -INFINITY)) return false;
     const float ref = m == -INFINITY ? 0.f : m - B8_BIAS;
     f32x2 sum = 0ull;
     uint32_t p[16];
-    tmem_ld32(s_at, s0);
-    b8_weights<MASKED>(s2, groups + 128, lower, ref, shown(2), sum, p);
-    tmem_st16(s_at + 96, p);
-    b8_weights<MASKED>(s3, groups + 192, lower, ref, shown(3), sum, p);
+    b8_weights<MASKED>(a, groups + 128, lower, ref, shown(2), sum, p);
+    tmem_ld32(s_at, a);
+    tmem_st16(s_at + 96, p);                                          // (over the scores of b, which are read)
+    b8_weights<MASKED>(b, groups + 192, lower, ref, shown(3), sum, p);
     tmem_st16(s_at + 112, p);
     bt_hand_over(p_bar, 1);
-    tmem_wait_ld(s0);
-    tmem_ld32(s_at + 32, s1);
-    b8_weights<MASKED>(s0, groups, lower, ref, shown(0), sum, p);
+    tmem_wait_ld(a);
+    tmem_ld32(s_at + 32, b);
+    b8_weights<MASKED>(a, groups, lower, ref, shown(0), sum, p);
     tmem_st16(s_at + 64, p);
-    tmem_wait_ld(s1);
-    b8_weights<MASKED>(s1, groups + 64, lower, ref, shown(1), sum, p);
+    tmem_wait_ld(b);
+    b8_weights<MASKED>(b, groups + 64, lower, ref, shown(1), sum, p);
     tmem_st16(s_at + 80, p);
     bt_hand_over(p_bar, 0);
     float l0, l1;
@@ -192,9 +198,16 @@ __device__ __forceinline__ void b8_store16(uint32_t at, uint32_t a, uint32_t b, 
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// grid: one block per piece (PART: persistent blocks that take pieces blockIdx.x, + gridDim.x, ...); block = 384.
+__device__ __forceinline__ uint4 b8_load16(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+
+// grid: one block per piece (PART: persistent blocks that take pieces blockIdx.x, + gridDim.x, ...); block = 512.
 template <int HALVES, bool PART>
-__global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView b, B8TcArgs ga)
+__global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __grid_constant__ CUtensorMap map_kv, BatchView b, B8TcArgs ga)
 {
     typedef B8TcShape<HALVES> S;
     const BtArgs& g = ga.t;
@@ -205,10 +218,12 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView
     pdl_trigger();
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t q_sh = base, ring = base + 2 * S::Q_BYTES, lower_sh = ring + S::SLOTS * S::SLOT_BYTES, scale_sh = lower_sh + S::LOWER_BYTES, bars = scale_sh + S::SCALE_BYTES;
+    const uint32_t q_sh = base, ring = base + 2 * S::Q_BYTES, raw_ring = ring + S::SLOTS * S::SLOT_BYTES, lower_sh = raw_ring + S::SLOTS * S::RAW_BYTES, scale_sh = lower_sh + S::LOWER_BYTES, bars = scale_sh + S::SCALE_BYTES;
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (S::SLOTS + s); };
-    const uint32_t b2 = bars + 16u * S::SLOTS;
+    auto raw_full = [&](int s) { return bars + 8u * (2 * S::SLOTS + s); };
+    auto raw_empty = [&](int s) { return bars + 8u * (3 * S::SLOTS + s); };
+    const uint32_t b2 = bars + 32u * S::SLOTS;
     auto q_full = [&](int x) { return b2 + 8u * x; };
     auto q_empty = [&](int x) { return b2 + 16u + 8u * x; };
     auto s_full = [&](int x) { return b2 + 32u + 8u * x; };
@@ -224,7 +239,12 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView
     const int G = g.a.n_heads / g.a.n_kv_heads, TQ = g.rows_per_tile;
     if (warp == 9) {
         if (lane == 0) {
-            for (int s = 0; s < S::SLOTS; ++s) { mbar_init(full(s), B8_MAKERS); mbar_init(empty(s), 1); }
+            for (int s = 0; s < S::SLOTS; ++s) {
+                mbar_init(full(s), B8_MAKERS);
+                mbar_init(empty(s), 1);
+                mbar_init(raw_full(s), 1);
+                mbar_init(raw_empty(s), B8_MAKERS);
+            }
             for (int x = 0; x < 2; ++x) {
                 mbar_init(q_full(x), B8_MAKERS); mbar_init(q_empty(x), 1); mbar_init(s_full(x), 1); mbar_init(o_full(x), 1);
                 mbar_init(p_ready(x, 0), 4); mbar_init(p_ready(x, 1), 4);
@@ -238,6 +258,7 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_sh)), "r"(512));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
+    if (tid == 256) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_kv) : "memory");
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -248,24 +269,22 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView
     auto s_col = [&](int x) { return tmem + 128u * x; };              // S, then P, of tile x
     auto o_col = [&](int x) { return tmem + 256u + 128u * x; };
 
-    if (warp >= 8 && warp != 9) {
-        // ---------------------------------------------------------------- makers of operands: queries, K and V tiles in turn
-        constexpr int LANES = DP / 16, ROWS = 32 / LANES;             // lanes of a row (16 codes each), rows of a step
-        constexpr int STEPS = (BT_KEYS / ROWS + B8_MAKERS - 1) / B8_MAKERS;      // of a maker, per tile
-        const int maker = warp == 8 ? 0 : warp - 9, D = g.a.head_dim;
-        const int j16 = lane % LANES, my_row = lane / LANES;
+    auto keys_left = [&](const BtItem& it, int j) { return j < it.np ? b.prefix_len - (it.first_tile + j) * BT_KEYS : it.sp.len - (j - it.np) * BT_KEYS; };
+
+    if (warp == 8) {
+        // ---------------------------------------------------------------- TMA: codes of K and V tiles in turn; their pages and scales
         const int per_tile = BT_KEYS >> b.page_shift;                 // pages per key tile, 1..16
-        const uint8_t* pool = reinterpret_cast<const uint8_t*>(g.a.pool);
         const float c = g.a.scale * 1.4426950408889634f;
-        uint32_t slot = 0, turn = 0, q_turn[2] = {0, 0};
+        uint32_t slot = 0, turn = 0;
         int tile_no = 0;
         bool ok = true;
         BtItem it;
         for (; ok && more_pieces; more_pieces = ok && pieces.next(ok)) {
-            if (maker == 0) ok = pieces.ask();
+            ok = pieces.ask();
             if (!ok) break;
             if (!bt_locate(b, g, pieces.idx, it)) { if (PART) break; continue; }
             const int n_tiles = max(it.tiles[0], it.tiles[1]);
+            const int plane = g.block * 2 * g.a.n_kv_heads + it.kvh;
             // lane p: page p of a key tile, -1 where there is none
             auto look_up = [&](int j) {
                 const bool shared_part = j < it.np;
@@ -279,31 +298,7 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView
                 }
                 return page;
             };
-            auto keys_left = [&](int j) { return j < it.np ? b.prefix_len - (it.first_tile + j) * BT_KEYS : it.sp.len - (j - it.np) * BT_KEYS; };
-            uint4 v[STEPS];
-            auto fetch = [&](int i, int page_lane, int left, int kv) {            // step i of a tile of K or V
-                const int row = (i * B8_MAKERS + maker) * ROWS + my_row;
-                const int page = __shfl_sync(FULL_WARP, page_lane, (row & (BT_KEYS - 1)) >> b.page_shift);
-                v[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (row < BT_KEYS && row < left && page >= 0 && 16 * j16 < D)
-                    v[i] = __ldg(reinterpret_cast<const uint4*>(pool + (long long)page * g.a.page_elems + (kv ? g.a.kv_elems : 0) +
-                                                                ((long long)it.kvh * b.page_size + (row & (b.page_size - 1))) * D + 16 * j16));
-            };
-            auto keep = [&](int i, uint32_t dst) {                                // its operands, where the products read them
-                const int row = (i * B8_MAKERS + maker) * ROWS + my_row;
-                if (row >= BT_KEYS) return;
-                uint32_t r[8];
-                b8_widen(v[i], ga.e4m3 != 0, r);
-                const uint32_t p = 2 * (j16 & 3), at = dst + (j16 >> 2) * (BT_KEYS * 128) + row * 128, sw = row & 7;
-                if (j16 & 4) {                                                    // (the order keeps the eight lanes of a row in different banks)
-                    b8_store16(at + (((p + 1) ^ sw) << 4), r[4], r[5], r[6], r[7]);
-                    b8_store16(at + ((p ^ sw) << 4), r[0], r[1], r[2], r[3]);
-                } else {
-                    b8_store16(at + ((p ^ sw) << 4), r[0], r[1], r[2], r[3]);
-                    b8_store16(at + (((p + 1) ^ sw) << 4), r[4], r[5], r[6], r[7]);
-                }
-            };
-            auto group_scales = [&](int page_lane) {                              // lane i < 16: of keys 8 i ..
+            auto group_scales = [&](int page_lane) {                  // lane i < 16: of keys 8 i ..
                 const int page = __shfl_sync(FULL_WARP, page_lane, (8 * (lane & 15)) >> b.page_shift);
                 float2 s = make_float2(1.f, 1.f);
                 if (page >= 0) {
@@ -312,28 +307,64 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView
                 }
                 return s;
             };
-            int page = look_up(0), next_page = -1;
-            float2 scales = make_float2(1.f, 1.f);
-            if (n_tiles > 0) {
-#pragma unroll
-                for (int i = 0; i < STEPS; ++i) fetch(i, page, keys_left(0), 0);
-                if (maker == 0) scales = group_scales(page);
+            int page = look_up(0);
+            float2 scales = group_scales(page);
+            for (int j = 0; ok && j < n_tiles; ++j, ++tile_no) {
+                const int next_page = look_up(j + 1);
+                const unsigned pages = __ballot_sync(FULL_WARP, page >= 0);
+                if (lane < 16) {
+                    const B8Scale s = b8_scale(scales.x, scales.y, c);
+                    b8_store16(scale_sh + ((tile_no & (BT_PAGE_RING - 1)) * 16 + lane) * 16, __float_as_uint(s.c), __float_as_uint(s.lv), __float_as_uint(s.inv), 0u);
+                }
+                if (lane == 0) page_bits[tile_no & (BT_PAGE_RING - 1)] = pages;
+                __syncwarp();
+                for (int kv = 0; kv < 2; ++kv) {
+                    ok = bt_wait(raw_empty(slot), turn ^ 1u, waits);
+                    if (!ok) break;
+                    const bool asks = !(g.a.withhold && kv == 0 && tile_no == 0);
+                    if (asks && elect_one()) mbar_expect_tx(raw_full(slot), (uint32_t)S::RAW_BYTES);
+                    __syncwarp();
+                    for (int p = 0; asks && p < per_tile; ++p) {
+                        const int pg = __shfl_sync(FULL_WARP, page, p);
+                        // no page: beyond the last plane, which fills zeros
+                        if (elect_one()) tma_load_4d(raw_ring + slot * S::RAW_BYTES + (p << b.page_shift) * DP, &map_kv, 0, 0, kv, pg < 0 ? ga.planes : pg * (ga.planes / b.n_pages) + plane, raw_full(slot));
+                    }
+                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
+                }
+                page = next_page;
+                scales = group_scales(page);
             }
+        }
+    } else if (warp >= 10) {
+        // ---------------------------------------------------------------- makers of operands: queries, K and V tiles in turn
+        constexpr int LANES = DP / 16, ROWS = 32 / LANES;             // lanes of a row (16 codes each), rows of a step
+        constexpr int STEPS = BT_KEYS / ROWS;
+        const int maker = warp - 10, D = g.a.head_dim;
+        const int j16 = lane % LANES, my_row = lane / LANES;
+        const uint32_t raw_lane = my_row * DP + j16 * 16;
+        // where this lane's two pieces of 8 operands go within a row; the order keeps the eight lanes of a row in different banks
+        const uint32_t first_piece = 2 * (j16 & 3) + (j16 >> 2), half_at = (j16 >> 2) * (BT_KEYS * 128);
+        uint32_t slot = 0, turn = 0, q_turn[2] = {0, 0};
+        bool ok = true;
+        BtItem it;
+        for (; ok && more_pieces; more_pieces = ok && pieces.next(ok)) {
+            if (!bt_locate(b, g, pieces.idx, it)) { if (PART) break; continue; }
+            const int n_tiles = max(it.tiles[0], it.tiles[1]);
             // ---- queries
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 if (!ok || it.tiles[x] == 0) continue;
                 ok = bt_wait(q_empty(x), q_turn[x] ^ 1u, waits);
                 if (!ok) break;
-                constexpr int QL = DP / 8, QR = 32 / QL, QS = (BT_ROWS / QR + B8_MAKERS - 1) / B8_MAKERS;     // lanes of a row, rows of a step, steps
+                constexpr int QL = DP / 8, QR = 32 / QL, QS = BT_ROWS / QR;      // lanes of a row, rows of a step, steps
                 const int piece = lane % QL, q_row = lane / QL;
-                constexpr int AHEAD = 4;
+                constexpr int AHEAD = 3;
 #pragma unroll 1
-                for (int i0 = 0; i0 < QS; i0 += AHEAD) {
+                for (int i0 = maker; i0 < QS; i0 += AHEAD * B8_MAKERS) {
                     uint4 u[AHEAD];
 #pragma unroll
                     for (int e = 0; e < AHEAD; ++e) {
-                        const int rho = ((i0 + e) * B8_MAKERS + maker) * QR + q_row, tok = rho / G, tk = it.t0 + x * TQ + tok;
+                        const int rho = (i0 + e * B8_MAKERS) * QR + q_row, tok = rho / G, tk = it.t0 + x * TQ + tok;
                         u[e] = make_uint4(0u, 0u, 0u, 0u);
                         if (rho < BT_ROWS && tok < TQ && tk < it.sp.n && 8 * piece < D)
                             u[e] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(g.a.q) + (long long)(it.sp.r0 + tk) * g.a.q_row_stride +
@@ -341,7 +372,7 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView
                     }
 #pragma unroll
                     for (int e = 0; e < AHEAD; ++e) {
-                        const int rho = ((i0 + e) * B8_MAKERS + maker) * QR + q_row;
+                        const int rho = (i0 + e * B8_MAKERS) * QR + q_row;
                         const uint32_t w[4] = {u[e].x, u[e].y, u[e].z, u[e].w};
                         float y[8], top = 0.f;
 #pragma unroll
@@ -375,40 +406,40 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(BatchView
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full(x));
             }
-            // ---- key tiles: while one is kept, the next is fetched
-            for (int j = 0; ok && j < n_tiles; ++j, ++tile_no) {
-                const unsigned pages = __ballot_sync(FULL_WARP, page >= 0);
-                const float2 now = scales;
+            // ---- K and V tiles
+            for (int j = 0; ok && j < 2 * n_tiles; ++j) {
+                const int left = keys_left(it, j >> 1);
+                ok = bt_wait(raw_full(slot), turn, waits) && bt_wait(empty(slot), turn ^ 1u, waits);
+                if (!ok) break;
+                const uint32_t src = raw_ring + slot * S::RAW_BYTES + raw_lane, dst = ring + slot * S::SLOT_BYTES + half_at;
 #pragma unroll
-                for (int kv = 0; kv < 2; ++kv) {
-                    ok = bt_wait(empty(slot), turn ^ 1u, waits);
-                    if (!ok) break;
-                    const uint32_t dst = ring + slot * S::SLOT_BYTES;
-                    const int left = keys_left(kv ? j + 1 : j), pg = kv ? next_page : page;
-                    const bool more = kv == 0 || j + 1 < n_tiles;
-                    if (kv == 0) next_page = look_up(j + 1);
+                for (int i0 = 0; i0 < STEPS; i0 += 3 * B8_MAKERS) {
+                    uint4 v[3];
 #pragma unroll
-                    for (int i = 0; i < STEPS; ++i) {
-                        keep(i, dst);
-                        if (more) fetch(i, pg, left, kv ^ 1);
+                    for (int e = 0; e < 3; ++e) {
+                        const int step = i0 + e * B8_MAKERS + maker, row = step * ROWS + my_row;
+                        v[e] = make_uint4(0u, 0u, 0u, 0u);            // slots behind the end may hold anything
+                        if (step < STEPS && row < left) v[e] = b8_load16(src + step * (ROWS * DP));
                     }
-                    if (maker == 0) {
-                        if (kv == 0) {
-                            if (lane == 0) page_bits[tile_no & (BT_PAGE_RING - 1)] = pages;
-                            if (lane < 16) {
-                                const B8Scale s = b8_scale(now.x, now.y, c);
-                                b8_store16(scale_sh + ((tile_no & (BT_PAGE_RING - 1)) * 16 + lane) * 16, __float_as_uint(s.c), __float_as_uint(s.lv), __float_as_uint(s.inv), 0u);
-                            }
-                        } else if (more) {
-                            scales = group_scales(next_page);
-                        }
+#pragma unroll
+                    for (int e = 0; e < 3; ++e) {
+                        const int step = i0 + e * B8_MAKERS + maker, row = step * ROWS + my_row;
+                        if (step >= STEPS) break;
+                        uint32_t r[8];
+                        b8_widen(v[e], ga.e4m3 != 0, r);
+                        const uint32_t at = dst + row * 128, sw = row & 7;
+                        const bool odd = j16 >> 2;
+                        b8_store16(at + ((first_piece ^ sw) << 4), odd ? r[4] : r[0], odd ? r[5] : r[1], odd ? r[6] : r[2], odd ? r[7] : r[3]);
+                        b8_store16(at + ((first_piece ^ 1u ^ sw) << 4), odd ? r[0] : r[4], odd ? r[1] : r[5], odd ? r[2] : r[6], odd ? r[3] : r[7]);
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0 && !(g.a.withhold && maker == 0 && kv == 0 && tile_no == 0)) mbar_arrive(full(slot));
-                    if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
                 }
-                page = next_page;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(full(slot));
+                    mbar_arrive(raw_empty(slot));
+                }
+                if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
             }
         }
     } else if (warp == 9) {
