@@ -240,10 +240,11 @@ swift_status run_tc8(const swift_paged_kv* kv, int x_dtype, const BatchView& bv,
     CUtensorMap map;
     const swift_status st = make_codes_map(kv, wide ? 128 : 64, BT_KEYS, false, &map);
     if (st != SWIFT_OK) return st;
-    const B8TcArgs g = {t, kv->dtype == SWIFT_E4M3, x_dtype == SWIFT_BF16, 2 * kv->n_blocks * kv->n_kv_heads * kv->n_pages};
+    const B8TcArgs g = {t, kv->dtype == SWIFT_E4M3, x_dtype == SWIFT_BF16, kv->n_blocks};
     const int grid = (int)(items < most ? items : most);          // prompts: `most` does not limit, blocks take over one another's pieces
-    const cudaError_t e = t.mode == BT_PROMPT ? (wide ? launch_tc8<2, false>(map, bv, g, grid, s, after) : launch_tc8<1, false>(map, bv, g, grid, s, after))
-                                              : (wide ? launch_tc8<2, true>(map, bv, g, grid, s, after) : launch_tc8<1, true>(map, bv, g, grid, s, after));
+    const bool part = t.mode != BT_PROMPT;
+    const cudaError_t e = wide ? (part ? launch_tc8<2, true>(map, bv, g, grid, s, after) : launch_tc8<2, false>(map, bv, g, grid, s, after))
+                               : (part ? launch_tc8<1, true>(map, bv, g, grid, s, after) : launch_tc8<1, false>(map, bv, g, grid, s, after));
     if (e != cudaSuccess) return fail_batch(SWIFT_ECUDA, "kernel launch failed: %s", cudaGetErrorString(e));
     return SWIFT_OK;
 }
@@ -254,7 +255,6 @@ swift_status run_prompt8(const swift_paged_kv* kv, int x_dtype, const BatchView&
     g.mode = BT_PROMPT;
     g.block = block;
     g.rows_per_tile = BT_ROWS / (av.n_heads / av.n_kv_heads);
-    g.wide_out = aligned(av.out, 32) && av.head_dim % 16 == 0;
     g.tiles = piece_bound(bv, av.n_kv_heads, g.rows_per_tile) <= multiprocessors() ? 1 : 2;     // as for the 16-bit cache
     return run_tc8(kv, x_dtype, bv, g, piece_bound(bv, av.n_kv_heads, g.tiles * g.rows_per_tile), 0x7FFFFFFF, s, false);
 }

@@ -62,7 +62,7 @@ template <bool NEXT> __device__ __forceinline__ void b8_operands(uint32_t x, uin
 // A power of two that brings a largest magnitude to [2^14, 2^15), and its inverse
 __device__ __forceinline__ float b8_lift(float top, float& inverse)
 {
-    const int e = top > 0.f ? min(max(141 - (int)(__float_as_uint(top) >> 23), -126), 126) : 0;      // 14 - (exponent - 127)
+    const int e = __float_as_uint(top) ? min(141 - (int)(__float_as_uint(top) >> 23), 126) : 0;      // 14 - (exponent - 127)
     inverse = __uint_as_float((uint32_t)(127 - e) << 23);
     return __uint_as_float((uint32_t)(127 + e) << 23);
 }
@@ -123,6 +123,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
 
         // ---- the fetching side, by the worker's first warp.  Shared memory: box after box [K, V][slot][dim]
         const uint32_t box_v = box_rows * DP, box_bytes = 2 * box_v;
+        const int page_planes = g.planes / b.n_pages;                     // (kept out of the loops: a division costs as much as a box)
         BdWalk wf = w;
         int asked = 0, f_stage = 0, next_page = 0;                        // next_page: lane p: page of box p of unit `asked`
         uint32_t f_turn = 0;
@@ -136,7 +137,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
         };
         auto ask = [&]() {                                                // asks for unit `asked`; its stage is free
             const bool good = (unsigned)next_page < (unsigned)b.n_pages;
-            const int page = good ? next_page : b.n_pages;                // beyond the last page: zeros
+            const int page = next_page;                                   // no page: a box beyond the last plane, which fills zeros
             const unsigned pages = __ballot_sync(FULL_WARP, good) & all_boxes;
             const bool asks = !(g.a.withhold && asked == 0);
             if (elect_one()) {
@@ -145,10 +146,10 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
             }
             __syncwarp();
             const uint32_t dst = stages + f_stage * S::UNIT_BYTES;
-            const int plane = g.block * 2 * Hk + wf.kvh;
+            const int plane = good ? page * page_planes + g.block * 2 * Hk + wf.kvh : g.planes;
             for (int p = 0; asks && p < per_unit; ++p) {
-                const int pageu = __shfl_sync(FULL_WARP, page, p), slot0 = (wf.unit * KEYS + p * box_rows) & (b.page_size - 1);
-                if (elect_one()) tma_load_4d(dst + p * box_bytes, &map_kv, 0, slot0, 0, pageu == b.n_pages ? g.planes : pageu * (g.planes / b.n_pages) + plane, full(f_stage));
+                const int of = __shfl_sync(FULL_WARP, plane, p), slot0 = (wf.unit * KEYS + p * box_rows) & (b.page_size - 1);
+                if (elect_one()) tma_load_4d(dst + p * box_bytes, &map_kv, 0, slot0, 0, of, full(f_stage));
             }
             if (lane < per_unit && good) {                                // its scales; those of no page are not looked at
                 const float* s = g.a.scales + page * g.a.scale_page + wf.kvh;

@@ -37,7 +37,7 @@ template <int HALVES> struct B8TcShape {
 
 struct B8TcArgs {
     BtArgs t;
-    int e4m3, q_bf16, planes;                                         // types of the codes, and of q and out; planes of the pool
+    int e4m3, q_bf16, n_blocks;                                       // types of the codes, and of q and out; blocks of a page
 };
 
 __device__ __forceinline__ float4 b8_group(uint32_t at)               // {scale sk log2 e, log2 sv, 1 / sv}
@@ -53,21 +53,23 @@ __device__ __forceinline__ float b8_highest8(const float* s)          // NaN if 
 // The largest t of a quarter (32 keys); keys that are not shown do not count.
 template <bool MASKED> __device__ __forceinline__ float b8_top(float (&s)[32], uint32_t groups, float lower, unsigned shown)
 {
-    float top = -INFINITY;
+    float top[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float4 g = b8_group(groups + 16 * i);
         if (MASKED) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (!((shown >> (8 * i + e)) & 1u)) s[8 * i + e] = -INFINITY;
+            for (int e = 8 * i; e < 8 * i + 8; ++e)
+                if (!((shown >> e) & 1u)) s[e] = -INFINITY;
         }
         const float t = fmaf(b8_highest8(s + 8 * i), g.x * lower, g.y);
-        top = max2_nan(top, !MASKED || ((shown >> (8 * i)) & 0xFFu) ? t : -INFINITY);
+        top[i] = !MASKED || ((shown >> (8 * i)) & 0xFFu) ? t : -INFINITY;
     }
-    return top;
+    return max2_nan(max2_nan(top[0], top[1]), max2_nan(top[2], top[3]));
 }
-// 32 scores -> weights (fp16, two to a register), what they add to the sum of probabilities
+// 32 scores -> weights (fp16, two to a register), what they add to the sum of probabilities.  (The two softmax warps of a scheduler are bound by
+// their own latencies: part of the exponentials as polynomials, as for the 16-bit cache, makes no difference, nor does treating 32 keys of a page of
+// at least 32 as one group: 2048 rows behind 6144 630 to 644 us.)
 template <bool MASKED> __device__ __forceinline__ void b8_weights(const float (&s)[32], uint32_t groups, float lower, float ref, unsigned shown, f32x2& sum, uint32_t (&p)[16])
 {
 #pragma unroll
@@ -75,25 +77,22 @@ template <bool MASKED> __device__ __forceinline__ void b8_weights(const float (&
         const float4 g = b8_group(groups + 16 * i);
         const float c = g.x * lower, off = g.y - ref;
         const f32x2 c2 = pair2(c, c), off2 = pair2(off, off);
-        f32x2 part = 0ull;
+        f32x2 part[4];
 #pragma unroll
-        for (int j = 4 * i; j < 4 * i + 4; ++j) {
+        for (int j = 0; j < 4; ++j) {
+            const int e = 8 * i + 2 * j;
             float p0, p1;
-            split2(fma2(pair2(s[2 * j], s[2 * j + 1]), c2, off2), p0, p1);
-            if (!MASKED && ((BT_POLY >> j) & 1u)) {                   // (the polynomial gives a hidden key 2^-126, not 0)
-                ex2_poly<__half>(p0, p1, p0, p1);
-            } else {
-                p0 = ex2(p0);
-                p1 = ex2(p1);
-            }
+            split2(fma2(pair2(s[e], s[e + 1]), c2, off2), p0, p1);
+            p0 = ex2(p0);
+            p1 = ex2(p1);
             if (MASKED) {                                             // (a hidden score may have met a scale that is 0 or NaN)
-                p0 = (shown >> (2 * j)) & 1u ? p0 : 0.f;
-                p1 = (shown >> (2 * j + 1)) & 1u ? p1 : 0.f;
+                p0 = (shown >> e) & 1u ? p0 : 0.f;
+                p1 = (shown >> (e + 1)) & 1u ? p1 : 0.f;
             }
-            part = j == 4 * i ? pair2(p0, p1) : add2(part, pair2(p0, p1));
-            p[j] = pack2(p0, p1, __half());
+            part[j] = pair2(p0, p1);
+            p[4 * i + j] = pack2(p0, p1, __half());
         }
-        sum = fma2(part, pair2(g.z, g.z), sum);
+        sum = fma2(add2(add2(part[0], part[1]), add2(part[2], part[3])), pair2(g.z, g.z), sum);
     }
 }
 // The weights of a key tile with rows whose maximum is far from zero, from the scores in TMEM on: what they add to the sums.
@@ -179,6 +178,32 @@ __device__ __forceinline__ bool b8_softmax(uint32_t s_at, uint32_t o_at, uint32_
     split2(sum, l0, l1);
     l += l0 + l1;
     return true;
+}
+
+// A row's result to the output, by 16 bytes (32-byte stores out of a function of its own lose data with this compiler: it wrote 4 of the 32).
+// Every lane takes part in the reading; `live` lanes store.
+template <int COLS> __device__ __noinline__ void b8_store_out(uint32_t o_at, char* dst, int bf16, int dims, bool some, bool live, float l)
+{
+    const float inv = l == 0.f ? 0.f : 1.f / l;                       // 0: the row sees nothing
+#pragma unroll 1
+    for (int i = 0; i < COLS; i += 32) {
+        float o[32];
+        if (some) {
+            tmem_ld32(o_at + i, o);
+            tmem_wait_ld(o);
+        }
+        if (!live) continue;
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+            uint32_t v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float x = o[e + 2 * k] * inv, y = o[e + 2 * k + 1] * inv;
+                v[k] = l == 0.f ? 0u : bf16 ? pack2(x, y, __nv_bfloat16()) : pack2(x, y, __half());
+            }
+            if (i + e < dims) *reinterpret_cast<uint4*>(dst + 2 * (i + e)) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+    }
 }
 
 // 16 codes -> 16 operands
@@ -275,6 +300,7 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __g
         // ---------------------------------------------------------------- TMA: codes of K and V tiles in turn; their pages and scales
         const int per_tile = BT_KEYS >> b.page_shift;                 // pages per key tile, 1..16
         const float c = g.a.scale * 1.4426950408889634f;
+        const int page_planes = 2 * ga.n_blocks * g.a.n_kv_heads;
         uint32_t slot = 0, turn = 0;
         int tile_no = 0;
         bool ok = true;
@@ -318,6 +344,7 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __g
                 }
                 if (lane == 0) page_bits[tile_no & (BT_PAGE_RING - 1)] = pages;
                 __syncwarp();
+                const int at = page < 0 ? page_planes * b.n_pages : page * page_planes + plane;      // no page: beyond the last plane, which fills zeros
                 for (int kv = 0; kv < 2; ++kv) {
                     ok = bt_wait(raw_empty(slot), turn ^ 1u, waits);
                     if (!ok) break;
@@ -325,9 +352,8 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __g
                     if (asks && elect_one()) mbar_expect_tx(raw_full(slot), (uint32_t)S::RAW_BYTES);
                     __syncwarp();
                     for (int p = 0; asks && p < per_tile; ++p) {
-                        const int pg = __shfl_sync(FULL_WARP, page, p);
-                        // no page: beyond the last plane, which fills zeros
-                        if (elect_one()) tma_load_4d(raw_ring + slot * S::RAW_BYTES + (p << b.page_shift) * DP, &map_kv, 0, 0, kv, pg < 0 ? ga.planes : pg * (ga.planes / b.n_pages) + plane, raw_full(slot));
+                        const int of = __shfl_sync(FULL_WARP, at, p);
+                        if (elect_one()) tma_load_4d(raw_ring + slot * S::RAW_BYTES + (p << b.page_shift) * DP, &map_kv, 0, 0, kv, of, raw_full(slot));
                     }
                     if (++slot == S::SLOTS) { slot = 0; turn ^= 1u; }
                 }
@@ -339,11 +365,11 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __g
         // ---------------------------------------------------------------- makers of operands: queries, K and V tiles in turn
         constexpr int LANES = DP / 16, ROWS = 32 / LANES;             // lanes of a row (16 codes each), rows of a step
         constexpr int STEPS = BT_KEYS / ROWS;
-        const int maker = warp - 10, D = g.a.head_dim;
-        const int j16 = lane % LANES, my_row = lane / LANES;
+        const int maker = warp - 10, D = g.a.head_dim, per_head = (65535 + G) / G;   // rho / G = rho x per_head >> 16 for rho < 128
+        // eight lanes take 64 codes of two rows each: what they store then lies in different banks
+        const int j16 = (lane & 3) + (LANES == 8 ? (lane >> 1) & 4 : 0), my_row = LANES == 8 ? 2 * (lane >> 4) + ((lane >> 2) & 1) : lane >> 2;
         const uint32_t raw_lane = my_row * DP + j16 * 16;
-        // where this lane's two pieces of 8 operands go within a row; the order keeps the eight lanes of a row in different banks
-        const uint32_t first_piece = 2 * (j16 & 3) + (j16 >> 2), half_at = (j16 >> 2) * (BT_KEYS * 128);
+        const uint32_t first_piece = 2 * (j16 & 3), half_at = (j16 >> 2) * (BT_KEYS * 128);   // where its two pieces of 8 operands go
         uint32_t slot = 0, turn = 0, q_turn[2] = {0, 0};
         bool ok = true;
         BtItem it;
@@ -356,49 +382,52 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __g
                 if (!ok || it.tiles[x] == 0) continue;
                 ok = bt_wait(q_empty(x), q_turn[x] ^ 1u, waits);
                 if (!ok) break;
-                constexpr int QL = DP / 8, QR = 32 / QL, QS = BT_ROWS / QR;      // lanes of a row, rows of a step, steps
-                const int piece = lane % QL, q_row = lane / QL;
-                constexpr int AHEAD = 3;
-#pragma unroll 1
-                for (int i0 = maker; i0 < QS; i0 += AHEAD * B8_MAKERS) {
-                    uint4 u[AHEAD];
+                // Four lanes take a row, 8 rows a step: pieces of 8 dims 4 k + (lane & 3), odd rows in another order of k (banks).  fp16
+                // rows stay as they are; of bf16 ones, infinities and NaN included, the largest exponent goes to 14.
+                constexpr int PIECES = DP / 32;
+                const int sub = lane & 3, turned = (lane >> 2) & 1;
+                auto piece_of = [&](int k) { return 4 * (k ^ turned) + sub; };
+                uint4 u[PIECES];
+                auto fetch = [&](int rho) {
+                    const int tok = (rho * per_head) >> 16, tk = it.t0 + x * TQ + tok;
+                    const bool there = rho < BT_ROWS && tok < TQ && tk < it.sp.n;
+                    const uint16_t* src = reinterpret_cast<const uint16_t*>(g.a.q) + (long long)(it.sp.r0 + tk) * g.a.q_row_stride +
+                                          (long long)(it.kvh * G + rho - tok * G) * g.a.q_head_stride;
 #pragma unroll
-                    for (int e = 0; e < AHEAD; ++e) {
-                        const int rho = (i0 + e * B8_MAKERS) * QR + q_row, tok = rho / G, tk = it.t0 + x * TQ + tok;
-                        u[e] = make_uint4(0u, 0u, 0u, 0u);
-                        if (rho < BT_ROWS && tok < TQ && tk < it.sp.n && 8 * piece < D)
-                            u[e] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(g.a.q) + (long long)(it.sp.r0 + tk) * g.a.q_row_stride +
-                                                                        (long long)(it.kvh * G + rho - tok * G) * g.a.q_head_stride + 8 * piece));
+                    for (int k = 0; k < PIECES; ++k) {
+                        u[k] = make_uint4(0u, 0u, 0u, 0u);
+                        if (there && 8 * piece_of(k) < D) u[k] = __ldg(reinterpret_cast<const uint4*>(src + 8 * piece_of(k)));
                     }
+                };
+                int rho = 8 * maker + (lane >> 2);
+                fetch(rho);
+#pragma unroll 1
+                for (int step = 0; step < (16 + B8_MAKERS - 1) / B8_MAKERS; ++step, rho += 8 * B8_MAKERS) {
+                    uint4 y[PIECES];
 #pragma unroll
-                    for (int e = 0; e < AHEAD; ++e) {
-                        const int rho = (i0 + e * B8_MAKERS) * QR + q_row;
-                        const uint32_t w[4] = {u[e].x, u[e].y, u[e].z, u[e].w};
-                        float y[8], top = 0.f;
+                    for (int k = 0; k < PIECES; ++k) y[k] = u[k];
+                    if (rho + 8 * B8_MAKERS < BT_ROWS) fetch(rho + 8 * B8_MAKERS);       // (the same for the whole warp)
+                    float lower = 1.f;
+                    if (ga.q_bf16) {
+                        unsigned top = 0;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if (ga.q_bf16) {
-                                y[2 * i] = __uint_as_float(w[i] << 16);
-                                y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-                            } else {
-                                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-                                y[2 * i] = f.x;
-                                y[2 * i + 1] = f.y;
-                            }
+                        for (int k = 0; k < PIECES; ++k)
+                            top = __vmaxu2(__vmaxu2(top, __vmaxu2(y[k].x & 0x7FFF7FFFu, y[k].y & 0x7FFF7FFFu)), __vmaxu2(y[k].z & 0x7FFF7FFFu, y[k].w & 0x7FFF7FFFu));
+                        top = __vmaxu2(top, __shfl_xor_sync(FULL_WARP, top, 1));
+                        top = __vmaxu2(top, __shfl_xor_sync(FULL_WARP, top, 2));
+                        const float lift = b8_lift(__uint_as_float(max(top << 16, top & 0xFFFF0000u)), lower);
+#pragma unroll
+                        for (int k = 0; k < PIECES; ++k) {
+                            uint32_t* w = reinterpret_cast<uint32_t*>(&y[k]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) w[i] = pack2(__uint_as_float(w[i] << 16) * lift, __uint_as_float(w[i] & 0xFFFF0000u) * lift, __half());
                         }
+                    }
+                    if (rho < BT_ROWS) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (fabsf(y[i]) < INFINITY) top = fmaxf(top, fabsf(y[i]));
-#pragma unroll
-                        for (int o = QL / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_WARP, top, o));
-                        float lower;
-                        const float lift = b8_lift(top, lower);
-                        if (rho < BT_ROWS) {
-                            b8_store16(q_sh + x * S::Q_BYTES + (piece >> 3) * (BT_ROWS * 128) + rho * 128 + (((piece & 7) ^ (rho & 7)) << 4),
-                                       pack2(y[0] * lift, y[1] * lift, __half()), pack2(y[2] * lift, y[3] * lift, __half()),
-                                       pack2(y[4] * lift, y[5] * lift, __half()), pack2(y[6] * lift, y[7] * lift, __half()));
-                            if (piece == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(lower_sh + ((q_turn[x] * 2 + x) * BT_ROWS + rho) * 4), "f"(lower) : "memory");
-                        }
+                        for (int k = 0; k < PIECES; ++k)
+                            b8_store16(q_sh + x * S::Q_BYTES + (piece_of(k) >> 3) * (BT_ROWS * 128) + rho * 128 + (((piece_of(k) & 7) ^ (rho & 7)) << 4), y[k].x, y[k].y, y[k].z, y[k].w);
+                        if (sub == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(lower_sh + ((q_turn[x] * 2 + x) * BT_ROWS + rho) * 4), "f"(lower) : "memory");
                     }
                 }
                 q_turn[x] ^= 1u;
@@ -428,9 +457,8 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __g
                         uint32_t r[8];
                         b8_widen(v[e], ga.e4m3 != 0, r);
                         const uint32_t at = dst + row * 128, sw = row & 7;
-                        const bool odd = j16 >> 2;
-                        b8_store16(at + ((first_piece ^ sw) << 4), odd ? r[4] : r[0], odd ? r[5] : r[1], odd ? r[6] : r[2], odd ? r[7] : r[3]);
-                        b8_store16(at + ((first_piece ^ 1u ^ sw) << 4), odd ? r[0] : r[4], odd ? r[1] : r[5], odd ? r[2] : r[6], odd ? r[3] : r[7]);
+                        b8_store16(at + ((first_piece ^ sw) << 4), r[0], r[1], r[2], r[3]);
+                        b8_store16(at + ((first_piece ^ 1u ^ sw) << 4), r[4], r[5], r[6], r[7]);
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -542,17 +570,13 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __g
             const int own_seen = seen_own(it.sp, t);                  // own keys that this row sees
             const int all_see = seen_own(it.sp, it.t0 + x * TQ);      // ... that every row of the tile sees
             float m = -INFINITY, l = 0.f, lower = 0.f;
-            if (mine > 0) {
-                ok = bt_wait(q_full(x), q_turn, waits);
-                if (!ok) break;
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(lower) : "r"(lower_sh + ((q_turn * 2 + x) * BT_ROWS + rho) * 4) : "memory");
-                q_turn ^= 1u;
-            }
             for (int j = 0; j < mine; ++j) {
                 ok = bt_wait(s_full(x), s_turn, waits);
                 if (!ok) break;
                 s_turn ^= 1u;
                 tc_fence_after();
+                // Behind the first scores, which needed the queries: a wait for the queries themselves might come two pieces late.
+                if (j == 0) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(lower) : "r"(lower_sh + ((q_turn * 2 + x) * BT_ROWS + rho) * 4) : "memory");
                 const int key0 = (j < it.np ? it.first_tile + j : j - it.np) * BT_KEYS;
                 const int seen = j < it.np ? b.prefix_len - key0 : own_seen - key0;       // this row sees keys below this
                 const int at = (tile_no + j) & (BT_PAGE_RING - 1);
@@ -566,6 +590,7 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __g
             tile_no += n_tiles;
             if (!ok) break;
             if (mine > 0) {
+                q_turn ^= 1u;
                 ok = bt_wait(o_full(x), o_turn, waits);
                 if (!ok) break;
                 o_turn ^= 1u;
@@ -586,17 +611,12 @@ __global__ void __launch_bounds__(B8_THREADS, 1) attn_batch8_tc_kernel(const __g
                     if (live && l != 0.f) {
                         float* dst = g.part_o + at * DP + i;
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            store32(dst + e, __float_as_uint(o[e]), __float_as_uint(o[e + 1]), __float_as_uint(o[e + 2]), __float_as_uint(o[e + 3]),
-                                    __float_as_uint(o[e + 4]), __float_as_uint(o[e + 5]), __float_as_uint(o[e + 6]), __float_as_uint(o[e + 7]));
+                        for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                     }
                 }
-            } else if (ga.q_bf16) {
-                __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(g.a.out) + ((size_t)row * g.a.n_heads + head) * g.a.head_dim;
-                bt_store_out<__nv_bfloat16, DP>(o_at, dst, g.a.head_dim, mine > 0, live, g.wide_out != 0, l);
             } else {
-                __half* dst = reinterpret_cast<__half*>(g.a.out) + ((size_t)row * g.a.n_heads + head) * g.a.head_dim;
-                bt_store_out<__half, DP>(o_at, dst, g.a.head_dim, mine > 0, live, g.wide_out != 0, l);
+                char* dst = reinterpret_cast<char*>(g.a.out) + ((size_t)row * g.a.n_heads + head) * g.a.head_dim * 2;
+                b8_store_out<DP>(o_at, dst, ga.q_bf16, g.a.head_dim, mine > 0, live, l);
             }
             tc_fence_before();                                        // O is read: the next piece's product may overwrite it
         }
