@@ -12,8 +12,11 @@
 // fourth power (|r ln 2| < 2^-9.5: the rest is below 2^-53).
 //
 // A cluster of up to eight blocks holds a row's logits in shared memory, read from HBM once.  A cut is found by a histogram of the weights over
-// 512 bins of 1/16 in (max - l) / T, added up over the cluster; the tokens of the bin that it lies in (some hundred of them) are then gathered
-// and ordered.  Bins with more than a list holds (equal logits, flat rows) are divided again by the tokens' numbers.
+// 1024 bins of 1/32 in (max - l) / T, each block adding up a share of the bins over the cluster; the tokens of the bin that the cut lies in
+// (some ten to two hundred) are then gathered and ranked.  Bins with more than a list holds (equal logits, flat rows) are divided again by the
+// tokens' numbers.  Bins are sums of 15 bits of the weights at a time, since shared memory adds 32-bit words by itself but 64-bit ones in
+// a loop of trials (64 rows of 128000: 20 thousand cycles a block instead of 42).  What is left of the time is the latency of the steps in turn:
+// every trip to the other blocks' memory costs about half a microsecond, and their loads are therefore made together.
 #pragma once
 #include <cooperative_groups.h>
 
@@ -22,8 +25,9 @@
 namespace swk {
 
 constexpr int SA_THREADS = 512, SA_WARPS = SA_THREADS / 32;
-constexpr int SA_BINS = 512, SA_LIST = 512;               // one of each per thread
-constexpr int SA_CHUNK = 128;                             // tokens whose kept weights are summed up for the draw
+constexpr int SA_BINS = 1024;
+constexpr int SA_LIST = 256;
+constexpr int SA_CHUNK = 128;                             // tokens whose kept weights are summed up for the draw: four a lane
 constexpr int SA_BLOCKS = 8;                              // of a cluster, at most
 constexpr int SA_CHUNKS = 256;                            // of a block, at most
 constexpr int SA_UNIT_BITS = 45;
@@ -47,13 +51,13 @@ struct SampleView {
 
 struct SampleShared {
     double table[256];                                    // 2^(j / 256)
-    u64 mass[SA_BINS];
-    u64 list_at[2][SA_LIST], list_w[2][SA_LIST];          // [0]: this block's or the whole list's tokens, [1]: the other
+    unsigned bins[3][SA_BINS];                            // a block's counts, or 15 bits each of its sums of weights
+    u64 sums[SA_BINS];                                    // of the cluster, in the share of the bins that this block adds up
+    ulonglong2 list[2][SA_LIST];                          // number and weight (or 1): this block's tokens of the bin; then the cluster's
     u64 chunk[SA_CHUNKS];
     u64 warps[SA_WARPS];
-    u64 best, range[2], total, base, cut;
-    unsigned count[SA_BINS];
-    unsigned n_list, found, population, bad;
+    u64 best, range[2], total, share, base, cut;
+    unsigned n_list, found, bad;
 };
 
 __device__ __forceinline__ u64 sa_number(float x, int id) // rising in the order of the tokens
@@ -96,18 +100,26 @@ __device__ __forceinline__ u64 sa_block_scan(u64 v, SampleShared& sh, u64& all) 
     return before + v;
 }
 
+// A number in 64 bits by whole-number operations (the conversion unit takes a quarter of the lanes per cycle that these do); 0 and
+// numbers below 2^-126 become some number of about that size, infinities and NaN a large one.
+__device__ __forceinline__ double sa_widen(float x)
+{
+    const unsigned b = __float_as_uint(x);
+    return __hiloint2double((int)((b & 0x80000000u) | (((b & 0x7FFFFFFFu) >> 3) + 0x38000000u)), (int)(b << 29));
+}
+
 struct SampleWeight {
     double top, rate;                                     // log2(e) 256 / T
+    float least;                                          // below this logit a weight rounds to 0 (or is below min-p): not worth computing
     const double* table;
-    // exp((x - top) / T) 2^45, in 64 bits; 0 where it rounds to 0
+    // exp((x - top) / T) 2^45, in 64 bits, for x of at least `least`
     __device__ __forceinline__ double operator()(float x) const
     {
-        const double y = ((double)x - top) * rate;
-        if (!(y > -256.0 * (SA_UNIT_BITS + 1))) return 0.0;
-        const double round = 6755399441055744.0;          // 1.5 * 2^52: adding it leaves the nearest integer in the low bits
-        const double t = y + round, r = (y - (t - round)) * (0.69314718055994530942 / 256.0);
+        constexpr double ROUND = 6755399441055744.0;      // 1.5 * 2^52: adding it leaves the nearest integer in the low bits
+        constexpr double L = 0.69314718055994530942 / 256.0;
+        const double d = sa_widen(x) - top, t = fma(d, rate, ROUND), r = fma(d, rate, ROUND - t);
         const int n = __double2loint(t);
-        const double p = fma(fma(fma(fma(r, 1.0 / 24.0, 1.0 / 6.0), r, 0.5), r, 1.0), r, 1.0) * table[n & 255];
+        const double p = fma(fma(fma(fma(r, L * L * L * L / 24.0, L * L * L / 6.0), r, L * L / 2.0), r, L), r, 1.0) * table[n & 255];
         return __hiloint2double(__double2hiint(p) + (((n >> 8) + SA_UNIT_BITS) << 20), __double2loint(p));
     }
     static __device__ __forceinline__ u64 whole(double w) { return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull; }   // + 2^52
@@ -115,7 +127,7 @@ struct SampleWeight {
 
 // grid = rows x blocks of a cluster, block = 512
 template <typename T>
-__global__ void __launch_bounds__(SA_THREADS) sample_kernel(SampleView s)
+__global__ void __launch_bounds__(SA_THREADS, 2) sample_kernel(SampleView s)
 {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
@@ -125,8 +137,26 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(SampleView s)
     SampleShared& sh = *reinterpret_cast<SampleShared*>(sa_smem);
     T* vals = reinterpret_cast<T*>(sa_smem + (sizeof(SampleShared) + 15) / 16 * 16);
     const int id0 = rank * s.slice, n = max(0, min(s.slice, s.vocab - id0));
-    auto value = [&](int i) { return to_float(vals[i]) + 0.f; };          // (-0 as 0)
-    auto other = [&](int r) { return cluster.map_shared_rank(&sh, r); };
+    // the four logits from i on (i a multiple of 4; behind the end lie -infinities, whose weight is 0)
+    auto four = [&](int i, float (&x)[4]) {
+        T v[4];
+        if (sizeof(T) == 4) *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(vals + i);
+        else *reinterpret_cast<uint2*>(v) = *reinterpret_cast<const uint2*>(vals + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = to_float(v[j]) + 0.f;                          // (-0 as 0)
+    };
+    // Its own memory a block reads directly.  Through the cluster's window, with two blocks of different clusters on an SM, clusters of one or
+    // two blocks now and then read something else (1 row in 100 of 300 rows of 12000 under top-p; never with one block per SM).
+    auto other = [&](int r) -> SampleShared* { return r == rank ? &sh : cluster.map_shared_rank(&sh, r); };
+    // use(r, x) for what get gives of every block of the cluster; all loads before the first use
+    auto each = [&](auto get, auto use) {
+        decltype(get(&sh)) x[SA_BLOCKS];
+#pragma unroll
+        for (int r = 0; r < SA_BLOCKS; ++r) x[r] = r < blocks ? get(other(r)) : decltype(get(&sh))();
+#pragma unroll
+        for (int r = 0; r < SA_BLOCKS; ++r)
+            if (r < blocks) use(r, x[r]);
+    };
 
     // ---- the logits, their largest and whether all are numbers below infinity
     float best = -INFINITY;
@@ -167,6 +197,7 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(SampleView s)
             meet(v, i);
         }
     }
+    if (tid < SA_CHUNK && n + tid < (n + SA_CHUNK - 1) / SA_CHUNK * SA_CHUNK) store_val(vals + n + tid, -INFINITY);
     if (tid < 256) sh.table[tid] = exp2(tid / 256.0);
     if (tid == 0) sh.bad = 0;
     __syncthreads();
@@ -181,11 +212,8 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(SampleView s)
         sh.best = first;
     }
     cluster.sync();
-    for (int r = 0; r < blocks; ++r) {
-        const u64 x = other(r)->best;
-        first = r ? min(first, x) : x;
-        bad |= other(r)->bad != 0;
-    }
+    each([](const SampleShared* o) { return o->best; }, [&](int r, u64 x) { first = r ? min(first, x) : x; });
+    each([](const SampleShared* o) { return o->bad; }, [&](int, unsigned x) { bad |= x != 0; });
     const int first_id = (int)(unsigned)first;
     const float temperature = s.temperature ? s.temperature[row] : s.temperature_all, u = s.uniforms[row];
     const float top_p = s.top_p ? s.top_p[row] : s.top_p_all, min_p = s.min_p ? s.min_p[row] : s.min_p_all;
@@ -201,159 +229,181 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(SampleView s)
         cluster.sync();                                   // no block ends while another reads its memory
         return;
     }
-    const SampleWeight weight = {(double)top, 1.4426950408889634074 * 256.0 / (double)temperature, sh.table};
-    const float bin_rate = 16.f / temperature;
-    auto bin_of = [&](float x) { return min((int)((top - x) * bin_rate), SA_BINS - 1); };   // rises as x falls
-    u64 cut = ~0ull;
+    // ln of what rounds to half a unit is -31.9; a logit this far below the largest (and a little further, for the roundings here) has no weight
+    const double reach = -32.0 * (double)temperature;
+    const SampleWeight weight = {sa_widen(top), 1.4426950408889634074 * 256.0 / (double)temperature, fmaxf((float)((double)top + reach - 1e-6 * fabs((double)top)), -3.402823466e38f), sh.table};
+    const float bin_rate = 32.f / temperature;
+    auto bin_of = [&](float x) {                          // rises as x falls; the nearest whole number, by adding 2^23
+        return __float_as_int(fminf((top - x) * bin_rate, (float)(SA_BINS - 1)) + 8388608.f) & (SA_BINS - 1);
+    };
+    u64 cut = ~0ull;                                      // the number of the last token that is kept
+    float cut_x = -INFINITY;                              // its logit and id
+    int cut_id = 0x7FFFFFFF;
+    auto before_cut = [&](float x, int i) { return x > cut_x || (x == cut_x && id0 + i <= cut_id); };
 
-    // ---- the first token at which the count (MASS: the sum of weights) of what is kept reaches a target becomes the cut
+    // ---- the first token at which the count (by_mass: the sum of weights) of what is kept reaches a target becomes the cut
     auto shorten = [&](bool by_mass, u64 target) {
+        const int share = SA_BINS / blocks, mine0 = rank * share;         // bins that this block adds up
         u64 lo = 0, hi = cut, base = 0;                   // numbers that are searched; what lies before them
-        int shift = -1, at = 0;                           // bins of numbers >> shift; -1: of values
+        int shift = -1;                                   // bins of numbers >> shift; -1: of values
         for (bool again = true; again;) {
-            if (tid < SA_BINS) {
-                sh.count[tid] = 0;
-                sh.mass[tid] = 0;
-            }
+#pragma unroll
+            for (int w = 0; w < 3; ++w)
+                for (int i = tid; i < SA_BINS; i += SA_THREADS) sh.bins[w][i] = 0;        // (read by the others up to the round's second barrier)
             __syncthreads();
-            for (int i = tid; i < n; i += SA_THREADS) {
-                const float x = value(i);
+            auto bin_at = [&](float x, int i) -> int {    // -1: not searched
+                if (!(x >= weight.least)) return -1;     // its weight is 0: neither counted nor drawn
+                if (shift < 0) return before_cut(x, i) ? bin_of(x) : -1;
                 const u64 num = sa_number(x, id0 + i);
-                if (num < lo || num > hi) continue;
-                const int bin = shift < 0 ? bin_of(x) : (int)((num - lo) >> shift);
+                return num >= lo && num <= hi ? (int)((num - lo) >> shift) : -1;
+            };
+            for (int i = 4 * tid; i < n; i += 4 * SA_THREADS) {
+                float x[4];
+                four(i, x);
+                int bin[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) bin[j] = bin_at(x[j], i + j);
+                if (max(max(bin[0], bin[1]), max(bin[2], bin[3])) < 0) continue;
                 if (by_mass) {
-                    const u64 w = SampleWeight::whole(weight(x));
-                    if (w == 0) continue;
-                    atomicAdd(&sh.mass[bin], w);
+                    u64 w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = SampleWeight::whole(weight(x[j]));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (bin[j] < 0) continue;
+                        atomicAdd(&sh.bins[0][bin[j]], (unsigned)w[j] & 0x7FFFu);
+                        atomicAdd(&sh.bins[1][bin[j]], (unsigned)(w[j] >> 15) & 0x7FFFu);
+                        atomicAdd(&sh.bins[2][bin[j]], (unsigned)(w[j] >> 30));
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (bin[j] >= 0) atomicAdd(&sh.bins[0][bin[j]], 1u);
                 }
-                atomicAdd(&sh.count[bin], 1u);
             }
             cluster.sync();
-            unsigned c = 0;
-            u64 m = 0;
-            for (int r = 0; r < blocks; ++r) {
-                c += other(r)->count[tid];
-                if (by_mass) m += other(r)->mass[tid];
+            if (tid == 0) { sh.n_list = 0; sh.range[0] = ~0ull; sh.range[1] = 0; }        // (read by the others up to the barrier above)
+            // ---- this block's share of the bins, over the cluster
+            u64 sum = 0;
+            for (int i = tid; i < share; i += SA_THREADS) {
+                u64 m = 0;
+                const int bin = mine0 + i;
+                each([&](const SampleShared* o) { return o->bins[0][bin]; }, [&](int, unsigned x) { m += x; });
+                if (by_mass) {
+                    each([&](const SampleShared* o) { return o->bins[1][bin]; }, [&](int, unsigned x) { m += (u64)x << 15; });
+                    each([&](const SampleShared* o) { return o->bins[2][bin]; }, [&](int, unsigned x) { m += (u64)x << 30; });
+                }
+                sh.sums[i] = m;
+                sum += m;
             }
-            const u64 mine = by_mass ? m : c;
             u64 all;
-            const u64 upto = sa_block_scan(mine, sh, all);
-            if (by_mass && target == 0) target = max((u64)ceil((double)top_p * (double)all), 1ull);   // (of the first histogram, which holds all that is kept)
-            if (by_mass && target > base + all) target = base + all;
-            if (base + upto - mine < target && target <= base + upto) {
-                sh.found = tid;
-                sh.base = base + upto - mine;
-                sh.population = c;
-            }
-            cluster.sync();                               // (every block has read the others' bins)
-            at = sh.found;
-            base = sh.base;
-            again = sh.population > SA_LIST;
-            auto here = [&](float x, u64 num) { return num >= lo && num <= hi && (shift < 0 ? bin_of(x) == at : (int)((num - lo) >> shift) == at); };
-            if (!again) {
-                // ---- the bin's tokens, of all blocks
-                if (tid == 0) sh.n_list = 0;
-                __syncthreads();
-                for (int i = tid; i < n; i += SA_THREADS) {
-                    const float x = value(i);
-                    const u64 num = sa_number(x, id0 + i);
-                    if (!here(x, num)) continue;
-                    u64 w = 1;
-                    if (by_mass) w = SampleWeight::whole(weight(x));
-                    if (w == 0) continue;
-                    const unsigned k = atomicAdd(&sh.n_list, 1u);
-                    sh.list_at[0][k] = num;
-                    sh.list_w[0][k] = w;
-                }
-                cluster.sync();
-                int total = 0;
-                for (int r = 0; r < blocks; ++r) {
-                    const int here_n = other(r)->n_list;
-                    if (tid < here_n) {
-                        sh.list_at[1][total + tid] = other(r)->list_at[0][tid];
-                        sh.list_w[1][total + tid] = other(r)->list_w[0][tid];
-                    }
-                    total += here_n;
-                }
-                cluster.sync();
-                // ---- fewer and fewer of them, until a warp can order them
-                int from = 1;
-                while (total > 32) {
-                    u64 num = tid < total ? sh.list_at[from][tid] : ~0ull, w = tid < total ? sh.list_w[from][tid] : 0;
-                    u64 least = num, most = tid < total ? num : 0;
+            sa_block_scan(sum, sh, all);
+            if (tid == 0) sh.share = all;
+            cluster.sync();
+            // ---- the bin in which the target is reached: first the block that added it up, then the bin
+            u64 shares[SA_BLOCKS];
+            all = 0;
+            each([](const SampleShared* o) { return o->share; }, [&](int r, u64 x) { all += shares[r] = x; });
+            if (target == 0) target = max((u64)ceil((double)top_p * (double)all), 1ull);      // (the first histogram of top-p holds all that is kept)
+            if (target > base + all) target = base + all; // (rounded up beyond what there is)
+            int owner = -1;
 #pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) {
-                        least = min(least, __shfl_xor_sync(FULL_WARP, least, o));
-                        most = max(most, __shfl_xor_sync(FULL_WARP, most, o));
-                    }
-                    if (tid == 0) { sh.range[0] = ~0ull; sh.range[1] = 0; sh.n_list = 0; }
-                    sh.mass[tid] = 0;
-                    __syncthreads();
-                    if (lane == 0) { atomicMin(&sh.range[0], least); atomicMax(&sh.range[1], most); }
-                    __syncthreads();
-                    const u64 start = sh.range[0];
-                    const int down = max(0, 64 - __clzll((long long)(sh.range[1] - start)) - 9);
-                    const int bin = tid < total ? (int)((num - start) >> down) : 0;
-                    if (tid < total) atomicAdd(&sh.mass[bin], w);
-                    __syncthreads();
-                    const u64 part = sh.mass[tid];
-                    u64 sum;
-                    const u64 end = sa_block_scan(part, sh, sum);
-                    if (base + end - part < target && target <= base + end) {
-                        sh.found = tid;
-                        sh.base = base + end - part;
-                    }
-                    __syncthreads();
-                    base = sh.base;
-                    if (tid < total && bin == (int)sh.found) {
-                        const unsigned k = atomicAdd(&sh.n_list, 1u);
-                        sh.list_at[from ^ 1][k] = num;
-                        sh.list_w[from ^ 1][k] = w;
-                    }
-                    __syncthreads();
-                    total = sh.n_list;
-                    from ^= 1;
-                    __syncthreads();
+            for (int r = 0; r < SA_BLOCKS; ++r) {
+                if (r >= blocks) continue;
+                if (owner < 0 && target <= base + shares[r]) owner = r;
+                if (owner < 0) base += shares[r];
+            }
+            const u64* sums = other(owner < 0 ? 0 : owner)->sums;         // (there is an owner: the target is at most base + all)
+            u64 part[SA_BINS / SA_THREADS], part_sum = 0;
+            const int per = (share + SA_THREADS - 1) / SA_THREADS;        // consecutive bins of a thread
+#pragma unroll
+            for (int j = 0; j < SA_BINS / SA_THREADS; ++j) {
+                part[j] = j < per && tid * per + j < share ? sums[tid * per + j] : 0;
+                part_sum += part[j];
+            }
+            const u64 end = sa_block_scan(part_sum, sh, all);
+            u64 upto = base + end - part_sum;
+            if (tid == 0) sh.found = 0;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < SA_BINS / SA_THREADS; ++j) {
+                if (upto < target && target <= upto + part[j]) {
+                    sh.found = owner * share + tid * per + j;
+                    sh.base = upto;
                 }
-                if (warp == 0) {
-                    const u64 num = lane < total ? sh.list_at[from][lane] : ~0ull, w = lane < total ? sh.list_w[from][lane] : 0;
+                upto += part[j];
+            }
+            __syncthreads();
+            const int at = sh.found;
+            base = sh.base;
+            // ---- the bin's tokens: into a list, as many as it holds
+            for (int i = 4 * tid; i < n; i += 4 * SA_THREADS) {
+                float x[4];
+                four(i, x);
+                bool in[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) in[j] = bin_at(x[j], i + j) == at;
+                if (!(in[0] || in[1] || in[2] || in[3])) continue;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (!in[j]) continue;
+                    const unsigned k = atomicAdd(&sh.n_list, 1u);
+                    if (k < SA_LIST) sh.list[0][k] = make_ulonglong2(sa_number(x[j], id0 + i + j), by_mass ? SampleWeight::whole(weight(x[j])) : 1);
+                }
+            }
+            cluster.sync();
+            int from[SA_BLOCKS], total = 0;
+            each([](const SampleShared* o) { return o->n_list; }, [&](int r, unsigned x) {
+                from[r] = total;
+                total += (int)min(x, (unsigned)SA_LIST + 1u);
+            });
+            again = total > SA_LIST;
+            if (!again) {
+                // the list of the whole cluster, in no order; then the token at which the target is reached
+#pragma unroll
+                for (int r = 0; r < SA_BLOCKS; ++r)
+                    if (r < blocks && tid >= from[r] && tid < (r + 1 < blocks ? from[r + 1 < SA_BLOCKS ? r + 1 : r] : total)) sh.list[1][tid] = other(r)->list[0][tid - from[r]];
+                __syncthreads();
+                if (tid < total) {
+                    const ulonglong2 me = sh.list[1][tid];
                     u64 before = base;
-                    for (int j = 0; j < 32; ++j) {
-                        const u64 num_j = __shfl_sync(FULL_WARP, num, j), w_j = __shfl_sync(FULL_WARP, w, j);
-                        if (num_j < num) before += w_j;
+                    for (int j = 0; j < total; ++j) {
+                        const ulonglong2 x = sh.list[1][j];
+                        if (x.x < me.x) before += x.y;
                     }
-                    if (lane < total && before < target && target <= before + w) sh.cut = num;
+                    if (before < target && target <= before + me.y) sh.cut = me.x;
                 }
                 __syncthreads();
                 cut = sh.cut;
-                __syncthreads();
+                const unsigned high = (unsigned)(cut >> 32);
+                cut_x = __uint_as_float(high & 0x80000000u ? high : ~high & 0x7FFFFFFFu);
+                cut_id = (int)(unsigned)cut;
             } else {
-                // ---- too many for a list: the range of their numbers is divided in the next round
+                // too many for a list: the range of their numbers is divided in the next round
                 u64 least = ~0ull, most = 0;
-                for (int i = tid; i < n; i += SA_THREADS) {
-                    const float x = value(i);
-                    const u64 num = sa_number(x, id0 + i);
-                    if (!here(x, num)) continue;
-                    least = min(least, num);
-                    most = max(most, num);
+                for (int i = 4 * tid; i < n; i += 4 * SA_THREADS) {
+                    float x[4];
+                    four(i, x);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (bin_at(x[j], i + j) != at) continue;
+                        const u64 num = sa_number(x[j], id0 + i + j);
+                        least = min(least, num);
+                        most = max(most, num);
+                    }
                 }
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
                     least = min(least, __shfl_xor_sync(FULL_WARP, least, o));
                     most = max(most, __shfl_xor_sync(FULL_WARP, most, o));
                 }
-                if (tid == 0) { sh.range[0] = ~0ull; sh.range[1] = 0; }
-                __syncthreads();
                 if (lane == 0) { atomicMin(&sh.range[0], least); atomicMax(&sh.range[1], most); }
                 cluster.sync();
                 lo = ~0ull;
                 hi = 0;
-                for (int r = 0; r < blocks; ++r) {
-                    lo = min(lo, other(r)->range[0]);
-                    hi = max(hi, other(r)->range[1]);
-                }
-                shift = max(0, 64 - __clzll((long long)(hi - lo)) - 9);
-                cluster.sync();
+                each([](const SampleShared* o) { return o->range[0]; }, [&](int, u64 x) { lo = min(lo, x); });
+                each([](const SampleShared* o) { return o->range[1]; }, [&](int, u64 x) { hi = max(hi, x); });
+                shift = max(0, 64 - __clzll((long long)(hi - lo)) - 10);
             }
         }
     };
@@ -362,19 +412,30 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(SampleView s)
 
     // ---- the draw: kept weights by chunks of consecutive ids, then by blocks
     const double least = (double)min_p * (double)(1ull << SA_UNIT_BITS);
-    auto kept = [&](int i) -> u64 {
-        if (i >= n) return 0;
-        const float x = value(i);
-        if (sa_number(x, id0 + i) > cut) return 0;
-        const double w = weight(x);
-        return w >= least ? SampleWeight::whole(w) : 0;
+    float least_x = weight.least;                         // (a little below what min-p keeps)
+    if (min_p > 0.f) least_x = fmaxf(least_x, (float)((double)top + (log((double)min_p) - 1e-6) * (double)temperature - 1e-6 * fabs((double)top)));
+    auto kept = [&](int i, u64 (&w)[4]) {                 // of the four tokens from i on
+        float x[4];
+        four(i, x);
+        bool in[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            in[j] = x[j] >= least_x && before_cut(x[j], i + j);
+            w[j] = 0;
+        }
+        if (!__any_sync(FULL_WARP, in[0] || in[1] || in[2] || in[3])) return;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const double v = weight(x[j]);
+            w[j] = in[j] && v >= least ? SampleWeight::whole(v) : 0;
+        }
     };
     const int chunks = (n + SA_CHUNK - 1) / SA_CHUNK;
+#pragma unroll 2
     for (int c = warp; c < chunks; c += SA_WARPS) {
-        u64 sum = 0;
-#pragma unroll
-        for (int j = 0; j < SA_CHUNK / 32; ++j) sum += kept(c * SA_CHUNK + 32 * j + lane);
-        sum = sa_warp_sum(sum);
+        u64 w[4];
+        kept(c * SA_CHUNK + 4 * lane, w);
+        const u64 sum = sa_warp_sum(w[0] + w[1] + w[2] + w[3]);
         if (lane == 0) sh.chunk[c] = sum;
     }
     __syncthreads();
@@ -384,11 +445,10 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(SampleView s)
     if (tid == 0) sh.total = mine;
     cluster.sync();
     u64 total = 0, before = 0;
-    for (int r = 0; r < blocks; ++r) {
-        const u64 x = other(r)->total;
+    each([](const SampleShared* o) { return o->total; }, [&](int r, u64 x) {
         if (r < rank) before += x;
         total += x;
-    }
+    });
     const u64 goal = (u64)((double)u * (double)total);    // the lowest id whose running sum is above it
     if (before <= goal && goal < before + mine) {
         if (before + end - part <= goal && goal < before + end) {
@@ -397,15 +457,17 @@ __global__ void __launch_bounds__(SA_THREADS) sample_kernel(SampleView s)
         }
         __syncthreads();
         if (warp == 0) {
-            u64 upto = sh.base;
-            for (int j = 0; j < SA_CHUNK / 32; ++j) {
-                const int i = sh.found * SA_CHUNK + 32 * j + lane;
-                const u64 w = kept(i), incl = upto + sa_warp_scan(w);
-                if (incl - w <= goal && goal < incl) {
-                    s.tokens[row] = id0 + i;
-                    if (s.probs) s.probs[row] = (float)((double)w / (double)total);
+            const int i = sh.found * SA_CHUNK + 4 * lane;
+            u64 w[4];
+            kept(i, w);
+            u64 upto = sh.base + sa_warp_scan(w[0] + w[1] + w[2] + w[3]) - (w[0] + w[1] + w[2] + w[3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (upto <= goal && goal < upto + w[j]) {
+                    s.tokens[row] = id0 + i + j;
+                    if (s.probs) s.probs[row] = (float)((double)w[j] / (double)total);
                 }
-                upto = __shfl_sync(FULL_WARP, incl, 31);
+                upto += w[j];
             }
         }
     }

@@ -160,6 +160,18 @@ def test_a_rows_token_does_not_depend_on_the_batch():
             assert t[0] == tokens[r] and q[0] == probs[r]
 
 
+@pytest.mark.parametrize("V", [5000, 12000, 20000, 40000, 128000])
+def test_the_same_call_gives_the_same_bits(V):
+    from paper_2410_06916_b200 import sample_rows
+    x, u = make(300, V, seed=20 + V)
+    x, u = x.cuda(), u.cuda()
+    for kw in (dict(top_p=0.9), dict(top_k=77, top_p=0.8), dict(top_k=500), dict()):
+        want = sample_rows(x, u, **kw)
+        for _ in range(30):
+            got = sample_rows(x, u, **kw)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_draws_follow_the_distribution():
     """20000 draws from one row: each token's count within five standard deviations of what its probability says."""
     from paper_2410_06916_b200 import sample_rows
