@@ -88,26 +88,44 @@ long long page_bound(const BatchView& bv)
     return bound < bv.n_rows ? bound : bv.n_rows;
 }
 
-template <typename TX, typename CODE>
-cudaError_t launch_append8(const BatchView& bv, const Append8View& v, bool vec, cudaStream_t s)
+template <typename TX, typename CODE, int PIECE, int LPH>
+cudaError_t launch_append8_form(const BatchView& bv, Append8View& v, cudaStream_t s)
 {
-    const dim3 grid((unsigned)page_bound(bv), 2 * v.a.n_kv_heads);
-    if (!vec) return launch(append8_kernel<TX, CODE, 1, 32>, grid, 128, 0, s, false, bv, v);
+    v.pages = (int)page_bound(bv);
+    if (PIECE == 8 && v.a.n_heads > 0) {
+        // the queries, in blocks of the same launch: a row's heads to as many warps as make two waves of warps, as the 16-bit cache's append does
+        const int batch = 32 / LPH * AP_UNROLL<TX>, most = ceil_div(v.a.n_heads, batch), wanted = ceil_div(148 * 40, bv.n_rows);
+        v.q_chunks = wanted < most ? wanted : most;
+        v.q_per_warp = ceil_div(ceil_div(v.a.n_heads, v.q_chunks), 32 / LPH) * (32 / LPH);
+    }
+    const long long kv_blocks = (long long)v.pages * 2 * v.a.n_kv_heads, q_blocks = ((long long)bv.n_rows * v.q_chunks + AP_THREADS / 32 - 1) / (AP_THREADS / 32);
+    if (kv_blocks + q_blocks > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+    return launch(append8_kernel<TX, CODE, PIECE, LPH>, dim3((unsigned)(kv_blocks + q_blocks)), AP_THREADS, 0, s, false, bv, v);
+}
+template <typename TX, typename CODE>
+cudaError_t launch_append8(const BatchView& bv, Append8View& v, bool q_vec, bool kv_vec, cudaStream_t s)
+{
+    v.q_chunks = v.q_per_warp = 0;
+    if (!q_vec || !kv_vec) {
+        if (v.a.n_heads > 0) {
+            AppendView q = v.a;                           // the queries alone, by the 16-bit cache's kernels
+            q.n_kv_heads = 0;
+            const cudaError_t e = launch_append<TX, TX>(bv, q, q_vec, s);
+            if (e != cudaSuccess) return e;
+        }
+        return launch_append8_form<TX, CODE, 1, 32>(bv, v, s);
+    }
     const int pieces = v.a.head_dim / 16;
-    if (pieces <= 1) return launch(append8_kernel<TX, CODE, 8, 1>, grid, 128, 0, s, false, bv, v);
-    if (pieces <= 4) return launch(append8_kernel<TX, CODE, 8, 4>, grid, 128, 0, s, false, bv, v);
-    return launch(append8_kernel<TX, CODE, 8, 8>, grid, 128, 0, s, false, bv, v);
+    if (pieces <= 1) return launch_append8_form<TX, CODE, 8, 1>(bv, v, s);
+    if (pieces <= 2) return launch_append8_form<TX, CODE, 8, 2>(bv, v, s);
+    if (pieces <= 4) return launch_append8_form<TX, CODE, 8, 4>(bv, v, s);
+    if (pieces <= 8) return launch_append8_form<TX, CODE, 8, 8>(bv, v, s);
+    return launch_append8_form<TX, CODE, 8, 16>(bv, v, s);
 }
 template <typename TX>
-cudaError_t launch_append8_any(int dtype, const BatchView& bv, const Append8View& v, bool q_vec, bool kv_vec, cudaStream_t s)
+cudaError_t launch_append8_any(int dtype, const BatchView& bv, Append8View& v, bool q_vec, bool kv_vec, cudaStream_t s)
 {
-    if (v.a.n_heads > 0) {
-        AppendView q = v.a;                               // the queries alone, by the 16-bit cache's kernel
-        q.n_kv_heads = 0;
-        const cudaError_t e = launch_append<TX, TX>(bv, q, q_vec, s);
-        if (e != cudaSuccess) return e;
-    }
-    return dtype == SWIFT_I8 ? launch_append8<TX, int8_t>(bv, v, kv_vec, s) : launch_append8<TX, __nv_fp8_e4m3>(bv, v, kv_vec, s);
+    return dtype == SWIFT_I8 ? launch_append8<TX, int8_t>(bv, v, q_vec, kv_vec, s) : launch_append8<TX, __nv_fp8_e4m3>(bv, v, q_vec, kv_vec, s);
 }
 
 // ------------------------------------------------------------------------------ few rows per sequence
@@ -137,13 +155,14 @@ struct Plan8 {
     bool rows;                  // fp32 arithmetic: no tensor-core form
     bool prompt;                // too many rows for the few-row kernel, and no prefix or none worth sharing: each sequence by itself
     bool few, prefix_few;       // the few-row kernel takes the sequences' own parts; and the prefix
-    int group, dp, mt, grid, pre_grid;                    // grid: CTAs of the few-row kernel; pre_grid: of the prefix's
+    bool eight;                 // in its form for 8 rows
+    int group, dp, mt, workers, grid, pre_grid;                    // grid: CTAs of the few-row kernel; pre_grid: of the prefix's
     long long items;
     int splits;                 // cuts of the prefix by the many-row kernel (0: it has no prefix work)
     int slots;                  // parts per row that the many-row kernel leaves: splits, and the own part if it takes it
     size_t many_o, many_ml, few_o, few_ml, first, last, bytes;   // offsets in the workspace
 };
-inline int unit_keys8(int mt) { return mt == 1 ? 32 : 64; }
+inline int unit_keys8(const Plan8& p) { return p.mt == 1 && !p.eight ? 32 : 64; }
 
 swift_status plan_prefix8(const swift_coded_kv* c, const BatchView& bv, int n_heads, int max_rows, int x_dtype, Plan8* p)
 {
@@ -163,6 +182,8 @@ swift_status plan_prefix8(const swift_coded_kv* c, const BatchView& bv, int n_he
         p->few = own <= BD_MAX_ROWS;
         p->mt = own <= 16 ? 1 : own <= 32 ? 2 : 4;
         p->prefix_few = p->few && bv.prefix_len > 0 && all <= 16 * p->mt;
+        p->eight = p->few && own <= 8 && (!p->prefix_few || all <= 8);
+        p->workers = 8 / p->mt;                           // of a CTA
         p->prompt = !p->few && bv.prefix_len == 0;
         if (bv.prefix_len > 0 && !p->prefix_few && !p->prompt) {
             // The prefix is tensor work, the sequences' own parts are HBM work: both kernels run at once on SMs of their own, and the share
@@ -175,7 +196,7 @@ swift_status plan_prefix8(const swift_coded_kv* c, const BatchView& bv, int n_he
             for (int share = 2; share <= 12; ++share) {               // twelfths of the SMs
                 const int g = sms * share / 12, rest = g == sms ? sms : sms - g;
                 if (!p->few && g < sms) continue;
-                const double stream_us = own_bytes / (rest * SM_RATE < RATE ? rest * SM_RATE : RATE), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * (BD_WARPS / p->mt));
+                const double stream_us = own_bytes / (rest * SM_RATE < RATE ? rest * SM_RATE : RATE), item_us = 4.0 * ceil_div((long long)bv.n_seqs * Hk, rest * p->workers);
                 const double own_us = p->few ? 3.0 + (stream_us > item_us ? stream_us : item_us) : 0.0;
                 for (int waves = 1; waves <= 4; ++waves) {            // as many cuts as fill that many waves
                     long long n = (long long)waves * g / pairs;
@@ -210,10 +231,10 @@ swift_status plan_prefix8(const swift_coded_kv* c, const BatchView& bv, int n_he
         if (p->few) {
             p->items = (long long)(bv.n_seqs + (p->prefix_few ? 1 : 0)) * Hk;
             p->grid = p->splits > 0 && p->pre_grid < sms ? sms - p->pre_grid : sms;
-            const int keys = unit_keys8(p->mt);
+            const int keys = unit_keys8(*p);
             const long long units = ((long long)bv.n_seqs * ceil_div(bv.max_len, keys) + ceil_div(bv.prefix_len, keys)) * Hk;
             if (units > 0x7FFFFFFFll) return fail_batch(SWIFT_EUNSUPPORTED, "a page table of %d x %d for %d kv heads is beyond 2^31 units of work", bv.n_seqs, bv.table_stride, Hk);
-            const size_t rows_all = (size_t)(p->items + (long long)p->grid * (BD_WARPS / p->mt)) * 16 * p->mt;
+            const size_t rows_all = (size_t)(p->items + (long long)p->grid * p->workers) * 16 * p->mt;
             p->few_o = take(rows_all * p->dp * 4);
             p->few_ml = take(rows_all * 8);
             p->first = take((size_t)p->items * 4);
@@ -259,31 +280,33 @@ swift_status run_prompt8(const swift_paged_kv* kv, int x_dtype, const BatchView&
     return run_tc8(kv, x_dtype, bv, g, piece_bound(bv, av.n_kv_heads, g.tiles * g.rows_per_tile), 0x7FFFFFFF, s, false);
 }
 
-template <typename QT, typename CODE, int DP, int MT>
+template <typename QT, typename CODE, int DP, int MT, bool EIGHT = false>
 cudaError_t launch_dec8(const CUtensorMap& map, const BatchView& bv, const BdArgs& g, int grid, cudaStream_t s, bool after_previous)
 {
+    typedef B8Shape<DP, MT, EIGHT> S;
     static std::atomic<unsigned long long> done{0};
-    const cudaError_t e = allow_smem(attn_batch8_dec_kernel<QT, CODE, DP, MT>, B8Shape<DP, MT>::SMEM_BYTES, done);
+    const cudaError_t e = allow_smem(attn_batch8_dec_kernel<QT, CODE, DP, MT, EIGHT>, S::SMEM_BYTES, done);
     if (e != cudaSuccess) return e;
-    return launch(attn_batch8_dec_kernel<QT, CODE, DP, MT>, dim3(grid), BD_THREADS, B8Shape<DP, MT>::SMEM_BYTES, s, after_previous, map, bv, g);
+    return launch(attn_batch8_dec_kernel<QT, CODE, DP, MT, EIGHT>, dim3(grid), 32 * S::WARPS, S::SMEM_BYTES, s, after_previous, map, bv, g);
+}
+template <typename QT, typename CODE, int DP>
+cudaError_t launch_dec8_rows(const Plan8& p, const CUtensorMap& map, const BatchView& bv, const BdArgs& g, cudaStream_t s, bool after)
+{
+    if (p.eight) return launch_dec8<QT, CODE, DP, 1, true>(map, bv, g, p.grid, s, after);
+    if (p.mt == 1) return launch_dec8<QT, CODE, DP, 1>(map, bv, g, p.grid, s, after);
+    if (p.mt == 2) return launch_dec8<QT, CODE, DP, 2>(map, bv, g, p.grid, s, after);
+    return launch_dec8<QT, CODE, DP, 4>(map, bv, g, p.grid, s, after);
 }
 template <typename QT, typename CODE>
 cudaError_t launch_dec8_any(const Plan8& p, const CUtensorMap& map, const BatchView& bv, const BdArgs& g, cudaStream_t s, bool after)
 {
-    if (p.dp == 128) {
-        if (p.mt == 1) return launch_dec8<QT, CODE, 128, 1>(map, bv, g, p.grid, s, after);
-        if (p.mt == 2) return launch_dec8<QT, CODE, 128, 2>(map, bv, g, p.grid, s, after);
-        return launch_dec8<QT, CODE, 128, 4>(map, bv, g, p.grid, s, after);
-    }
-    if (p.mt == 1) return launch_dec8<QT, CODE, 64, 1>(map, bv, g, p.grid, s, after);
-    if (p.mt == 2) return launch_dec8<QT, CODE, 64, 2>(map, bv, g, p.grid, s, after);
-    return launch_dec8<QT, CODE, 64, 4>(map, bv, g, p.grid, s, after);
+    return p.dp == 128 ? launch_dec8_rows<QT, CODE, 128>(p, map, bv, g, s, after) : launch_dec8_rows<QT, CODE, 64>(p, map, bv, g, s, after);
 }
 
 template <typename T>
 cudaError_t launch_join8(const Plan8& p, const BatchView& bv, const BjArgs& j, cudaStream_t s)
 {
-    const bool cut = p.few && (long long)p.grid * (BD_WARPS / p.mt) > 8 * p.items;       // as for the 16-bit cache
+    const bool cut = p.few && (long long)p.grid * p.workers > 8 * p.items;       // as for the 16-bit cache
     return cut ? launch(attn_join_kernel<T, 8>, dim3(bv.n_rows, j.a.n_heads), 256, 0, s, true, bv, j)
                : launch(attn_join_kernel<T, 1>, dim3(bv.n_rows, ceil_div(j.a.n_heads, 8)), 256, 0, s, true, bv, j);
 }
@@ -320,7 +343,7 @@ swift_status run_prefix8(const swift_coded_kv* c, int x_dtype, const BatchView& 
     j.few_ml = reinterpret_cast<float2*>(ws + p.few_ml);
     j.item_first = reinterpret_cast<int*>(ws + p.first);
     j.item_last = reinterpret_cast<int*>(ws + p.last);
-    j.workers = p.grid * (BD_WARPS / p.mt);
+    j.workers = p.grid * p.workers;
     cudaError_t e = cudaSuccess;
     if (p.few) {
         BdArgs g = {};
@@ -333,7 +356,7 @@ swift_status run_prefix8(const swift_coded_kv* c, int x_dtype, const BatchView& 
         g.item_first = reinterpret_cast<int*>(ws + p.first);
         g.item_last = reinterpret_cast<int*>(ws + p.last);
         CUtensorMap map;
-        const swift_status st = make_codes_map(kv, p.dp, unit_keys8(p.mt), true, &map);
+        const swift_status st = make_codes_map(kv, p.dp, unit_keys8(p), true, &map);
         if (st != SWIFT_OK) return st;
         e = kv->dtype == SWIFT_I8 ? launch_dec8_any<QT, int8_t>(p, map, bv, g, s, before) : launch_dec8_any<QT, __nv_fp8_e4m3>(p, map, bv, g, s, before);
     } else {

@@ -233,11 +233,11 @@ constexpr int AP_THREADS = 128;
 template <typename TX> constexpr int AP_UNROLL = sizeof(TX) == 2 ? 4 : 2;      // 32 registers of loads in flight
 
 template <typename TX, typename TC, int LPH>
-__global__ void __launch_bounds__(AP_THREADS, 5) append_vec_kernel(BatchView b, AppendView a, int per_warp, int chunks)
+__device__ __forceinline__ void append_vec_rows(const BatchView& b, const AppendView& a, int per_warp, int chunks, unsigned block)
 {
     constexpr int GROUPS = 32 / LPH, UNROLL = AP_UNROLL<TX>;
     const int lane = threadIdx.x & 31, c = lane & (LPH - 1), grp = lane / LPH;
-    const long long job = (long long)blockIdx.x * (AP_THREADS / 32) + (threadIdx.x >> 5);
+    const long long job = (long long)block * (AP_THREADS / 32) + (threadIdx.x >> 5);
     const int row = (int)(job / chunks);
     if (row >= b.n_rows) return;
     const int D = a.head_dim, half = a.rotary_dim >> 1, pieces = D >> 4;
@@ -340,6 +340,12 @@ __global__ void __launch_bounds__(AP_THREADS, 5) append_vec_kernel(BatchView b, 
         }
         if (first + UNROLL * GROUPS < units) fetch(first + UNROLL * GROUPS);
     }
+}
+
+template <typename TX, typename TC, int LPH>
+__global__ void __launch_bounds__(AP_THREADS, 5) append_vec_kernel(BatchView b, AppendView a, int per_warp, int chunks)
+{
+    append_vec_rows<TX, TC, LPH>(b, a, per_warp, chunks, blockIdx.x);
 }
 
 // Scalar form: any even head_dim and rotary_dim, any alignment.  One warp per head of a row, lanes over pairs.

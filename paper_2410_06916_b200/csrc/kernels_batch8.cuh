@@ -23,6 +23,8 @@ struct Append8View {
     AppendView a;                                         // x[1], x[2]; pool: codes
     float* scales;                                        // this block's [K, V][kv head] of page 0
     long long scale_page;
+    int pages;                                            // pages that get rows, at most
+    int q_chunks, q_per_warp;                             // warps of a row's queries and heads of each; 0: no queries in this launch
 };
 
 __device__ __forceinline__ double widen(float v) { return (double)v; }
@@ -32,6 +34,15 @@ __device__ __forceinline__ double widen(__half v) { return (double)__half2float(
 // value / scale -> code
 __device__ __forceinline__ uint32_t code_of(double t, int8_t) { return (uint32_t)min(max(__double2int_rn(t), -127), 127) & 0xFFu; }
 __device__ __forceinline__ uint32_t code_of(double t, __nv_fp8_e4m3) { return __nv_cvt_float_to_fp8((float)t, __NV_SATFINITE, __NV_E4M3); }
+// the same code of an exact x: an int8 one in 32 bits, unless that lies so near the border between two (2^-13; it is off by 2^-16 at most) that
+// 64 have to tell
+__device__ __forceinline__ uint32_t code_near(float x, float inv32, double inv, int8_t)
+{
+    const float t = x * inv32, n = rintf(t);
+    if (fabsf(t - n) > 0.5f - 1.220703125e-4f) return code_of((double)x * inv, int8_t());
+    return (uint32_t)(int)n & 0xFFu;
+}
+__device__ __forceinline__ uint32_t code_near(float x, float, double inv, __nv_fp8_e4m3) { return code_of((double)x * inv, __nv_fp8_e4m3()); }
 __device__ __forceinline__ float largest_code(int8_t) { return 127.f; }
 __device__ __forceinline__ float largest_code(__nv_fp8_e4m3) { return 448.f; }
 
@@ -67,16 +78,26 @@ __device__ __forceinline__ bool a8_locate(const BatchView& b, int idx, A8Page& i
 
 // One block per (page, K or V of a kv head): first the largest value of its rows, which a second pass over them (now in L1 or L2)
 // divides by.  PIECE dims at a time: 8 where sizes and alignment allow 16-byte loads, else 1; LPH lanes share a row, each with two pieces that a
-// rotation pairs up, as in the 16-bit cache's kernel.  grid = (pages, 2 x kv heads), block = 128.
+// rotation pairs up, as in the 16-bit cache's kernel, whose code finishes the queries in the blocks behind the pages': their 32-bit work and
+// HBM traffic run beside the 64-bit work of K and V.  grid = pages x 2 x kv heads + blocks of queries, block = 128.
 template <typename TX, typename CODE, int PIECE, int LPH>
 __global__ void __launch_bounds__(128) append8_kernel(BatchView b, Append8View v)
 {
     constexpr int GROUPS = 32 / LPH;                      // rows a warp takes at once
     const AppendView& a = v.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, grp = lane / LPH, c0 = lane % LPH;
-    const int kind = blockIdx.y >= a.n_kv_heads, h = blockIdx.y - kind * a.n_kv_heads, D = a.head_dim;
+    const unsigned kv_blocks = (unsigned)v.pages * 2u * (unsigned)a.n_kv_heads;
+    if (blockIdx.x >= kv_blocks) {
+        if constexpr (PIECE == 8) {
+            AppendView q = a;
+            q.n_kv_heads = 0;
+            append_vec_rows<TX, TX, LPH>(b, q, v.q_per_warp, v.q_chunks, blockIdx.x - kv_blocks);
+        }
+        return;
+    }
+    const int unit = (int)(blockIdx.x % (2u * (unsigned)a.n_kv_heads)), kind = unit >= a.n_kv_heads, h = unit - kind * a.n_kv_heads, D = a.head_dim;
     A8Page it;
-    if (!a8_locate(b, blockIdx.x, it)) return;
+    if (!a8_locate(b, (int)(blockIdx.x / (2u * (unsigned)a.n_kv_heads)), it)) return;
     const int page = b.page_table[(size_t)it.seq * b.table_stride + it.page_no];
     if ((unsigned)page >= (unsigned)b.n_pages) return;
     const int base = it.page_no << b.page_shift;
@@ -182,10 +203,40 @@ __global__ void __launch_bounds__(128) append8_kernel(BatchView b, Append8View v
         return (unsigned)at < (unsigned)a.rope_positions;
     };
 
+    // V is stored as it comes, so its values are exact in 32 bits: its row's pieces, 8 of each at a time
+    auto v_pieces = [&](int o, auto use) {
+        const TX* src = src0 + (long long)(it.sp.r0 + (int)((long long)o - it.sp.pos0)) * a.row_stride[2];
+        for (int j = c0; j < D / 8; j += LPH) {
+            Raw8<TX> raw;
+            fetch8(src + 8 * j, raw);
+            float x[8];
+            widen8(raw, x);
+            use(8 * j, x);
+        }
+    };
+    const bool plain = PIECE == 8 && kind == 1;           // the same for the whole block
+
     // ---- the largest value
     double top = 0.0;
     bool bad = false, some = false, whole = true;         // whole: no row between lo and hi is left out
-    for (int o0 = lo + warp * GROUPS; o0 < hi; o0 += 4 * GROUPS) {
+    if constexpr (PIECE == 8) {
+        float most = 0.f;
+        for (int o0 = lo + warp * GROUPS; plain && o0 < hi; o0 += 4 * GROUPS) {
+            const bool live = live_row(o0 + grp);
+            some |= live;
+            whole &= live || o0 + grp >= hi;
+            if (!live) continue;
+            v_pieces(o0 + grp, [&](int, const float (&x)[8]) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    bad |= !(fabsf(x[e]) < INFINITY);
+                    most = fmaxf(most, fabsf(x[e]));
+                }
+            });
+        }
+        top = most;
+    }
+    for (int o0 = lo + warp * GROUPS; !plain && o0 < hi; o0 += 4 * GROUPS) {
         const bool live = live_row(o0 + grp);
         some |= live;
         whole &= live || o0 + grp >= hi;
@@ -231,7 +282,21 @@ __global__ void __launch_bounds__(128) append8_kernel(BatchView b, Append8View v
         }
     }
     // ---- the new codes
-    for (int o0 = lo + warp * GROUPS; o0 < hi; o0 += 4 * GROUPS) {
+    if constexpr (PIECE == 8) {
+        const float inv32 = (float)inv;
+        for (int o0 = lo + warp * GROUPS; plain && o0 < hi; o0 += 4 * GROUPS) {
+            const int o = o0 + grp;
+            if (!live_row(o)) continue;
+            uint8_t* dst = codes + (long long)(o - base) * D;
+            v_pieces(o, [&](int d, const float (&x)[8]) {
+                uint32_t w[2] = {0u, 0u};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e >> 2] |= (inv > 0.0 ? code_near(x[e], inv32, inv, CODE()) : 0u) << (8 * (e & 3));
+                *reinterpret_cast<uint2*>(dst + d) = make_uint2(w[0], w[1]);
+            });
+        }
+    }
+    for (int o0 = lo + warp * GROUPS; !plain && o0 < hi; o0 += 4 * GROUPS) {
         const int o = o0 + grp;
         uint8_t* dst = codes + (long long)(o - base) * D;
         finish(o, live_row(o), [&](int oa, int ob, const double (&xa)[PIECE], const double (&xb)[PIECE]) {

@@ -22,17 +22,23 @@ namespace swk {
 
 constexpr float B8_BIAS = 7.f;                            // weights are at most 2^(BT_GROW + 7)
 
-template <int DP_, int MT> struct B8Shape {               // DP: bytes of a staged row, 64 or 128
+// DP: bytes of a staged row, 64 or 128.  EIGHT: at most 8 packed rows an item, half of what an instruction computes: the others are left out
+// wherever they are not part of one, and the registers they would take make room for 64 keys a unit, whose bookkeeping then weighs half
+// (64 conversations of 8000 positions, 8 heads on a kv head: all 16 rows 125 us, 8 rows 117, and 64 keys 111, although that leaves one stage; 10 or
+// 12 warps spill: 150).
+template <int DP_, int MT, bool EIGHT> struct B8Shape {
     static constexpr int DP = DP_;
-    static constexpr int KEYS = MT == 1 ? 32 : 64;        // per unit
-    static constexpr int WORKERS = BD_WARPS / MT;
+    static constexpr int WARPS = 8;
+    static constexpr int KEYS = MT == 1 && !EIGHT ? 32 : 64;          // per unit
+    static constexpr int WORKERS = WARPS / MT;
     static constexpr int UNIT_BYTES = 2 * KEYS * DP;
     static constexpr int STAGES = 192 * 1024 / (WORKERS * UNIT_BYTES);
     static constexpr int RING_BYTES = WORKERS * STAGES * UNIT_BYTES;
-    static constexpr int Q_BYTES = 16 * 2 * DP;           // a warp's queries, 16 bits
+    static constexpr int Q_ROWS = EIGHT ? 8 : 16;
+    static constexpr int Q_BYTES = Q_ROWS * 2 * DP;       // a warp's queries, 16 bits
     static constexpr int BOXES = KEYS / 8;                // most pages of a unit
     static constexpr int SCALE_BYTES = WORKERS * STAGES * BOXES * 8;
-    static constexpr int SMEM_BYTES = 1024 + RING_BYTES + BD_WARPS * Q_BYTES + SCALE_BYTES;
+    static constexpr int SMEM_BYTES = 1024 + RING_BYTES + WARPS * Q_BYTES + SCALE_BYTES;
 };
 
 // What a key group needs of its page's scales.  0 stands for a page of zeros, whose codes are 0.
@@ -68,11 +74,12 @@ __device__ __forceinline__ float b8_lift(float top, float& inverse)
 }
 
 // QT: q's type; CODE: the codes'; the rest as attn_batch_dec_kernel.
-template <typename QT, typename CODE, int DPT, int MT>
-__global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __grid_constant__ CUtensorMap map_kv, BatchView b, BdArgs g)
+template <typename QT, typename CODE, int DPT, int MT, bool EIGHT>
+__global__ void __launch_bounds__(32 * B8Shape<DPT, MT, EIGHT>::WARPS, 1) attn_batch8_dec_kernel(const __grid_constant__ CUtensorMap map_kv, BatchView b, BdArgs g)
 {
-    typedef B8Shape<DPT, MT> S;
-    constexpr int DP = DPT, KEYS = S::KEYS, R = 16 * MT, CHUNKS = DP / 16;
+    typedef B8Shape<DPT, MT, EIGHT> S;
+    constexpr int DP = DPT, KEYS = S::KEYS, R = 16 * MT, CHUNKS = DP / 16, THREADS = 32 * S::WARPS;
+    constexpr int E = EIGHT ? 1 : 2;                      // rows of a thread: gq, and gq + 8
     constexpr bool MAY_BE_NAN = !std::is_same<CODE, int8_t>::value;
     pdl_trigger();
 
@@ -80,7 +87,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     __shared__ __align__(8) unsigned long long bars[S::WORKERS * S::STAGES * 2];
     __shared__ unsigned page_bits[S::WORKERS * S::STAGES];
-    __shared__ int sums[BD_THREADS / 32];
+    __shared__ int sums[S::WARPS];
     __shared__ int waits_sh[2];
     volatile int* waits = waits_sh;
 
@@ -88,7 +95,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
     const int wk = warp / MT, mt = warp % MT, gq = lane >> 2, t = lane & 3;
     auto full = [&](int s) { return smem_u32(&bars[wk * S::STAGES + s]); };
     auto empty = [&](int s) { return smem_u32(&bars[(S::WORKERS + wk) * S::STAGES + s]); };
-    const uint32_t scales_sh = base + S::RING_BYTES + BD_WARPS * S::Q_BYTES + wk * S::STAGES * S::BOXES * 8;
+    const uint32_t scales_sh = base + S::RING_BYTES + S::WARPS * S::Q_BYTES + wk * S::STAGES * S::BOXES * 8;
     if (tid == 0) {
         // a stage is full when its boxes have landed (one arrival and their bytes) and the lanes' copies of its scales (an arrival each)
         for (int s = 0; s < S::WORKERS * S::STAGES; ++s) { mbar_init(smem_u32(&bars[s]), 33); mbar_init(smem_u32(&bars[S::WORKERS * S::STAGES + s]), MT); }
@@ -100,13 +107,13 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
     // units of the whole batch (the host has made sure that they fit an int)
     const int prefix_units = g.prefix_here ? (b.prefix_len + KEYS - 1) / KEYS : 0;
     int own = 0;
-    for (int i = tid; i < b.n_seqs; i += BD_THREADS) own += bd_units<KEYS>(seq_span(b, i));
+    for (int i = tid; i < b.n_seqs; i += THREADS) own += bd_units<KEYS>(seq_span(b, i));
     own = __reduce_add_sync(FULL_WARP, own);
     if (lane == 0) sums[warp] = own;
     __syncthreads();
     long long U = prefix_units;
 #pragma unroll
-    for (int w = 0; w < BD_THREADS / 32; ++w) U += sums[w];
+    for (int w = 0; w < S::WARPS; ++w) U += sums[w];
     U *= Hk;
     const int all = gridDim.x * S::WORKERS, workers = (int)(U < (long long)all ? U : (long long)all), me = blockIdx.x * S::WORKERS + wk;
     const long long u0 = me < workers ? U * me / workers : 0, u1 = me < workers ? U * (me + 1) / workers : 0;
@@ -182,14 +189,14 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
         bool ok = true, fresh = true;                                     // fresh: first unit of an item here
         uint32_t qf[CHUNKS][4];
         float lower[2] = {1.f, 1.f};                                      // undo the rows' powers of two
-        float o[2 * CHUNKS][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        float o[2 * CHUNKS][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};   // (EIGHT: the second of two and the last two of four are never used)
         const int rho[2] = {16 * mt + gq, 16 * mt + gq + 8};              // this thread's two packed rows, their tokens
         const int tok[2] = {rho[0] / G, rho[1] / G};
         unsigned char* q_mem = smem_raw + (base - smem_u32(smem_raw)) + S::RING_BYTES + warp * S::Q_BYTES;
         const uint32_t q_sh = base + S::RING_BYTES + warp * S::Q_BYTES;
         auto fetch_q = [&](const BdWalk& item) {                          // this warp's 16 rows of an item's queries; dead rows zero
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) {
+            for (int i = 0; i < CHUNKS * S::Q_ROWS / 16; ++i) {
                 const int row = (i * 32 + lane) / (2 * CHUNKS), piece = (i * 32 + lane) % (2 * CHUNKS), r = 16 * mt + row, tk = r / G;
                 const bool live = r < item.sp.n * G && 8 * piece < g.a.head_dim;
                 const QT* q = reinterpret_cast<const QT*>(g.a.q) + (size_t)(item.sp.r0 + (live ? tk : 0)) * g.a.q_row_stride +
@@ -204,7 +211,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 __syncwarp();
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
+                for (int e = 0; e < E; ++e) {
                     float x[CHUNKS][4], top = 0.f;
 #pragma unroll
                     for (int ks = 0; ks < CHUNKS; ++ks) {
@@ -225,6 +232,10 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
                         qf[ks][e] = pack2(x[ks][0] * lift, x[ks][1] * lift, __half());
                         qf[ks][2 + e] = pack2(x[ks][2] * lift, x[ks][3] * lift, __half());
                     }
+                }
+                if (EIGHT) {
+#pragma unroll
+                    for (int ks = 0; ks < CHUNKS; ++ks) qf[ks][1] = qf[ks][3] = 0;
                 }
                 __syncwarp();
                 if (count - k > w.units - w.unit) {
@@ -280,20 +291,17 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
                 const int box = (8 * n) >> box_shift;
                 const float cn = __shfl_sync(FULL_WARP, mine.c, box), lv = __shfl_sync(FULL_WARP, mine.lv, box);
                 inv[n] = __shfl_sync(FULL_WARP, mine.inv, box);
-                const float c0 = cn * lower[0], c1 = cn * lower[1];
-                s[n][0] = fmaf(s[n][0], c0, lv);
-                s[n][1] = fmaf(s[n][1], c0, lv);
-                s[n][2] = fmaf(s[n][2], c1, lv);
-                s[n][3] = fmaf(s[n][3], c1, lv);
+#pragma unroll
+                for (int e = 0; e < 2 * E; ++e) s[n][e] = fmaf(s[n][e], cn * lower[e >> 1], lv);
             }
             int seen[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) seen[e] = w.seq < 0 ? left : min(left, w.sp.pos0 + tok[e] + 1 - key0);
-            if (__any_sync(FULL_WARP, min(seen[0], seen[1]) < KEYS) || pages != all_boxes) {
+            for (int e = 0; e < E; ++e) seen[e] = w.seq < 0 ? left : min(left, w.sp.pos0 + tok[e] + 1 - key0);
+            if (__any_sync(FULL_WARP, min(seen[0], seen[E - 1]) < KEYS) || pages != all_boxes) {
 #pragma unroll
                 for (int n = 0; n < KEYS / 8; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                    for (int e = 0; e < 2 * E; ++e) {
                         const int key = 8 * n + 2 * t + (e & 1);
                         if (key >= seen[e >> 1] || !((pages >> (key >> box_shift)) & 1u)) s[n][e] = -INFINITY;
                     }
@@ -302,12 +310,12 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
 #pragma unroll
             for (int n = 0; n < KEYS / 8; ++n) {
                 top[0] = max3(top[0], s[n][0], s[n][1]);
-                top[1] = max3(top[1], s[n][2], s[n][3]);
+                if (!EIGHT) top[1] = max3(top[1], s[n][2], s[n][3]);
             }
             // a row's sums are rescaled when its maximum has grown by more than 2^8
-            bool moved[2];
+            bool moved[2] = {false, false};
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < E; ++e) {
                 top[e] = fmaxf(top[e], __shfl_xor_sync(FULL_WARP, top[e], 1));
                 top[e] = fmaxf(top[e], __shfl_xor_sync(FULL_WARP, top[e], 2));
                 moved[e] = bt_outgrown(top[e], m[e], 1.f);
@@ -315,7 +323,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
             if (__any_sync(FULL_WARP, moved[0] || moved[1])) {
                 float shrink[2];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
+                for (int e = 0; e < E; ++e) {
                     const float from = m[e] - B8_BIAS, to = top[e] - B8_BIAS;     // (as the weights are made: both rounded)
                     shrink[e] = moved[e] ? ex2(from - to) : 1.f;
                     if (moved[e]) m[e] = top[e];
@@ -324,22 +332,22 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
 #pragma unroll
                 for (int nt = 0; nt < 2 * CHUNKS; ++nt) {
                     o[nt][0] *= shrink[0]; o[nt][1] *= shrink[0];
-                    o[nt][2] *= shrink[1]; o[nt][3] *= shrink[1];
+                    if (!EIGHT) { o[nt][2] *= shrink[1]; o[nt][3] *= shrink[1]; }
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) off[e] = m[e] == -INFINITY ? 0.f : m[e] - B8_BIAS;
+            for (int e = 0; e < E; ++e) off[e] = m[e] == -INFINITY ? 0.f : m[e] - B8_BIAS;
 #pragma unroll
             for (int n = 0; n < KEYS / 8; ++n) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] = ex2(s[n][e] - off[e >> 1]);
+                for (int e = 0; e < 2 * E; ++e) s[n][e] = ex2(s[n][e] - off[e >> 1]);
                 l[0] = fmaf(s[n][0] + s[n][1], inv[n], l[0]);
-                l[1] = fmaf(s[n][2] + s[n][3], inv[n], l[1]);
+                if (!EIGHT) l[1] = fmaf(s[n][2] + s[n][3], inv[n], l[1]);
             }
 #pragma unroll
             for (int n = 0; n < KEYS / 16; ++n) {
-                const uint32_t pf[4] = {pack2(s[2 * n][0], s[2 * n][1], __half()), pack2(s[2 * n][2], s[2 * n][3], __half()),
-                                        pack2(s[2 * n + 1][0], s[2 * n + 1][1], __half()), pack2(s[2 * n + 1][2], s[2 * n + 1][3], __half())};
+                const uint32_t pf[4] = {pack2(s[2 * n][0], s[2 * n][1], __half()), EIGHT ? 0u : pack2(s[2 * n][2], s[2 * n][3], __half()),
+                                        pack2(s[2 * n + 1][0], s[2 * n + 1][1], __half()), EIGHT ? 0u : pack2(s[2 * n + 1][2], s[2 * n + 1][3], __half())};
                 const uint32_t v_at = kv_sh + box_v + group_at(16 * n + v_key) + row_at;
 #pragma unroll
                 for (int d = 0; d < CHUNKS / 2; ++d) {                    // keys 16 n .. + 15 x dims 32 d .. + 31
@@ -368,7 +376,7 @@ __global__ void __launch_bounds__(BD_THREADS, 1) attn_batch8_dec_kernel(const __
                 // ---- the item, or this worker's share of it, ends
                 const size_t slot = (size_t)(w.item + me) * R;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
+                for (int e = 0; e < E; ++e) {
                     l[e] += __shfl_xor_sync(FULL_WARP, l[e], 1);
                     l[e] += __shfl_xor_sync(FULL_WARP, l[e], 2);
                     if (rho[e] < w.sp.n * G) {
