@@ -1,13 +1,13 @@
 // Attention of many query rows over a cache of 8-bit codes on the 5th-generation tensor cores: the many-row kernel of the 16-bit cache
 // (kernels_batch_tc.cuh: tiles, overlap, rescaling, pieces and modes are its own), whose operands are made on the way.
 //
-// Operands.  TMA brings a key tile's codes page by page into a ring of raw tiles; six warps make them fp16, which holds int8 and e4m3
+// Operands.  TMA brings a key tile's codes page by page into a ring of raw tiles; four warps make them fp16, which holds int8 and e4m3
 // exactly, and store them in the swizzled layout of the products.  (Three warps that fetched the codes themselves, 16 bytes a lane, took
-// 6300 cycles for a key tile, twice what the products and the softmax need.)  They stage the queries too, each row at the power of two that
-// brings it to [2^14, 2^15), so the products are fp16 for every type of q.  (8-bit operands on both sides would round q to 8 bits; a 16-bit copy
+// 6300 cycles for a key tile, twice what the products and the softmax need.)  They stage the queries too, bf16 rows at the power of two that
+// brings them to [2^14, 2^15), so the products are fp16 for every type of q.  (8-bit operands on both sides would round q to 8 bits; a 16-bit copy
 // of the cache would be written and read by every call.)
 //
-// Registers.  With 16 warps a thread has 128, so a softmax thread holds half a row of scores at a time and reads three quarters of the row from
+// Registers.  With 14 warps a thread has 144, so a softmax thread holds half a row of scores at a time and reads three quarters of the row from
 // TMEM twice (half of it with 168 registers and 11 warps).
 //
 // Scales.  As in the few-row kernel: a weight is 2^(c s + log2 sv - r), and a group of 8 keys, which lies in one page, adds its sum times

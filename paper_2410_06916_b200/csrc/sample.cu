@@ -59,7 +59,7 @@ extern "C" swift_status swift_sample_rows(const swift_sample_args* a, void* cuda
     v.tokens = a->tokens;
     v.probs = a->probs;
     // Two blocks to an SM: 80 KB of logits each beside what they keep.  As few blocks as that allows, which wait for one another less
-    // (64 rows of 128000 in bf16: NNN us with four blocks a row, 100 with eight); for few rows more, down to 2048 tokens (one row of 32000: 27 us
+    // (64 rows of 128000 in bf16: 76 us with four blocks a row, 100 with eight); for few rows more, down to 2048 tokens (one row of 32000: 27 us
     // with eight, 40 with two).
     int blocks = 1;
     while (blocks < SA_BLOCKS && (long long)ceil_div(a->vocab, blocks) * type_size(a->dtype) > 80000) blocks *= 2;

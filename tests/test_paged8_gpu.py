@@ -312,3 +312,176 @@ def test_append_then_attention_then_a_token():
     logits = o.float().view(6, 512) @ w
     tokens, probs = sample_rows(logits, torch.full((6,), 0.5, device="cuda"), temperature=0.0)
     assert torch.equal(tokens.long(), logits.argmax(1)) and (probs == 1).all()
+
+
+# ----------------------------------------------------------------------------------------------- how the calls are used
+def run(batch, form, q, **kw):
+    return (batch.prompt_attention if form == "prompt" else batch.prefix_attention)(0, q, **kw)
+
+
+@pytest.mark.parametrize("form", ["prompt", "prefix"])
+@pytest.mark.parametrize("rows,cached,heads,kv_heads", [(1, 40, 8, 2), (20, 0, 8, 1), (70, 300, 4, 4), (9, 500, 14, 2)])
+def test_many_short_sequences_give_the_same_bits_every_time(form, rows, cached, heads, kv_heads):
+    """Pieces of one or a few key tiles, many per SM: what one role of the many-row kernel does runs ahead of another's."""
+    n = [rows + i % 3 for i in range(200)]
+    b = Batch8(n, [x + (i * 37) % (cached + 1) for i, x in enumerate(n)], heads, kv_heads, 64, 16, I8)
+    pool, scales, batch = setup(b)
+    q = b.q.cuda()
+    want, tol = attention8(b, b.pool, b.scales, b.q, dev="cuda")
+    first = run(batch, form, q)
+    close(first, want, tol)
+    for _ in range(20):
+        assert torch.equal(run(batch, form, q), first)
+
+
+@pytest.mark.parametrize("codes", [I8, E4M3], ids=str)
+def test_pools_beyond_2_to_the_32_bytes(codes):
+    """Pages at the end of a pool of 5 GB."""
+    from paper_2410_06916_b200 import PagedKV, RowBatch
+    b = Batch8([3, 40], [200, 300], 16, 8, 128, 128, codes, prefix_len=130)
+    far = 20000
+    pool = torch.zeros((far,) + b.pool.shape[1:], dtype=torch.uint8, device="cuda").view(codes)
+    scales = torch.full((far,) + b.scales.shape[1:], float("nan"), device="cuda")
+    shift = far - b.n_pages
+    pool.view(torch.uint8)[shift:] = b.pool.view(torch.uint8).cuda()
+    scales[shift:] = b.scales.cuda()
+    args, kw = b.device_args()
+    live = args[2] < b.n_pages
+    args[2][live] += shift
+    kw["prefix_pages"] += shift
+    batch = RowBatch(PagedKV(pool, scales), *args, **kw)
+    want, tol = attention8(b, b.pool, b.scales, b.q)
+    for form in ("prompt", "prefix"):
+        close(run(batch, form, b.q.cuda()), want, tol)
+    b32 = Batch8([3, 40], [200, 300], 16, 8, 128, 128, codes, F32, prefix_len=130)
+    want, tol = attention8(b32, b.pool, b.scales, b32.q)
+    close(run(batch, "prompt", b32.q.cuda()), want, tol)
+    x, cut, _, table = rows_of(b, 128, False)
+    batch.append(0, *cut(x.cuda()), rope=table.cuda())
+    code, sc, near = append8(b, b.pool, b.scales, *cut(x)[1:], table)
+    got = pool[shift:].view(torch.uint8).view(codes).cpu().to(F64)
+    assert ((got == code) | (got.isnan() & code.isnan()) | (near & ((got - code).abs() <= 1))).all()
+    got = scales[shift:].cpu()
+    assert ((got == sc) | (got.isnan() & sc.isnan())).all()
+
+
+def test_four_thousand_sequences():
+    n = [1] * 4096
+    b = Batch8(n, [1 + i % 40 for i in range(4096)], 2, 1, 64, 8, I8)
+    pool, scales, batch = setup(b)
+    q = b.q.cuda()
+    a, c = run(batch, "prompt", q), run(batch, "prefix", q)
+    pick = [0, 1, 31, 32, 33, 1023, 2048, 4095]
+    small = Batch8(n, b.kv, 2, 1, 64, 8, I8)
+    small.n = [1 if i in pick else 0 for i in range(4096)]              # the definition, for a few of them
+    want, tol = attention8(small, b.pool, b.scales, b.q)
+    close(a[pick], want[pick], tol[pick])
+    close(c[pick], want[pick], tol[pick])
+
+
+def test_a_captured_step_follows_lengths_tables_and_values():
+    b = Batch8([1] * 5, [30, 17, 64, 1, 100], 8, 2, 64, 16, I8)
+    pool, scales, batch = setup(b)
+    x, cut, _, table = rows_of(b, 64, False)
+    table, xd = table.cuda(), x.cuda()
+
+    def step():
+        q = batch.append(0, *cut(xd), rope=table)
+        return run(batch, "prefix", q), run(batch, "prompt", q)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for _ in range(2):                                                   # two graphs, each with workspaces of its own
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs = step()
+        graphs.append((g, outs))
+    for seed, shorter in ((6, 0), (7, 12)):
+        pool.copy_(b.pool), scales.copy_(b.scales)
+        new = rows_of(b, 64, False, seed=seed)[0]
+        xd.copy_(new)
+        kv = [max(1, l - shorter) for l in b.kv]
+        batch._keep[1].copy_(torch.tensor(kv, dtype=torch.int32))
+        for g, outs in graphs:
+            pool.copy_(b.pool), scales.copy_(b.scales)
+            g.replay()
+            moved = Batch8(b.n, b.kv, 8, 2, 64, 16, I8)
+            moved.kv = kv
+            code, sc, _ = append8(moved, b.pool, b.scales, *cut(new)[1:], table.cpu())
+            q = torch.empty_like(moved.q)
+            batch2 = setup(b)[2]
+            batch2._keep[1].copy_(torch.tensor(kv, dtype=torch.int32))
+            q = batch2.append(0, *cut(new.cuda()), rope=table).cpu()
+            want, tol = attention8(moved, as_codes(code.nan_to_num(0.0), I8), sc, q)
+            for o in outs:
+                close(o, want, tol)
+
+
+def test_a_given_stream_and_inputs_that_are_freed():
+    b = Batch8([3, 40], [200, 90], 8, 2, 128, 32, E4M3, F16)
+    pool, scales, batch = setup(b)
+    want = [run(batch, form, b.q.cuda()) for form in ("prompt", "prefix")]
+    side = torch.cuda.Stream()
+    for form, w in zip(("prompt", "prefix"), want):
+        q = b.q.cuda()
+        side.wait_stream(torch.cuda.current_stream())
+        got = run(batch, form, q, stream=side)
+        del q
+        junk = torch.full((b.n_rows, 8, 128), 7.0, dtype=F16, device="cuda")   # (memory of q, were it handed out)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, w) and (junk == 7).all()
+
+
+@pytest.mark.parametrize("max_rows", [0, 1, 40])
+def test_a_wait_that_runs_out_is_reported_and_leads_nowhere(max_rows):
+    import ctypes as C
+    from paper_2410_06916_b200 import SwiftError, batch_sync, paged
+    from paper_2410_06916_b200.binding import _DevBuf, lib
+    b = Batch8([1, 40] if max_rows != 1 else [1, 1], [300, 90], 8, 2, 128, 16, I8)
+    pool, scales, batch = setup(b)
+    q, out = b.q.cuda(), torch.zeros(b.n_rows, 8, 128, dtype=BF16, device="cuda")
+    want = run(batch, "prompt", q)
+    batch_sync()
+    a = paged._Attention(0, 8, batch._rows("q", q, None, batch._types), 128 ** -0.5, out.data_ptr())
+    need = lib().swift_coded_prefix_workspace_bytes(batch._kv_p, batch._c_p, 8, max(1, max_rows), 1)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    assert lib().swift_probe_coded_wait_limit(batch._kv_p, batch._c_p, C.byref(a), 1, max_rows, _DevBuf(ws.data_ptr(), need), 1000, s) == 0
+    with pytest.raises(SwiftError):
+        batch_sync()
+    batch_sync()
+    assert torch.equal(run(batch, "prompt", q), want)
+    assert lib().swift_probe_coded_wait_limit(batch._kv_p, batch._c_p, C.byref(a), 0, max_rows, _DevBuf(ws.data_ptr(), need), 1000, s) == 6
+
+
+def test_refusals_of_the_python_side():
+    from paper_2410_06916_b200 import PagedKV, sample_rows
+    pool = torch.zeros(4, 1, 2, 2, 16, 64, dtype=torch.int8, device="cuda")
+    scales = torch.zeros(4, 1, 2, 2, device="cuda")
+    for p, s in ((pool, scales[:3]), (pool, scales.half()), (pool.to(BF16), scales), (pool, None), (pool, scales.cpu()), (pool.transpose(3, 4), scales),
+                 (pool, scales.clone().requires_grad_())):
+        with pytest.raises(ValueError):
+            PagedKV(p, s)
+    b = Batch8([2], [5], 4, 2, 64, 16, I8)
+    _, _, batch = setup(b)
+    with pytest.raises(TypeError):
+        batch.prompt_attention(0, b.q.cuda().double())
+    with pytest.raises(TypeError):
+        batch.append(0, b.q.cuda(), b.q.cuda()[:, :2].float(), b.q.cuda()[:, :2])
+    with pytest.raises(ValueError):
+        batch.prefix_attention(0, b.q.cuda(), out=torch.empty(2, 4, 64, device="cuda"))
+    with pytest.raises(ValueError):
+        batch.prefix_attention(0, b.q.cuda().requires_grad_())
+    x, u = torch.zeros(2, 10, device="cuda"), torch.zeros(2, device="cuda")
+    for bad in (dict(uniforms=u[:1]), dict(uniforms=u.double()), dict(temperature=-1.0), dict(temperature=float("nan")), dict(top_p=float("nan")),
+                dict(min_p=1.5), dict(top_k=1 << 40), dict(top_k=torch.zeros(2, device="cuda")), dict(tokens=torch.zeros(2, device="cuda")),
+                dict(logits=x.t()), dict(logits=x.double()), dict(logits=x.clone().requires_grad_()), dict(logits=x[0])):
+        with pytest.raises(ValueError):
+            sample_rows(**{"logits": x, "uniforms": u, **bad})
+    from paper_2410_06916_b200 import SwiftError
+    with pytest.raises(SwiftError):
+        sample_rows(torch.zeros(1, 262145, device="cuda"), u[:1])
