@@ -492,7 +492,7 @@ swift_status swift_probe_batch_wait_limit(const swift_paged_kv* kv, const swift_
 swift_status swift_batch_sync(void* cuda_stream);
 
 /*
- * The same cache held in 8 bits: int8 codes in -127..127, or float8 e4m3 ones.  A page's K (or V) of one kv head in one block shares one
+ * The same cache held in 8 bits: int8 codes in -127..127, or finite float8 e4m3 ones.  A page's K (or V) of one kv head in one block shares one
  * scale, scales[page][block][0 = K, 1 = V][kv head], fp32: value = code x scale.  Half the bytes of a 16-bit cache, and as much less to
  * read per decoding step.  Everything about batches, pages, positions, prefixes, streams and capture holds as above, and the calls are
  * chosen and used as theirs.  Scales are 0 or in 2^-50..2^50; a page with scale 0 holds codes 0.  A scale of NaN makes every row NaN that
