@@ -436,26 +436,60 @@ def test_a_given_stream_and_inputs_that_are_freed():
         assert torch.equal(got, w) and (junk == 7).all()
 
 
-@pytest.mark.parametrize("max_rows", [0, 1, 40])
-def test_a_wait_that_runs_out_is_reported_and_leads_nowhere(max_rows):
+WAITS = [
+    # rows of each of four sequences, cached, heads, kv heads, dim, codes, type, prefix, form
+    (40, 300, 8, 2, 128, I8, BF16, 0, "prompt"),
+    (1, 300, 8, 2, 64, E4M3, F16, 100, "prefix"),                # the few-row kernel, 8 rows, and the prefix with it
+    (9, 900, 14, 2, 128, I8, F16, 2000, "prefix"),               # ... 64 rows, beside the many-row kernel
+    (40, 100, 8, 1, 128, I8, BF16, 20000, "prefix"),             # the many-row kernel alone
+]
+
+
+def waits_run_out(case):
+    """In a process of its own: the probe gives up, the report comes once, the next call on the same workspace is right."""
     import ctypes as C
-    from paper_2410_06916_b200 import SwiftError, batch_sync, paged
-    from paper_2410_06916_b200.binding import _DevBuf, lib
-    b = Batch8([1, 40] if max_rows != 1 else [1, 1], [300, 90], 8, 2, 128, 16, I8)
+    from paper_2410_06916_b200 import SwiftError, batch_sync, lib
+    from paper_2410_06916_b200.binding import _DevBuf
+    each, kv, H, Hk, dim, codes, xt, prefix, form = WAITS[case]
+    b = Batch8([each] * 4, [kv, kv - 9, kv // 2, kv], H, Hk, dim, 16, codes, xt, prefix_len=prefix)
     pool, scales, batch = setup(b)
-    q, out = b.q.cuda(), torch.zeros(b.n_rows, 8, 128, dtype=BF16, device="cuda")
-    want = run(batch, "prompt", q)
-    batch_sync()
-    a = paged._Attention(0, 8, batch._rows("q", q, None, batch._types), 128 ** -0.5, out.data_ptr())
-    need = lib().swift_coded_prefix_workspace_bytes(batch._kv_p, batch._c_p, 8, max(1, max_rows), 1)
-    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
-    s = torch.cuda.current_stream().cuda_stream
-    assert lib().swift_probe_coded_wait_limit(batch._kv_p, batch._c_p, C.byref(a), 1, max_rows, _DevBuf(ws.data_ptr(), need), 1000, s) == 0
-    with pytest.raises(SwiftError):
+    want, tol = attention8(b, b.pool, b.scales, b.q, dev="cuda")
+    q = b.q.cuda()
+    rows, x = 0 if form == "prompt" else batch.max_rows, {BF16: 1, F16: 2}[xt]
+    need = lib().swift_coded_prefix_workspace_bytes(batch._kv_p, batch._c_p, H, max(rows, 1), x)
+    out = torch.empty_like(q)
+    a = batch._attention(0, q, None)
+    a.out = out.data_ptr()
+    stream = torch.cuda.current_stream().cuda_stream
+    for fill in (0, 0x7F, 0xFF, 0x01):
+        ws = torch.full((need,), fill, dtype=torch.uint8, device="cuda")       # what an entry no one wrote may hold
+        where = _DevBuf(ws.data_ptr(), need)
+        assert lib().swift_probe_coded_wait_limit(batch._kv_p, batch._c_p, C.byref(a), x, rows, where, 1000, stream) == 0
+        try:
+            batch_sync()
+            raise AssertionError("no report")
+        except SwiftError as e:
+            assert "ETIMEOUT" in str(e), e
         batch_sync()
-    batch_sync()
-    assert torch.equal(run(batch, "prompt", q), want)
-    assert lib().swift_probe_coded_wait_limit(batch._kv_p, batch._c_p, C.byref(a), 0, max_rows, _DevBuf(ws.data_ptr(), need), 1000, s) == 6
+        if form == "prefix":
+            assert lib().swift_coded_prefix_attention(batch._kv_p, batch._c_p, C.byref(a), x, rows, where, stream) == 0
+        else:
+            assert lib().swift_coded_prompt_attention(batch._kv_p, batch._c_p, C.byref(a), x, stream) == 0
+        batch_sync()
+        close(out, want, tol)
+    assert lib().swift_probe_coded_wait_limit(batch._kv_p, batch._c_p, C.byref(a), 0, rows, where, 1000, stream) == 6
+
+
+@pytest.mark.parametrize("case", range(len(WAITS)))
+def test_a_wait_that_runs_out_is_a_status(case):
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = (f"import sys; sys.path[:0] = [{here!r}, {os.path.dirname(here)!r}]\nimport torch\nimport test_paged8_gpu as t\n"
+            f"t.waits_run_out({case})\ntorch.cuda.synchronize()\nprint('fine')\n")
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "fine" in done.stdout, done.stderr[-2000:]
 
 
 def test_refusals_of_the_python_side():
