@@ -126,11 +126,15 @@ __global__ void __launch_bounds__(128) append8_kernel(BatchView b, Append8View v
         }
     };
     // row of own position o: the finished values of this lane's pieces, handed to use(j, oa, ob, xa, xb)
-    auto finish = [&](int o, bool live, auto use) {
+    __shared__ double norm_sh[128];                       // of each row of the page, from the first pass
+    const double one_of = 1.0 / D;
+    auto finish = [&](int o, bool live, bool again, auto use) {
         const int row = it.sp.r0 + (int)((long long)o - it.sp.pos0);
         const TX* src = src0 + (long long)row * a.row_stride[1 + kind];
         double norm = 1.0;
-        if (gain) {                                       // the same for the whole block
+        if (gain && again) {
+            if (live) norm = norm_sh[o - base];
+        } else if (gain) {                                // the same for the whole block
             double ss = 0.0;
             if (live)
                 for (int j = c0; j < pairs; j += LPH) {
@@ -144,7 +148,8 @@ __global__ void __launch_bounds__(128) append8_kernel(BatchView b, Append8View v
                 }
 #pragma unroll
             for (int x = LPH / 2; x > 0; x >>= 1) ss += __shfl_xor_sync(FULL_WARP, ss, x);
-            norm = 1.0 / sqrt(ss / D + (double)a.eps);
+            norm = rsqrt(ss * one_of + (double)a.eps);
+            if (live && c0 == 0) norm_sh[o - base] = norm;
         }
         if (!live) return;
         const float2* turn = R ? a.rope + (size_t)(a.positions ? a.positions[row] : b.prefix_len + o) * half : nullptr;
@@ -241,7 +246,7 @@ __global__ void __launch_bounds__(128) append8_kernel(BatchView b, Append8View v
         const bool live = live_row(o0 + grp);
         some |= live;
         whole &= live || o0 + grp >= hi;
-        finish(o0 + grp, live, [&](int, int, const double (&xa)[PIECE], const double (&xb)[PIECE]) {
+        finish(o0 + grp, live, false, [&](int, int, const double (&xa)[PIECE], const double (&xb)[PIECE]) {
 #pragma unroll
             for (int e = 0; e < PIECE; ++e) {
                 const double m = fmax(fabs(xa[e]), fabs(xb[e]));
@@ -300,7 +305,7 @@ __global__ void __launch_bounds__(128) append8_kernel(BatchView b, Append8View v
     for (int o0 = lo + warp * GROUPS; !plain && o0 < hi; o0 += 4 * GROUPS) {
         const int o = o0 + grp;
         uint8_t* dst = codes + (long long)(o - base) * D;
-        finish(o, live_row(o), [&](int oa, int ob, const double (&xa)[PIECE], const double (&xb)[PIECE]) {
+        finish(o, live_row(o), true, [&](int oa, int ob, const double (&xa)[PIECE], const double (&xb)[PIECE]) {
             uint32_t wa[(PIECE + 3) / 4] = {}, wb[(PIECE + 3) / 4] = {};
 #pragma unroll
             for (int e = 0; e < PIECE; ++e) {
