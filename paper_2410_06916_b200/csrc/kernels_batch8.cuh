@@ -79,8 +79,8 @@ __device__ __forceinline__ bool a8_locate(const BatchView& b, int idx, A8Page& i
 // One block per (page, K or V of a kv head): first the largest value of its rows, which a second pass over them (now in L1 or L2)
 // divides by.  PIECE dims at a time: 8 where sizes and alignment allow 16-byte loads, else 1; LPH lanes share a row, each with two pieces that a
 // rotation pairs up, as in the 16-bit cache's kernel, whose code finishes the queries in the blocks behind the pages': one launch
-// (16 rows of the 13B shape: 8.7 us, 12.4 with two; 8192 rows of the 70B shape: 66 us for K and V, 121 in all either way, and 134 with the two kinds of
-// blocks in turn).  grid = pages x 2 x kv heads + blocks of queries, block = 128.
+// (16 rows of the 13B shape: 8.7 us, 12.4 with two; 8192 rows of the 70B shape: 114 us, K and V some 60 of them, as long as two launches, and a tenth
+// more with the two kinds of blocks in turn).  grid = pages x 2 x kv heads + blocks of queries, block = 128.
 template <typename TX, typename CODE, int PIECE, int LPH>
 __global__ void __launch_bounds__(128) append8_kernel(BatchView b, Append8View v)
 {
